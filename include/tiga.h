@@ -47,7 +47,8 @@ typedef enum {
     TIGA_ERR_INVALID_POINTS = 7 /* tiga_validate_points found a coordinate that is not finite or lies outside the box */
 } tiga_status;
 
-typedef enum { TIGA_F32 = 0, TIGA_F16 = 1 } tiga_dtype;   /* feature storage; accumulation is fp32 */
+typedef enum { TIGA_F32 = 0, TIGA_F16 = 1, TIGA_BF16 = 2 } tiga_dtype;   /* feature storage; accumulation is fp32.  TIGA_BF16:
+                                                                          * attention over dense and paged relations, rotary positions */
 typedef enum { TIGA_I32 = 0, TIGA_I64 = 1 } tiga_itype;   /* rowptr storage; col is always int32 */
 /* TIGA_MAX64: the max reducer with 64-bit edge positions in argmax (an int64 array); any relation may use
  * it, relations of 2^31 edges or more must (TIGA_MAX keeps 32-bit positions). */
@@ -353,6 +354,132 @@ size_t tiga_csr_attention_workspace_bytes(const tiga_csr* g, int32_t D);
 tiga_status tiga_apply_csr_attention(const tiga_csr* g, const float* q, const float* key, const float* value,
                                      int32_t D, float scale, float* out, float* lse,
                                      void* ws, size_t ws_bytes, void* stream);
+
+/* ----------------------------------------------------------------- dense and paged relations, online-softmax reducer */
+
+/* The online-softmax reducer of Section 5 over relations that are never stored, with heads and 16-bit storage (the
+ * paper's streaming attention runs over an implicit dense or triangular relation in fp16):
+ *     s_ij = scale * <q[i,h,:], key[j,h',:]>,   p_ij = exp(s_ij) / sum_j exp(s_ij),   out[i,h,:] = sum_j p_ij value[j,h',:],
+ *     lse[i,h] = log sum_j exp(s_ij),           h' = h / (heads / kv_heads).
+ * Scores, maxima, masses, sums over keys and the gradients' sums are fp32; the weights p (and the gradient's
+ * p (dP - delta)) are rounded to the storage type before they enter the tensor cores.
+ *
+ * Arrays with heads: element (row i, head h, feature d) lies at base + i * row + h * head + d, strides in elements.  Bases are
+ * 16-byte aligned, row and head strides multiples of 8 and not negative (0: the rows, or heads, share storage; inputs only).
+ * Outputs without strides are dense: [rows, heads, D]; lse is fp32 [rows, heads].
+ *   dtype TIGA_F16 or TIGA_BF16 (TIGA_ERR_UNSUPPORTED: fp32);  D a multiple of 8, 8..128 (TIGA_ERR_UNSUPPORTED above);
+ *   heads a multiple of kv_heads;  scale finite.
+ *
+ * Segment bounds are read on the device and need no host copy, so calls may be captured in a graph and replayed with other
+ * lengths.  Bounds are clamped to the arrays, so no bound leads outside of them.  A row that reads no key yields the zero vector
+ * and lse = -inf, and zero gradients.  Rows outside of every segment (in front of start[0], behind start[n_seg]) are not
+ * touched, in outputs and gradients alike.  What lies in keys that no row of the segment reads (masked keys, places behind
+ * the last key of a page), NaN and infinities included, has no influence.  No atomics on results: they are reproducible. */
+typedef struct { int64_t row, head; } tiga_stride;
+
+typedef struct {
+    int32_t dtype;              /* of q, key, value, out and their gradients */
+    int32_t heads, kv_heads, D;
+    float scale;
+    tiga_stride q, key, value;  /* strides; key and value are not read for a paged relation */
+    tiga_stride grad_out;       /* read by the backward call only */
+} tiga_heads;
+
+/* Block-diagonal dense relation: every row of segment s, [q_start[s], q_start[s+1]), reads every key of segment s,
+ * [kv_start[s], kv_start[s+1]) (another length: cross attention of rows to an encoder's states). */
+typedef struct {
+    const int32_t* q_start;     /* device, int32 [n_seg + 1], ascending */
+    const int32_t* kv_start;    /* device, int32 [n_seg + 1], ascending */
+    const uint8_t* kv_mask;     /* device [n_kv], 0: the key is not read; NULL: all are */
+    int64_t n_seg;
+    int64_t n_q, n_kv;          /* rows of q / out, and of key / value; below 2^31 */
+} tiga_dense;
+
+/* out [n_q, heads, D], lse [n_q, heads] or NULL.  ws: tiga_dense_attention_workspace_bytes(g, h, 0) bytes. */
+size_t tiga_dense_attention_workspace_bytes(const tiga_dense* g, const tiga_heads* h, int backward);
+tiga_status tiga_apply_dense_attention(const tiga_dense* g, const tiga_heads* h, const void* q, const void* key, const void* value,
+                                       void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* Reverse mode: with delta_i = <grad_out_i, out_i>, dP_ij = <grad_out_i, value_j>, dS_ij = p_ij (dP_ij - delta_i),
+ *     grad_q_i = scale sum_j dS_ij key_j,   grad_key_j = scale sum_i dS_ij q_i,   grad_value_j = sum_i p_ij grad_out_i,
+ * key and value gradients summed over the heads of their group.  p is recomputed from lse; nothing of size rows x keys is
+ * stored.  out and lse are the forward's outputs for these inputs.  Gradients have the storage type and are dense,
+ * [n_q, heads, D] and [n_kv, kv_heads, D]; any of them may be NULL (skipped).  Masked keys have zero gradients.
+ * TIGA_F16: p and dS are scaled by powers of two before they are rounded (dS by one that all segments of a call
+ * share, from the largest row norms of grad_out and value), so that small weights and small gradients keep their digits.
+ * ws: tiga_dense_attention_workspace_bytes(g, h, 1) bytes. */
+tiga_status tiga_apply_dense_attention_backward(const tiga_dense* g, const tiga_heads* h, const void* q, const void* key,
+                                                const void* value, const void* out, const float* lse, const void* grad_out,
+                                                void* grad_q, void* grad_key, void* grad_value,
+                                                void* ws, size_t ws_bytes, void* stream);
+
+/* Keys and values in the pages of a cache: position p of sequence s lies in slot p % page_size of page
+ * table[s * table_stride + p / page_size].  Element (page, slot, head, d) of either array lies at
+ * page * page_stride + slot * slot_stride + head * head_stride + d, in elements.  A table entry outside [0, n_pages)
+ * names no page: its positions are read as masked keys and written nowhere.  Sequences may share pages that are only read. */
+typedef struct {
+    void* key;                  /* device */
+    void* value;                /* device */
+    const int32_t* table;       /* device, int32 */
+    const int32_t* kv_len;      /* device, int32 [n_seg]: tokens in the cache, those of the current chunk included */
+    int64_t n_seg, n_pages, page_size;
+    int64_t table_stride;       /* entries from one sequence's row to the next */
+    int64_t max_pages;          /* entries of a sequence's row; positions from max_pages * page_size on do not exist */
+    int64_t page_stride, slot_stride, head_stride;
+} tiga_pages;
+
+/* Attention of a chunk of new tokens over a paged cache (the triangular relation, its sources in pages): rows
+ * [q_start[s], q_start[s+1]) are the last n tokens of sequence s, their keys and values are in the cache already.
+ * Token t of them reads the positions up to kv_len[s] - n + t (causal != 0), or all kv_len[s].
+ *   q [n_q, heads, D] strided (h->q);  out [n_q, heads, D];  lse [n_q, heads] or NULL;  n_q below 2^31.
+ *   ws: tiga_paged_attention_workspace_bytes(c, h, n_q) bytes. */
+size_t tiga_paged_attention_workspace_bytes(const tiga_pages* c, const tiga_heads* h, int64_t n_q);
+tiga_status tiga_apply_paged_attention(const tiga_pages* c, const tiga_heads* h, const void* q, const int32_t* q_start, int64_t n_q,
+                                       int causal, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* ----------------------------------------------------------------- rotary positions */
+
+typedef enum {
+    TIGA_ROT_HALVES = 0,        /* pair i is (d, d') = (i, i + turned / 2) */
+    TIGA_ROT_PAIRS = 1          /* pair i is (2 i, 2 i + 1) */
+} tiga_rot_layout;
+
+typedef enum {
+    TIGA_ROT_PLAIN = 0,         /* f_i = base^(-2 i / turned) */
+    TIGA_ROT_LINEAR = 1,        /* f_i / factor (position interpolation) */
+    TIGA_ROT_BASE = 2,          /* base * factor^(turned / (turned - 2)) in place of base */
+    TIGA_ROT_BANDS = 3          /* g_i f_i + (1 - g_i) f_i / factor, g_i = (r_i - slow) / (fast - slow) clamped to [0, 1],
+                                 * r_i = length f_i / (2 pi) turns over the original context; magnitude 0.1 log(factor) + 1 */
+} tiga_rot_scaling;
+
+/* Frequencies in radians per position, computed on the HOST in 64 bits: freq [turned / 2] and *magnitude (1 but for
+ * TIGA_ROT_BANDS) are host pointers.  factor >= 1; length, slow, fast are read for TIGA_ROT_BANDS (fast > slow). */
+tiga_status tiga_rotary_frequencies(int32_t turned, double base, int32_t scaling, double factor, double length, double slow, double fast,
+                                    double* freq, float* magnitude);
+
+/* Rotary positions: the first `turned` features of every head are rotated in pairs,
+ *     (a, b) -> magnitude (a cos t - b sin t, a sin t + b cos t),   t = position * freq[pair],
+ * the others are copied.  t is formed and reduced in 64 bits, so far positions keep their angle.  inverse != 0 applies the
+ * transpose (t -> -t, the same magnitude): the gradient of the call.
+ *   x, y : dtype TIGA_F32, TIGA_F16 or TIGA_BF16, [n, heads, D], strided as above but without the rule on alignment (bases aligned to
+ *          their element); y == x with equal strides rotates in place, other overlaps are not allowed;
+ *   turned even, 0 < turned <= D;  positions: device int32 or int64 [n]. */
+typedef struct {
+    const double* freq;         /* device, fp64 [turned / 2] */
+    int32_t turned, layout;
+    float magnitude;
+} tiga_rotary;
+
+tiga_status tiga_apply_rotary(const tiga_rotary* r, const void* x, const tiga_stride* xs, void* y, const tiga_stride* ys, tiga_dtype dtype,
+                              int64_t n, int32_t heads, int32_t D, const void* positions, int32_t position_type, int inverse, void* stream);
+
+/* Writes the keys and values of a chunk into the pages of the cache: token t of the n rows of sequence s goes to position
+ * kv_len[s] - n + t, its key rotated to that position on the way (r == NULL: as it is).  Run before the attention call of the
+ * same chunk, with the same kv_len and start.  Tokens whose position is negative or has no page are written nowhere.
+ *   key, value : [n_new, kv_heads, D] strided (h->key, h->value), dtype TIGA_F16 or TIGA_BF16, D a multiple of 8.
+ *   Pages that the chunk reaches must belong to one sequence alone. */
+tiga_status tiga_paged_append(const tiga_pages* c, const tiga_heads* h, const void* key, const void* value, const int32_t* start,
+                              int64_t n_new, const tiga_rotary* r, void* stream);
 
 /* ----------------------------------------------------------------- generated exact kNN */
 

@@ -6,6 +6,7 @@ missing the import fails, there is no fallback of any kind.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 import struct
@@ -22,12 +23,17 @@ __all__ = [
     "tiga_apply_radius", "tiga_apply_radius_backward", "tiga_apply_radius_mlp",
     "tiga_apply_radius_mlp_backward", "tiga_knn_workspace_bytes", "tiga_apply_knn",
     "tiga_csr_attention_workspace_bytes", "tiga_apply_csr_attention", "launch_count",
+    "BF16", "DenseRelation", "tiga_dense_attention_workspace_bytes", "tiga_apply_dense_attention",
+    "tiga_apply_dense_attention_backward", "PagedCache", "tiga_paged_attention_workspace_bytes", "tiga_apply_paged_attention",
+    "tiga_paged_append", "ROT_PLAIN", "ROT_LINEAR", "ROT_BASE", "ROT_BANDS", "tiga_rotary_frequencies", "Rotary", "tiga_apply_rotary",
 ]
 
 SUM, MAX, MAX64 = 0, 1, 2      # MAX64: max reducer whose argmax holds 64-bit edge positions (int64)
-F32, F16 = 0, 1
+F32, F16, BF16 = 0, 1, 2
 I32, I64 = 0, 1
 MSG_COPY, MSG_WEIGHTED, MSG_GAUSS, MSG_DIST, MSG_LJ = 0, 1, 2, 3, 4
+ROT_HALVES, ROT_PAIRS = 0, 1
+ROT_PLAIN, ROT_LINEAR, ROT_BASE, ROT_BANDS = 0, 1, 2, 3
 
 EXPORTS = [
     "tiga_status_string", "tiga_kernel_launches", "tiga_checked_status", "tiga_is_checked_build", "tiga_csr_workspace_bytes", "tiga_validate_csr", "tiga_apply_csr",
@@ -37,6 +43,8 @@ EXPORTS = [
     "tiga_validate_points", "tiga_radius_workspace_bytes", "tiga_radius_bin", "tiga_apply_radius",
     "tiga_apply_radius_backward", "tiga_apply_radius_mlp", "tiga_apply_radius_mlp_backward",
     "tiga_knn_workspace_bytes", "tiga_apply_knn", "tiga_csr_attention_workspace_bytes", "tiga_apply_csr_attention",
+    "tiga_dense_attention_workspace_bytes", "tiga_apply_dense_attention", "tiga_apply_dense_attention_backward",
+    "tiga_paged_attention_workspace_bytes", "tiga_apply_paged_attention", "tiga_paged_append", "tiga_rotary_frequencies", "tiga_apply_rotary",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -73,6 +81,30 @@ class _Plan(ctypes.Structure):
     _fields_ = [("n_dst", ctypes.c_int64), ("n_src", ctypes.c_int64), ("n_edges", ctypes.c_int64), ("n_hot", ctypes.c_int64),
                 ("min_hot_degree", ctypes.c_int64), ("hot_edges", ctypes.c_int64), ("off_col", ctypes.c_int64),
                 ("off_hot_id", ctypes.c_int64), ("used_bytes", ctypes.c_int64)]
+
+
+class _Stride(ctypes.Structure):
+    _fields_ = [("row", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class _Heads(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("q", _Stride), ("key", _Stride), ("value", _Stride), ("grad_out", _Stride)]
+
+
+class _Dense(ctypes.Structure):
+    _fields_ = [("q_start", ctypes.c_void_p), ("kv_start", ctypes.c_void_p), ("kv_mask", ctypes.c_void_p),
+                ("n_seg", ctypes.c_int64), ("n_q", ctypes.c_int64), ("n_kv", ctypes.c_int64)]
+
+
+class _Pages(ctypes.Structure):
+    _fields_ = [("key", ctypes.c_void_p), ("value", ctypes.c_void_p), ("table", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
+                ("n_seg", ctypes.c_int64), ("n_pages", ctypes.c_int64), ("page_size", ctypes.c_int64), ("table_stride", ctypes.c_int64),
+                ("max_pages", ctypes.c_int64), ("page_stride", ctypes.c_int64), ("slot_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class _Rotary(ctypes.Structure):
+    _fields_ = [("freq", ctypes.c_void_p), ("turned", ctypes.c_int32), ("layout", ctypes.c_int32), ("magnitude", ctypes.c_float)]
 
 
 _lib = None
@@ -144,6 +176,23 @@ def load_library() -> ctypes.CDLL:
     lib.tiga_csr_attention_workspace_bytes.argtypes = [ctypes.POINTER(_Csr), i32]
     lib.tiga_apply_csr_attention.restype = ctypes.c_int
     lib.tiga_apply_csr_attention.argtypes = [ctypes.POINTER(_Csr), vp, vp, vp, i32, f, vp, vp, vp, sz, vp]
+    d, ref = ctypes.c_double, ctypes.POINTER
+    lib.tiga_dense_attention_workspace_bytes.restype = sz
+    lib.tiga_dense_attention_workspace_bytes.argtypes = [ref(_Dense), ref(_Heads), ctypes.c_int]
+    lib.tiga_apply_dense_attention.restype = ctypes.c_int
+    lib.tiga_apply_dense_attention.argtypes = [ref(_Dense), ref(_Heads), vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.tiga_apply_dense_attention_backward.restype = ctypes.c_int
+    lib.tiga_apply_dense_attention_backward.argtypes = [ref(_Dense), ref(_Heads), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.tiga_paged_attention_workspace_bytes.restype = sz
+    lib.tiga_paged_attention_workspace_bytes.argtypes = [ref(_Pages), ref(_Heads), i64]
+    lib.tiga_apply_paged_attention.restype = ctypes.c_int
+    lib.tiga_apply_paged_attention.argtypes = [ref(_Pages), ref(_Heads), vp, vp, i64, ctypes.c_int, vp, vp, vp, sz, vp]
+    lib.tiga_paged_append.restype = ctypes.c_int
+    lib.tiga_paged_append.argtypes = [ref(_Pages), ref(_Heads), vp, vp, vp, i64, ref(_Rotary), vp]
+    lib.tiga_rotary_frequencies.restype = ctypes.c_int
+    lib.tiga_rotary_frequencies.argtypes = [i32, d, i32, d, d, d, d, ref(d), ref(f)]
+    lib.tiga_apply_rotary.restype = ctypes.c_int
+    lib.tiga_apply_rotary.argtypes = [ref(_Rotary), vp, ref(_Stride), vp, ref(_Stride), ctypes.c_int, i64, i32, i32, vp, i32, ctypes.c_int, vp]
     lib.tiga_knn_workspace_bytes.restype = sz
     lib.tiga_knn_workspace_bytes.argtypes = [i64, i32, ctypes.POINTER(_Box)]
     lib.tiga_apply_knn.restype = ctypes.c_int
@@ -540,3 +589,244 @@ def tiga_apply_csr_attention(g: CsrRelation, q, key, value, scale: float, out=No
     _ok(_L.tiga_apply_csr_attention(g.ref, _ptr(q), _ptr(key), _ptr(value), D, float(scale), _ptr(out),
                                                 _ptr(lse), _ptr(ws), ws.numel(), _stream(stream)), "tiga_apply_csr_attention")
     return out, lse, ws
+
+
+# ------------------------------------------------------------------------------------ dense and paged relations, rotary positions
+
+_HALF = {torch.float16: F16, torch.bfloat16: BF16}
+_REAL = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
+_NO_CONTEXT = contextlib.nullcontext()
+
+
+def _on(like, stream):
+    """The device and stream that a call allocates and launches on: `stream`, or the current stream of the device of `like`."""
+    if not like.is_cuda:
+        raise ValueError("device arrays must be CUDA tensors")
+    if stream is not None:
+        if stream.device != like.device:
+            raise ValueError("the stream belongs to another device than the arrays")
+        return torch.cuda.stream(stream)
+    current = _current_device() if _current_device else torch.cuda.current_device()
+    return _NO_CONTEXT if like.device.index == current else torch.cuda.device(like.device)
+
+
+def _same(like, *arrays):
+    for t in arrays:
+        if t is not None and t.device != like.device:
+            raise ValueError("all arrays of a call must lie on one device")
+
+
+def _ints(t, n, name):
+    if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or (n is not None and t.numel() != n):
+        raise ValueError(f"{name} must be a contiguous int32 array" + ("" if n is None else f" of {n} entries"))
+    return t.data_ptr()
+
+
+def _step(t, d):
+    return t.stride(d) if t.shape[d] > 1 else 0       # the stride of a single entry means nothing
+
+
+def _stride_of(t, shape, dtype, name):
+    """(row, head) strides of an array [rows, heads, D] whose features are contiguous."""
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    if t.shape[2] > 1 and t.stride(2) != 1:
+        raise ValueError(f"the features of {name} must be contiguous")
+    return _Stride(_step(t, 0), _step(t, 1))
+
+
+def _dense_out(t, shape, dtype, name):
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} array {tuple(shape)}")
+    return t.data_ptr()
+
+
+def _type_of(t, types):
+    if t.dtype not in types:
+        raise TypeError(f"storage must be one of {[str(k) for k in types]}, got {t.dtype}")
+    if t.dim() != 3:
+        raise ValueError("arrays with heads have three dimensions: [rows, heads, D]")
+    return types[t.dtype]
+
+
+class DenseRelation:
+    """Block-diagonal dense relation: the rows [q_start[s], q_start[s+1]) read the keys [kv_start[s], kv_start[s+1]) of their
+    segment, those that `mask` (bool or uint8 [n_kv], optional) leaves."""
+
+    def __init__(self, q_start, kv_start, mask=None):
+        _ints(q_start, None, "q_start")
+        _ints(kv_start, q_start.numel(), "kv_start")
+        if q_start.numel() < 1:
+            raise ValueError("q_start has one entry more than there are segments")
+        if mask is not None and (mask.dtype not in (torch.bool, torch.uint8) or mask.dim() != 1 or not mask.is_contiguous()):
+            raise ValueError("mask must be a contiguous bool or uint8 array")
+        _same(q_start, kv_start, mask)
+        self.q_start, self.kv_start, self.mask = q_start, kv_start, mask
+        self.n_seg = q_start.numel() - 1
+
+
+def _dense_args(g, q, key, value, scale, grad_out=None):
+    dt = _type_of(q, _HALF)
+    n_q, heads, D = q.shape
+    if key.dim() != 3:
+        raise ValueError("arrays with heads have three dimensions: [rows, heads, D]")
+    n_kv, kv_heads = key.shape[:2]
+    _same(q, key, value, grad_out, g.q_start)
+    if g.mask is not None and g.mask.numel() != n_kv:
+        raise ValueError("the mask has one entry per key")
+    h = _Heads(dt, heads, kv_heads, D, scale, _stride_of(q, (n_q, heads, D), q.dtype, "q"),
+               _stride_of(key, (n_kv, kv_heads, D), q.dtype, "key"), _stride_of(value, (n_kv, kv_heads, D), q.dtype, "value"),
+               _Stride() if grad_out is None else _stride_of(grad_out, (n_q, heads, D), q.dtype, "grad_out"))
+    return _Dense(g.q_start.data_ptr(), g.kv_start.data_ptr(), 0 if g.mask is None else g.mask.data_ptr(), g.n_seg, n_q, n_kv), h
+
+
+def tiga_dense_attention_workspace_bytes(g: DenseRelation, q, key, value, backward: bool = False) -> int:
+    c, h = _dense_args(g, q, key, value, 1.0)
+    return int(_L.tiga_dense_attention_workspace_bytes(ctypes.byref(c), ctypes.byref(h), int(backward)))
+
+
+def tiga_apply_dense_attention(g: DenseRelation, q, key, value, scale: float, out=None, lse=None, want_lse=True, ws=None, stream=None):
+    """out[i,h] = sum_j softmax_j(scale <q[i,h], key[j,h']>) value[j,h'] over the keys of the row's segment, h' the head of h's
+    group.  q [n_q, heads, D], key and value [n_kv, kv_heads, D], fp16 or bf16, rows and heads strided.  Returns (out, lse, ws)."""
+    with _on(q, stream):
+        c, h = _dense_args(g, q, key, value, scale)
+        if out is None:
+            out = q.new_empty(q.shape)
+        if want_lse and lse is None:
+            lse = q.new_empty(q.shape[:2], dtype=torch.float32)
+        _same(q, out, lse, ws)
+        if ws is None:
+            ws = _ws(_L.tiga_dense_attention_workspace_bytes(ctypes.byref(c), ctypes.byref(h), 0), q)
+        _ok(_L.tiga_apply_dense_attention(ctypes.byref(c), ctypes.byref(h), q.data_ptr(), key.data_ptr(), value.data_ptr(),
+                                          _dense_out(out, q.shape, q.dtype, "out"),
+                                          None if lse is None else _dense_out(lse, q.shape[:2], torch.float32, "lse"),
+                                          _ptr(ws), ws.numel(), _stream(stream)), "tiga_apply_dense_attention")
+    return out, lse, ws
+
+
+def tiga_apply_dense_attention_backward(g: DenseRelation, q, key, value, out, lse, grad_out, scale: float, grad_q=None, grad_key=None,
+                                        grad_value=None, want_q=True, want_kv=True, ws=None, stream=None):
+    """Reverse mode of tiga_apply_dense_attention; out and lse are its outputs.  Returns (grad_q, grad_key, grad_value, ws); a
+    gradient is None where it is not wanted."""
+    with _on(q, stream):
+        c, h = _dense_args(g, q, key, value, scale, grad_out)
+        if want_q and grad_q is None:
+            grad_q = q.new_empty(q.shape)
+        if want_kv and grad_key is None:
+            grad_key = q.new_empty(key.shape)
+        if want_kv and grad_value is None:
+            grad_value = q.new_empty(key.shape)
+        _same(q, out, lse, grad_q, grad_key, grad_value, ws)
+        if ws is None:
+            ws = _ws(_L.tiga_dense_attention_workspace_bytes(ctypes.byref(c), ctypes.byref(h), 1), q)
+        grads = [None if t is None else _dense_out(t, like.shape, q.dtype, name)
+                 for t, like, name in ((grad_q, q, "grad_q"), (grad_key, key, "grad_key"), (grad_value, key, "grad_value"))]
+        _ok(_L.tiga_apply_dense_attention_backward(ctypes.byref(c), ctypes.byref(h), q.data_ptr(), key.data_ptr(), value.data_ptr(),
+                                                   _dense_out(out, q.shape, q.dtype, "out"),
+                                                   _dense_out(lse, q.shape[:2], torch.float32, "lse"), grad_out.data_ptr(), *grads,
+                                                   _ptr(ws), ws.numel(), _stream(stream)), "tiga_apply_dense_attention_backward")
+    return grad_q, grad_key, grad_value, ws
+
+
+class PagedCache:
+    """Keys and values in pages: key and value [n_pages, page_size, kv_heads, D] with equal strides, table int32 [n_seg, max_pages]
+    (entries outside [0, n_pages) name no page), kv_len int32 [n_seg]: tokens in the cache, the current chunk's included."""
+
+    def __init__(self, key, value, table, kv_len):
+        if key.dim() != 4 or key.shape != value.shape or key.dtype != value.dtype or key.dtype not in _HALF:
+            raise ValueError("key and value must be fp16 or bf16 arrays [n_pages, page_size, kv_heads, D] of one shape")
+        step = [_step(key, d) for d in range(3)]
+        if step != [_step(value, d) for d in range(3)] or (key.shape[3] > 1 and (key.stride(3) != 1 or value.stride(3) != 1)):
+            raise ValueError("key and value must have the same strides and contiguous features")
+        if table.dtype != torch.int32 or table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
+            raise ValueError("table must be an int32 array [n_seg, max_pages] with contiguous rows")
+        _ints(kv_len, table.shape[0], "kv_len")
+        _same(key, value, table, kv_len)
+        self.key, self.value, self.table, self.kv_len = key, value, table, kv_len
+        self.c = _Pages(key.data_ptr(), value.data_ptr(), table.data_ptr(), kv_len.data_ptr(), table.shape[0], key.shape[0], key.shape[1],
+                        _step(table, 0), table.shape[1], *step)
+        self.ref = ctypes.byref(self.c)
+
+
+def _paged_heads(cache, q, scale):
+    if _type_of(q, _HALF) != _HALF[cache.key.dtype] or q.shape[2] != cache.key.shape[3]:
+        raise ValueError("queries and cache must have one storage type and width")
+    _same(q, cache.key)
+    return _Heads(_HALF[q.dtype], q.shape[1], cache.key.shape[2], q.shape[2], scale, _stride_of(q, q.shape, q.dtype, "q"))
+
+
+def tiga_paged_attention_workspace_bytes(cache: PagedCache, q) -> int:
+    return int(_L.tiga_paged_attention_workspace_bytes(cache.ref, ctypes.byref(_paged_heads(cache, q, 1.0)), q.shape[0]))
+
+
+def tiga_apply_paged_attention(cache: PagedCache, q, q_start, scale: float, causal=True, out=None, lse=None, want_lse=True, ws=None, stream=None):
+    """Attention of a chunk of new tokens over a paged cache: the rows [q_start[s], q_start[s+1]) of q [n_q, heads, D] are the last
+    tokens of sequence s, and read its cache up to themselves (causal) or all of it.  Returns (out, lse, ws)."""
+    with _on(q, stream):
+        h = _paged_heads(cache, q, scale)
+        _same(q, q_start, out, lse, ws)
+        start = _ints(q_start, cache.c.n_seg + 1, "q_start")
+        if out is None:
+            out = q.new_empty(q.shape)
+        if want_lse and lse is None:
+            lse = q.new_empty(q.shape[:2], dtype=torch.float32)
+        if ws is None:
+            ws = _ws(_L.tiga_paged_attention_workspace_bytes(cache.ref, ctypes.byref(h), q.shape[0]), q)
+        _ok(_L.tiga_apply_paged_attention(cache.ref, ctypes.byref(h), q.data_ptr(), start, q.shape[0], int(bool(causal)),
+                                          _dense_out(out, q.shape, q.dtype, "out"),
+                                          None if lse is None else _dense_out(lse, q.shape[:2], torch.float32, "lse"),
+                                          _ptr(ws), ws.numel(), _stream(stream)), "tiga_apply_paged_attention")
+    return out, lse, ws
+
+
+def tiga_rotary_frequencies(turned: int, base: float = 10000.0, scaling: int = ROT_PLAIN, factor: float = 1.0, length: float = 0.0,
+                            slow: float = 1.0, fast: float = 32.0):
+    """Radians per position of every pair, on the host in 64 bits.  Returns (freq float64 [turned / 2] on the CPU, magnitude)."""
+    freq = torch.empty(max(int(turned), 0) // 2, dtype=torch.float64)
+    m = ctypes.c_float()
+    _ok(_L.tiga_rotary_frequencies(int(turned), float(base), int(scaling), float(factor), float(length), float(slow), float(fast),
+                                   ctypes.cast(freq.data_ptr(), ctypes.POINTER(ctypes.c_double)), ctypes.byref(m)), "tiga_rotary_frequencies")
+    return freq, m.value
+
+
+class Rotary:
+    """Descriptor of rotary positions: freq float64 [turned / 2] on the device, the layout of the pairs (halves, or interleaved with
+    pairs=True) and the magnitude."""
+
+    def __init__(self, freq, pairs=False, magnitude=1.0):
+        if freq.dtype != torch.float64 or freq.dim() != 1 or not freq.is_cuda or not freq.is_contiguous():
+            raise ValueError("freq must be a contiguous float64 CUDA array")
+        self.freq = freq
+        self.c = _Rotary(freq.data_ptr(), 2 * freq.numel(), ROT_PAIRS if pairs else ROT_HALVES, magnitude)
+        self.ref = ctypes.byref(self.c)
+
+
+def tiga_apply_rotary(rotary: Rotary, x, positions, out=None, inverse=False, stream=None):
+    """x [n, heads, D] with its first 2 * len(freq) features turned by positions (int32 or int64 [n]); inverse: the gradient of that.
+    out may be x (in place).  Returns out."""
+    with _on(x, stream):
+        dt = _type_of(x, _REAL)
+        if positions.dtype not in (torch.int32, torch.int64) or positions.shape != x.shape[:1] or not positions.is_contiguous():
+            raise ValueError("positions must be a contiguous int32 or int64 array with one entry per row")
+        if out is None:
+            out = x.new_empty(x.shape)
+        _same(x, positions, out, rotary.freq)
+        xs, ys = _stride_of(x, x.shape, x.dtype, "x"), _stride_of(out, x.shape, x.dtype, "out")
+        _ok(_L.tiga_apply_rotary(rotary.ref, x.data_ptr(), ctypes.byref(xs), out.data_ptr(), ctypes.byref(ys), dt, x.shape[0], x.shape[1],
+                                 x.shape[2], positions.data_ptr(), I32 if positions.dtype == torch.int32 else I64, int(bool(inverse)),
+                                 _stream(stream)), "tiga_apply_rotary")
+    return out
+
+
+def tiga_paged_append(cache: PagedCache, key, value, start, rotary: Rotary = None, stream=None) -> None:
+    """Writes key (rotated to its position) and value [n_new, kv_heads, D] of the rows [start[s], start[s+1]) to the last positions of
+    sequence s in the cache.  Pages that are written must belong to one sequence alone."""
+    with _on(key, stream):
+        dt = _type_of(key, _HALF)
+        if key.dtype != cache.key.dtype or key.shape[1:] != cache.key.shape[2:]:
+            raise ValueError("the rows must have the cache's storage type, heads and width")
+        _same(key, value, start, cache.key, None if rotary is None else rotary.freq)
+        n, heads, D = key.shape
+        h = _Heads(dt, heads, heads, D, 1.0, _Stride(), _stride_of(key, key.shape, key.dtype, "key"), _stride_of(value, key.shape, key.dtype, "value"))
+        _ok(_L.tiga_paged_append(cache.ref, ctypes.byref(h), key.data_ptr(), value.data_ptr(), _ints(start, cache.c.n_seg + 1, "start"), n,
+                                 None if rotary is None else rotary.ref, _stream(stream)), "tiga_paged_append")
