@@ -1,5 +1,4 @@
-// Online-softmax reducer over dense and paged relations: a warp per row (forward, query gradients) or per key (key and
-// value gradients), features across the lanes, fp32 throughout.
+// Online-softmax reducer over dense and paged relations: entry points; gradients by a warp per row or per key.
 #include "attention_shared.cuh"
 
 namespace tiga {
@@ -30,43 +29,6 @@ __device__ __forceinline__ void load4(const T* base, int D, int lane, float (&r)
 }
 __device__ __forceinline__ float dot4(const float (&a)[4], const float (&b)[4]) {
     return warp_sum(a[0] * b[0] + a[1] * b[1] + a[2] * b[2] + a[3] * b[3]);
-}
-
-template <typename T>
-__global__ void attn_forward_kernel(const AttnParams p) {
-    const long long w = (long long)blockIdx.x * ATTN_WARPS + threadIdx.x / 32;
-    const int lane = threadIdx.x % 32;
-    if (w >= (long long)p.n_q * p.heads) return;
-    const int i = (int)(w / p.heads), h = (int)(w % p.heads), hk = h / p.group;
-    const int s = segment_of_row(p.q_start, p.n_seg, p.n_q, i);
-    if (s < 0) return;
-    const Segment g = segment_of(p, s);
-    float q[4], o[4] = {0, 0, 0, 0}, m = -INFINITY, l = 0.f;
-    load4((const T*)p.q + i * p.q_row + h * p.q_head, p.D, lane, q);
-    const int n = min(keys_of_row(p, g, i - g.q0), g.nk);
-    for (int j = 0; j < n; ++j) {
-        long long ko, vo;
-        if (p.table) ko = vo = paged_offset(p, s, j);
-        else {
-            const bool on = !p.mask || p.mask[g.k0 + j];
-            ko = on ? (g.k0 + j) * p.k_row : -1;
-            vo = (g.k0 + j) * p.v_row;
-        }
-        if (ko < 0) continue;
-        float k[4], v[4];
-        load4((const T*)p.k + ko + hk * p.k_head, p.D, lane, k);
-        load4((const T*)p.v + vo + hk * p.v_head, p.D, lane, v);
-        const float sc = dot4(q, k) * p.scale * LOG2E_F;
-        const float M = fmaxf(m, sc), c = m == -INFINITY ? 0.f : exp2f(m - M), e = exp2f(sc - M);
-        l = l * c + e;
-#pragma unroll
-        for (int x = 0; x < 4; ++x) o[x] = o[x] * c + e * v[x];
-        m = M;
-    }
-#pragma unroll
-    for (int x = 0; x < 4; ++x)
-        if (lane + 32 * x < p.D) ((T*)p.out)[w * p.D + lane + 32 * x] = Half<T>::from(l > 0.f ? o[x] / l : 0.f);
-    if (lane == 0 && p.lse) p.lse[w] = l > 0.f ? (m + log2f(l)) * LN2_F : -INFINITY;
 }
 
 template <typename T>
@@ -131,14 +93,6 @@ __global__ void attn_grad_kv_kernel(const AttnParams p) {
 }
 
 static unsigned warps_grid(long long n) { return (unsigned)((n + ATTN_WARPS - 1) / ATTN_WARPS); }
-
-static size_t attn_carve(const AttnParams&, void*, int) { return 0; }
-
-template <typename T>
-static tiga_status attn_forward(const AttnParams& p, void*, cudaStream_t s) {
-    attn_forward_kernel<T><<<counted(warps_grid((long long)p.n_q * p.heads)), ATTN_WARPS * 32, 0, s>>>(p);
-    return launch_status();
-}
 
 template <typename T>
 static tiga_status attn_backward(const AttnParams& p, void*, cudaStream_t s) {
@@ -212,7 +166,7 @@ using namespace tiga;
 extern "C" size_t tiga_dense_attention_workspace_bytes(const tiga_dense* g, const tiga_heads* h, int backward) {
     AttnParams p;
     if (dense_check(g, h, &p) != TIGA_OK) return 0;
-    return attn_carve(p, nullptr, backward != 0) + 256;
+    return (backward ? 0 : attention_forward_bytes(p)) + 256;
 }
 
 extern "C" tiga_status tiga_apply_dense_attention(const tiga_dense* g, const tiga_heads* h, const void* q, const void* key, const void* value,
@@ -228,7 +182,7 @@ extern "C" tiga_status tiga_apply_dense_attention(const tiga_dense* g, const tig
     if (!ws || !aligned16(ws) || ws_bytes < tiga_dense_attention_workspace_bytes(g, h, 0)) return TIGA_ERR_WORKSPACE;
     p.q = q; p.k = key; p.v = value; p.out = out; p.lse = lse;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return h->dtype == TIGA_F16 ? attn_forward<__half>(p, ws, s) : attn_forward<__nv_bfloat16>(p, ws, s);
+    return attention_forward(p, h->dtype == TIGA_BF16, ws, s);
 }
 
 extern "C" tiga_status tiga_apply_dense_attention_backward(const tiga_dense* g, const tiga_heads* h, const void* q, const void* key,
@@ -255,7 +209,7 @@ extern "C" tiga_status tiga_apply_dense_attention_backward(const tiga_dense* g, 
 extern "C" size_t tiga_paged_attention_workspace_bytes(const tiga_pages* c, const tiga_heads* h, int64_t n_q) {
     AttnParams p;
     if (paged_check(c, h, n_q, &p) != TIGA_OK) return 0;
-    return attn_carve(p, nullptr, 0) + 256;
+    return attention_forward_bytes(p) + 256;
 }
 
 extern "C" tiga_status tiga_apply_paged_attention(const tiga_pages* c, const tiga_heads* h, const void* q, const int32_t* q_start, int64_t n_q,
@@ -271,5 +225,5 @@ extern "C" tiga_status tiga_apply_paged_attention(const tiga_pages* c, const tig
     if (!ws || !aligned16(ws) || ws_bytes < tiga_paged_attention_workspace_bytes(c, h, n_q)) return TIGA_ERR_WORKSPACE;
     p.q = q; p.q_start = q_start; p.causal = causal != 0; p.out = out; p.lse = lse;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return h->dtype == TIGA_F16 ? attn_forward<__half>(p, ws, s) : attn_forward<__nv_bfloat16>(p, ws, s);
+    return attention_forward(p, h->dtype == TIGA_BF16, ws, s);
 }

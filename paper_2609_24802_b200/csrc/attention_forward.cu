@@ -1,0 +1,515 @@
+// Online-softmax reducer over dense and paged relations, forward, on the fifth-generation tensor cores.
+#include "attention_shared.cuh"
+#include "tcgen.cuh"
+
+namespace tiga {
+
+// A block holds a tile of 256 packed rows as two halves of 128, one warpgroup of softmax threads for each (a thread has a row), and
+// goes through the keys in steps of 128:
+//   producers (4 warps)   copy query and key / value rows to shared memory, 16 bytes a lane, any stride or page, zeros for what is
+//                         masked, missing or behind the head's width; a ring of key and value tiles in the order K0 V0 K1 V1 ...
+//   one thread            issues S = Q K^T (to tensor memory) and O += P V (P from tensor memory, O stays there for the whole tile)
+//   softmax warpgroups    running maximum, P = exp2(S - m) in 16 bits over S's own columns, running mass
+// While one half's softmax runs, the tensor cores work for the other.  A tile of at most 128 rows has one half; then the two
+// warpgroups take the even and the odd steps with a state each, joined at the end, so a single token keeps both busy too.
+// The accumulator is rescaled only when a row's maximum grew by more than 2^8 since the last time: weights up to 2^8 do no harm,
+// and the mass carries the same factor.
+constexpr int FWD_THREADS = 416, FWD_ROWS = 256, FWD_STEP = 128;
+constexpr Geometry FWD_GEO = {FWD_ROWS, FWD_STEP, 0};
+constexpr int FWD_LEAST = 2;            // units a block at least
+constexpr int MASK_RING = 8;            // the producers are at most 6 steps ahead of the softmax (ring of at most 10 tiles)
+constexpr float RESCALE_AT = 8.f;
+
+template <int DP> struct Fwd {
+    static constexpr int TILE = 128 * DP * 2;
+    static constexpr int SLOTS = DP == 128 ? 5 : 10;
+    static constexpr int CONTROL = 2 * TILE + SLOTS * TILE;
+    static constexpr int SMEM = CONTROL + 2560;
+};
+
+struct FwdControl {
+    unsigned long long full[10], empty[10], q_full, q_empty, s_full[2], p_full[2], o_full[2], mask_full[MASK_RING], drain;
+    uint32_t tmem, abort_word, never, mask[MASK_RING][4];
+    float m[2][128], l[2][128];
+};
+static_assert(sizeof(FwdControl) <= 2560, "control block");
+
+struct FwdWork {
+    const long long* unit_start;
+    float2* part_ml;                // [2 * grid][rows]: reference of the exponents (log2), mass
+    float* part_o;                  // [2 * grid][rows][DP]: unnormalised
+    int rows;                       // packed rows that a partial state holds at most
+};
+
+// packed row r of kv head h: offsets of its row in arrays with strides
+struct PackedRow { int row, head; };
+__device__ __forceinline__ PackedRow packed_row(const AttnParams& p, const Segment& g, int h, int r) {
+    const int t = r / p.group;
+    return {g.q0 + t, h * p.group + (r - t * p.group)};
+}
+
+// 32 rows of a tile by one warp: lane l holds row l's element offset (or -1: zeros; `any` is an
+// address that may be read).  The tile consists of blocks of 64 features, rows
+// of 128 bytes swizzled in groups of eight.
+template <int DP, int TILE_ROWS>
+__device__ __forceinline__ void copy_rows(uint32_t tile, int first_row, const void* base, long long off, int D, const void* any) {
+    constexpr int CH = DP / 8;
+    const int lane = threadIdx.x % 32, c = lane % CH;
+    const bool in_width = c * 8 < D;
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+        const int r = k * (32 / CH) + lane / CH;
+        const long long o = __shfl_sync(~0u, off, r);
+        const int row = first_row + r;
+        const bool on = o >= 0 && in_width;
+        cp_async16(tile + (c / 8) * (TILE_ROWS * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4),
+                   on ? (const char*)base + (o + c * 8) * 2 : (const char*)any, on);
+    }
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const AttnParams p, const FwdWork w) {
+    typedef Fwd<DP> C;
+    extern __shared__ __align__(1024) unsigned char smem[];
+    FwdControl& ctl = *reinterpret_cast<FwdControl*>(smem + C::CONTROL);
+    const uint32_t q_tile = smem_u32(smem), ring = q_tile + 2 * C::TILE;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    volatile uint32_t* abort_word = &ctl.abort_word;
+    auto bar = [&](unsigned long long& b) { return smem_u32(&b); };
+
+    const long long units = w.unit_start[p.n_seg];
+    const long long blocks = blocks_for(units, gridDim.x, FWD_LEAST);
+    if (blockIdx.x >= blocks || units == 0) return;
+    const long long unit0 = blockIdx.x * units / blocks, unit1 = (blockIdx.x + 1LL) * units / blocks;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < C::SLOTS; ++i) { mbar_init(bar(ctl.full[i]), 128); mbar_init(bar(ctl.empty[i]), 1); }
+        mbar_init(bar(ctl.q_full), 128);
+        mbar_init(bar(ctl.q_empty), 1);
+        for (int x = 0; x < 2; ++x) { mbar_init(bar(ctl.s_full[x]), 1); mbar_init(bar(ctl.p_full[x]), 128); mbar_init(bar(ctl.o_full[x]), 1); }
+        for (int i = 0; i < MASK_RING; ++i) mbar_init(bar(ctl.mask_full[i]), 4);
+        mbar_init(bar(ctl.drain), 1);
+        ctl.abort_word = ctl.never = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 12) tmem_alloc(smem_u32(&ctl.tmem), 512);
+    tmem_fence_before();
+    __syncthreads();
+    tmem_fence_after();
+    const uint32_t tmem = ctl.tmem;
+    const uint32_t s_at[2] = {tmem, tmem + 128}, o_at[2] = {tmem + 256, tmem + 256 + DP};
+
+    Walker it;
+    if (warp >= 8 && warp < 12) {
+        // ---------------------------------------------------------------- producers
+        const int pw = warp - 8;
+        uint32_t tiles = 0, steps = 0, items = 0;
+        bool ok = true;
+        auto slot_free = [&]() { return tiles < (uint32_t)C::SLOTS || mbar_wait(bar(ctl.empty[tiles % C::SLOTS]), (tiles / C::SLOTS + 1) & 1, abort_word); };
+        for (bool more = it.begin(p, FWD_GEO, w.unit_start, unit0, unit1); more && ok; more = it.next(p, FWD_GEO), ++items) {
+            const int rows = min(it.g.nq * p.group - it.t * FWD_ROWS, FWD_ROWS);
+            auto place = [&](int i) {
+                const int j = i * FWD_STEP + 32 * pw + lane;
+                return j < it.g.nk ? key_place(p, it.g, it.s, j) : -1LL;
+            };
+            long long at = place(it.i0);
+            if (items && !(ok = mbar_wait(bar(ctl.q_empty), (items - 1) & 1, abort_word))) break;
+            for (int x = 0; x < (rows > 128 ? 2 : 1); ++x) {
+                const int r = x * 128 + 32 * pw + lane;
+                long long off = -1;
+                if (r < rows) {
+                    const PackedRow pr = packed_row(p, it.g, it.h, it.t * FWD_ROWS + r);
+                    off = pr.row * p.q_row + pr.head * p.q_head;
+                }
+                copy_rows<DP, 128>(q_tile + x * C::TILE, 32 * pw, p.q, off, p.D, p.q);
+            }
+            cp_async_arrive(bar(ctl.q_full));
+            for (int i = it.i0; i < it.i1; ++i, ++steps) {
+                const long long here = at;
+                const uint32_t valid = __ballot_sync(~0u, here >= 0);
+                if (lane == 0) {
+                    ctl.mask[steps % MASK_RING][pw] = valid;
+                    mbar_arrive(bar(ctl.mask_full[steps % MASK_RING]));
+                }
+                if (i + 1 < it.i1) at = place(i + 1);
+                for (int kv = 0; kv < 2; ++kv, ++tiles) {
+                    if (!(ok = slot_free())) break;
+                    const long long row = p.table ? 1 : kv ? p.v_row : p.k_row;
+                    const long long off = here < 0 ? -1 : here * row + it.h * (kv ? p.v_head : p.k_head);
+                    copy_rows<DP, 128>(ring + (tiles % C::SLOTS) * C::TILE, 32 * pw, kv ? p.v : p.k, off, p.D, p.q);
+                    cp_async_arrive(bar(ctl.full[tiles % C::SLOTS]));
+                }
+                if (!ok) break;
+            }
+        }
+        cp_async_wait_all();
+    } else if (warp == 12) {
+        // ---------------------------------------------------------------- matrix instructions
+        if (lane == 0) {
+            const uint32_t s_shape = mma_shape<T>(128, false) | (p.scale < 0.f ? MMA_NEGATE_A : 0), o_shape = mma_shape<T>(DP, true);
+            uint32_t tile0 = 0, items = 0, done[2] = {0, 0};     // done: p_full phases consumed
+            bool ok = true;
+            const int k_pieces = (p.D + 15) / 16;
+            auto slot = [&](uint32_t tile) { return ring + (tile % C::SLOTS) * C::TILE; };
+            auto wait_tile = [&](uint32_t tile) {
+                ok = ok && mbar_wait(bar(ctl.full[tile % C::SLOTS]), (tile / C::SLOTS) & 1, abort_word);
+                fence_async_proxy();
+            };
+            auto release = [&](uint32_t tile) { mma_commit(bar(ctl.empty[tile % C::SLOTS])); };
+            auto scores = [&](int x, int half, uint32_t tile) {
+                for (int k = 0; k < k_pieces; ++k) {
+                    const uint32_t at = (k / 4) * (128 * 128) + (k % 4) * 32;
+                    mma_ss(s_at[x], smem_desc(q_tile + half * C::TILE + at, 16), smem_desc(slot(tile) + at, 16), s_shape, k > 0);
+                }
+                mma_commit(bar(ctl.s_full[x]));
+            };
+            auto values = [&](int x, uint32_t tile, bool add) {
+                ok = ok && mbar_wait(bar(ctl.p_full[x]), done[x] & 1, abort_word);
+                ++done[x];
+                if (!ok) return;
+                tmem_fence_after();
+#pragma unroll
+                for (int k = 0; k < 8; ++k) mma_ts(o_at[x], s_at[x] + k * 8, smem_desc(slot(tile) + k * 2048, 128 * 128), o_shape, add || k > 0);
+                mma_commit(bar(ctl.o_full[x]));
+            };
+            for (bool more = it.begin(p, FWD_GEO, w.unit_start, unit0, unit1); more && ok; more = it.next(p, FWD_GEO), ++items) {
+                const int n = it.i1 - it.i0;
+                const bool two = it.g.nq * p.group - it.t * FWD_ROWS > 128;
+                ok = ok && mbar_wait(bar(ctl.q_full), items & 1, abort_word);
+                wait_tile(tile0);
+                if (!ok) break;
+                scores(0, 0, tile0);
+                if (two) {
+                    scores(1, 1, tile0);
+                    release(tile0);
+                } else {
+                    release(tile0);
+                    if (n > 1) {
+                        wait_tile(tile0 + 2);
+                        if (!ok) break;
+                        scores(1, 0, tile0 + 2);
+                        release(tile0 + 2);
+                    }
+                }
+                const int ahead = two ? 1 : 2;
+                for (int i = 0; i < n && ok; ++i) {
+                    const uint32_t v = tile0 + 2 * i + 1, k_next = tile0 + 2 * (i + ahead);
+                    const bool more_keys = i + ahead < n;
+                    wait_tile(v);
+                    const int x = two ? 0 : i & 1;
+                    values(x, v, i >= ahead);
+                    if (!two && ok) release(v);
+                    if (more_keys) {
+                        wait_tile(k_next);
+                        if (!ok) break;
+                        scores(x, 0, k_next);
+                        if (!two) release(k_next);
+                    }
+                    if (two) {
+                        values(1, v, i > 0);
+                        if (!ok) break;
+                        release(v);
+                        if (more_keys) { scores(1, 1, k_next); release(k_next); }
+                    }
+                }
+                if (!ok) break;
+                mma_commit(bar(ctl.q_empty));
+                tile0 += 2 * n;
+            }
+            mma_commit(bar(ctl.drain));
+            mbar_wait(bar(ctl.drain), 0, &ctl.never);
+        }
+        __syncwarp();
+    } else {
+        // ---------------------------------------------------------------- softmax
+        const int x = warp / 4;
+        const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
+        const int row = threadIdx.x & 127;
+        const uint32_t S = s_at[x] + lanes;
+        const float scale2 = fmaxf(fabsf(p.scale) * LOG2E_F, 1e-30f);     // (not zero: masked scores are -inf)
+        constexpr float BIAS = sizeof(T) == 2 && operand_type<T>() == 0 ? 7.f : 0.f;     // fp16: weights up to 2^15, so that small ones keep their digits
+        uint32_t step0 = 0, s_done = 0, o_base[2] = {0, 0};
+        bool ok = true;
+        for (bool more = it.begin(p, FWD_GEO, w.unit_start, unit0, unit1); more; more = it.next(p, FWD_GEO)) {
+            const int n = it.i1 - it.i0;
+            const int rows = min(it.g.nq * p.group - it.t * FWD_ROWS, FWD_ROWS);
+            const bool two = rows > 128;
+            const int tile_row = two ? x * 128 + row : row;
+            const bool valid = tile_row < rows;
+            const bool warp_on = (tile_row & ~31) < rows;
+            const int packed = it.t * FWD_ROWS + tile_row;
+            const int limit = p.causal && valid ? keys_of_row(p, it.g, packed / p.group) : it.g.nk;
+            float m = -INFINITY, l = 0.f;               // reference of the exponents (log2), mass relative to 2^(m - BIAS)
+            uint32_t mine = 0;                          // steps of this warpgroup in this item
+            for (int i = two ? 0 : x; i < n; i += two ? 1 : 2, ++mine, ++s_done) {
+                const uint32_t step = step0 + i, ring_at = step % MASK_RING;
+                ok = ok && mbar_wait(bar(ctl.mask_full[ring_at]), (step / MASK_RING) & 1, abort_word) && mbar_wait(bar(ctl.s_full[x]), s_done & 1, abort_word);
+                ok = __all_sync(~0u, ok);
+                if (!ok) { m = l = __int_as_float(0x7fffffff); continue; }
+                tmem_fence_after();
+                if (warp_on) {
+                    uint32_t keep[4];
+                    const int lim = limit - (it.i0 + i) * FWD_STEP;
+                    bool whole = true;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int bits = lim - 32 * k;
+                        keep[k] = ctl.mask[ring_at][k] & (bits >= 32 ? ~0u : bits <= 0 ? 0u : (1u << bits) - 1);
+                        whole = whole && keep[k] == ~0u;
+                    }
+                    whole = __all_sync(~0u, whole);
+                    float top = -INFINITY;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t v[32];
+                        tmem_ld32(S + 32 * c, v);
+                        tmem_wait_ld();
+                        if (!whole)
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) if (!(keep[c] >> k & 1)) v[k] = 0xff800000u;
+#pragma unroll
+                        for (int k = 0; k < 32; k += 2) top = max3(top, __uint_as_float(v[k]), __uint_as_float(v[k + 1]));
+                    }
+                    top *= scale2;
+                    const bool grown = top > m + RESCALE_AT || (m == -INFINITY && top > -INFINITY);
+                    const float m_new = grown ? top : m;
+                    const float fade = grown ? ex2(m - m_new) : 1.f;
+                    if (mine && __any_sync(~0u, grown)) {
+                        ok = mbar_wait(bar(ctl.o_full[x]), (o_base[x] + mine - 1) & 1, abort_word);
+                        ok = __all_sync(~0u, ok);
+                        if (!ok) { m = l = __int_as_float(0x7fffffff); continue; }
+                        tmem_fence_after();
+#pragma unroll
+                        for (int c = 0; c < DP / 32; ++c) {
+                            uint32_t v[32];
+                            tmem_ld32(o_at[x] + lanes + 32 * c, v);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * fade);
+                            tmem_st32(o_at[x] + lanes + 32 * c, v);
+                        }
+                    }
+                    m = m_new;
+                    l *= fade;
+                    const float shift = m == -INFINITY ? 0.f : BIAS - m;
+                    const f32x2 sc2 = dup2(scale2), sh2 = dup2(shift);
+                    f32x2 sum = pack2(0.f, 0.f);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t v[32], out[16];
+                        tmem_ld32(S + 32 * c, v);
+                        tmem_wait_ld();
+                        if (!whole)
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) if (!(keep[c] >> k & 1)) v[k] = 0xff800000u;
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {
+                            float a, b;
+                            unpack2(fma2(pack2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), sc2, sh2), a, b);
+                            a = ex2(a);
+                            b = ex2(b);
+                            sum = add2(sum, pack2(a, b));
+                            out[k] = pack_half<T>(a, b);
+                        }
+                        tmem_st16(S + 16 * c, out);
+                    }
+                    float a, b;
+                    unpack2(sum, a, b);
+                    l += a + b;
+                    tmem_wait_st();
+                }
+                tmem_fence_before();
+                mbar_arrive(bar(ctl.p_full[x]));
+            }
+            // ---- the item's end: join the two states of a short tile, then finish the rows or put them aside
+            const uint32_t made[2] = {two ? (uint32_t)n : (uint32_t)(n + 1) / 2, two ? (uint32_t)n : (uint32_t)n / 2};
+            for (int y = 0; y < 2; ++y)
+                if (made[y] && ok && (!two || y == x)) ok = mbar_wait(bar(ctl.o_full[y]), (o_base[y] + made[y] - 1) & 1, abort_word);
+            ok = __all_sync(~0u, ok);
+            if (!ok) l = __int_as_float(0x7fffffff);
+            tmem_fence_after();
+            float w0 = 1.f, w1 = 0.f;               // factors of this warpgroup's rows: two halves have one state each
+            if (!two) {
+                ctl.m[x][row] = m;
+                ctl.l[x][row] = l;
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                const float ma = ctl.m[0][row], mb = ctl.m[1][row];
+                m = fmaxf(ma, mb);
+                w0 = ma == -INFINITY ? 0.f : ex2(ma - m);
+                w1 = mb == -INFINITY ? 0.f : ex2(mb - m);
+                l = ctl.l[0][row] * w0 + ctl.l[1][row] * w1;
+            }
+            const bool whole_tile = it.i0 == 0 && it.i1 == it.steps;
+            const long long part = (2LL * blockIdx.x + (it.i0 == 0)) * w.rows + tile_row;
+            const PackedRow pr = packed_row(p, it.g, it.h, packed);
+            const long long out_row = (long long)pr.row * p.heads + pr.head;
+            const float finish = l > 0.f || l != l ? 1.f / l : 0.f;
+            const int c0 = two ? 0 : x * (DP / 64), c1 = two ? DP / 32 : c0 + DP / 64;
+            if (warp_on)
+                for (int c = c0; c < c1; ++c) {
+                    uint32_t v[32], u[32];
+                    tmem_ld32(o_at[two ? x : 0] + lanes + 32 * c, v);
+                    if (!two && made[1]) tmem_ld32(o_at[1] + lanes + 32 * c, u);
+                    tmem_wait_ld();
+                    if (!two)
+#pragma unroll
+                        for (int k = 0; k < 32; ++k)
+                            v[k] = __float_as_uint(__uint_as_float(v[k]) * w0 + (made[1] ? __uint_as_float(u[k]) * w1 : 0.f));
+                    if (!valid) continue;
+                    if (whole_tile) {
+                        uint4* out = reinterpret_cast<uint4*>((T*)p.out + out_row * p.D + 32 * c);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            if (32 * c + 8 * k >= p.D) continue;
+                            uint32_t o[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                o[e] = pack_half<T>(finish == 0.f ? 0.f : __uint_as_float(v[8 * k + 2 * e]) * finish, finish == 0.f ? 0.f : __uint_as_float(v[8 * k + 2 * e + 1]) * finish);
+                            out[k] = make_uint4(o[0], o[1], o[2], o[3]);
+                        }
+                    } else {
+                        uint4* out = reinterpret_cast<uint4*>(w.part_o + part * DP + 32 * c);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) out[k] = make_uint4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+                    }
+                }
+            if (valid && (two || x == 0)) {
+                if (!whole_tile) w.part_ml[part] = make_float2(m - BIAS, l);
+                else if (p.lse) p.lse[out_row] = l == 0.f ? -INFINITY : (m - BIAS + log2f(l)) * LN2_F;
+            }
+            tmem_fence_before();
+            if (!two) asm volatile("bar.sync 2, 256;" ::: "memory");
+            step0 += n;
+            o_base[0] += made[0];
+            o_base[1] += made[1];
+        }
+    }
+    tmem_fence_before();
+    __syncthreads();
+    if (warp == 12) { tmem_fence_after(); tmem_free(tmem, 512); }
+}
+
+// Joins the partial states of a tile that several blocks shared, in the order of its steps.  blockIdx.x: the block in which a tile
+// ends that began in an earlier one; its rows are dealt over blockIdx.y.  Up to FEW parts: a warp per row.  More (few rows, a long
+// axis): the block's warps share a row's parts.
+constexpr int JOIN_WARPS = 8, JOIN_Y = 16, JOIN_FEW = 8;
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(JOIN_WARPS * 32) attention_join_kernel(const AttnParams p, const FwdWork w) {
+    const long long units = w.unit_start[p.n_seg];
+    const long long blocks = blocks_for(units, gridDim.x, FWD_LEAST);
+    if (blockIdx.x >= blocks || units == 0) return;
+    const long long unit0 = blockIdx.x * units / blocks, unit1 = (blockIdx.x + 1LL) * units / blocks;
+    Walker it;
+    if (!it.begin(p, FWD_GEO, w.unit_start, unit0, unit1) || it.i0 == 0 || it.i1 < it.steps) return;
+    const int first = (int)(((unit0 - it.i0 + 1) * blocks - 1) / units);        // the block in which the tile begins
+    const int parts = (int)blockIdx.x - first + 1;
+    const int rows = min(it.g.nq * p.group - it.t * FWD_ROWS, FWD_ROWS);
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    constexpr int E = DP / 32;
+    __shared__ float sh_m[JOIN_WARPS], sh_l[JOIN_WARPS], sh_o[JOIN_WARPS][DP];
+    const bool few = parts <= JOIN_FEW;
+    for (int r = few ? blockIdx.y * JOIN_WARPS + warp : blockIdx.y; r < rows; r += few ? JOIN_Y * JOIN_WARPS : JOIN_Y) {
+        const int a = few ? 0 : parts * warp / JOIN_WARPS, b = few ? parts : parts * (warp + 1) / JOIN_WARPS;
+        float m = -INFINITY, l = 0.f, o[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = 0.f;
+        for (int k0 = a; k0 < b; k0 += 32) {
+            const int k = k0 + lane;
+            float2 ml = make_float2(-INFINITY, 0.f);
+            if (k < b) ml = w.part_ml[(2LL * (first + k) + (k == 0)) * w.rows + r];
+            float top = ml.x != ml.x ? INFINITY : ml.x;
+#pragma unroll
+            for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+            top = fmaxf(top, m);
+            const float fade = m == -INFINITY ? 0.f : ex2(m - top);
+            const float f = ml.x == -INFINITY ? 0.f : ex2(ml.x - top);
+            float mass = f * ml.y;
+#pragma unroll
+            for (int d = 16; d; d >>= 1) mass += __shfl_xor_sync(~0u, mass, d);
+            l = l * fade + mass;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] *= fade;
+            m = top;
+            const int here = min(32, b - k0);
+#pragma unroll 8
+            for (int j = 0; j < here; ++j) {
+                const float fj = __shfl_sync(~0u, f, j);
+                const float* src = w.part_o + ((2LL * (first + k0 + j) + (k0 + j == 0)) * w.rows + r) * DP;
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[e] += fj * src[lane + 32 * e];
+            }
+        }
+        if (!few) {
+            if (lane == 0) { sh_m[warp] = m; sh_l[warp] = l; }
+#pragma unroll
+            for (int e = 0; e < E; ++e) sh_o[warp][lane + 32 * e] = o[e];
+            __syncthreads();
+            if (warp == 0) {
+                float top = -INFINITY;
+                for (int k = 0; k < JOIN_WARPS; ++k) top = fmaxf(top, sh_m[k]);
+                l = 0.f;
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[e] = 0.f;
+                for (int k = 0; k < JOIN_WARPS; ++k) {
+                    const float f = sh_m[k] == -INFINITY ? 0.f : ex2(sh_m[k] - top);
+                    l += f * sh_l[k];
+#pragma unroll
+                    for (int e = 0; e < E; ++e) o[e] += f * sh_o[k][lane + 32 * e];
+                }
+                m = top;
+            }
+            __syncthreads();
+        }
+        if (few || warp == 0) {
+            const PackedRow pr = packed_row(p, it.g, it.h, it.t * FWD_ROWS + r);
+            const long long out_row = (long long)pr.row * p.heads + pr.head;
+            const float finish = l > 0.f || l != l ? 1.f / l : 0.f;
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (lane + 32 * e < p.D) ((T*)p.out)[out_row * p.D + lane + 32 * e] = Half<T>::from(finish == 0.f ? 0.f : o[e] * finish);
+            if (lane == 0 && p.lse) p.lse[out_row] = l == 0.f ? -INFINITY : (m + log2f(l)) * LN2_F;
+        }
+    }
+}
+
+static int device_sms() {
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    return sms;
+}
+
+size_t attention_forward_carve(const AttnParams& p, void* ws, FwdWork* w) {
+    const size_t slots = 2 * (size_t)MAX_SMS;
+    const long long packed = (long long)p.n_q * p.group;
+    w->rows = (int)(packed < FWD_ROWS ? packed : FWD_ROWS);
+    Carver cv(ws);
+    w->unit_start = cv.take<long long>((size_t)p.n_seg + 1);
+    w->part_ml = cv.take<float2>(slots * w->rows);
+    w->part_o = cv.take<float>(slots * w->rows * (p.D > 64 ? 128 : 64));
+    return cv.off;
+}
+size_t attention_forward_bytes(const AttnParams& p) { FwdWork w; return attention_forward_carve(p, nullptr, &w); }
+
+template <typename T, int DP>
+static tiga_status launch_forward(const AttnParams& p, const FwdWork& w, cudaStream_t s) {
+    int sms = device_sms();
+    if (sms <= 0) return TIGA_ERR_CUDA;
+    if (sms > MAX_SMS) sms = MAX_SMS;
+    // asked for on every call: the attribute belongs to the current device
+    TIGA_CUDA_TRY(cudaFuncSetAttribute(attention_forward_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, Fwd<DP>::SMEM));
+    attention_plan_kernel<<<counted(1), PLAN_THREADS, 0, s>>>(p, FWD_GEO, const_cast<long long*>(w.unit_start));
+    attention_forward_kernel<T, DP><<<counted((unsigned)sms), FWD_THREADS, Fwd<DP>::SMEM, s>>>(p, w);
+    note_launch();
+    attention_join_kernel<T, DP><<<dim3(sms, JOIN_Y), JOIN_WARPS * 32, 0, s>>>(p, w);
+    return launch_status();
+}
+
+tiga_status attention_forward(const AttnParams& p, bool bf16, void* ws, cudaStream_t s) {
+    FwdWork w;
+    attention_forward_carve(p, ws, &w);
+    if (bf16) return p.D > 64 ? launch_forward<__nv_bfloat16, 128>(p, w, s) : launch_forward<__nv_bfloat16, 64>(p, w, s);
+    return p.D > 64 ? launch_forward<__half, 128>(p, w, s) : launch_forward<__half, 64>(p, w, s);
+}
+
+}  // namespace tiga
