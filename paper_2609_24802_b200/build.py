@@ -12,7 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libtiga.so")
 LIB_CHECKED = os.path.join(HERE, "libtiga_checked.so")      # same sources with -DTIGA_CHECKED (range-checked indices)
-SOURCES = ["csr.cu", "csr_plan.cu", "csr_attention.cu", "attention.cu", "attention_forward.cu", "rotary.cu", "radius.cu", "radius_lj.cu", "radius_mlp.cu", "knn.cu"]
+SOURCES = ["csr.cu", "csr_plan.cu", "csr_attention.cu", "attention.cu", "attention_forward.cu", "attention_backward.cu", "rotary.cu", "radius.cu", "radius_lj.cu", "radius_mlp.cu", "knn.cu"]
 NVCC_FLAGS = ["-std=c++17", "-O3", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
               "-Xcompiler", "-fPIC", "-I" + INCLUDE, "-I" + CSRC]
 

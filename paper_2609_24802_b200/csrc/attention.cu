@@ -1,105 +1,7 @@
-// Online-softmax reducer over dense and paged relations: entry points; gradients by a warp per row or per key.
+// Online-softmax reducer over dense and paged relations: entry points and their checks.
 #include "attention_shared.cuh"
 
 namespace tiga {
-
-constexpr int ATTN_WARPS = 4;
-
-__device__ __forceinline__ float warp_sum(float v) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
-    return v;
-}
-
-// the segment that holds row i (the last one that starts at or before it), or -1
-__device__ __forceinline__ int segment_of_row(const int32_t* start, int n_seg, int n_rows, int i) {
-    int lo = 0, hi = n_seg;
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (start[mid] <= i) lo = mid + 1; else hi = mid;
-    }
-    if (lo == 0 || i >= clamp_to(start[lo], n_rows)) return -1;
-    return lo - 1;
-}
-
-template <typename T>
-__device__ __forceinline__ void load4(const T* base, int D, int lane, float (&r)[4]) {
-#pragma unroll
-    for (int c = 0; c < 4; ++c) r[c] = lane + 32 * c < D ? Half<T>::to(base[lane + 32 * c]) : 0.f;
-}
-__device__ __forceinline__ float dot4(const float (&a)[4], const float (&b)[4]) {
-    return warp_sum(a[0] * b[0] + a[1] * b[1] + a[2] * b[2] + a[3] * b[3]);
-}
-
-template <typename T>
-__global__ void attn_grad_q_kernel(const AttnParams p) {
-    const long long w = (long long)blockIdx.x * ATTN_WARPS + threadIdx.x / 32;
-    const int lane = threadIdx.x % 32;
-    if (w >= (long long)p.n_q * p.heads) return;
-    const int i = (int)(w / p.heads), h = (int)(w % p.heads), hk = h / p.group;
-    const int s = segment_of_row(p.q_start, p.n_seg, p.n_q, i);
-    if (s < 0) return;
-    const Segment g = segment_of(p, s);
-    float q[4], go[4], o[4], a[4] = {0, 0, 0, 0};
-    load4((const T*)p.q + i * p.q_row + h * p.q_head, p.D, lane, q);
-    load4((const T*)p.go + i * p.go_row + h * p.go_head, p.D, lane, go);
-    load4((const T*)p.o + w * p.D, p.D, lane, o);
-    const float delta = dot4(go, o), lse = p.lse_in[w];
-    for (int j = 0; j < g.nk; ++j) {
-        if (p.mask && !p.mask[g.k0 + j]) continue;
-        float k[4], v[4];
-        load4((const T*)p.k + (g.k0 + j) * p.k_row + hk * p.k_head, p.D, lane, k);
-        load4((const T*)p.v + (g.k0 + j) * p.v_row + hk * p.v_head, p.D, lane, v);
-        const float ds = exp2f((dot4(q, k) * p.scale - lse) * LOG2E_F) * (dot4(go, v) - delta) * p.scale;
-#pragma unroll
-        for (int x = 0; x < 4; ++x) a[x] += ds * k[x];
-    }
-#pragma unroll
-    for (int x = 0; x < 4; ++x)
-        if (lane + 32 * x < p.D) ((T*)p.gq)[w * p.D + lane + 32 * x] = Half<T>::from(a[x]);
-}
-
-template <typename T>
-__global__ void attn_grad_kv_kernel(const AttnParams p) {
-    const long long w = (long long)blockIdx.x * ATTN_WARPS + threadIdx.x / 32;
-    const int lane = threadIdx.x % 32;
-    if (w >= (long long)p.n_kv * p.kv_heads) return;
-    const int j = (int)(w / p.kv_heads), hk = (int)(w % p.kv_heads);
-    const int s = segment_of_row(p.kv_start, p.n_seg, p.n_kv, j);
-    if (s < 0) return;
-    const Segment g = segment_of(p, s);
-    float k[4], v[4], a[4] = {0, 0, 0, 0}, b[4] = {0, 0, 0, 0};
-    load4((const T*)p.k + j * p.k_row + hk * p.k_head, p.D, lane, k);
-    load4((const T*)p.v + j * p.v_row + hk * p.v_head, p.D, lane, v);
-    const bool on = !p.mask || p.mask[j];
-    for (int i = g.q0; on && i < g.q0 + g.nq; ++i)
-        for (int h = hk * p.group; h < (hk + 1) * p.group; ++h) {
-            const long long r = (long long)i * p.heads + h;
-            float q[4], go[4], o[4];
-            load4((const T*)p.q + i * p.q_row + h * p.q_head, p.D, lane, q);
-            load4((const T*)p.go + i * p.go_row + h * p.go_head, p.D, lane, go);
-            load4((const T*)p.o + r * p.D, p.D, lane, o);
-            const float pr = exp2f((dot4(q, k) * p.scale - p.lse_in[r]) * LOG2E_F);
-            const float ds = pr * (dot4(go, v) - dot4(go, o)) * p.scale;
-#pragma unroll
-            for (int x = 0; x < 4; ++x) { a[x] += ds * q[x]; b[x] += pr * go[x]; }
-        }
-#pragma unroll
-    for (int x = 0; x < 4; ++x)
-        if (lane + 32 * x < p.D) {
-            if (p.gk) ((T*)p.gk)[w * p.D + lane + 32 * x] = Half<T>::from(a[x]);
-            if (p.gv) ((T*)p.gv)[w * p.D + lane + 32 * x] = Half<T>::from(b[x]);
-        }
-}
-
-static unsigned warps_grid(long long n) { return (unsigned)((n + ATTN_WARPS - 1) / ATTN_WARPS); }
-
-template <typename T>
-static tiga_status attn_backward(const AttnParams& p, void*, cudaStream_t s) {
-    if (p.gq && p.n_q) attn_grad_q_kernel<T><<<counted(warps_grid((long long)p.n_q * p.heads)), ATTN_WARPS * 32, 0, s>>>(p);
-    if ((p.gk || p.gv) && p.n_kv) attn_grad_kv_kernel<T><<<counted(warps_grid((long long)p.n_kv * p.kv_heads)), ATTN_WARPS * 32, 0, s>>>(p);
-    return launch_status();
-}
 
 // ------------------------------------------------------------------------------------------------ host checks
 
@@ -166,7 +68,7 @@ using namespace tiga;
 extern "C" size_t tiga_dense_attention_workspace_bytes(const tiga_dense* g, const tiga_heads* h, int backward) {
     AttnParams p;
     if (dense_check(g, h, &p) != TIGA_OK) return 0;
-    return (backward ? 0 : attention_forward_bytes(p)) + 256;
+    return (backward ? attention_backward_bytes(p) : attention_forward_bytes(p)) + 256;
 }
 
 extern "C" tiga_status tiga_apply_dense_attention(const tiga_dense* g, const tiga_heads* h, const void* q, const void* key, const void* value,
@@ -203,7 +105,7 @@ extern "C" tiga_status tiga_apply_dense_attention_backward(const tiga_dense* g, 
     p.q = q; p.k = key; p.v = value; p.o = out; p.lse_in = lse; p.go = grad_out;
     p.gq = grad_q; p.gk = grad_key; p.gv = grad_value;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return h->dtype == TIGA_F16 ? attn_backward<__half>(p, ws, s) : attn_backward<__nv_bfloat16>(p, ws, s);
+    return attention_backward(p, h->dtype == TIGA_BF16, ws, s);
 }
 
 extern "C" size_t tiga_paged_attention_workspace_bytes(const tiga_pages* c, const tiga_heads* h, int64_t n_q) {

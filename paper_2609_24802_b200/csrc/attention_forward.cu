@@ -1,6 +1,6 @@
 // Online-softmax reducer over dense and paged relations, forward, on the fifth-generation tensor cores.
 #include "attention_shared.cuh"
-#include "tcgen.cuh"
+#include "attention_tiles.cuh"
 
 namespace tiga {
 
@@ -41,31 +41,7 @@ struct FwdWork {
     int rows;                       // packed rows that a partial state holds at most
 };
 
-// packed row r of kv head h: offsets of its row in arrays with strides
-struct PackedRow { int row, head; };
-__device__ __forceinline__ PackedRow packed_row(const AttnParams& p, const Segment& g, int h, int r) {
-    const int t = r / p.group;
-    return {g.q0 + t, h * p.group + (r - t * p.group)};
-}
-
-// 32 rows of a tile by one warp: lane l holds row l's element offset (or -1: zeros; `any` is an
-// address that may be read).  The tile consists of blocks of 64 features, rows
-// of 128 bytes swizzled in groups of eight.
-template <int DP, int TILE_ROWS>
-__device__ __forceinline__ void copy_rows(uint32_t tile, int first_row, const void* base, long long off, int D, const void* any) {
-    constexpr int CH = DP / 8;
-    const int lane = threadIdx.x % 32, c = lane % CH;
-    const bool in_width = c * 8 < D;
-#pragma unroll
-    for (int k = 0; k < CH; ++k) {
-        const int r = k * (32 / CH) + lane / CH;
-        const long long o = __shfl_sync(~0u, off, r);
-        const int row = first_row + r;
-        const bool on = o >= 0 && in_width;
-        cp_async16(tile + (c / 8) * (TILE_ROWS * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4),
-                   on ? (const char*)base + (o + c * 8) * 2 : (const char*)any, on);
-    }
-}
+static __global__ void __launch_bounds__(PLAN_THREADS) forward_plan_kernel(const AttnParams p, long long* unit_start) { plan_units(p, FWD_GEO, unit_start); }
 
 template <typename T, int DP>
 __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const AttnParams p, const FwdWork w) {
@@ -121,7 +97,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
                     const PackedRow pr = packed_row(p, it.g, it.h, it.t * FWD_ROWS + r);
                     off = pr.row * p.q_row + pr.head * p.q_head;
                 }
-                copy_rows<DP, 128>(q_tile + x * C::TILE, 32 * pw, p.q, off, p.D, p.q);
+                copy_rows<DP, 128, 32>(q_tile + x * C::TILE, 32 * pw, p.q, off, p.D, p.q);
             }
             cp_async_arrive(bar(ctl.q_full));
             for (int i = it.i0; i < it.i1; ++i, ++steps) {
@@ -136,7 +112,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
                     if (!(ok = slot_free())) break;
                     const long long row = p.table ? 1 : kv ? p.v_row : p.k_row;
                     const long long off = here < 0 ? -1 : here * row + it.h * (kv ? p.v_head : p.k_head);
-                    copy_rows<DP, 128>(ring + (tiles % C::SLOTS) * C::TILE, 32 * pw, kv ? p.v : p.k, off, p.D, p.q);
+                    copy_rows<DP, 128, 32>(ring + (tiles % C::SLOTS) * C::TILE, 32 * pw, kv ? p.v : p.k, off, p.D, p.q);
                     cp_async_arrive(bar(ctl.full[tiles % C::SLOTS]));
                 }
                 if (!ok) break;
@@ -473,12 +449,6 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) attention_join_kernel(const A
     }
 }
 
-static int device_sms() {
-    int dev = 0, sms = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
-    return sms;
-}
-
 size_t attention_forward_carve(const AttnParams& p, void* ws, FwdWork* w) {
     const size_t slots = 2 * (size_t)MAX_SMS;
     const long long packed = (long long)p.n_q * p.group;
@@ -493,15 +463,13 @@ size_t attention_forward_bytes(const AttnParams& p) { FwdWork w; return attentio
 
 template <typename T, int DP>
 static tiga_status launch_forward(const AttnParams& p, const FwdWork& w, cudaStream_t s) {
-    int sms = device_sms();
+    const int sms = attention_grid();
     if (sms <= 0) return TIGA_ERR_CUDA;
-    if (sms > MAX_SMS) sms = MAX_SMS;
     // asked for on every call: the attribute belongs to the current device
     TIGA_CUDA_TRY(cudaFuncSetAttribute(attention_forward_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, Fwd<DP>::SMEM));
-    attention_plan_kernel<<<counted(1), PLAN_THREADS, 0, s>>>(p, FWD_GEO, const_cast<long long*>(w.unit_start));
+    forward_plan_kernel<<<counted(1), PLAN_THREADS, 0, s>>>(p, const_cast<long long*>(w.unit_start));
     attention_forward_kernel<T, DP><<<counted((unsigned)sms), FWD_THREADS, Fwd<DP>::SMEM, s>>>(p, w);
-    note_launch();
-    attention_join_kernel<T, DP><<<dim3(sms, JOIN_Y), JOIN_WARPS * 32, 0, s>>>(p, w);
+    attention_join_kernel<T, DP><<<counted(dim3(sms, JOIN_Y)), JOIN_WARPS * 32, 0, s>>>(p, w);
     return launch_status();
 }
 

@@ -149,9 +149,9 @@ struct Walker {
     }
 };
 
-// unit_start[s]: units in front of segment s.  One block.
+// unit_start[s]: units in front of segment s.  By one block.
 constexpr int PLAN_THREADS = 1024;
-static __global__ void __launch_bounds__(PLAN_THREADS) attention_plan_kernel(const AttnParams p, const Geometry geo, long long* unit_start) {
+static __device__ void plan_units(const AttnParams& p, const Geometry geo, long long* unit_start) {
     __shared__ long long warp_total[PLAN_THREADS / 32];
     long long before = 0;
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
@@ -179,6 +179,8 @@ static __global__ void __launch_bounds__(PLAN_THREADS) attention_plan_kernel(con
 constexpr int MAX_SMS = 160;            // blocks that workspaces provide for
 
 size_t attention_forward_bytes(const AttnParams& p);
+size_t attention_backward_bytes(const AttnParams& p);
+tiga_status attention_backward(const AttnParams& p, bool bf16, void* ws, cudaStream_t s);
 tiga_status attention_forward(const AttnParams& p, bool bf16, void* ws, cudaStream_t s);
 
 // host checks of the descriptors (attention.cu)
