@@ -1,7 +1,62 @@
 // Online-softmax reducer over dense and paged relations: entry points and their checks.
-#include "attention_shared.cuh"
+#include "attention_tiles.cuh"
 
 namespace tiga {
+
+// ------------------------------------------------------------------------------------------------ tensor maps
+
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// the driver's encoder (NULL: there is none, rows are copied one by one)
+static EncodeTiled encoder() {
+    static const EncodeTiled f = [] {
+        void* fn = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            return (EncodeTiled) nullptr;
+        }
+        return (EncodeTiled)fn;
+    }();
+    return f;
+}
+
+// dims and strides (elements) from the features outwards; boxes of 64 features.  Strides of zero (shared storage) have no map.
+static bool encode(CUtensorMap* m, bool bf16, const void* base, const long long (&dim)[4], const long long (&stride)[3], int box1, int box2) {
+    cuuint64_t d[4], st[3];
+    for (int i = 0; i < 4; ++i) {
+        if (dim[i] < 1 || dim[i] > 0xffffffffLL) return false;
+        d[i] = dim[i];
+    }
+    for (int i = 0; i < 3; ++i) {
+        if (stride[i] <= 0 && dim[i + 1] > 1) return false;
+        if (stride[i] >= 1LL << 38) return false;
+        st[i] = (dim[i + 1] > 1 ? stride[i] : 64) * 2;          // (of a single entry: any)
+    }
+    const cuuint32_t box[4] = {64, (cuuint32_t)box1, (cuuint32_t)box2, 1}, one[4] = {1, 1, 1, 1};
+    return encoder()(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void*>(base), d, st, box, one,
+                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+void make_tile_maps(AttnParams* p, bool bf16, TileMaps* m) {
+    p->kv_box = p->q_box = 0;
+    if (!encoder()) return;
+    if (p->n_q > 0 && 32 % p->group == 0) {
+        const long long dim[4] = {p->D, p->heads, p->n_q, 1};
+        const bool q = encode(&m->q, bf16, p->q, dim, {p->q_head, p->q_row, 64}, p->group, 32 / p->group);
+        p->q_box = q && (!p->go || encode(&m->go, bf16, p->go, dim, {p->go_head, p->go_row, 64}, p->group, 32 / p->group)) ? 32 : 0;
+    }
+    // pages: the rows of a box lie in one page and begin on a group of eight
+    int box = 32;
+    while (p->table && box >= 8 && p->page_size % box) box /= 2;
+    if (box < 8) return;
+    const long long dense[4] = {p->D, p->n_kv, p->kv_heads, 1}, paged[4] = {p->D, p->page_size, p->kv_heads, p->n_pages};
+    const bool ok = p->table
+        ? encode(&m->k, bf16, p->k, paged, {p->slot_stride, p->k_head, p->page_stride}, box, 1) && encode(&m->v, bf16, p->v, paged, {p->slot_stride, p->v_head, p->page_stride}, box, 1)
+        : encode(&m->k, bf16, p->k, dense, {p->k_row, p->k_head, 64}, box, 1) && encode(&m->v, bf16, p->v, dense, {p->v_row, p->v_head, 64}, box, 1);
+    p->kv_box = ok ? box : 0;
+}
 
 // ------------------------------------------------------------------------------------------------ host checks
 

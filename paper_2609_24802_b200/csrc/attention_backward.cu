@@ -4,36 +4,46 @@
 namespace tiga {
 
 // Two kernels of one form.  A block keeps a stationary tile of 128 rows of two arrays, X1 and X2, and goes through the other side in
-// steps of 64 rows of Y1 and Y2:
+// steps of 128 rows of Y1 and Y2:
 //     keys and values:  X = (key, value), Y = (q, grad_out):   S = X1 Y1^T, dP = X2 Y2^T (both transposed), grad_value += P Y2,
 //                                                               grad_key += dS Y1;      all heads of a group pass by: their sum
 //     queries:          X = (q, grad_out), Y = (key, value):   S = X1 Y1^T, dP = X2 Y2^T, grad_q += dS Y1
 // with P = exp2(S - lse) and dS = P (dP - delta).  Seven products instead of the five of one kernel that adds grad_q up in memory:
 // the sums stay in tensor memory, in one order, so results are reproducible, and no fp32 gradient is written and read again.
-// S and dP have two buffers of 64 columns each, so the tensor cores form the next step's while this step's weights are made; P and dS
-// lie over them in 16 bits.  Tensor memory: 4 * 64 + 2 * 128 columns, all there is at a width of 128.
+// P lies over S and dS over dP in 16 bits (tensor memory: 128 + 128 + 2 * 128 columns, all there is).  The products run in two
+// streams that take turns: while the threads turn S into P, dP and the last step's grad_key are formed; while they turn dP into dS,
+// grad_value and the next step's S.
 // fp16: P carries 2^14 and dS a power of two from the largest norms of the rows of grad_out and value, which bound |dP - delta|: the
 // largest value cannot overflow, the smallest keep as many digits as there are.
-constexpr int BWD_THREADS = 416, BWD_ROWS = 128, BWD_STEP = 64, BWD_LEAST = 4;
-constexpr Geometry KV_GEO = {BWD_ROWS, BWD_STEP, 1}, Q_GEO = {BWD_ROWS, BWD_STEP, 0};
+constexpr int BWD_THREADS = 512, BWD_ROWS = 128, BWD_STEP = 128, BWD_LEAST = 2;
+typedef Cut<BWD_ROWS, BWD_STEP, true> KvCut;
+typedef Cut<BWD_ROWS, BWD_STEP, false> QCut;
+template <bool KV> struct CutOf { typedef QCut type; };
+template <> struct CutOf<true> { typedef KvCut type; };
+// registers of a weight, producer and matrix thread: 2 * 184 + 88 + 56 = 4 * 128, what the block is launched with
+constexpr int BWD_WEIGHT_REGS = 184, BWD_PRODUCER_REGS = 88, BWD_MMA_REGS = 56;
+// What goes along with a step's rows.  A step's first tile waits for the place of the one SLOTS tiles before, of which SLOTS / 2
+// steps at most are behind: the steps in front of those are done with their entries.
+constexpr int BWD_AUX = 4;
 
 template <int DP> struct Bwd {
-    static constexpr int X_TILE = BWD_ROWS * DP * 2, Y_TILE = BWD_STEP * DP * 2;
-    static constexpr int STAGES = DP == 128 ? 4 : 8;
-    static constexpr int CONTROL = 2 * X_TILE + STAGES * 2 * Y_TILE;
+    static constexpr int TILE = 128 * DP * 2;
+    static constexpr int SLOTS = DP == 128 ? 4 : 8;         // tiles of the ring, in the order Y1 Y2 Y1 Y2 ...
+    static_assert(SLOTS / 2 <= BWD_AUX, "entries of steps in flight");
+    static constexpr int CONTROL = (2 + SLOTS) * TILE;
     static constexpr int SMEM = CONTROL + 5120;
 };
 
 struct BwdControl {
-    unsigned long long full[8], aux_full[8], empty[8], x_full, x_empty, sp_full[2], ps_full[2], acc_full, acc_empty, drain;
+    unsigned long long full[8], empty[8], aux_full[BWD_AUX], x_full, x_empty, s_full, dp_full, p_full, ds_full, acc_full, acc_empty, drain;
     uint32_t tmem, abort_word, never, pad;
-    alignas(16) float minus_lse[8][BWD_STEP], minus_delta[8][BWD_STEP];       // keys stationary: of the step's rows
-    uint32_t mask[8][4];                                          // queries stationary: the step's keys, 16 bits a producer warp
+    alignas(16) float minus_lse[BWD_AUX][BWD_STEP], minus_delta[BWD_AUX][BWD_STEP];     // keys stationary: of the step's rows
+    uint32_t mask[BWD_AUX][4];                                                          // queries stationary: the step's keys
 };
 static_assert(sizeof(BwdControl) <= 5120, "control block");
 
 struct BwdWork {
-    const long long *kv_start_unit, *q_start_unit;
+    long long *kv_start_unit, *q_start_unit;        // NULL: the blocks count for themselves
     float2* stats;                  // [n_q, heads]: lse in log2 (+inf: the row reads nothing), delta
     uint32_t* norms;                // largest squared norms of grad_out and value rows, as bits
     float* part;                    // [2 * grid][rows][sides][DP]
@@ -52,6 +62,8 @@ constexpr int PREP_THREADS = 256;
 template <typename T>
 __global__ void __launch_bounds__(PREP_THREADS) attention_prepare_kernel(const AttnParams p, const BwdWork w) {
     constexpr bool NORMS = operand_type<T>() == 0;
+    wait_for_previous_kernel();
+    let_next_kernel_start();
     const int lane = threadIdx.x % 16;
     const int q_first = clamp_to(p.q_start[0], p.n_q), q_end = max(clamp_to(p.q_start[p.n_seg], p.n_q), q_first);
     const int k_first = clamp_to(p.kv_start[0], p.n_kv), k_end = max(clamp_to(p.kv_start[p.n_seg], p.n_kv), k_first);
@@ -106,29 +118,33 @@ __global__ void __launch_bounds__(PREP_THREADS) attention_prepare_kernel(const A
 }
 
 template <typename T, int DP, bool KV>
-__global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(const AttnParams p, const BwdWork w) {
+__global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(const AttnParams p, const BwdWork w, const __grid_constant__ TileMaps maps) {
     typedef Bwd<DP> C;
-    constexpr Geometry GEO = KV ? KV_GEO : Q_GEO;
+    typedef typename CutOf<KV>::type WorkCut;
     constexpr bool F16 = operand_type<T>() == 0;
     constexpr float BIAS = F16 ? 14.f : 0.f;
     extern __shared__ __align__(1024) unsigned char smem[];
     BwdControl& ctl = *reinterpret_cast<BwdControl*>(smem + C::CONTROL);
-    const uint32_t x_tile = smem_u32(smem), ring = x_tile + 2 * C::X_TILE;
+    const uint32_t x_tile = smem_u32(smem), ring = x_tile + 2 * C::TILE;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     volatile uint32_t* abort_word = &ctl.abort_word;
     auto bar = [&](unsigned long long& b) { return smem_u32(&b); };
 
-    const long long* unit_start = KV ? w.kv_start_unit : w.q_start_unit;
-    const long long units = unit_start[p.n_seg];
-    const long long blocks = blocks_for(units, gridDim.x, BWD_LEAST);
-    if (blockIdx.x >= blocks || units == 0) return;
-    const long long unit0 = blockIdx.x * units / blocks, unit1 = (blockIdx.x + 1LL) * units / blocks;
+    wait_for_previous_kernel();
+    let_next_kernel_start();
+    Walker<WorkCut> it;
+    bool more = it.begin(p, KV ? w.kv_start_unit : w.q_start_unit, blockIdx.x, gridDim.x, BWD_LEAST);
+    if (!more) return;
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < C::STAGES; ++i) { mbar_init(bar(ctl.full[i]), 128); mbar_init(bar(ctl.aux_full[i]), 4); mbar_init(bar(ctl.empty[i]), 1); }
-        mbar_init(bar(ctl.x_full), 128);
+        for (int i = 0; i < C::SLOTS; ++i) { mbar_init(bar(ctl.full[i]), 128); mbar_init(bar(ctl.empty[i]), 1); }
+        for (int i = 0; i < BWD_AUX; ++i) mbar_init(bar(ctl.aux_full[i]), 4);
+        mbar_init(bar(ctl.x_full), 256);
         mbar_init(bar(ctl.x_empty), 1);
-        for (int b = 0; b < 2; ++b) { mbar_init(bar(ctl.sp_full[b]), 1); mbar_init(bar(ctl.ps_full[b]), 256); }
+        mbar_init(bar(ctl.s_full), 1);
+        mbar_init(bar(ctl.dp_full), 1);
+        mbar_init(bar(ctl.p_full), 256);
+        mbar_init(bar(ctl.ds_full), 256);
         mbar_init(bar(ctl.acc_full), 1);
         mbar_init(bar(ctl.acc_empty), 256);
         mbar_init(bar(ctl.drain), 1);
@@ -140,154 +156,173 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
     __syncthreads();
     tmem_fence_after();
     const uint32_t tmem = ctl.tmem;
-    const uint32_t s_at[2] = {tmem, tmem + 128}, dp_at[2] = {tmem + 64, tmem + 192}, acc1 = tmem + 256, acc2 = tmem + 384;
+    const uint32_t s_at = tmem, dp_at = tmem + 128, acc1 = tmem + 256, acc2 = tmem + 384;
 
-    Walker it;
     if (warp >= 8 && warp < 12) {
         // ---------------------------------------------------------------- producers
+        registers_down<BWD_PRODUCER_REGS>();
         const int pw = warp - 8;
-        uint32_t steps = 0, items = 0;
+        uint32_t tiles = 0, steps = 0, items = 0;
         bool ok = true;
-        for (bool more = it.begin(p, GEO, unit_start, unit0, unit1); more && ok; more = it.next(p, GEO), ++items) {
+        auto slot_free = [&]() { return tiles < (uint32_t)C::SLOTS || mbar_wait(bar(ctl.empty[tiles % C::SLOTS]), (tiles / C::SLOTS + 1) & 1, abort_word); };
+        for (; more && ok; more = it.next(p), ++items) {
             const int packed_rows = it.g.nq * p.group;
-            if (items && !(ok = mbar_wait(bar(ctl.x_empty), (items - 1) & 1, abort_word))) break;
-            {
-                const int r = it.t * BWD_ROWS + 32 * pw + lane;
-                long long off1 = -1, off2 = -1;
-                if (KV) {
-                    const long long j = r < it.g.nk ? key_place(p, it.g, it.s, r) : -1;
-                    if (j >= 0) { off1 = j * p.k_row + it.h * p.k_head; off2 = j * p.v_row + it.h * p.v_head; }
+            // a row of the other side, or of the tile itself: where key r lies, or whether packed row r is wanted
+            Place at;
+            bool on;
+            float2 stat;
+            auto look = [&](bool keys, int r) {
+                at = {-1, 0};
+                on = false;
+                stat = make_float2(INFINITY, 0.f);
+                if (keys) {
+                    if (r < it.g.nk) at = key_place(p, it.g, it.s, r);
                 } else if (r < packed_rows) {
                     const PackedRow pr = packed_row(p, it.g, it.h, r);
-                    off1 = pr.row * p.q_row + pr.head * p.q_head;
-                    off2 = pr.row * p.go_row + pr.head * p.go_head;
-                }
-                copy_rows<DP, 128, 32>(x_tile, 32 * pw, KV ? p.k : p.q, off1, p.D, unit_start);
-                copy_rows<DP, 128, 32>(x_tile + C::X_TILE, 32 * pw, KV ? p.v : p.go, off2, p.D, unit_start);
-                cp_async_arrive(bar(ctl.x_full));
-            }
-            // a step's rows: lane l < 16 has row 16 pw + l
-            long long off1, off2;
-            float2 stat;
-            auto look = [&](int i) {
-                const int r = i * BWD_STEP + 16 * pw + lane;
-                off1 = off2 = -1;
-                stat = make_float2(INFINITY, 0.f);
-                if (lane >= 16) return;
-                if (KV) {
-                    if (r >= packed_rows) return;
-                    const PackedRow pr = packed_row(p, it.g, it.h, r);
-                    off1 = pr.row * p.q_row + pr.head * p.q_head;
-                    off2 = pr.row * p.go_row + pr.head * p.go_head;
                     stat = w.stats[(long long)pr.row * p.heads + pr.head];
-                    if (stat.x == INFINITY) off1 = off2 = -1;       // reads nothing: whatever lies there stays out of the products
-                } else {
-                    const long long j = r < it.g.nk ? key_place(p, it.g, it.s, r) : -1;
-                    if (j >= 0) { off1 = j * p.k_row + it.h * p.k_head; off2 = j * p.v_row + it.h * p.v_head; }
+                    on = stat.x != INFINITY;            // a row that reads nothing: whatever lies there stays out of the products
                 }
             };
-            look(it.i0);
+            auto fetch = [&](uint32_t tile, uint32_t full, bool keys, bool second, Place a, bool wanted, int r) {
+                if (keys) fetch_keys<DP>(tile, 32 * pw, full, p, maps, second, a, it.h, w.stats);
+                else fetch_packed<DP>(tile, 32 * pw, full, p, it.g, maps, second, it.h, r, wanted, w.stats);
+            };
+            if (items && !(ok = mbar_wait(bar(ctl.x_empty), (items - 1) & 1, abort_word))) break;
+            look(KV, it.t * BWD_ROWS + 32 * pw + lane);
+            for (int y = 0; y < 2; ++y) fetch(x_tile + y * C::TILE, bar(ctl.x_full), KV, y, at, on, it.t * BWD_ROWS + 32 * pw + lane);
+            look(!KV, it.i0 * BWD_STEP + 32 * pw + lane);
             for (int i = it.i0; i < it.i1; ++i, ++steps) {
-                const int st = steps % C::STAGES;
-                if (steps >= (uint32_t)C::STAGES && !(ok = mbar_wait(bar(ctl.empty[st]), (steps / C::STAGES + 1) & 1, abort_word))) break;
-                const long long o1 = off1, o2 = off2;
+                const Place here = at;
+                const bool wanted = on;
+                const float2 st = stat;
+                const int aux = steps % BWD_AUX;
+                if (!(ok = slot_free())) break;
                 if (KV) {
-                    if (lane < 16) { ctl.minus_lse[st][16 * pw + lane] = BIAS - stat.x; ctl.minus_delta[st][16 * pw + lane] = -stat.y; }
+                    ctl.minus_lse[aux][32 * pw + lane] = BIAS - st.x;
+                    ctl.minus_delta[aux][32 * pw + lane] = -st.y;
                 } else {
-                    const uint32_t valid = __ballot_sync(~0u, off1 >= 0) & 0xffffu;
-                    if (lane == 0) ctl.mask[st][pw] = valid;
+                    const uint32_t valid = __ballot_sync(~0u, here.at >= 0);
+                    if (lane == 0) ctl.mask[aux][pw] = valid;
                 }
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar(ctl.aux_full[st]));
-                if (i + 1 < it.i1) look(i + 1);
-                const uint32_t at = ring + st * 2 * C::Y_TILE;
-                copy_rows<DP, BWD_STEP, 16>(at, 16 * pw, KV ? p.q : p.k, o1, p.D, unit_start);
-                copy_rows<DP, BWD_STEP, 16>(at + C::Y_TILE, 16 * pw, KV ? p.go : p.v, o2, p.D, unit_start);
-                cp_async_arrive(bar(ctl.full[st]));
+                if (lane == 0) mbar_arrive(bar(ctl.aux_full[aux]));
+                if (i + 1 < it.i1) look(!KV, (i + 1) * BWD_STEP + 32 * pw + lane);
+                for (int y = 0; y < 2; ++y, ++tiles) {
+                    if (y && !(ok = slot_free())) break;
+                    fetch(ring + (tiles % C::SLOTS) * C::TILE, bar(ctl.full[tiles % C::SLOTS]), !KV, y, here, wanted, i * BWD_STEP + 32 * pw + lane);
+                }
+                if (!ok) break;
             }
         }
         cp_async_wait_all();
-    } else if (warp == 12) {
+        if (*abort_word) {          // boxes may still be on their way: their tiles, as far as they were asked for
+            for (uint32_t k = tiles < (uint32_t)C::SLOTS ? 0 : tiles - C::SLOTS; k < tiles; ++k) mbar_wait(bar(ctl.full[k % C::SLOTS]), (k / C::SLOTS) & 1, &ctl.never);
+            if (items) mbar_wait(bar(ctl.x_full), (items - 1) & 1, &ctl.never);
+        }
+    } else if (warp >= 12) {
         // ---------------------------------------------------------------- matrix instructions
-        if (lane == 0) {
+        registers_down<BWD_MMA_REGS>();
+        if (warp == 12 && lane == 0) {
             const uint32_t s_shape = mma_shape<T>(BWD_STEP, false), acc_shape = mma_shape<T>(DP, true);
             const uint32_t sign = p.scale < 0.f ? MMA_NEGATE_A : 0;
-            uint32_t step0 = 0, items = 0;
+            uint32_t tile0 = 0, steps = 0, items = 0;
             bool ok = true;
             const int pieces = (p.D + 15) / 16;
-            auto wait_full = [&](uint32_t step) {
-                ok = ok && mbar_wait(bar(ctl.full[step % C::STAGES]), (step / C::STAGES) & 1, abort_word);
+            auto slot = [&](uint32_t tile) { return ring + (tile % C::SLOTS) * C::TILE; };
+            auto wait_tile = [&](uint32_t tile) {
+                ok = ok && mbar_wait(bar(ctl.full[tile % C::SLOTS]), (tile / C::SLOTS) & 1, abort_word);
                 fence_async_proxy();
             };
-            auto stage = [&](uint32_t step) { return ring + (step % C::STAGES) * 2 * C::Y_TILE; };
-            auto scores = [&](uint32_t step) {
-                const uint32_t b = step & 1, y = stage(step);
-                for (int k = 0; k < pieces; ++k) {
-                    const uint32_t xa = (k / 4) * (BWD_ROWS * 128) + (k % 4) * 32, ya = (k / 4) * (BWD_STEP * 128) + (k % 4) * 32;
-                    mma_ss(s_at[b], smem_desc(x_tile + xa, 16), smem_desc(y + ya, 16), s_shape | sign, k > 0);
-                }
-                for (int k = 0; k < pieces; ++k) {
-                    const uint32_t xa = (k / 4) * (BWD_ROWS * 128) + (k % 4) * 32, ya = (k / 4) * (BWD_STEP * 128) + (k % 4) * 32;
-                    mma_ss(dp_at[b], smem_desc(x_tile + C::X_TILE + xa, 16), smem_desc(y + C::Y_TILE + ya, 16), s_shape, k > 0);
-                }
-                mma_commit(bar(ctl.sp_full[b]));
+            auto wait_threads = [&](unsigned long long& b, uint32_t parity) {
+                ok = ok && mbar_wait(bar(b), parity & 1, abort_word);
+                tmem_fence_after();
             };
-            for (bool more = it.begin(p, GEO, unit_start, unit0, unit1); more && ok; more = it.next(p, GEO), ++items) {
+            auto release = [&](uint32_t tile) { mma_commit(bar(ctl.empty[tile % C::SLOTS])); };
+            // d = X Y^T, features in pieces of 16
+            auto inner = [&](uint32_t d, uint32_t x, uint32_t tile, uint32_t shape) {
+                for (int k = 0; k < pieces; ++k) {
+                    const uint32_t at = (k / 4) * (128 * 128) + (k % 4) * 32;
+                    mma_ss(d, smem_desc(x + at, 16), smem_desc(slot(tile) + at, 16), shape, k > 0);
+                }
+            };
+            // acc (+)= (16-bit weights at a: 64 columns of them in the first half of each 64) Y
+            auto outer = [&](uint32_t acc, uint32_t a, uint32_t tile, bool add) {
+#pragma unroll
+                for (int k = 0; k < BWD_STEP / 16; ++k)
+                    mma_ts(acc, a + (k / 4) * 64 + (k % 4) * 8, smem_desc(slot(tile) + k * 2048, 128 * 128), acc_shape, add || k > 0);
+            };
+            for (; more && ok; more = it.next(p), ++items) {
                 const int n = it.i1 - it.i0;
                 ok = ok && mbar_wait(bar(ctl.x_full), items & 1, abort_word);
-                wait_full(step0);
+                wait_tile(tile0);
                 if (!ok) break;
-                scores(step0);
+                inner(s_at, x_tile, tile0, s_shape | sign);
+                mma_commit(bar(ctl.s_full));
+                wait_tile(tile0 + 1);
+                if (!ok) break;
+                inner(dp_at, x_tile + C::TILE, tile0 + 1, s_shape);
+                mma_commit(bar(ctl.dp_full));
+                if (!KV) release(tile0 + 1);
                 if (n == 1) mma_commit(bar(ctl.x_empty));
-                for (int i = 0; i < n; ++i) {
-                    const uint32_t step = step0 + i, b = step & 1;
-                    if (i + 1 < n) {
-                        wait_full(step + 1);
+                for (int i = 0; i < n; ++i, ++steps) {
+                    const uint32_t y1 = tile0 + 2 * i, y2 = y1 + 1;
+                    const bool again = i + 1 < n;
+                    wait_threads(ctl.p_full, steps);
+                    if (i == 0 && items) ok = ok && mbar_wait(bar(ctl.acc_empty), (items - 1) & 1, abort_word);
+                    if (!ok) break;
+                    if (KV) {
+                        outer(acc2, s_at, y2, i > 0);
+                        release(y2);
+                    }
+                    if (again) {
+                        wait_tile(y1 + 2);
                         if (!ok) break;
-                        scores(step + 1);
+                        inner(s_at, x_tile, y1 + 2, s_shape | sign);
+                        mma_commit(bar(ctl.s_full));
+                    }
+                    wait_threads(ctl.ds_full, steps);
+                    if (!ok) break;
+                    outer(acc1, dp_at, y1, i > 0);
+                    release(y1);
+                    if (again) {
+                        wait_tile(y2 + 2);
+                        if (!ok) break;
+                        inner(dp_at, x_tile + C::TILE, y2 + 2, s_shape);
+                        mma_commit(bar(ctl.dp_full));
+                        if (!KV) release(y2 + 2);
                         if (i + 2 == n) mma_commit(bar(ctl.x_empty));
                     }
-                    if (i == 0 && items) ok = ok && mbar_wait(bar(ctl.acc_empty), (items - 1) & 1, abort_word);
-                    ok = ok && mbar_wait(bar(ctl.ps_full[b]), (step / 2) & 1, abort_word);
-                    if (!ok) break;
-                    tmem_fence_after();
-                    const uint32_t y = stage(step);
-#pragma unroll
-                    for (int k = 0; k < BWD_STEP / 16; ++k) {
-                        const uint32_t a = (k / 2) * 32 + (k % 2) * 8;
-                        if (KV) mma_ts(acc2, s_at[b] + a, smem_desc(y + C::Y_TILE + k * 2048, BWD_STEP * 128), acc_shape, i > 0 || k > 0);
-                        mma_ts(acc1, dp_at[b] + a, smem_desc(y + k * 2048, BWD_STEP * 128), acc_shape, i > 0 || k > 0);
-                    }
-                    mma_commit(bar(ctl.empty[step % C::STAGES]));
                 }
                 if (!ok) break;
                 mma_commit(bar(ctl.acc_full));
-                step0 += n;
+                tile0 += 2 * n;
             }
             mma_commit(bar(ctl.drain));
             mbar_wait(bar(ctl.drain), 0, &ctl.never);
         }
         __syncwarp();
     } else {
-        // ---------------------------------------------------------------- weights: warpgroup x has 32 of a step's 64 columns
+        // ---------------------------------------------------------------- weights: warpgroup x has 64 of a step's 128 columns
+        registers_up<BWD_WEIGHT_REGS>();
         const int x = warp / 4;
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const int row = threadIdx.x & 127;
+        const uint32_t S = s_at + lanes + 64 * x, dP = dp_at + lanes + 64 * x;
         const float scale2 = fmaxf(fabsf(p.scale) * LOG2E_F, 1e-30f);
         const float factor = F16 ? gradient_factor(w.norms) : 1.f;
         const f32x2 sc2 = dup2(scale2), ds2 = dup2(F16 ? factor * 0x1p-14f : 1.f);
-        uint32_t step0 = 0, items = 0;
+        uint32_t steps = 0, items = 0;
         bool ok = true;
-        for (bool more = it.begin(p, GEO, unit_start, unit0, unit1); more; more = it.next(p, GEO), ++items) {
-            const int n = it.i1 - it.i0, r = it.t * BWD_ROWS + row;
-            const bool valid = r < stationary_rows(p, it.g, GEO);
-            const bool warp_on = (r & ~31) < stationary_rows(p, it.g, GEO);
+        for (; more; more = it.next(p), ++items) {
+            const int n = it.i1 - it.i0, r = it.t * BWD_ROWS + row, n_rows = WorkCut::rows(p, it.g);
+            const bool valid = r < n_rows;
+            const bool warp_on = (r & ~31) < n_rows;
             f32x2 my_lse = 0, my_delta = 0;
             long long out_row = 0;
             bool masked = false;
             if (KV) {
                 out_row = (long long)(it.g.k0 + r) * p.kv_heads + it.h;
-                masked = valid && key_place(p, it.g, it.s, r) < 0;
+                masked = valid && key_place(p, it.g, it.s, r).at < 0;
             } else if (valid) {
                 const PackedRow pr = packed_row(p, it.g, it.h, r);
                 out_row = (long long)pr.row * p.heads + pr.head;
@@ -296,52 +331,73 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
                 my_delta = dup2(-st.y);
                 masked = st.x == INFINITY;
             }
-            for (int i = 0; i < n; ++i) {
-                const uint32_t step = step0 + i, b = step & 1, st = step % C::STAGES;
-                ok = ok && mbar_wait(bar(ctl.aux_full[st]), (step / C::STAGES) & 1, abort_word) && mbar_wait(bar(ctl.sp_full[b]), (step / 2) & 1, abort_word);
+            for (int i = 0; i < n; ++i, ++steps) {
+                const uint32_t aux = steps % BWD_AUX;
+                ok = ok && mbar_wait(bar(ctl.aux_full[aux]), (steps / BWD_AUX) & 1, abort_word) && mbar_wait(bar(ctl.s_full), steps & 1, abort_word);
+                ok = __all_sync(~0u, ok);
+                if (!ok) continue;
+                tmem_fence_after();
+                f32x2 e[32];
+                if (warp_on) {
+                    uint32_t v[2][32];
+                    tmem_ld32(S, v[0]);
+                    tmem_ld32(S + 32, v[1]);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        const float4* nl = reinterpret_cast<const float4*>(ctl.minus_lse[aux] + 64 * x + 32 * c);
+                        const uint32_t keep = KV ? ~0u : ctl.mask[aux][2 * x + c];
+                        uint32_t out[16];
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {
+                            f32x2 lse = my_lse;
+                            if (KV) { const float4 l4 = nl[k / 2]; lse = k & 1 ? pack2(l4.z, l4.w) : pack2(l4.x, l4.y); }
+                            float a, b;
+                            unpack2(fma2(pack2(__uint_as_float(v[c][2 * k]), __uint_as_float(v[c][2 * k + 1])), sc2, lse), a, b);
+                            a = ex2(a);
+                            b = ex2(b);
+                            if (!KV && keep != ~0u) {
+                                if (!(keep >> (2 * k) & 1)) a = 0.f;
+                                if (!(keep >> (2 * k + 1) & 1)) b = 0.f;
+                            }
+                            e[16 * c + k] = pack2(a, b);
+                            if (KV) out[k] = pack_half<T>(a, b);
+                        }
+                        if (KV) tmem_st16(S + 16 * c, out);
+                    }
+                    if (KV) tmem_wait_st();
+                }
+                tmem_fence_before();
+                mbar_arrive(bar(ctl.p_full));
+                ok = mbar_wait(bar(ctl.dp_full), steps & 1, abort_word);
                 ok = __all_sync(~0u, ok);
                 if (!ok) continue;
                 tmem_fence_after();
                 if (warp_on) {
-                    uint32_t s[32], d[32];
-                    tmem_ld32(s_at[b] + lanes + 32 * x, s);
-                    tmem_ld32(dp_at[b] + lanes + 32 * x, d);
-                    uint32_t keep = ~0u;
-                    if (!KV) keep = ctl.mask[st][2 * x] | ctl.mask[st][2 * x + 1] << 16;
+                    uint32_t v[2][32];
+                    tmem_ld32(dP, v[0]);
+                    tmem_ld32(dP + 32, v[1]);
                     tmem_wait_ld();
-                    uint32_t pk[16], dk[16];
-                    const float4* nl = reinterpret_cast<const float4*>(ctl.minus_lse[st] + 32 * x);
-                    const float4* nd = reinterpret_cast<const float4*>(ctl.minus_delta[st] + 32 * x);
 #pragma unroll
-                    for (int k = 0; k < 16; k += 2) {
-                        float4 l4, d4;
-                        if (KV) { l4 = nl[k / 2]; d4 = nd[k / 2]; }
+                    for (int c = 0; c < 2; ++c) {
+                        const float4* nd = reinterpret_cast<const float4*>(ctl.minus_delta[aux] + 64 * x + 32 * c);
+                        uint32_t out[16];
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const f32x2 lse = KV ? (e ? pack2(l4.z, l4.w) : pack2(l4.x, l4.y)) : my_lse;
-                            const f32x2 delta = KV ? (e ? pack2(d4.z, d4.w) : pack2(d4.x, d4.y)) : my_delta;
-                            const int c = 2 * (k + e);
-                            float a0, a1, g0, g1;
-                            unpack2(fma2(pack2(__uint_as_float(s[c]), __uint_as_float(s[c + 1])), sc2, lse), a0, a1);
-                            a0 = ex2(a0);
-                            a1 = ex2(a1);
-                            if (!KV && keep != ~0u) {
-                                if (!(keep >> c & 1)) a0 = 0.f;
-                                if (!(keep >> (c + 1) & 1)) a1 = 0.f;
-                            }
-                            if (KV) pk[k + e] = pack_half<T>(a0, a1);
-                            f32x2 g = mul2(pack2(a0, a1), add2(pack2(__uint_as_float(d[c]), __uint_as_float(d[c + 1])), delta));
+                        for (int k = 0; k < 16; ++k) {
+                            f32x2 delta = my_delta;
+                            if (KV) { const float4 d4 = nd[k / 2]; delta = k & 1 ? pack2(d4.z, d4.w) : pack2(d4.x, d4.y); }
+                            f32x2 g = mul2(e[16 * c + k], add2(pack2(__uint_as_float(v[c][2 * k]), __uint_as_float(v[c][2 * k + 1])), delta));
                             if (F16) g = mul2(g, ds2);
-                            unpack2(g, g0, g1);
-                            dk[k + e] = pack_half<T>(g0, g1);
+                            float a, b;
+                            unpack2(g, a, b);
+                            out[k] = pack_half<T>(a, b);
                         }
+                        tmem_st16(dP + 16 * c, out);
                     }
-                    if (KV) tmem_st16(s_at[b] + lanes + 32 * x, pk);
-                    tmem_st16(dp_at[b] + lanes + 32 * x, dk);
                     tmem_wait_st();
                 }
                 tmem_fence_before();
-                mbar_arrive(bar(ctl.ps_full[b]));
+                mbar_arrive(bar(ctl.ds_full));
             }
             ok = ok && mbar_wait(bar(ctl.acc_full), items & 1, abort_word);
             ok = __all_sync(~0u, ok);
@@ -384,7 +440,6 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
                 }
             tmem_fence_before();
             mbar_arrive(bar(ctl.acc_empty));
-            step0 += n;
         }
     }
     tmem_fence_before();
@@ -398,19 +453,16 @@ constexpr int SUM_WARPS = 8, SUM_Y = 16, SUM_FEW = 8;
 
 template <typename T, int DP, bool KV>
 __global__ void __launch_bounds__(SUM_WARPS * 32) attention_sum_kernel(const AttnParams p, const BwdWork w) {
-    constexpr Geometry GEO = KV ? KV_GEO : Q_GEO;
+    typedef typename CutOf<KV>::type WorkCut;
     constexpr int SIDES = KV ? 2 : 1, E = DP / 32;
     constexpr bool F16 = operand_type<T>() == 0;
-    const long long* unit_start = KV ? w.kv_start_unit : w.q_start_unit;
-    const long long units = unit_start[p.n_seg];
-    const long long blocks = blocks_for(units, gridDim.x, BWD_LEAST);
-    if (blockIdx.x >= blocks || units == 0) return;
-    const long long unit0 = blockIdx.x * units / blocks, unit1 = (blockIdx.x + 1LL) * units / blocks;
-    Walker it;
-    if (!it.begin(p, GEO, unit_start, unit0, unit1) || it.i0 == 0 || it.i1 < it.steps) return;
-    const int first = (int)(((unit0 - it.i0 + 1) * blocks - 1) / units);        // the block in which the tile begins
+    wait_for_previous_kernel();
+    let_next_kernel_start();
+    Walker<WorkCut> it;
+    if (!it.begin(p, KV ? w.kv_start_unit : w.q_start_unit, blockIdx.x, gridDim.x, BWD_LEAST) || it.i0 == 0 || it.i1 < it.steps) return;
+    const int first = it.first_block(blockIdx.x);
     const int parts = (int)blockIdx.x - first + 1;
-    const int rows = min(stationary_rows(p, it.g, GEO) - it.t * BWD_ROWS, BWD_ROWS), cap = KV ? w.kv_rows : w.q_rows;
+    const int rows = min(WorkCut::rows(p, it.g) - it.t * BWD_ROWS, BWD_ROWS), cap = KV ? w.kv_rows : w.q_rows;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const float factor = F16 ? gradient_factor(w.norms) : 1.f;
     __shared__ float sh[SUM_WARPS][DP];
@@ -445,7 +497,7 @@ __global__ void __launch_bounds__(SUM_WARPS * 32) attention_sum_kernel(const Att
             bool masked;
             if (KV) {
                 out_row = (long long)(it.g.k0 + n) * p.kv_heads + it.h;
-                masked = key_place(p, it.g, it.s, n) < 0;
+                masked = key_place(p, it.g, it.s, n).at < 0;
             } else {
                 const PackedRow pr = packed_row(p, it.g, it.h, n);
                 out_row = (long long)pr.row * p.heads + pr.head;
@@ -460,11 +512,12 @@ __global__ void __launch_bounds__(SUM_WARPS * 32) attention_sum_kernel(const Att
     }
 }
 
-static __global__ void __launch_bounds__(PLAN_THREADS) backward_plan_kernel(const AttnParams p, long long* kv_units, long long* q_units, uint32_t* norms) {
-    if (blockIdx.x == 0) {
-        if (threadIdx.x < 2) norms[threadIdx.x] = 0;
-        plan_units(p, KV_GEO, kv_units);
-    } else plan_units(p, Q_GEO, q_units);
+// clears the norms; counts the units of every segment where the blocks do not
+static __global__ void __launch_bounds__(PLAN_THREADS) backward_plan_kernel(const AttnParams p, const BwdWork w) {
+    let_next_kernel_start();
+    if (blockIdx.x == 0 && threadIdx.x < 2) w.norms[threadIdx.x] = 0;
+    if (blockIdx.x == 0) { if (w.kv_start_unit) plan_units<KvCut>(p, w.kv_start_unit); }
+    else if (w.q_start_unit) plan_units<QCut>(p, w.q_start_unit);
 }
 
 static size_t backward_carve(const AttnParams& p, void* ws, BwdWork* w) {
@@ -474,8 +527,9 @@ static size_t backward_carve(const AttnParams& p, void* ws, BwdWork* w) {
     w->q_rows = (int)(packed < BWD_ROWS ? packed : BWD_ROWS);
     const size_t floats = (size_t)w->kv_rows * 2 > (size_t)w->q_rows ? (size_t)w->kv_rows * 2 : (size_t)w->q_rows;
     Carver cv(ws);
-    w->kv_start_unit = cv.take<long long>((size_t)p.n_seg + 1);
-    w->q_start_unit = cv.take<long long>((size_t)p.n_seg + 1);
+    const bool counted_there = counts_itself(p, BWD_ROWS);
+    w->kv_start_unit = counted_there ? nullptr : cv.take<long long>((size_t)p.n_seg + 1);
+    w->q_start_unit = counted_there ? nullptr : cv.take<long long>((size_t)p.n_seg + 1);
     w->norms = cv.take<uint32_t>(2);
     w->stats = cv.take<float2>((size_t)p.n_q * p.heads);
     w->part = cv.take<float>(slots * floats * dp);          // the key kernel's, then the query kernel's
@@ -484,25 +538,27 @@ static size_t backward_carve(const AttnParams& p, void* ws, BwdWork* w) {
 size_t attention_backward_bytes(const AttnParams& p) { BwdWork w; return backward_carve(p, nullptr, &w); }
 
 template <typename T, int DP, bool KV>
-static tiga_status launch_side(const AttnParams& p, const BwdWork& w, int sms, cudaStream_t s) {
+static tiga_status launch_side(const AttnParams& p, const BwdWork& w, const TileMaps& maps, int sms, cudaStream_t s) {
     TIGA_CUDA_TRY(cudaFuncSetAttribute(attention_backward_kernel<T, DP, KV>, cudaFuncAttributeMaxDynamicSharedMemorySize, Bwd<DP>::SMEM));
-    attention_backward_kernel<T, DP, KV><<<counted((unsigned)sms), BWD_THREADS, Bwd<DP>::SMEM, s>>>(p, w);
-    attention_sum_kernel<T, DP, KV><<<counted(dim3(sms, SUM_Y)), SUM_WARPS * 32, 0, s>>>(p, w);
-    return launch_status();
+    TIGA_CUDA_TRY(launch_after(attention_backward_kernel<T, DP, KV>, dim3(sms), BWD_THREADS, Bwd<DP>::SMEM, s, p, w, maps));
+    TIGA_CUDA_TRY(launch_after(attention_sum_kernel<T, DP, KV>, dim3(sms, SUM_Y), SUM_WARPS * 32, 0, s, p, w));
+    return TIGA_OK;
 }
 
 template <typename T, int DP>
-static tiga_status launch_backward(const AttnParams& p, const BwdWork& w, cudaStream_t s) {
+static tiga_status launch_backward(AttnParams p, const BwdWork& w, cudaStream_t s) {
+    TileMaps maps;
+    make_tile_maps(&p, operand_type<T>() == 1, &maps);
     const int sms = attention_grid();
     if (sms <= 0) return TIGA_ERR_CUDA;
-    backward_plan_kernel<<<counted(2), PLAN_THREADS, 0, s>>>(p, const_cast<long long*>(w.kv_start_unit), const_cast<long long*>(w.q_start_unit), w.norms);
+    backward_plan_kernel<<<counted(2), PLAN_THREADS, 0, s>>>(p, w);
     const long long rows = (long long)p.n_q * p.heads + (long long)p.n_kv * p.kv_heads;
     const long long grid = (rows * 16 + PREP_THREADS - 1) / PREP_THREADS;
-    attention_prepare_kernel<T><<<counted((unsigned)(grid < 8 * sms ? grid : 8 * sms)), PREP_THREADS, 0, s>>>(p, w);
-    tiga_status st = launch_status();
-    if (st == TIGA_OK && (p.gk || p.gv) && p.n_kv) st = launch_side<T, DP, true>(p, w, sms, s);
-    if (st == TIGA_OK && p.gq && p.n_q) st = launch_side<T, DP, false>(p, w, sms, s);
-    return st;
+    TIGA_CUDA_TRY(launch_after(attention_prepare_kernel<T>, dim3((unsigned)(grid < 8 * sms ? grid : 8 * sms)), PREP_THREADS, 0, s, p, w));
+    tiga_status st = TIGA_OK;
+    if ((p.gk || p.gv) && p.n_kv) st = launch_side<T, DP, true>(p, w, maps, sms, s);
+    if (st == TIGA_OK && p.gq && p.n_q) st = launch_side<T, DP, false>(p, w, maps, sms, s);
+    return st == TIGA_OK ? launch_status() : st;
 }
 
 tiga_status attention_backward(const AttnParams& p, bool bf16, void* ws, cudaStream_t s) {

@@ -15,7 +15,7 @@ namespace tiga {
 // The accumulator is rescaled only when a row's maximum grew by more than 2^8 since the last time: weights up to 2^8 do no harm,
 // and the mass carries the same factor.
 constexpr int FWD_THREADS = 416, FWD_ROWS = 256, FWD_STEP = 128;
-constexpr Geometry FWD_GEO = {FWD_ROWS, FWD_STEP, 0};
+typedef Cut<FWD_ROWS, FWD_STEP, false> FwdCut;
 constexpr int FWD_LEAST = 2;            // units a block at least
 constexpr int MASK_RING = 8;            // the producers are at most 6 steps ahead of the softmax (ring of at most 10 tiles)
 constexpr float RESCALE_AT = 8.f;
@@ -35,16 +35,16 @@ struct FwdControl {
 static_assert(sizeof(FwdControl) <= 2560, "control block");
 
 struct FwdWork {
-    const long long* unit_start;
+    long long* unit_start;          // NULL: the blocks count for themselves
     float2* part_ml;                // [2 * grid][rows]: reference of the exponents (log2), mass
     float* part_o;                  // [2 * grid][rows][DP]: unnormalised
     int rows;                       // packed rows that a partial state holds at most
 };
 
-static __global__ void __launch_bounds__(PLAN_THREADS) forward_plan_kernel(const AttnParams p, long long* unit_start) { plan_units(p, FWD_GEO, unit_start); }
+static __global__ void __launch_bounds__(PLAN_THREADS) forward_plan_kernel(const AttnParams p, long long* unit_start) { plan_units<FwdCut>(p, unit_start); }
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const AttnParams p, const FwdWork w) {
+__global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const AttnParams p, const FwdWork w, const __grid_constant__ TileMaps maps) {
     typedef Fwd<DP> C;
     extern __shared__ __align__(1024) unsigned char smem[];
     FwdControl& ctl = *reinterpret_cast<FwdControl*>(smem + C::CONTROL);
@@ -53,14 +53,15 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
     volatile uint32_t* abort_word = &ctl.abort_word;
     auto bar = [&](unsigned long long& b) { return smem_u32(&b); };
 
-    const long long units = w.unit_start[p.n_seg];
-    const long long blocks = blocks_for(units, gridDim.x, FWD_LEAST);
-    if (blockIdx.x >= blocks || units == 0) return;
-    const long long unit0 = blockIdx.x * units / blocks, unit1 = (blockIdx.x + 1LL) * units / blocks;
+    wait_for_previous_kernel();
+    let_next_kernel_start();
+    Walker<FwdCut> it;
+    bool more = it.begin(p, w.unit_start, blockIdx.x, gridDim.x, FWD_LEAST);
+    if (!more) return;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < C::SLOTS; ++i) { mbar_init(bar(ctl.full[i]), 128); mbar_init(bar(ctl.empty[i]), 1); }
-        mbar_init(bar(ctl.q_full), 128);
+        mbar_init(bar(ctl.q_full), 256);
         mbar_init(bar(ctl.q_empty), 1);
         for (int x = 0; x < 2; ++x) { mbar_init(bar(ctl.s_full[x]), 1); mbar_init(bar(ctl.p_full[x]), 128); mbar_init(bar(ctl.o_full[x]), 1); }
         for (int i = 0; i < MASK_RING; ++i) mbar_init(bar(ctl.mask_full[i]), 4);
@@ -75,34 +76,22 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
     const uint32_t tmem = ctl.tmem;
     const uint32_t s_at[2] = {tmem, tmem + 128}, o_at[2] = {tmem + 256, tmem + 256 + DP};
 
-    Walker it;
     if (warp >= 8 && warp < 12) {
         // ---------------------------------------------------------------- producers
         const int pw = warp - 8;
         uint32_t tiles = 0, steps = 0, items = 0;
         bool ok = true;
         auto slot_free = [&]() { return tiles < (uint32_t)C::SLOTS || mbar_wait(bar(ctl.empty[tiles % C::SLOTS]), (tiles / C::SLOTS + 1) & 1, abort_word); };
-        for (bool more = it.begin(p, FWD_GEO, w.unit_start, unit0, unit1); more && ok; more = it.next(p, FWD_GEO), ++items) {
+        for (; more && ok; more = it.next(p), ++items) {
             const int rows = min(it.g.nq * p.group - it.t * FWD_ROWS, FWD_ROWS);
             auto place = [&](int i) {
                 const int j = i * FWD_STEP + 32 * pw + lane;
-                return j < it.g.nk ? key_place(p, it.g, it.s, j) : -1LL;
+                return j < it.g.nk ? key_place(p, it.g, it.s, j) : Place{-1, 0};
             };
-            long long at = place(it.i0);
-            if (items && !(ok = mbar_wait(bar(ctl.q_empty), (items - 1) & 1, abort_word))) break;
-            for (int x = 0; x < (rows > 128 ? 2 : 1); ++x) {
-                const int r = x * 128 + 32 * pw + lane;
-                long long off = -1;
-                if (r < rows) {
-                    const PackedRow pr = packed_row(p, it.g, it.h, it.t * FWD_ROWS + r);
-                    off = pr.row * p.q_row + pr.head * p.q_head;
-                }
-                copy_rows<DP, 128, 32>(q_tile + x * C::TILE, 32 * pw, p.q, off, p.D, p.q);
-            }
-            cp_async_arrive(bar(ctl.q_full));
-            for (int i = it.i0; i < it.i1; ++i, ++steps) {
-                const long long here = at;
-                const uint32_t valid = __ballot_sync(~0u, here >= 0);
+            Place at = place(it.i0);
+            for (int i = it.i0; i < it.i1 && ok; ++i, ++steps) {
+                const Place here = at;
+                const uint32_t valid = __ballot_sync(~0u, here.at >= 0);
                 if (lane == 0) {
                     ctl.mask[steps % MASK_RING][pw] = valid;
                     mbar_arrive(bar(ctl.mask_full[steps % MASK_RING]));
@@ -110,15 +99,24 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
                 if (i + 1 < it.i1) at = place(i + 1);
                 for (int kv = 0; kv < 2; ++kv, ++tiles) {
                     if (!(ok = slot_free())) break;
-                    const long long row = p.table ? 1 : kv ? p.v_row : p.k_row;
-                    const long long off = here < 0 ? -1 : here * row + it.h * (kv ? p.v_head : p.k_head);
-                    copy_rows<DP, 128, 32>(ring + (tiles % C::SLOTS) * C::TILE, 32 * pw, kv ? p.v : p.k, off, p.D, p.q);
-                    cp_async_arrive(bar(ctl.full[tiles % C::SLOTS]));
+                    fetch_keys<DP>(ring + (tiles % C::SLOTS) * C::TILE, 32 * pw, bar(ctl.full[tiles % C::SLOTS]), p, maps, kv, here, it.h, p.q);
                 }
-                if (!ok) break;
+                if (i == it.i0 && ok) {         // the queries' tile may still be in use by the item before: its first keys are on their way
+                    if (items && !(ok = mbar_wait(bar(ctl.q_empty), (items - 1) & 1, abort_word))) break;
+                    for (int x = 0; x < 2; ++x) {
+                        const int r = x * 128 + 32 * pw + lane;
+                        if (x == 1 && rows <= 128) {
+                            if (lane == 0) mbar_arrive(bar(ctl.q_full), 32);
+                        } else fetch_packed<DP>(q_tile + x * C::TILE, 32 * pw, bar(ctl.q_full), p, it.g, maps, false, it.h, it.t * FWD_ROWS + r, r < rows, p.q);
+                    }
+                }
             }
         }
         cp_async_wait_all();
+        if (*abort_word) {          // boxes may still be on their way: their tiles, as far as they were asked for
+            for (uint32_t k = tiles < (uint32_t)C::SLOTS ? 0 : tiles - C::SLOTS; k < tiles; ++k) mbar_wait(bar(ctl.full[k % C::SLOTS]), (k / C::SLOTS) & 1, &ctl.never);
+            if (items) mbar_wait(bar(ctl.q_full), (items - 1) & 1, &ctl.never);
+        }
     } else if (warp == 12) {
         // ---------------------------------------------------------------- matrix instructions
         if (lane == 0) {
@@ -148,7 +146,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
                 for (int k = 0; k < 8; ++k) mma_ts(o_at[x], s_at[x] + k * 8, smem_desc(slot(tile) + k * 2048, 128 * 128), o_shape, add || k > 0);
                 mma_commit(bar(ctl.o_full[x]));
             };
-            for (bool more = it.begin(p, FWD_GEO, w.unit_start, unit0, unit1); more && ok; more = it.next(p, FWD_GEO), ++items) {
+            for (; more && ok; more = it.next(p), ++items) {
                 const int n = it.i1 - it.i0;
                 const bool two = it.g.nq * p.group - it.t * FWD_ROWS > 128;
                 ok = ok && mbar_wait(bar(ctl.q_full), items & 1, abort_word);
@@ -206,7 +204,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
         constexpr float BIAS = sizeof(T) == 2 && operand_type<T>() == 0 ? 7.f : 0.f;     // fp16: weights up to 2^15, so that small ones keep their digits
         uint32_t step0 = 0, s_done = 0, o_base[2] = {0, 0};
         bool ok = true;
-        for (bool more = it.begin(p, FWD_GEO, w.unit_start, unit0, unit1); more; more = it.next(p, FWD_GEO)) {
+        for (; more; more = it.next(p)) {
             const int n = it.i1 - it.i0;
             const int rows = min(it.g.nq * p.group - it.t * FWD_ROWS, FWD_ROWS);
             const bool two = rows > 128;
@@ -234,17 +232,27 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
                         whole = whole && keep[k] == ~0u;
                     }
                     whole = __all_sync(~0u, whole);
+                    // S is read twice: held whole it would not fit the registers
                     float top = -INFINITY;
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t v[32];
-                        tmem_ld32(S + 32 * c, v);
+                    for (int c = 0; c < 4; c += 2) {
+                        uint32_t v[2][32];
+                        tmem_ld32(S + 32 * c, v[0]);
+                        tmem_ld32(S + 32 * c + 32, v[1]);
                         tmem_wait_ld();
-                        if (!whole)
 #pragma unroll
-                            for (int k = 0; k < 32; ++k) if (!(keep[c] >> k & 1)) v[k] = 0xff800000u;
+                        for (int y = 0; y < 2; ++y) {
+                            if (!whole)
 #pragma unroll
-                        for (int k = 0; k < 32; k += 2) top = max3(top, __uint_as_float(v[k]), __uint_as_float(v[k + 1]));
+                                for (int k = 0; k < 32; ++k) if (!(keep[c + y] >> k & 1)) v[y][k] = 0xff800000u;
+                            float t0 = -INFINITY, t1 = -INFINITY;
+#pragma unroll
+                            for (int k = 0; k < 32; k += 4) {
+                                t0 = max3(t0, __uint_as_float(v[y][k]), __uint_as_float(v[y][k + 1]));
+                                t1 = max3(t1, __uint_as_float(v[y][k + 2]), __uint_as_float(v[y][k + 3]));
+                            }
+                            top = max3(top, t0, t1);
+                        }
                     }
                     top *= scale2;
                     const bool grown = top > m + RESCALE_AT || (m == -INFINITY && top > -INFINITY);
@@ -257,12 +265,12 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
                         tmem_fence_after();
 #pragma unroll
                         for (int c = 0; c < DP / 32; ++c) {
-                            uint32_t v[32];
-                            tmem_ld32(o_at[x] + lanes + 32 * c, v);
+                            uint32_t o[32];
+                            tmem_ld32(o_at[x] + lanes + 32 * c, o);
                             tmem_wait_ld();
 #pragma unroll
-                            for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * fade);
-                            tmem_st32(o_at[x] + lanes + 32 * c, v);
+                            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * fade);
+                            tmem_st32(o_at[x] + lanes + 32 * c, o);
                         }
                     }
                     m = m_new;
@@ -270,24 +278,26 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
                     const float shift = m == -INFINITY ? 0.f : BIAS - m;
                     const f32x2 sc2 = dup2(scale2), sh2 = dup2(shift);
                     f32x2 sum = pack2(0.f, 0.f);
+                    uint32_t v[2][16];                  // 16 columns at a time, the next on their way
+                    tmem_ld16(S, v[0]);
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t v[32], out[16];
-                        tmem_ld32(S + 32 * c, v);
+                    for (int c = 0; c < 8; ++c) {
                         tmem_wait_ld();
+                        if (c < 7) tmem_ld16(S + 16 * (c + 1), v[(c + 1) & 1]);
                         if (!whole)
 #pragma unroll
-                            for (int k = 0; k < 32; ++k) if (!(keep[c] >> k & 1)) v[k] = 0xff800000u;
+                            for (int k = 0; k < 16; ++k) if (!(keep[c / 2] >> (16 * (c & 1) + k) & 1)) v[c & 1][k] = 0xff800000u;
+                        uint32_t out[8];
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) {
+                        for (int k = 0; k < 8; ++k) {
                             float a, b;
-                            unpack2(fma2(pack2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), sc2, sh2), a, b);
+                            unpack2(fma2(pack2(__uint_as_float(v[c & 1][2 * k]), __uint_as_float(v[c & 1][2 * k + 1])), sc2, sh2), a, b);
                             a = ex2(a);
                             b = ex2(b);
                             sum = add2(sum, pack2(a, b));
                             out[k] = pack_half<T>(a, b);
                         }
-                        tmem_st16(S + 16 * c, out);
+                        tmem_st8(S + 8 * c, out);
                     }
                     float a, b;
                     unpack2(sum, a, b);
@@ -372,13 +382,10 @@ constexpr int JOIN_WARPS = 8, JOIN_Y = 16, JOIN_FEW = 8;
 
 template <typename T, int DP>
 __global__ void __launch_bounds__(JOIN_WARPS * 32) attention_join_kernel(const AttnParams p, const FwdWork w) {
-    const long long units = w.unit_start[p.n_seg];
-    const long long blocks = blocks_for(units, gridDim.x, FWD_LEAST);
-    if (blockIdx.x >= blocks || units == 0) return;
-    const long long unit0 = blockIdx.x * units / blocks, unit1 = (blockIdx.x + 1LL) * units / blocks;
-    Walker it;
-    if (!it.begin(p, FWD_GEO, w.unit_start, unit0, unit1) || it.i0 == 0 || it.i1 < it.steps) return;
-    const int first = (int)(((unit0 - it.i0 + 1) * blocks - 1) / units);        // the block in which the tile begins
+    wait_for_previous_kernel();
+    Walker<FwdCut> it;
+    if (!it.begin(p, w.unit_start, blockIdx.x, gridDim.x, FWD_LEAST) || it.i0 == 0 || it.i1 < it.steps) return;
+    const int first = it.first_block(blockIdx.x);
     const int parts = (int)blockIdx.x - first + 1;
     const int rows = min(it.g.nq * p.group - it.t * FWD_ROWS, FWD_ROWS);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -454,7 +461,7 @@ size_t attention_forward_carve(const AttnParams& p, void* ws, FwdWork* w) {
     const long long packed = (long long)p.n_q * p.group;
     w->rows = (int)(packed < FWD_ROWS ? packed : FWD_ROWS);
     Carver cv(ws);
-    w->unit_start = cv.take<long long>((size_t)p.n_seg + 1);
+    w->unit_start = counts_itself(p, FWD_ROWS) ? nullptr : cv.take<long long>((size_t)p.n_seg + 1);
     w->part_ml = cv.take<float2>(slots * w->rows);
     w->part_o = cv.take<float>(slots * w->rows * (p.D > 64 ? 128 : 64));
     return cv.off;
@@ -462,14 +469,17 @@ size_t attention_forward_carve(const AttnParams& p, void* ws, FwdWork* w) {
 size_t attention_forward_bytes(const AttnParams& p) { FwdWork w; return attention_forward_carve(p, nullptr, &w); }
 
 template <typename T, int DP>
-static tiga_status launch_forward(const AttnParams& p, const FwdWork& w, cudaStream_t s) {
+static tiga_status launch_forward(AttnParams p, const FwdWork& w, cudaStream_t s) {
+    TileMaps maps;
+    make_tile_maps(&p, operand_type<T>() == 1, &maps);
     const int sms = attention_grid();
     if (sms <= 0) return TIGA_ERR_CUDA;
     // asked for on every call: the attribute belongs to the current device
     TIGA_CUDA_TRY(cudaFuncSetAttribute(attention_forward_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, Fwd<DP>::SMEM));
-    forward_plan_kernel<<<counted(1), PLAN_THREADS, 0, s>>>(p, const_cast<long long*>(w.unit_start));
-    attention_forward_kernel<T, DP><<<counted((unsigned)sms), FWD_THREADS, Fwd<DP>::SMEM, s>>>(p, w);
-    attention_join_kernel<T, DP><<<counted(dim3(sms, JOIN_Y)), JOIN_WARPS * 32, 0, s>>>(p, w);
+    if (w.unit_start) forward_plan_kernel<<<counted(1), PLAN_THREADS, 0, s>>>(p, w.unit_start);
+    if (w.unit_start) TIGA_CUDA_TRY(launch_after(attention_forward_kernel<T, DP>, dim3(sms), FWD_THREADS, Fwd<DP>::SMEM, s, p, w, maps));
+    else attention_forward_kernel<T, DP><<<counted((unsigned)sms), FWD_THREADS, Fwd<DP>::SMEM, s>>>(p, w, maps);
+    TIGA_CUDA_TRY(launch_after(attention_join_kernel<T, DP>, dim3(sms, JOIN_Y), JOIN_WARPS * 32, 0, s, p, w));
     return launch_status();
 }
 

@@ -19,6 +19,7 @@ struct AttnParams {
     int n_seg, n_q, n_kv, heads, kv_heads, group, D, causal;
     long long n_pages, page_size, table_stride, max_pages, page_stride, slot_stride;
     float scale;
+    int kv_box, q_box;              // rows that a box of the tensor maps brings (0: rows are copied one by one)
 };
 
 // A segment's rows [q0, q0 + nq) and its keys [k0, k0 + nk) (paged: k0 = 0), bounds clamped to the arrays.
@@ -45,17 +46,22 @@ __device__ __forceinline__ int keys_of_row(const AttnParams& p, const Segment& g
     return p.causal ? min(max(g.nk - g.nq + t + 1, 0), g.nk) : g.nk;
 }
 
-// Where key j of segment s (0 <= j < g.nk) lies, or -1 where it is masked or has no page.  Paged: the offset of its slot in either
-// array, in elements (row_scale 1).  Dense: its row (row_scale: the row stride of the array that is read).
-__device__ __forceinline__ long long key_place(const AttnParams& p, const Segment& g, int s, int j) {
+// Where key j of segment s (0 <= j < g.nk) lies: paged, its page and slot; dense, its row and 0.  at < 0: it is masked, or has no page.
+struct Place { int at, slot; };
+__device__ __forceinline__ Place key_place(const AttnParams& p, const Segment& g, int s, int j) {
     if (p.table) {
         const int page = j / (int)p.page_size;
         const int id = p.table[(long long)s * p.table_stride + page];
-        if (id < 0 || id >= p.n_pages) return -1;
-        return (long long)id * p.page_stride + (long long)(j - page * (int)p.page_size) * p.slot_stride;
+        return {id >= p.n_pages ? -1 : id, j - page * (int)p.page_size};
     }
-    if (p.mask && !p.mask[g.k0 + j]) return -1;
-    return g.k0 + j;
+    if (p.mask && !p.mask[g.k0 + j]) return {-1, 0};
+    return {g.k0 + j, 0};
+}
+__device__ __forceinline__ long long key_offset(const AttnParams& p, Place a, int h) {
+    return a.at < 0 ? -1 : p.table ? a.at * p.page_stride + a.slot * p.slot_stride + h * p.k_head : a.at * p.k_row + h * p.k_head;
+}
+__device__ __forceinline__ long long value_offset(const AttnParams& p, Place a, int h) {
+    return a.at < 0 ? -1 : p.table ? a.at * p.page_stride + a.slot * p.slot_stride + h * p.v_head : a.at * p.v_row + h * p.v_head;
 }
 
 // ---- How the work is cut.  A segment's heads share keys, so the rows of a group's heads are packed: packed row r of a kv head is row
@@ -63,117 +69,199 @@ __device__ __forceinline__ long long key_place(const AttnParams& p, const Segmen
 // side in steps; a unit is one step of one tile of one kv head.  All units of a call stand in one line (segment, kv head, tile,
 // step), and the blocks take equal pieces of it: a piece that begins or ends inside a tile leaves a partial state in the
 // workspace, and a last kernel joins those in order.  So short and long, few and many rows are balanced by one rule.
-struct Geometry { int tile, step, keys_stationary; };
+template <int TILE_, int STEP_, bool KEYS_>
+struct Cut {
+    static constexpr int TILE = TILE_, STEP = STEP_;      // stationary rows of a tile, rows of a step: powers of two
+    static constexpr bool KEYS = KEYS_;                   // the keys are stationary
 
-__device__ __forceinline__ int stationary_rows(const AttnParams& p, const Segment& g, const Geometry geo) {
-    return geo.keys_stationary ? g.nk : g.nq * p.group;
-}
-__device__ __forceinline__ int tiles_of(const AttnParams& p, const Segment& g, const Geometry geo) {
-    return (int)(((long long)stationary_rows(p, g, geo) + geo.tile - 1) / geo.tile);
-}
-// steps of tile t; one (in which nothing is read) where there is nothing on the other side, so that empty rows are written
-__device__ __forceinline__ int steps_of(const AttnParams& p, const Segment& g, const Geometry geo, int t) {
-    long long n;
-    if (geo.keys_stationary) n = (long long)g.nq * p.group;
-    else if (!p.causal) n = g.nk;
-    else {
-        const long long last = min(((long long)t + 1) * geo.tile, (long long)g.nq * p.group) - 1;
-        n = keys_of_row(p, g, (int)(last / p.group));
+    static __device__ __forceinline__ int rows(const AttnParams& p, const Segment& g) { return KEYS ? g.nk : g.nq * p.group; }
+    static __device__ __forceinline__ int tiles(const AttnParams& p, const Segment& g) {
+        const int n = rows(p, g);
+        return n / TILE + (n % TILE != 0);
     }
-    return (int)max((n + geo.step - 1) / geo.step, 1LL);
-}
-__device__ __forceinline__ long long units_of_head(const AttnParams& p, const Segment& g, const Geometry geo) {
-    const int tiles = tiles_of(p, g, geo);
-    if (!p.causal || geo.keys_stationary) return (long long)tiles * (tiles ? steps_of(p, g, geo, 0) : 0);
-    long long n = 0;
-    for (int t = 0; t < tiles; ++t) n += steps_of(p, g, geo, t);
-    return n;
-}
+    // steps of tile t; one (in which nothing is read) where there is nothing on the other side, so that empty rows are written
+    static __device__ __forceinline__ int steps(const AttnParams& p, const Segment& g, int t) {
+        int n;
+        if (KEYS) n = g.nq * p.group;
+        else if (!p.causal) n = g.nk;
+        else n = keys_of_row(p, g, (min((t + 1) * TILE, g.nq * p.group) - 1) / p.group);
+        return max(n / STEP + (n % STEP != 0), 1);
+    }
+    // units of a kv head
+    static __device__ __forceinline__ long long units(const AttnParams& p, const Segment& g) {
+        const int n = tiles(p, g);
+        if (KEYS || !p.causal) return n ? (long long)n * steps(p, g, 0) : 0;
+        long long sum = 0;
+        for (int t = 0; t < n; ++t) sum += steps(p, g, t);
+        return sum;
+    }
+};
 
-// Blocks that take part: `least` units each at least, so that tiny work is not spread thin.
-__device__ __forceinline__ long long blocks_for(long long units, int grid, int least) {
-    return min((long long)grid, max((units + least - 1) / least, 1LL));
+__device__ __forceinline__ long long warp_total(long long v) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
+    return v;
+}
+__device__ __forceinline__ long long warp_running(long long v) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long u = __shfl_up_sync(~0u, v, o);
+        if ((int)(threadIdx.x % 32) >= o) v += u;
+    }
+    return v;
+}
+// a / b for 0 <= a, 0 < b; the short division where both are short
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+    return (a | b) >> 32 ? a / b : (long long)((unsigned)a / (unsigned)b);
 }
 
 // A block's way through its piece of the line: one tile, or a part of one, after the other.
+template <typename C>
 struct Walker {
     Segment g;
     int s, h, t;                // segment, kv head, tile
     int steps, i0, i1;          // steps of the tile, and which of them are this block's
     long long left;             // units behind this item
+    long long units, blocks;    // of the whole line: units, and blocks that share them
 
-    __device__ __forceinline__ void open(const AttnParams& p, const Geometry geo) {
-        steps = steps_of(p, g, geo, t);
+    __device__ __forceinline__ void open(const AttnParams& p) {
+        steps = C::steps(p, g, t);
         i1 = (int)min((long long)steps, i0 + left);
         left -= i1 - i0;
     }
-    // false: the piece is empty
-    __device__ __forceinline__ bool begin(const AttnParams& p, const Geometry geo, const long long* unit_start, long long unit, long long end) {
-        left = end - unit;
-        if (left <= 0) return false;
-        int lo = 0, hi = p.n_seg;               // the last segment that begins at or before this unit
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (unit_start[mid] <= unit) lo = mid; else hi = mid;
+    __device__ __forceinline__ long long first_unit(long long block) const { return quotient(block * units, blocks); }
+
+    // The piece of block `block` of `grid`, which takes part only if there are `least` units a block.  Every warp of a block calls it
+    // with all its lanes.  unit_start: units in front of every segment; NULL (few segments, few tiles): they are counted here.
+    // false: nothing to do.
+    __device__ __forceinline__ bool begin(const AttnParams& p, const long long* unit_start, int block, int grid, int least) {
+        const int lane = threadIdx.x % 32;
+        if (unit_start) units = unit_start[p.n_seg];
+        else {
+            units = 0;
+            for (int k = 0; k < p.n_seg; k += 32) units += k + lane < p.n_seg ? C::units(p, segment_of(p, k + lane)) * p.kv_heads : 0;
+            units = warp_total(units);
         }
-        s = lo;
+        blocks = min((long long)grid, max(quotient(units + least - 1, least), 1LL));
+        if (block >= blocks || units == 0) return false;
+        long long off = first_unit(block), mine = 0;
+        left = first_unit(block + 1) - off;
+        if (unit_start) {
+            int lo = 0, hi = p.n_seg;               // the last segment that begins at or before this unit: 32 places a round
+            while (hi - lo > 1) {
+                const int gap = (hi - lo + 31) / 32, at = lo + lane * gap;
+                const unsigned before = __ballot_sync(~0u, at < hi && unit_start[at] <= off);
+                lo += (31 - __clz(before)) * gap;
+                hi = min(hi, lo + gap);
+            }
+            s = lo;
+            off -= unit_start[s];
+            mine = unit_start[s + 1] - unit_start[s];
+        } else {
+            for (int k = 0;; k += 32) {
+                const long long n = k + lane < p.n_seg ? C::units(p, segment_of(p, k + lane)) * p.kv_heads : 0;
+                const long long run = warp_running(n);
+                const unsigned beyond = __ballot_sync(~0u, run > off);
+                if (beyond) {
+                    const int at = __ffs(beyond) - 1;
+                    s = k + at;
+                    mine = __shfl_sync(~0u, n, at);
+                    off -= __shfl_sync(~0u, run, at) - mine;
+                    break;
+                }
+                off -= __shfl_sync(~0u, run, 31);
+            }
+        }
         g = segment_of(p, s);
-        long long off = unit - unit_start[s];
-        const long long per_head = (unit_start[s + 1] - unit_start[s]) / p.kv_heads;
-        h = (int)(off / per_head);
+        const long long per_head = quotient(mine, p.kv_heads);
+        h = (int)quotient(off, per_head);
         off -= h * per_head;
-        if (!p.causal || geo.keys_stationary) {
-            const int n = steps_of(p, g, geo, 0);
-            t = (int)(off / n);
+        if (C::KEYS || !p.causal) {
+            const int n = C::steps(p, g, 0);
+            t = (int)quotient(off, n);
             i0 = (int)(off - (long long)t * n);
         } else {
-            t = 0;
-            for (int n; off >= (n = steps_of(p, g, geo, t)); ++t) off -= n;
+            const int tiles = C::tiles(p, g);
+            for (t = 0;; t += 32) {
+                const long long run = warp_running(t + lane < tiles ? C::steps(p, g, t + lane) : 0);
+                const unsigned beyond = __ballot_sync(~0u, run > off);
+                if (beyond) {
+                    const int at = __ffs(beyond) - 1;
+                    if (at) off -= __shfl_sync(~0u, run, at - 1);
+                    t += at;
+                    break;
+                }
+                off -= __shfl_sync(~0u, run, 31);
+            }
             i0 = (int)off;
         }
-        open(p, geo);
+        open(p);
         return true;
     }
-    __device__ __forceinline__ bool next(const AttnParams& p, const Geometry geo) {
+    __device__ __forceinline__ bool next(const AttnParams& p) {
         if (left <= 0) return false;
         i0 = 0;
-        if (++t >= tiles_of(p, g, geo)) {
+        if (++t >= C::tiles(p, g)) {
             t = 0;
             if (++h >= p.kv_heads) {
                 h = 0;
-                do { g = segment_of(p, ++s); } while (tiles_of(p, g, geo) == 0);
+                do { g = segment_of(p, ++s); } while (C::rows(p, g) == 0);
             }
         }
-        open(p, geo);
+        open(p);
         return true;
+    }
+    // after begin(): the block in which this item's tile begins
+    __device__ __forceinline__ int first_block(int block) const {
+        return (int)quotient((first_unit(block) - i0 + 1) * blocks - 1, units);
     }
 };
 
 // unit_start[s]: units in front of segment s.  By one block.
 constexpr int PLAN_THREADS = 1024;
-static __device__ void plan_units(const AttnParams& p, const Geometry geo, long long* unit_start) {
-    __shared__ long long warp_total[PLAN_THREADS / 32];
+template <typename C>
+static __device__ void plan_units(const AttnParams& p, long long* unit_start) {
+    __shared__ long long totals[PLAN_THREADS / 32];
     long long before = 0;
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     for (int s0 = 0; s0 < p.n_seg; s0 += PLAN_THREADS) {
         const int s = s0 + threadIdx.x;
-        long long n = 0;
-        if (s < p.n_seg) n = units_of_head(p, segment_of(p, s), geo) * p.kv_heads;
-        for (int o = 1; o < 32; o <<= 1) {
-            const long long v = __shfl_up_sync(~0u, n, o);
-            if (lane >= o) n += v;
-        }
-        if (lane == 31) warp_total[warp] = n;
+        const long long n = warp_running(s < p.n_seg ? C::units(p, segment_of(p, s)) * p.kv_heads : 0);
+        if (lane == 31) totals[warp] = n;
         __syncthreads();
         long long sum = before;
         for (int w = 0; w < PLAN_THREADS / 32; ++w) {
-            if (w < warp) sum += warp_total[w];
-            before += warp_total[w];
+            if (w < warp) sum += totals[w];
+            before += totals[w];
         }
         if (s < p.n_seg) unit_start[s + 1] = sum + n;
         __syncthreads();
     }
     if (threadIdx.x == 0) unit_start[0] = 0;
+}
+// Whether the blocks count the units themselves: a launch less, for a few hundred instructions in every warp.
+constexpr int COUNT_SEGMENTS = 256, COUNT_TILES = 64;
+static inline bool counts_itself(const AttnParams& p, int tile) {
+    return p.n_seg <= COUNT_SEGMENTS && (!p.causal || (long long)p.n_q * p.group <= (long long)COUNT_TILES * tile);
+}
+
+// A kernel may start before the one in front of it in the stream has ended; it waits where it first reads what that one wrote.
+__device__ __forceinline__ void wait_for_previous_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_kernel_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+template <typename... A, typename... B>
+static inline cudaError_t launch_after(void (*kernel)(A...), dim3 grid, int threads, size_t smem, cudaStream_t s, B... args) {
+    cudaLaunchConfig_t c{};
+    c.gridDim = grid;
+    c.blockDim = dim3(threads);
+    c.dynamicSmemBytes = smem;
+    c.stream = s;
+    cudaLaunchAttribute a{};
+    a.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    a.val.programmaticStreamSerializationAllowed = 1;
+    c.attrs = &a;
+    c.numAttrs = 1;
+    note_launch();
+    return cudaLaunchKernelEx(&c, kernel, args...);
 }
 
 constexpr int MAX_SMS = 160;            // blocks that workspaces provide for

@@ -31,6 +31,45 @@ __device__ __forceinline__ void copy_rows(uint32_t tile, int first_row, const vo
     }
 }
 
+// Tensor maps of the arrays: q and grad_out as [rows][heads][D], boxes of 32 packed rows of a kv head (32 / group rows of its group
+// heads: one box where group divides 32); key and value as [heads][rows][D] or [pages][heads][slots][D], boxes of kv_box rows of a head.
+struct TileMaps { CUtensorMap q, go, k, v; };
+
+// 32 rows of a tile by one warp, and its 32 arrivals on the barrier.  Rows that all exist come in boxes (lane l holds the coordinates of
+// the box that begins at its row), issued by one lane each; rows of which some are masked, missing or behind the end come one by one.
+// (With copies of 16 bytes alone, the addresses cost a producer warp about 2000 instructions a step and bounded the kernels: chunk of
+// 2048 on 16384 508 us with the softmax left out.)
+template <int DP>
+__device__ __forceinline__ void fetch_rows(uint32_t tile, int first_row, uint32_t bar, int box, const CUtensorMap* map, int c1, int c2, int c3,
+                                           const void* base, long long off, int D, const void* any) {
+    if (box && __all_sync(~0u, off >= 0)) {
+        const int lane = threadIdx.x % 32;
+        if (lane == 0) { mbar_arrive(bar, 31); mbar_arrive_expect(bar, 32 * DP * 2); }
+        __syncwarp();
+        if (lane % box == 0)
+#pragma unroll
+            for (int f = 0; f < DP / 64; ++f) box_copy(tile + f * (128 * 128) + (first_row + lane) * 128, map, bar, 64 * f, c1, c2, c3);
+    } else {
+        copy_rows<DP, 128, 32>(tile, first_row, base, off, D, any);
+        cp_async_arrive(bar);
+    }
+}
+template <int DP>
+__device__ __forceinline__ void fetch_keys(uint32_t tile, int first_row, uint32_t bar, const AttnParams& p, const TileMaps& m, bool values, Place a, int h, const void* any) {
+    fetch_rows<DP>(tile, first_row, bar, p.kv_box, values ? &m.v : &m.k, p.table ? a.slot : a.at, h, p.table ? a.at : 0, values ? p.v : p.k,
+                   values ? value_offset(p, a, h) : key_offset(p, a, h), p.D, any);
+}
+// lane l's packed row is first + l of kv head h; `on`: it exists and is wanted
+template <int DP>
+__device__ __forceinline__ void fetch_packed(uint32_t tile, int first_row, uint32_t bar, const AttnParams& p, const Segment& g, const TileMaps& m, bool grads, int h, int r, bool on, const void* any) {
+    const PackedRow pr = packed_row(p, g, h, on ? r : 0);
+    fetch_rows<DP>(tile, first_row, bar, p.q_box, grads ? &m.go : &m.q, h * p.group, pr.row, 0, grads ? p.go : p.q,
+                   !on ? -1 : grads ? pr.row * p.go_row + pr.head * p.go_head : pr.row * p.q_row + pr.head * p.q_head, p.D, any);
+}
+
+// host: the maps, and the boxes that they allow (attention.cu)
+void make_tile_maps(AttnParams* p, bool bf16, TileMaps* m);
+
 // blocks of the persistent kernels: one on every SM (their shared memory admits one), 0 if the device does not answer
 static inline int attention_grid() {
     int dev = 0, sms = 0;
