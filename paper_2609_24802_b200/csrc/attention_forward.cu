@@ -14,8 +14,10 @@ namespace tiga {
 // warpgroups take the even and the odd steps with a state each, joined at the end, so a single token keeps both busy too.
 // The accumulator is rescaled only when a row's maximum grew by more than 2^8 since the last time: weights up to 2^8 do no harm,
 // and the mass carries the same factor.
-constexpr int FWD_THREADS = 416, FWD_ROWS = 256, FWD_STEP = 128;
+constexpr int FWD_THREADS = 512, FWD_ROWS = 256, FWD_STEP = 128;
 typedef Cut<FWD_ROWS, FWD_STEP, false> FwdCut;
+// registers of a softmax, producer and matrix thread: 2 * 192 + 80 + 48 = 4 * 128, what the block is launched with
+constexpr int FWD_SOFTMAX_REGS = 192, FWD_PRODUCER_REGS = 80, FWD_MMA_REGS = 48;
 constexpr int FWD_LEAST = 2;            // units a block at least
 constexpr int MASK_RING = 8;            // the producers are at most 6 steps ahead of the softmax (ring of at most 10 tiles)
 constexpr float RESCALE_AT = 8.f;
@@ -78,6 +80,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
 
     if (warp >= 8 && warp < 12) {
         // ---------------------------------------------------------------- producers
+        registers_down<FWD_PRODUCER_REGS>();
         const int pw = warp - 8;
         uint32_t tiles = 0, steps = 0, items = 0;
         bool ok = true;
@@ -117,9 +120,10 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
             for (uint32_t k = tiles < (uint32_t)C::SLOTS ? 0 : tiles - C::SLOTS; k < tiles; ++k) mbar_wait(bar(ctl.full[k % C::SLOTS]), (k / C::SLOTS) & 1, &ctl.never);
             if (items) mbar_wait(bar(ctl.q_full), (items - 1) & 1, &ctl.never);
         }
-    } else if (warp == 12) {
+    } else if (warp >= 12) {
+        registers_down<FWD_MMA_REGS>();
         // ---------------------------------------------------------------- matrix instructions
-        if (lane == 0) {
+        if (warp == 12 && lane == 0) {
             const uint32_t s_shape = mma_shape<T>(128, false) | (p.scale < 0.f ? MMA_NEGATE_A : 0), o_shape = mma_shape<T>(DP, true);
             uint32_t tile0 = 0, items = 0, done[2] = {0, 0};     // done: p_full phases consumed
             bool ok = true;
@@ -196,6 +200,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
         __syncwarp();
     } else {
         // ---------------------------------------------------------------- softmax
+        registers_up<FWD_SOFTMAX_REGS>();
         const int x = warp / 4;
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const int row = threadIdx.x & 127;
@@ -232,27 +237,23 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
                         whole = whole && keep[k] == ~0u;
                     }
                     whole = __all_sync(~0u, whole);
-                    // S is read twice: held whole it would not fit the registers
+                    uint32_t v[4][32];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) tmem_ld32(S + 32 * c, v[c]);
+                    tmem_wait_ld();
                     float top = -INFINITY;
 #pragma unroll
-                    for (int c = 0; c < 4; c += 2) {
-                        uint32_t v[2][32];
-                        tmem_ld32(S + 32 * c, v[0]);
-                        tmem_ld32(S + 32 * c + 32, v[1]);
-                        tmem_wait_ld();
+                    for (int c = 0; c < 4; ++c) {
+                        if (!whole)
 #pragma unroll
-                        for (int y = 0; y < 2; ++y) {
-                            if (!whole)
+                            for (int k = 0; k < 32; ++k) if (!(keep[c] >> k & 1)) v[c][k] = 0xff800000u;
+                        float t0 = -INFINITY, t1 = -INFINITY;
 #pragma unroll
-                                for (int k = 0; k < 32; ++k) if (!(keep[c + y] >> k & 1)) v[y][k] = 0xff800000u;
-                            float t0 = -INFINITY, t1 = -INFINITY;
-#pragma unroll
-                            for (int k = 0; k < 32; k += 4) {
-                                t0 = max3(t0, __uint_as_float(v[y][k]), __uint_as_float(v[y][k + 1]));
-                                t1 = max3(t1, __uint_as_float(v[y][k + 2]), __uint_as_float(v[y][k + 3]));
-                            }
-                            top = max3(top, t0, t1);
+                        for (int k = 0; k < 32; k += 4) {
+                            t0 = max3(t0, __uint_as_float(v[c][k]), __uint_as_float(v[c][k + 1]));
+                            t1 = max3(t1, __uint_as_float(v[c][k + 2]), __uint_as_float(v[c][k + 3]));
                         }
+                        top = max3(top, t0, t1);
                     }
                     top *= scale2;
                     const bool grown = top > m + RESCALE_AT || (m == -INFINITY && top > -INFINITY);
@@ -263,14 +264,14 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
                         ok = __all_sync(~0u, ok);
                         if (!ok) { m = l = __int_as_float(0x7fffffff); continue; }
                         tmem_fence_after();
-#pragma unroll
-                        for (int c = 0; c < DP / 32; ++c) {
-                            uint32_t o[32];
-                            tmem_ld32(o_at[x] + lanes + 32 * c, o);
+#pragma unroll 1
+                        for (int c = 0; c < DP / 16; ++c) {         // (rare, and S is held: few registers)
+                            uint32_t o[16];
+                            tmem_ld16(o_at[x] + lanes + 16 * c, o);
                             tmem_wait_ld();
 #pragma unroll
-                            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * fade);
-                            tmem_st32(o_at[x] + lanes + 32 * c, o);
+                            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * fade);
+                            tmem_st16(o_at[x] + lanes + 16 * c, o);
                         }
                     }
                     m = m_new;
@@ -278,26 +279,18 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
                     const float shift = m == -INFINITY ? 0.f : BIAS - m;
                     const f32x2 sc2 = dup2(scale2), sh2 = dup2(shift);
                     f32x2 sum = pack2(0.f, 0.f);
-                    uint32_t v[2][16];                  // 16 columns at a time, the next on their way
-                    tmem_ld16(S, v[0]);
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        tmem_wait_ld();
-                        if (c < 7) tmem_ld16(S + 16 * (c + 1), v[(c + 1) & 1]);
-                        if (!whole)
+                    for (int c = 0; c < 4; ++c) {
 #pragma unroll
-                            for (int k = 0; k < 16; ++k) if (!(keep[c / 2] >> (16 * (c & 1) + k) & 1)) v[c & 1][k] = 0xff800000u;
-                        uint32_t out[8];
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) {
+                        for (int k = 0; k < 16; ++k) {
                             float a, b;
-                            unpack2(fma2(pack2(__uint_as_float(v[c & 1][2 * k]), __uint_as_float(v[c & 1][2 * k + 1])), sc2, sh2), a, b);
+                            unpack2(fma2(pack2(__uint_as_float(v[c][2 * k]), __uint_as_float(v[c][2 * k + 1])), sc2, sh2), a, b);
                             a = ex2(a);
                             b = ex2(b);
                             sum = add2(sum, pack2(a, b));
-                            out[k] = pack_half<T>(a, b);
+                            v[c][k] = pack_half<T>(a, b);
                         }
-                        tmem_st8(S + 8 * c, out);
+                        tmem_st16(S + 16 * c, v[c]);
                     }
                     float a, b;
                     unpack2(sum, a, b);

@@ -95,7 +95,8 @@ __device__ __forceinline__ void tmem_st32(uint32_t at, const uint32_t (&r)[32]) 
                  "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
                  ::"r"(at), TIGA_W8(r, 0), TIGA_W8(r, 8), TIGA_W8(r, 16), TIGA_W8(r, 24) : "memory");
 }
-__device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&r)[16]) {
+template <int N>
+__device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&r)[N]) {          // the first 16
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
                  ::"r"(at), TIGA_W8(r, 0), TIGA_W8(r, 8) : "memory");
 }
