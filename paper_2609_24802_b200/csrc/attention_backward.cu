@@ -15,13 +15,12 @@ namespace tiga {
 // grad_value and the next step's S.
 // fp16: P carries 2^14 and dS a power of two from the largest norms of the rows of grad_out and value, which bound |dP - delta|: the
 // largest value cannot overflow, the smallest keep as many digits as there are.
-constexpr int BWD_THREADS = 512, BWD_ROWS = 128, BWD_STEP = 128, BWD_LEAST = 2;
+constexpr int BWD_WEIGHT_WARPS = 16, BWD_PRODUCER = BWD_WEIGHT_WARPS, BWD_MMA = BWD_PRODUCER + 4;
+constexpr int BWD_THREADS = 32 * (BWD_MMA + 1), BWD_ROWS = 128, BWD_STEP = 128, BWD_LEAST = 2;
 typedef Cut<BWD_ROWS, BWD_STEP, true> KvCut;
 typedef Cut<BWD_ROWS, BWD_STEP, false> QCut;
 template <bool KV> struct CutOf { typedef QCut type; };
 template <> struct CutOf<true> { typedef KvCut type; };
-// registers of a weight, producer and matrix thread: 2 * 184 + 88 + 56 = 4 * 128, what the block is launched with
-constexpr int BWD_WEIGHT_REGS = 184, BWD_PRODUCER_REGS = 88, BWD_MMA_REGS = 56;
 // What goes along with a step's rows.  A step's first tile waits for the place of the one SLOTS tiles before, of which SLOTS / 2
 // steps at most are behind: the steps in front of those are done with their entries.
 constexpr int BWD_AUX = 4;
@@ -143,28 +142,28 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
         mbar_init(bar(ctl.x_empty), 1);
         mbar_init(bar(ctl.s_full), 1);
         mbar_init(bar(ctl.dp_full), 1);
-        mbar_init(bar(ctl.p_full), 256);
-        mbar_init(bar(ctl.ds_full), 256);
+        mbar_init(bar(ctl.p_full), 32 * BWD_WEIGHT_WARPS);
+        mbar_init(bar(ctl.ds_full), 32 * BWD_WEIGHT_WARPS);
         mbar_init(bar(ctl.acc_full), 1);
-        mbar_init(bar(ctl.acc_empty), 256);
+        mbar_init(bar(ctl.acc_empty), 32 * BWD_WEIGHT_WARPS);
         mbar_init(bar(ctl.drain), 1);
         ctl.abort_word = ctl.never = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 12) tmem_alloc(smem_u32(&ctl.tmem), 512);
+    if (warp == BWD_MMA) tmem_alloc(smem_u32(&ctl.tmem), 512);
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
     const uint32_t tmem = ctl.tmem;
     const uint32_t s_at = tmem, dp_at = tmem + 128, acc1 = tmem + 256, acc2 = tmem + 384;
 
-    if (warp >= 8 && warp < 12) {
+    if (warp >= BWD_PRODUCER && warp < BWD_MMA) {
         // ---------------------------------------------------------------- producers
-        registers_down<BWD_PRODUCER_REGS>();
-        const int pw = warp - 8;
+        const int pw = warp - BWD_PRODUCER;
         uint32_t tiles = 0, steps = 0, items = 0;
         bool ok = true;
-        auto slot_free = [&]() { return tiles < (uint32_t)C::SLOTS || mbar_wait(bar(ctl.empty[tiles % C::SLOTS]), (tiles / C::SLOTS + 1) & 1, abort_word); };
+        auto wait = [&](unsigned long long& b, uint32_t parity) { return ok = __all_sync(~0u, mbar_wait(bar(b), parity & 1, abort_word)); };
+        auto slot_free = [&]() { return tiles < (uint32_t)C::SLOTS || wait(ctl.empty[tiles % C::SLOTS], tiles / C::SLOTS + 1); };
         for (; more && ok; more = it.next(p), ++items) {
             const int packed_rows = it.g.nq * p.group;
             // a row of the other side, or of the tile itself: where key r lies, or whether packed row r is wanted
@@ -187,7 +186,7 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
                 if (keys) fetch_keys<DP>(tile, 32 * pw, full, p, maps, second, a, it.h, w.stats);
                 else fetch_packed<DP>(tile, 32 * pw, full, p, it.g, maps, second, it.h, r, wanted, w.stats);
             };
-            if (items && !(ok = mbar_wait(bar(ctl.x_empty), (items - 1) & 1, abort_word))) break;
+            if (items && !wait(ctl.x_empty, items - 1)) break;
             look(KV, it.t * BWD_ROWS + 32 * pw + lane);
             for (int y = 0; y < 2; ++y) fetch(x_tile + y * C::TILE, bar(ctl.x_full), KV, y, at, on, it.t * BWD_ROWS + 32 * pw + lane);
             look(!KV, it.i0 * BWD_STEP + 32 * pw + lane);
@@ -196,7 +195,7 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
                 const bool wanted = on;
                 const float2 st = stat;
                 const int aux = steps % BWD_AUX;
-                if (!(ok = slot_free())) break;
+                if (!slot_free()) break;
                 if (KV) {
                     ctl.minus_lse[aux][32 * pw + lane] = BIAS - st.x;
                     ctl.minus_delta[aux][32 * pw + lane] = -st.y;
@@ -208,7 +207,7 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
                 if (lane == 0) mbar_arrive(bar(ctl.aux_full[aux]));
                 if (i + 1 < it.i1) look(!KV, (i + 1) * BWD_STEP + 32 * pw + lane);
                 for (int y = 0; y < 2; ++y, ++tiles) {
-                    if (y && !(ok = slot_free())) break;
+                    if (y && !slot_free()) break;
                     fetch(ring + (tiles % C::SLOTS) * C::TILE, bar(ctl.full[tiles % C::SLOTS]), !KV, y, here, wanted, i * BWD_STEP + 32 * pw + lane);
                 }
                 if (!ok) break;
@@ -219,95 +218,101 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
             for (uint32_t k = tiles < (uint32_t)C::SLOTS ? 0 : tiles - C::SLOTS; k < tiles; ++k) mbar_wait(bar(ctl.full[k % C::SLOTS]), (k / C::SLOTS) & 1, &ctl.never);
             if (items) mbar_wait(bar(ctl.x_full), (items - 1) & 1, &ctl.never);
         }
-    } else if (warp >= 12) {
+    } else if (warp == BWD_MMA) {
         // ---------------------------------------------------------------- matrix instructions
-        registers_down<BWD_MMA_REGS>();
-        if (warp == 12 && lane == 0) {
-            const uint32_t s_shape = mma_shape<T>(BWD_STEP, false), acc_shape = mma_shape<T>(DP, true);
-            const uint32_t sign = p.scale < 0.f ? MMA_NEGATE_A : 0;
-            uint32_t tile0 = 0, steps = 0, items = 0;
-            bool ok = true;
-            const int pieces = (p.D + 15) / 16;
-            auto slot = [&](uint32_t tile) { return ring + (tile % C::SLOTS) * C::TILE; };
-            auto wait_tile = [&](uint32_t tile) {
-                ok = ok && mbar_wait(bar(ctl.full[tile % C::SLOTS]), (tile / C::SLOTS) & 1, abort_word);
-                fence_async_proxy();
-            };
-            auto wait_threads = [&](unsigned long long& b, uint32_t parity) {
-                ok = ok && mbar_wait(bar(b), parity & 1, abort_word);
-                tmem_fence_after();
-            };
-            auto release = [&](uint32_t tile) { mma_commit(bar(ctl.empty[tile % C::SLOTS])); };
-            // d = X Y^T, features in pieces of 16
-            auto inner = [&](uint32_t d, uint32_t x, uint32_t tile, uint32_t shape) {
-                for (int k = 0; k < pieces; ++k) {
-                    const uint32_t at = (k / 4) * (128 * 128) + (k % 4) * 32;
-                    mma_ss(d, smem_desc(x + at, 16), smem_desc(slot(tile) + at, 16), shape, k > 0);
-                }
-            };
-            // acc (+)= (16-bit weights at a: 64 columns of them in the first half of each 64) Y
-            auto outer = [&](uint32_t acc, uint32_t a, uint32_t tile, bool add) {
+        const bool lead = lane == 0;            // the warp goes its way together, one thread issues
+        const uint32_t s_shape = mma_shape<T>(BWD_STEP, false), acc_shape = mma_shape<T>(DP, true);
+        const uint32_t sign = p.scale < 0.f ? MMA_NEGATE_A : 0;
+        uint32_t tile0 = 0, steps = 0, items = 0;
+        bool ok = true;
+        // descriptors differ in their address alone (see the forward kernel)
+        const uint32_t x_desc = smem_desc(x_tile, 16), inner_desc = smem_desc(ring, 16), outer_desc = smem_desc(ring, 128 * 128);
+        auto slot = [&](uint32_t tile) { return (tile % C::SLOTS) * (uint32_t)(C::TILE / 16); };
+        auto wait = [&](unsigned long long& b, uint32_t parity) { ok = __all_sync(~0u, ok && mbar_wait(bar(b), parity & 1, abort_word)); };
+        auto wait_tile = [&](uint32_t tile) {
+            wait(ctl.full[tile % C::SLOTS], tile / C::SLOTS);
+            fence_async_proxy();
+        };
+        auto wait_threads = [&](unsigned long long& b, uint32_t parity) {
+            wait(b, parity);
+            tmem_fence_after();
+        };
+        auto commit = [&](unsigned long long& b) { if (lead) mma_commit(bar(b)); };
+        auto release = [&](uint32_t tile) { commit(ctl.empty[tile % C::SLOTS]); };
+        // d = X Y^T, features in pieces of 16
+        auto inner = [&](uint32_t d, int second, uint32_t tile, uint32_t shape) {
+            const uint32_t x = x_desc + second * (C::TILE / 16), y = inner_desc + slot(tile);
+            if (lead)
 #pragma unroll
-                for (int k = 0; k < BWD_STEP / 16; ++k)
-                    mma_ts(acc, a + (k / 4) * 64 + (k % 4) * 8, smem_desc(slot(tile) + k * 2048, 128 * 128), acc_shape, add || k > 0);
-            };
-            for (; more && ok; more = it.next(p), ++items) {
-                const int n = it.i1 - it.i0;
-                ok = ok && mbar_wait(bar(ctl.x_full), items & 1, abort_word);
-                wait_tile(tile0);
-                if (!ok) break;
-                inner(s_at, x_tile, tile0, s_shape | sign);
-                mma_commit(bar(ctl.s_full));
-                wait_tile(tile0 + 1);
-                if (!ok) break;
-                inner(dp_at, x_tile + C::TILE, tile0 + 1, s_shape);
-                mma_commit(bar(ctl.dp_full));
-                if (!KV) release(tile0 + 1);
-                if (n == 1) mma_commit(bar(ctl.x_empty));
-                for (int i = 0; i < n; ++i, ++steps) {
-                    const uint32_t y1 = tile0 + 2 * i, y2 = y1 + 1;
-                    const bool again = i + 1 < n;
-                    wait_threads(ctl.p_full, steps);
-                    if (i == 0 && items) ok = ok && mbar_wait(bar(ctl.acc_empty), (items - 1) & 1, abort_word);
-                    if (!ok) break;
-                    if (KV) {
-                        outer(acc2, s_at, y2, i > 0);
-                        release(y2);
-                    }
-                    if (again) {
-                        wait_tile(y1 + 2);
-                        if (!ok) break;
-                        inner(s_at, x_tile, y1 + 2, s_shape | sign);
-                        mma_commit(bar(ctl.s_full));
-                    }
-                    wait_threads(ctl.ds_full, steps);
-                    if (!ok) break;
-                    outer(acc1, dp_at, y1, i > 0);
-                    release(y1);
-                    if (again) {
-                        wait_tile(y2 + 2);
-                        if (!ok) break;
-                        inner(dp_at, x_tile + C::TILE, y2 + 2, s_shape);
-                        mma_commit(bar(ctl.dp_full));
-                        if (!KV) release(y2 + 2);
-                        if (i + 2 == n) mma_commit(bar(ctl.x_empty));
-                    }
-                }
-                if (!ok) break;
-                mma_commit(bar(ctl.acc_full));
-                tile0 += 2 * n;
+                for (int k = 0; k < DP / 16; ++k)
+                    if (k * 16 < p.D) mma_ss(d, x + piece(k), y + piece(k), shape, k > 0);
+            __syncwarp();
+        };
+        // acc (+)= (16-bit weights at a: 32 of them in the first half of each 32 columns) Y
+        auto outer = [&](uint32_t acc, uint32_t a, uint32_t tile, bool add) {
+            const uint32_t y = outer_desc + slot(tile);
+            if (lead) {
+                mma_ts(acc, a, y, acc_shape, add);
+#pragma unroll
+                for (int k = 1; k < BWD_STEP / 16; ++k) mma_ts(acc, a + (k / 2) * 32 + (k % 2) * 8, y + k * (2048 / 16), acc_shape, true);
             }
-            mma_commit(bar(ctl.drain));
-            mbar_wait(bar(ctl.drain), 0, &ctl.never);
+            __syncwarp();
+        };
+        for (; more && ok; more = it.next(p), ++items) {
+            const int n = it.i1 - it.i0;
+            wait(ctl.x_full, items);
+            wait_tile(tile0);
+            if (!ok) break;
+            inner(s_at, 0, tile0, s_shape | sign);
+            commit(ctl.s_full);
+            wait_tile(tile0 + 1);
+            if (!ok) break;
+            inner(dp_at, 1, tile0 + 1, s_shape);
+            commit(ctl.dp_full);
+            if (!KV) release(tile0 + 1);
+            if (n == 1) commit(ctl.x_empty);
+            for (int i = 0; i < n; ++i, ++steps) {
+                const uint32_t y1 = tile0 + 2 * i, y2 = y1 + 1;
+                const bool again = i + 1 < n;
+                wait_threads(ctl.p_full, steps);
+                if (i == 0 && items) wait(ctl.acc_empty, items - 1);
+                if (!ok) break;
+                if (KV) {
+                    outer(acc2, s_at, y2, i > 0);
+                    release(y2);
+                }
+                if (again) {
+                    wait_tile(y1 + 2);
+                    if (!ok) break;
+                    inner(s_at, 0, y1 + 2, s_shape | sign);
+                    commit(ctl.s_full);
+                }
+                wait_threads(ctl.ds_full, steps);
+                if (!ok) break;
+                outer(acc1, dp_at, y1, i > 0);
+                release(y1);
+                if (again) {
+                    wait_tile(y2 + 2);
+                    if (!ok) break;
+                    inner(dp_at, 1, y2 + 2, s_shape);
+                    commit(ctl.dp_full);
+                    if (!KV) release(y2 + 2);
+                    if (i + 2 == n) commit(ctl.x_empty);
+                }
+            }
+            if (!ok) break;
+            commit(ctl.acc_full);
+            tile0 += 2 * n;
         }
+        commit(ctl.drain);
+        mbar_wait(bar(ctl.drain), 0, &ctl.never);
         __syncwarp();
     } else {
-        // ---------------------------------------------------------------- weights: warpgroup x has 64 of a step's 128 columns
-        registers_up<BWD_WEIGHT_REGS>();
+        // ---------------------------------------------------------------- weights: warpgroup x has 32 of a step's 128 columns
         const int x = warp / 4;
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const int row = threadIdx.x & 127;
-        const uint32_t S = s_at + lanes + 64 * x, dP = dp_at + lanes + 64 * x;
+        const uint32_t S = s_at + lanes + 32 * x, dP = dp_at + lanes + 32 * x;
         const float scale2 = fmaxf(fabsf(p.scale) * LOG2E_F, 1e-30f);
         const float factor = F16 ? gradient_factor(w.norms) : 1.f;
         const f32x2 sc2 = dup2(scale2), ds2 = dup2(F16 ? factor * 0x1p-14f : 1.f);
@@ -337,35 +342,32 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
                 ok = __all_sync(~0u, ok);
                 if (!ok) continue;
                 tmem_fence_after();
-                f32x2 e[32];
+                f32x2 e[16];
                 if (warp_on) {
-                    uint32_t v[2][32];
-                    tmem_ld32(S, v[0]);
-                    tmem_ld32(S + 32, v[1]);
-                    tmem_wait_ld();
+                    uint32_t v[32];
+                    tmem_ld32(S, v);
+                    const float4* nl = reinterpret_cast<const float4*>(ctl.minus_lse[aux] + 32 * x);
+                    const uint32_t keep = KV ? ~0u : ctl.mask[aux][x];
+                    tmem_wait_ld(v);
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        const float4* nl = reinterpret_cast<const float4*>(ctl.minus_lse[aux] + 64 * x + 32 * c);
-                        const uint32_t keep = KV ? ~0u : ctl.mask[aux][2 * x + c];
-                        uint32_t out[16];
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) {
-                            f32x2 lse = my_lse;
-                            if (KV) { const float4 l4 = nl[k / 2]; lse = k & 1 ? pack2(l4.z, l4.w) : pack2(l4.x, l4.y); }
-                            float a, b;
-                            unpack2(fma2(pack2(__uint_as_float(v[c][2 * k]), __uint_as_float(v[c][2 * k + 1])), sc2, lse), a, b);
-                            a = ex2(a);
-                            b = ex2(b);
-                            if (!KV && keep != ~0u) {
-                                if (!(keep >> (2 * k) & 1)) a = 0.f;
-                                if (!(keep >> (2 * k + 1) & 1)) b = 0.f;
-                            }
-                            e[16 * c + k] = pack2(a, b);
-                            if (KV) out[k] = pack_half<T>(a, b);
+                    for (int k = 0; k < 16; ++k) {
+                        f32x2 lse = my_lse;
+                        if (KV) { const float4 l4 = nl[k / 2]; lse = k & 1 ? pack2(l4.z, l4.w) : pack2(l4.x, l4.y); }
+                        float a, b;
+                        unpack2(fma2(pack2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), sc2, lse), a, b);
+                        a = ex2(a);
+                        b = ex2(b);
+                        if (!KV && keep != ~0u) {
+                            if (!(keep >> (2 * k) & 1)) a = 0.f;
+                            if (!(keep >> (2 * k + 1) & 1)) b = 0.f;
                         }
-                        if (KV) tmem_st16(S + 16 * c, out);
+                        e[k] = pack2(a, b);
+                        if (KV) v[k] = pack_half<T>(a, b);
                     }
-                    if (KV) tmem_wait_st();
+                    if (KV) {
+                        tmem_st16(S, v);
+                        tmem_wait_st();
+                    }
                 }
                 tmem_fence_before();
                 mbar_arrive(bar(ctl.p_full));
@@ -374,26 +376,21 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
                 if (!ok) continue;
                 tmem_fence_after();
                 if (warp_on) {
-                    uint32_t v[2][32];
-                    tmem_ld32(dP, v[0]);
-                    tmem_ld32(dP + 32, v[1]);
-                    tmem_wait_ld();
+                    uint32_t v[32];
+                    tmem_ld32(dP, v);
+                    const float4* nd = reinterpret_cast<const float4*>(ctl.minus_delta[aux] + 32 * x);
+                    tmem_wait_ld(v);
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        const float4* nd = reinterpret_cast<const float4*>(ctl.minus_delta[aux] + 64 * x + 32 * c);
-                        uint32_t out[16];
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) {
-                            f32x2 delta = my_delta;
-                            if (KV) { const float4 d4 = nd[k / 2]; delta = k & 1 ? pack2(d4.z, d4.w) : pack2(d4.x, d4.y); }
-                            f32x2 g = mul2(e[16 * c + k], add2(pack2(__uint_as_float(v[c][2 * k]), __uint_as_float(v[c][2 * k + 1])), delta));
-                            if (F16) g = mul2(g, ds2);
-                            float a, b;
-                            unpack2(g, a, b);
-                            out[k] = pack_half<T>(a, b);
-                        }
-                        tmem_st16(dP + 16 * c, out);
+                    for (int k = 0; k < 16; ++k) {
+                        f32x2 delta = my_delta;
+                        if (KV) { const float4 d4 = nd[k / 2]; delta = k & 1 ? pack2(d4.z, d4.w) : pack2(d4.x, d4.y); }
+                        f32x2 g = mul2(e[k], add2(pack2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), delta));
+                        if (F16) g = mul2(g, ds2);
+                        float a, b;
+                        unpack2(g, a, b);
+                        v[k] = pack_half<T>(a, b);
                     }
+                    tmem_st16(dP, v);
                     tmem_wait_st();
                 }
                 tmem_fence_before();
@@ -402,30 +399,30 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
             ok = ok && mbar_wait(bar(ctl.acc_full), items & 1, abort_word);
             ok = __all_sync(~0u, ok);
             tmem_fence_after();
-            // keys stationary: warpgroup 0 writes grad_key, 1 grad_value; queries: a half of grad_q's features each
+            // keys stationary: warpgroups 0 and 1 write grad_key, 2 and 3 grad_value, a half of the features each; queries: a quarter each
             const bool whole_tile = it.i0 == 0 && it.i1 == it.steps;
             const int rows = KV ? w.kv_rows : w.q_rows;
-            constexpr int SIDES = KV ? 2 : 1;
-            const uint32_t acc = KV && x ? acc2 : acc1;
-            const float finish = KV && x ? (F16 ? 0x1p-14f : 1.f) : p.scale / factor;
-            T* out = (T*)(KV ? (x ? p.gv : p.gk) : p.gq);
-            float* part = w.part + ((((2LL * blockIdx.x + (it.i0 == 0)) * rows + row) * SIDES) + (KV ? x : 0)) * DP;
-            const int c0 = KV ? 0 : x * (DP / 64), c1 = KV ? DP / 32 : c0 + DP / 64;
+            constexpr int SIDES = KV ? 2 : 1, PIECES = DP / 16 * SIDES / 4;        // pieces of 16 features a thread
+            const int side = KV ? x / 2 : 0, c0 = (KV ? x % 2 : x) * PIECES;
+            const uint32_t acc = side ? acc2 : acc1;
+            const float finish = side ? (F16 ? 0x1p-14f : 1.f) : p.scale / factor;
+            T* out = (T*)(KV ? (side ? p.gv : p.gk) : p.gq);
+            float* part = w.part + ((((2LL * blockIdx.x + (it.i0 == 0)) * rows + row) * SIDES) + side) * DP;
             if (warp_on)
-                for (int c = c0; c < c1; ++c) {
-                    uint32_t v[32];
-                    tmem_ld32(acc + lanes + 32 * c, v);
-                    tmem_wait_ld();
+                for (int c = c0; c < c0 + PIECES; ++c) {
+                    uint32_t v[16];
+                    tmem_ld16(acc + lanes + 16 * c, v);
+                    tmem_wait_ld(v);
                     if (!valid) continue;
                     if (!ok)
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) v[k] = 0x7fffffffu;
+                        for (int k = 0; k < 16; ++k) v[k] = 0x7fffffffu;
                     if (whole_tile) {
                         if (!out) continue;
-                        uint4* o4 = reinterpret_cast<uint4*>(out + out_row * p.D + 32 * c);
+                        uint4* o4 = reinterpret_cast<uint4*>(out + out_row * p.D + 16 * c);
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            if (32 * c + 8 * k >= p.D) continue;
+                        for (int k = 0; k < 2; ++k) {
+                            if (16 * c + 8 * k >= p.D) continue;
                             uint32_t o[4];
 #pragma unroll
                             for (int e = 0; e < 4; ++e)
@@ -433,9 +430,9 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
                             o4[k] = make_uint4(o[0], o[1], o[2], o[3]);
                         }
                     } else {
-                        uint4* o4 = reinterpret_cast<uint4*>(part + 32 * c);
+                        uint4* o4 = reinterpret_cast<uint4*>(part + 16 * c);
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) o4[k] = make_uint4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+                        for (int k = 0; k < 4; ++k) o4[k] = make_uint4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
                     }
                 }
             tmem_fence_before();
@@ -444,7 +441,7 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
     }
     tmem_fence_before();
     __syncthreads();
-    if (warp == 12) { tmem_fence_after(); tmem_free(tmem, 512); }
+    if (warp == BWD_MMA) { tmem_fence_after(); tmem_free(tmem, 512); }
 }
 
 // Adds up the partial sums of a tile that several blocks shared, in the order of its steps.  A warp has a row of one gradient; many parts

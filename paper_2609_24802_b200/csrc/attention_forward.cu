@@ -4,20 +4,21 @@
 
 namespace tiga {
 
-// A block holds a tile of 256 packed rows as two halves of 128, one warpgroup of softmax threads for each (a thread has a row), and
-// goes through the keys in steps of 128:
-//   producers (4 warps)   copy query and key / value rows to shared memory, 16 bytes a lane, any stride or page, zeros for what is
-//                         masked, missing or behind the head's width; a ring of key and value tiles in the order K0 V0 K1 V1 ...
+// A block holds a tile of 256 packed rows as two halves of 128, two warpgroups of softmax threads for each (a row has two threads,
+// for 64 of a step's columns each), and goes through the keys in steps of 128:
+//   producers (4 warps)   bring query and key / value rows to shared memory (attention_tiles.cuh), zeros for what is masked, missing
+//                         or behind the head's width; a ring of key and value tiles in the order K0 V0 K1 V1 ...
 //   one thread            issues S = Q K^T (to tensor memory) and O += P V (P from tensor memory, O stays there for the whole tile)
 //   softmax warpgroups    running maximum, P = exp2(S - m) in 16 bits over S's own columns, running mass
-// While one half's softmax runs, the tensor cores work for the other.  A tile of at most 128 rows has one half; then the two
-// warpgroups take the even and the odd steps with a state each, joined at the end, so a single token keeps both busy too.
+// While one half's softmax runs, the tensor cores work for the other.  A tile of at most 128 rows has one half; then the warpgroups
+// of the halves take the even and the odd steps with a state each, joined at the end, so a single token keeps both busy too.
 // The accumulator is rescaled only when a row's maximum grew by more than 2^8 since the last time: weights up to 2^8 do no harm,
 // and the mass carries the same factor.
-constexpr int FWD_THREADS = 512, FWD_ROWS = 256, FWD_STEP = 128;
+// What bounds it: the chain S -> maximum -> P -> O of a half.  A warp alone on its scheduler takes about 13 cycles a column for the
+// exponentials (8 are the unit's), so a row's two threads halve the chain; the exchange of their maxima costs about 100 cycles.
+constexpr int FWD_SOFTMAX_WARPS = 16, FWD_PRODUCER = FWD_SOFTMAX_WARPS, FWD_MMA = FWD_PRODUCER + 4;
+constexpr int FWD_THREADS = 32 * (FWD_MMA + 1), FWD_ROWS = 256, FWD_STEP = 128;
 typedef Cut<FWD_ROWS, FWD_STEP, false> FwdCut;
-// registers of a softmax, producer and matrix thread: 2 * 192 + 80 + 48 = 4 * 128, what the block is launched with
-constexpr int FWD_SOFTMAX_REGS = 192, FWD_PRODUCER_REGS = 80, FWD_MMA_REGS = 48;
 constexpr int FWD_LEAST = 2;            // units a block at least
 constexpr int MASK_RING = 8;            // the producers are at most 6 steps ahead of the softmax (ring of at most 10 tiles)
 constexpr float RESCALE_AT = 8.f;
@@ -26,15 +27,15 @@ template <int DP> struct Fwd {
     static constexpr int TILE = 128 * DP * 2;
     static constexpr int SLOTS = DP == 128 ? 5 : 10;
     static constexpr int CONTROL = 2 * TILE + SLOTS * TILE;
-    static constexpr int SMEM = CONTROL + 2560;
+    static constexpr int SMEM = CONTROL + 3072;
 };
 
 struct FwdControl {
     unsigned long long full[10], empty[10], q_full, q_empty, s_full[2], p_full[2], o_full[2], mask_full[MASK_RING], drain;
     uint32_t tmem, abort_word, never, mask[MASK_RING][4];
-    float m[2][128], l[2][128];
+    float share[2][2][128];             // what a row's threads tell each other
 };
-static_assert(sizeof(FwdControl) <= 2560, "control block");
+static_assert(sizeof(FwdControl) <= 3072, "control block");
 
 struct FwdWork {
     long long* unit_start;          // NULL: the blocks count for themselves
@@ -65,26 +66,26 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
         for (int i = 0; i < C::SLOTS; ++i) { mbar_init(bar(ctl.full[i]), 128); mbar_init(bar(ctl.empty[i]), 1); }
         mbar_init(bar(ctl.q_full), 256);
         mbar_init(bar(ctl.q_empty), 1);
-        for (int x = 0; x < 2; ++x) { mbar_init(bar(ctl.s_full[x]), 1); mbar_init(bar(ctl.p_full[x]), 128); mbar_init(bar(ctl.o_full[x]), 1); }
+        for (int x = 0; x < 2; ++x) { mbar_init(bar(ctl.s_full[x]), 1); mbar_init(bar(ctl.p_full[x]), 256); mbar_init(bar(ctl.o_full[x]), 1); }
         for (int i = 0; i < MASK_RING; ++i) mbar_init(bar(ctl.mask_full[i]), 4);
         mbar_init(bar(ctl.drain), 1);
         ctl.abort_word = ctl.never = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 12) tmem_alloc(smem_u32(&ctl.tmem), 512);
+    if (warp == FWD_MMA) tmem_alloc(smem_u32(&ctl.tmem), 512);
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
     const uint32_t tmem = ctl.tmem;
     const uint32_t s_at[2] = {tmem, tmem + 128}, o_at[2] = {tmem + 256, tmem + 256 + DP};
 
-    if (warp >= 8 && warp < 12) {
+    if (warp >= FWD_PRODUCER && warp < FWD_MMA) {
         // ---------------------------------------------------------------- producers
-        registers_down<FWD_PRODUCER_REGS>();
-        const int pw = warp - 8;
+        const int pw = warp - FWD_PRODUCER;
         uint32_t tiles = 0, steps = 0, items = 0;
         bool ok = true;
-        auto slot_free = [&]() { return tiles < (uint32_t)C::SLOTS || mbar_wait(bar(ctl.empty[tiles % C::SLOTS]), (tiles / C::SLOTS + 1) & 1, abort_word); };
+        auto wait = [&](unsigned long long& b, uint32_t parity) { return ok = __all_sync(~0u, mbar_wait(bar(b), parity & 1, abort_word)); };
+        auto slot_free = [&]() { return tiles < (uint32_t)C::SLOTS || wait(ctl.empty[tiles % C::SLOTS], tiles / C::SLOTS + 1); };
         for (; more && ok; more = it.next(p), ++items) {
             const int rows = min(it.g.nq * p.group - it.t * FWD_ROWS, FWD_ROWS);
             auto place = [&](int i) {
@@ -101,11 +102,11 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
                 }
                 if (i + 1 < it.i1) at = place(i + 1);
                 for (int kv = 0; kv < 2; ++kv, ++tiles) {
-                    if (!(ok = slot_free())) break;
+                    if (!slot_free()) break;
                     fetch_keys<DP>(ring + (tiles % C::SLOTS) * C::TILE, 32 * pw, bar(ctl.full[tiles % C::SLOTS]), p, maps, kv, here, it.h, p.q);
                 }
                 if (i == it.i0 && ok) {         // the queries' tile may still be in use by the item before: its first keys are on their way
-                    if (items && !(ok = mbar_wait(bar(ctl.q_empty), (items - 1) & 1, abort_word))) break;
+                    if (items && !wait(ctl.q_empty, items - 1)) break;
                     for (int x = 0; x < 2; ++x) {
                         const int r = x * 128 + 32 * pw + lane;
                         if (x == 1 && rows <= 128) {
@@ -120,93 +121,90 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
             for (uint32_t k = tiles < (uint32_t)C::SLOTS ? 0 : tiles - C::SLOTS; k < tiles; ++k) mbar_wait(bar(ctl.full[k % C::SLOTS]), (k / C::SLOTS) & 1, &ctl.never);
             if (items) mbar_wait(bar(ctl.q_full), (items - 1) & 1, &ctl.never);
         }
-    } else if (warp >= 12) {
-        registers_down<FWD_MMA_REGS>();
+    } else if (warp == FWD_MMA) {
         // ---------------------------------------------------------------- matrix instructions
-        if (warp == 12 && lane == 0) {
-            const uint32_t s_shape = mma_shape<T>(128, false) | (p.scale < 0.f ? MMA_NEGATE_A : 0), o_shape = mma_shape<T>(DP, true);
-            uint32_t tile0 = 0, items = 0, done[2] = {0, 0};     // done: p_full phases consumed
-            bool ok = true;
-            const int k_pieces = (p.D + 15) / 16;
-            auto slot = [&](uint32_t tile) { return ring + (tile % C::SLOTS) * C::TILE; };
-            auto wait_tile = [&](uint32_t tile) {
-                ok = ok && mbar_wait(bar(ctl.full[tile % C::SLOTS]), (tile / C::SLOTS) & 1, abort_word);
-                fence_async_proxy();
-            };
-            auto release = [&](uint32_t tile) { mma_commit(bar(ctl.empty[tile % C::SLOTS])); };
-            auto scores = [&](int x, int half, uint32_t tile) {
-                for (int k = 0; k < k_pieces; ++k) {
-                    const uint32_t at = (k / 4) * (128 * 128) + (k % 4) * 32;
-                    mma_ss(s_at[x], smem_desc(q_tile + half * C::TILE + at, 16), smem_desc(slot(tile) + at, 16), s_shape, k > 0);
-                }
-                mma_commit(bar(ctl.s_full[x]));
-            };
-            auto values = [&](int x, uint32_t tile, bool add) {
-                ok = ok && mbar_wait(bar(ctl.p_full[x]), done[x] & 1, abort_word);
-                ++done[x];
-                if (!ok) return;
-                tmem_fence_after();
+        const bool lead = lane == 0;            // the warp goes its way together, one thread issues
+        const uint32_t s_shape = mma_shape<T>(128, false) | (p.scale < 0.f ? MMA_NEGATE_A : 0), o_shape = mma_shape<T>(DP, true);
+        uint32_t tile0 = 0, items = 0, done0 = 0, done1 = 0;     // done: p_full phases consumed
+        bool ok = true;
+        // descriptors differ in their address alone: a product costs its instruction and an addition (built anew each time, about
+        // 100 cycles of this one thread, they bounded the kernel)
+        const uint32_t q_desc = smem_desc(q_tile, 16), k_desc = smem_desc(ring, 16), v_desc = smem_desc(ring, 128 * 128);
+        auto slot = [&](uint32_t tile) { return (tile % C::SLOTS) * (uint32_t)(C::TILE / 16); };
+        auto wait = [&](unsigned long long& b, uint32_t parity) { ok = __all_sync(~0u, ok && mbar_wait(bar(b), parity & 1, abort_word)); };
+        auto wait_tile = [&](uint32_t tile) {
+            wait(ctl.full[tile % C::SLOTS], tile / C::SLOTS);
+            fence_async_proxy();
+        };
+        auto release = [&](uint32_t tile) { if (lead) mma_commit(bar(ctl.empty[tile % C::SLOTS])); };
+        auto scores = [&](int x, int half, uint32_t tile) {
+            const uint32_t q = q_desc + half * (C::TILE / 16), k = k_desc + slot(tile);
+            if (lead) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) mma_ts(o_at[x], s_at[x] + k * 8, smem_desc(slot(tile) + k * 2048, 128 * 128), o_shape, add || k > 0);
+                for (int c = 0; c < DP / 16; ++c)
+                    if (c * 16 < p.D) mma_ss(tmem + 128 * x, q + piece(c), k + piece(c), s_shape, c > 0);
+                mma_commit(bar(ctl.s_full[x]));
+            }
+            __syncwarp();
+        };
+        auto values = [&](int x, uint32_t tile, bool add) {
+            wait(ctl.p_full[x], x ? done1++ : done0++);
+            if (!ok) return;
+            tmem_fence_after();
+            const uint32_t v = v_desc + slot(tile);
+            const uint32_t o = tmem + 256 + DP * x, a = tmem + 128 * x;
+            if (lead) {
+                mma_ts(o, a, v, o_shape, add);
+#pragma unroll
+                for (int k = 1; k < 8; ++k) mma_ts(o, a + (k / 2) * 32 + (k % 2) * 8, v + k * (2048 / 16), o_shape, true);
                 mma_commit(bar(ctl.o_full[x]));
-            };
-            for (; more && ok; more = it.next(p), ++items) {
-                const int n = it.i1 - it.i0;
-                const bool two = it.g.nq * p.group - it.t * FWD_ROWS > 128;
-                ok = ok && mbar_wait(bar(ctl.q_full), items & 1, abort_word);
-                wait_tile(tile0);
-                if (!ok) break;
-                scores(0, 0, tile0);
-                if (two) {
-                    scores(1, 1, tile0);
-                    release(tile0);
-                } else {
-                    release(tile0);
-                    if (n > 1) {
-                        wait_tile(tile0 + 2);
-                        if (!ok) break;
-                        scores(1, 0, tile0 + 2);
-                        release(tile0 + 2);
-                    }
-                }
-                const int ahead = two ? 1 : 2;
-                for (int i = 0; i < n && ok; ++i) {
-                    const uint32_t v = tile0 + 2 * i + 1, k_next = tile0 + 2 * (i + ahead);
-                    const bool more_keys = i + ahead < n;
+            }
+            __syncwarp();
+        };
+        for (; more && ok; more = it.next(p), ++items) {
+            const int n = it.i1 - it.i0;
+            const bool two = it.g.nq * p.group - it.t * FWD_ROWS > 128;
+            const int ahead = two ? 1 : 2;              // steps between two of a half
+            wait(ctl.q_full, items);
+            // i: the step whose values are next; its half's (two: both halves') next scores follow
+            for (int i = -ahead; i < n && ok; ++i) {
+                const uint32_t v = tile0 + 2 * i + 1, k_next = tile0 + 2 * (i + ahead);
+                const bool more_keys = i + ahead < n;
+                const int x = two ? 0 : i & 1;
+                if (i >= 0) {
                     wait_tile(v);
-                    const int x = two ? 0 : i & 1;
                     values(x, v, i >= ahead);
                     if (!two && ok) release(v);
-                    if (more_keys) {
-                        wait_tile(k_next);
-                        if (!ok) break;
-                        scores(x, 0, k_next);
-                        if (!two) release(k_next);
-                    }
-                    if (two) {
-                        values(1, v, i > 0);
-                        if (!ok) break;
-                        release(v);
-                        if (more_keys) { scores(1, 1, k_next); release(k_next); }
-                    }
                 }
+                if (more_keys) wait_tile(k_next);
                 if (!ok) break;
-                mma_commit(bar(ctl.q_empty));
-                tile0 += 2 * n;
+                if (more_keys) scores(x, 0, k_next);
+                if (two && i >= 0) {
+                    values(1, v, i > 0);
+                    if (!ok) break;
+                    release(v);
+                }
+                if (two && more_keys) scores(1, 1, k_next);
+                if (more_keys) release(k_next);
             }
-            mma_commit(bar(ctl.drain));
-            mbar_wait(bar(ctl.drain), 0, &ctl.never);
+            if (!ok) break;
+            if (lead) mma_commit(bar(ctl.q_empty));
+            tile0 += 2 * n;
         }
+        if (lead) mma_commit(bar(ctl.drain));
+        mbar_wait(bar(ctl.drain), 0, &ctl.never);
         __syncwarp();
     } else {
         // ---------------------------------------------------------------- softmax
-        registers_up<FWD_SOFTMAX_REGS>();
-        const int x = warp / 4;
+        const int x = warp / 8, y = warp / 4 % 2;           // half, and which of its columns
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const int row = threadIdx.x & 127;
-        const uint32_t S = s_at[x] + lanes;
-        const float scale2 = fmaxf(fabsf(p.scale) * LOG2E_F, 1e-30f);     // (not zero: masked scores are -inf)
-        constexpr float BIAS = sizeof(T) == 2 && operand_type<T>() == 0 ? 7.f : 0.f;     // fp16: weights up to 2^15, so that small ones keep their digits
+        const uint32_t S = s_at[x] + lanes + 64 * y;
+        const float scale2 = fmaxf(fabsf(p.scale) * LOG2E_F, 1e-30f);       // (not zero: masked scores are -inf)
+        constexpr float BIAS = operand_type<T>() == 0 ? 7.f : 0.f;          // fp16: weights up to 2^15, so that small ones keep their digits
+        // The threads of a half, and all of them, meet here; everyone comes the same number of times, after a failed wait too.
+        auto meet_half = [&]() { if (x) asm volatile("bar.sync 2, 256;" ::: "memory"); else asm volatile("bar.sync 1, 256;" ::: "memory"); };
+        auto meet_all = [&]() { asm volatile("bar.sync 3, 512;" ::: "memory"); };
         uint32_t step0 = 0, s_done = 0, o_base[2] = {0, 0};
         bool ok = true;
         for (; more; more = it.next(p)) {
@@ -217,80 +215,92 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
             const bool valid = tile_row < rows;
             const bool warp_on = (tile_row & ~31) < rows;
             const int packed = it.t * FWD_ROWS + tile_row;
-            const int limit = p.causal && valid ? keys_of_row(p, it.g, packed / p.group) : it.g.nk;
-            float m = -INFINITY, l = 0.f;               // reference of the exponents (log2), mass relative to 2^(m - BIAS)
-            uint32_t mine = 0;                          // steps of this warpgroup in this item
+            const int limit = (p.causal && valid ? keys_of_row(p, it.g, packed / p.group) : it.g.nk) - it.i0 * FWD_STEP - 64 * y;
+            float m = -INFINITY, l = 0.f;               // reference of the exponents (log2), this thread's mass relative to 2^(m - BIAS)
+            uint32_t mine = 0;                          // steps of this half's threads in this item
             for (int i = two ? 0 : x; i < n; i += two ? 1 : 2, ++mine, ++s_done) {
                 const uint32_t step = step0 + i, ring_at = step % MASK_RING;
                 ok = ok && mbar_wait(bar(ctl.mask_full[ring_at]), (step / MASK_RING) & 1, abort_word) && mbar_wait(bar(ctl.s_full[x]), s_done & 1, abort_word);
                 ok = __all_sync(~0u, ok);
-                if (!ok) { m = l = __int_as_float(0x7fffffff); continue; }
                 tmem_fence_after();
-                if (warp_on) {
-                    uint32_t keep[4];
-                    const int lim = limit - (it.i0 + i) * FWD_STEP;
-                    bool whole = true;
+                const bool work = ok && warp_on;
+                uint32_t v[32], keep[2];            // 32 of the 64 columns are held, the others read twice: registers
+                bool whole = true;
+                float top = -INFINITY;
+                auto hide = [&](uint32_t kept) {
+                    if (!whole)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int bits = lim - 32 * k;
-                        keep[k] = ctl.mask[ring_at][k] & (bits >= 32 ? ~0u : bits <= 0 ? 0u : (1u << bits) - 1);
-                        whole = whole && keep[k] == ~0u;
+                        for (int k = 0; k < 32; ++k) if (!(kept >> k & 1)) v[k] = 0xff800000u;
+                };
+                if (work) {
+                    tmem_ld32(S, v);
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        const int bits = limit - i * FWD_STEP - 32 * c;
+                        keep[c] = ctl.mask[ring_at][2 * y + c] & (bits >= 32 ? ~0u : bits <= 0 ? 0u : (1u << bits) - 1);
                     }
-                    whole = __all_sync(~0u, whole);
-                    uint32_t v[4][32];
+                    whole = __all_sync(~0u, (keep[0] & keep[1]) == ~0u);
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) tmem_ld32(S + 32 * c, v[c]);
-                    tmem_wait_ld();
-                    float top = -INFINITY;
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        if (!whole)
-#pragma unroll
-                            for (int k = 0; k < 32; ++k) if (!(keep[c] >> k & 1)) v[c][k] = 0xff800000u;
+                    for (int c = 0; c < 2; ++c) {
+                        if (c) tmem_ld32(S + 32, v);
+                        tmem_wait_ld(v);
+                        hide(keep[c]);
                         float t0 = -INFINITY, t1 = -INFINITY;
 #pragma unroll
                         for (int k = 0; k < 32; k += 4) {
-                            t0 = max3(t0, __uint_as_float(v[c][k]), __uint_as_float(v[c][k + 1]));
-                            t1 = max3(t1, __uint_as_float(v[c][k + 2]), __uint_as_float(v[c][k + 3]));
+                            t0 = max3(t0, __uint_as_float(v[k]), __uint_as_float(v[k + 1]));
+                            t1 = max3(t1, __uint_as_float(v[k + 2]), __uint_as_float(v[k + 3]));
                         }
                         top = max3(top, t0, t1);
                     }
-                    top *= scale2;
+                }
+                ctl.share[x][y][row] = top;
+                meet_half();
+                if (work) {
+                    top = fmaxf(top, ctl.share[x][1 - y][row]) * scale2;
                     const bool grown = top > m + RESCALE_AT || (m == -INFINITY && top > -INFINITY);
-                    const float m_new = grown ? top : m;
-                    const float fade = grown ? ex2(m - m_new) : 1.f;
-                    if (mine && __any_sync(~0u, grown)) {
-                        ok = mbar_wait(bar(ctl.o_full[x]), (o_base[x] + mine - 1) & 1, abort_word);
-                        ok = __all_sync(~0u, ok);
-                        if (!ok) { m = l = __int_as_float(0x7fffffff); continue; }
-                        tmem_fence_after();
+                    if (__any_sync(~0u, grown)) {
+                        const float m_new = grown ? top : m;
+                        const float fade = grown ? ex2(m - m_new) : 1.f;
+                        if (mine) {
+                            ok = mbar_wait(bar(ctl.o_full[x]), (o_base[x] + mine - 1) & 1, abort_word);
+                            ok = __all_sync(~0u, ok);
+                            tmem_fence_after();
+                            if (ok)
 #pragma unroll 1
-                        for (int c = 0; c < DP / 16; ++c) {         // (rare, and S is held: few registers)
-                            uint32_t o[16];
-                            tmem_ld16(o_at[x] + lanes + 16 * c, o);
-                            tmem_wait_ld();
+                                for (int c = 0; c < DP / 16; ++c) {         // this thread's half of the features, eight at a time
+                                    const uint32_t at = o_at[x] + lanes + y * (DP / 2) + 8 * c;
+                                    uint32_t o[8];
+                                    tmem_ld8(at, o);
+                                    tmem_wait_ld(o);
 #pragma unroll
-                            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * fade);
-                            tmem_st16(o_at[x] + lanes + 16 * c, o);
+                                    for (int k = 0; k < 8; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * fade);
+                                    tmem_st8(at, o);
+                                }
                         }
+                        m = m_new;
+                        l *= fade;
                     }
-                    m = m_new;
-                    l *= fade;
                     const float shift = m == -INFINITY ? 0.f : BIAS - m;
                     const f32x2 sc2 = dup2(scale2), sh2 = dup2(shift);
                     f32x2 sum = pack2(0.f, 0.f);
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
+                    for (int c = 1; c >= 0; --c) {
+                        if (c == 0) {
+                            tmem_ld32(S, v);
+                            tmem_wait_ld(v);
+                            hide(keep[0]);
+                        }
 #pragma unroll
                         for (int k = 0; k < 16; ++k) {
                             float a, b;
-                            unpack2(fma2(pack2(__uint_as_float(v[c][2 * k]), __uint_as_float(v[c][2 * k + 1])), sc2, sh2), a, b);
+                            unpack2(fma2(pack2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), sc2, sh2), a, b);
                             a = ex2(a);
                             b = ex2(b);
                             sum = add2(sum, pack2(a, b));
-                            v[c][k] = pack_half<T>(a, b);
+                            v[k] = pack_half<T>(a, b);
                         }
-                        tmem_st16(S + 16 * c, v[c]);
+                        tmem_st16(S + 32 * c, v);           // in the first half of their own columns
                     }
                     float a, b;
                     unpack2(sum, a, b);
@@ -300,64 +310,73 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
                 tmem_fence_before();
                 mbar_arrive(bar(ctl.p_full[x]));
             }
-            // ---- the item's end: join the two states of a short tile, then finish the rows or put them aside
+            // ---- the item's end: the row's mass; a short tile's two states are joined; then the rows are finished or put aside
             const uint32_t made[2] = {two ? (uint32_t)n : (uint32_t)(n + 1) / 2, two ? (uint32_t)n : (uint32_t)n / 2};
-            for (int y = 0; y < 2; ++y)
-                if (made[y] && ok && (!two || y == x)) ok = mbar_wait(bar(ctl.o_full[y]), (o_base[y] + made[y] - 1) & 1, abort_word);
+            for (int z = 0; z < 2; ++z)
+                if (made[z] && ok && (!two || z == x)) ok = mbar_wait(bar(ctl.o_full[z]), (o_base[z] + made[z] - 1) & 1, abort_word);
             ok = __all_sync(~0u, ok);
             if (!ok) l = __int_as_float(0x7fffffff);
             tmem_fence_after();
-            float w0 = 1.f, w1 = 0.f;               // factors of this warpgroup's rows: two halves have one state each
-            if (!two) {
-                ctl.m[x][row] = m;
-                ctl.l[x][row] = l;
-                asm volatile("bar.sync 1, 256;" ::: "memory");
-                const float ma = ctl.m[0][row], mb = ctl.m[1][row];
+            ctl.share[x][y][row] = l;
+            float w0 = 1.f, w1 = 0.f;               // factors of the accumulators: two halves have one each
+            if (two) {
+                meet_half();
+                l += ctl.share[x][1 - y][row];
+            } else {
+                meet_all();
+                const float la = ctl.share[0][0][row] + ctl.share[0][1][row], lb = ctl.share[1][0][row] + ctl.share[1][1][row];
+                meet_all();
+                if (y == 0) ctl.share[x][0][row] = m;
+                meet_all();
+                const float ma = ctl.share[0][0][row], mb = ctl.share[1][0][row];
                 m = fmaxf(ma, mb);
                 w0 = ma == -INFINITY ? 0.f : ex2(ma - m);
                 w1 = mb == -INFINITY ? 0.f : ex2(mb - m);
-                l = ctl.l[0][row] * w0 + ctl.l[1][row] * w1;
+                l = la * w0 + lb * w1;
             }
             const bool whole_tile = it.i0 == 0 && it.i1 == it.steps;
             const long long part = (2LL * blockIdx.x + (it.i0 == 0)) * w.rows + tile_row;
             const PackedRow pr = packed_row(p, it.g, it.h, packed);
             const long long out_row = (long long)pr.row * p.heads + pr.head;
             const float finish = l > 0.f || l != l ? 1.f / l : 0.f;
-            const int c0 = two ? 0 : x * (DP / 64), c1 = two ? DP / 32 : c0 + DP / 64;
+            const int c0 = two ? y * (DP / 32) : (2 * x + y) * (DP / 64), c1 = c0 + (two ? DP / 32 : DP / 64);      // pieces of 16 features
             if (warp_on)
                 for (int c = c0; c < c1; ++c) {
-                    uint32_t v[32], u[32];
-                    tmem_ld32(o_at[two ? x : 0] + lanes + 32 * c, v);
-                    if (!two && made[1]) tmem_ld32(o_at[1] + lanes + 32 * c, u);
-                    tmem_wait_ld();
+                    uint32_t v[16], u[16];
+                    tmem_ld16(o_at[two ? x : 0] + lanes + 16 * c, v);
+                    tmem_ld16(o_at[1] + lanes + 16 * c, u);         // (read in short tiles with a second state only)
+                    tmem_wait_ld(v);
+                    tmem_wait_ld(u);
                     if (!two)
 #pragma unroll
-                        for (int k = 0; k < 32; ++k)
+                        for (int k = 0; k < 16; ++k)
                             v[k] = __float_as_uint(__uint_as_float(v[k]) * w0 + (made[1] ? __uint_as_float(u[k]) * w1 : 0.f));
                     if (!valid) continue;
                     if (whole_tile) {
-                        uint4* out = reinterpret_cast<uint4*>((T*)p.out + out_row * p.D + 32 * c);
+                        uint4* out = reinterpret_cast<uint4*>((T*)p.out + out_row * p.D + 16 * c);
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            if (32 * c + 8 * k >= p.D) continue;
+                        for (int k = 0; k < 2; ++k) {
+                            if (16 * c + 8 * k >= p.D) continue;
                             uint32_t o[4];
 #pragma unroll
                             for (int e = 0; e < 4; ++e)
-                                o[e] = pack_half<T>(finish == 0.f ? 0.f : __uint_as_float(v[8 * k + 2 * e]) * finish, finish == 0.f ? 0.f : __uint_as_float(v[8 * k + 2 * e + 1]) * finish);
+                                o[e] = finish == 0.f ? 0u : pack_half<T>(__uint_as_float(v[8 * k + 2 * e]) * finish, __uint_as_float(v[8 * k + 2 * e + 1]) * finish);
                             out[k] = make_uint4(o[0], o[1], o[2], o[3]);
                         }
                     } else {
-                        uint4* out = reinterpret_cast<uint4*>(w.part_o + part * DP + 32 * c);
+                        uint4* out = reinterpret_cast<uint4*>(w.part_o + part * DP + 16 * c);
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) out[k] = make_uint4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+                        for (int k = 0; k < 4; ++k) out[k] = make_uint4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
                     }
                 }
-            if (valid && (two || x == 0)) {
+            if (valid && y == 0 && (two || x == 0)) {
                 if (!whole_tile) w.part_ml[part] = make_float2(m - BIAS, l);
                 else if (p.lse) p.lse[out_row] = l == 0.f ? -INFINITY : (m - BIAS + log2f(l)) * LN2_F;
             }
             tmem_fence_before();
-            if (!two) asm volatile("bar.sync 2, 256;" ::: "memory");
+            // what was read here (accumulators of both halves, shared words) is free for the next item
+            if (two) meet_half();
+            else meet_all();
             step0 += n;
             o_base[0] += made[0];
             o_base[1] += made[1];
@@ -365,7 +384,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
     }
     tmem_fence_before();
     __syncthreads();
-    if (warp == 12) { tmem_fence_after(); tmem_free(tmem, 512); }
+    if (warp == FWD_MMA) { tmem_fence_after(); tmem_free(tmem, 512); }
 }
 
 // Joins the partial states of a tile that several blocks shared, in the order of its steps.  blockIdx.x: the block in which a tile

@@ -31,6 +31,9 @@ __device__ __forceinline__ void copy_rows(uint32_t tile, int first_row, const vo
     }
 }
 
+// distance of a tile's piece of 16 features from its beginning, in the descriptors' unit
+__device__ __forceinline__ constexpr uint32_t piece(int k) { return ((k / 4) * (128 * 128) + (k % 4) * 32) / 16; }
+
 // Tensor maps of the arrays: q and grad_out as [rows][heads][D], boxes of 32 packed rows of a kv head (32 / group rows of its group
 // heads: one box where group divides 32); key and value as [heads][rows][D] or [pages][heads][slots][D], boxes of kv_box rows of a head.
 struct TileMaps { CUtensorMap q, go, k, v; };

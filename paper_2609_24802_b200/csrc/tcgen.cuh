@@ -71,11 +71,19 @@ __device__ __forceinline__ void tmem_free(uint32_t base, uint32_t columns) {
 }
 __device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 #define TIGA_R8(r, o) "=r"(r[o]), "=r"(r[o + 1]), "=r"(r[o + 2]), "=r"(r[o + 3]), "=r"(r[o + 4]), "=r"(r[o + 5]), "=r"(r[o + 6]), "=r"(r[o + 7])
 #define TIGA_W8(r, o) "r"(r[o]), "r"(r[o + 1]), "r"(r[o + 2]), "r"(r[o + 3]), "r"(r[o + 4]), "r"(r[o + 5]), "r"(r[o + 6]), "r"(r[o + 7])
+
+// Waits for this thread's loads.  The arrays that they fill are named, so that no use of them is moved in front of the wait, and no other
+// value takes their registers before it (both happened: the load's results are outputs of the load as far as the compiler can see).
+#define TIGA_RW8(r, o) "+r"(r[o]), "+r"(r[o + 1]), "+r"(r[o + 2]), "+r"(r[o + 3]), "+r"(r[o + 4]), "+r"(r[o + 5]), "+r"(r[o + 6]), "+r"(r[o + 7])
+__device__ __forceinline__ void tmem_wait_ld(uint32_t (&r)[8]) { asm volatile("tcgen05.wait::ld.sync.aligned;" : TIGA_RW8(r, 0) :: "memory"); }
+__device__ __forceinline__ void tmem_wait_ld(uint32_t (&r)[16]) { asm volatile("tcgen05.wait::ld.sync.aligned;" : TIGA_RW8(r, 0), TIGA_RW8(r, 8) :: "memory"); }
+__device__ __forceinline__ void tmem_wait_ld(uint32_t (&r)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : TIGA_RW8(r, 0), TIGA_RW8(r, 8), TIGA_RW8(r, 16), TIGA_RW8(r, 24) :: "memory");
+}
 
 // 32 columns of this thread's lane
 __device__ __forceinline__ void tmem_ld32(uint32_t at, uint32_t (&r)[32]) {
@@ -86,6 +94,9 @@ __device__ __forceinline__ void tmem_ld32(uint32_t at, uint32_t (&r)[32]) {
 __device__ __forceinline__ void tmem_ld16(uint32_t at, uint32_t (&r)[16]) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
                  : TIGA_R8(r, 0), TIGA_R8(r, 8) : "r"(at));
+}
+__device__ __forceinline__ void tmem_ld8(uint32_t at, uint32_t (&r)[8]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];" : TIGA_R8(r, 0) : "r"(at));
 }
 __device__ __forceinline__ void tmem_st8(uint32_t at, const uint32_t (&r)[8]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(at), TIGA_W8(r, 0) : "memory");
@@ -105,9 +116,10 @@ __device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&r)[N]) {
 // Shared-memory operands are rows of 128 bytes (64 elements) in groups of eight, swizzled: the 16-byte piece c of row r lies at
 // place c ^ (r & 7).  The same tile serves as a K-major operand (its rows are M or N, its features K) and as an MN-major one (its
 // features are N, its rows K): then `next_block` is the distance to the next 64 features.
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t next_block) {
-    return (uint64_t)((addr >> 4) & 0x3fff) | ((uint64_t)((next_block >> 4) & 0x3fff) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
-}
+// A descriptor's low word: address and next_block; tiles differ in the address alone, which is added to it (in units of 16 bytes).  The
+// high word is the same for all: 1024 bytes from one group of eight rows to the next, the swizzle of 128 bytes.
+__device__ __forceinline__ uint32_t smem_desc(uint32_t addr, uint32_t next_block) { return (addr >> 4) | (next_block >> 4) << 16; }
+#define TIGA_DESC_HIGH "0x40004040"
 template <typename T> __device__ constexpr uint32_t operand_type();
 template <> __device__ constexpr uint32_t operand_type<__half>() { return 0; }
 template <> __device__ constexpr uint32_t operand_type<__nv_bfloat16>() { return 1; }
@@ -117,23 +129,21 @@ __device__ __forceinline__ constexpr uint32_t mma_shape(int N, bool b_mn_major) 
 }
 constexpr uint32_t MMA_NEGATE_A = 1u << 13;
 
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, bool add) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(shape), "r"((uint32_t)add) : "memory");
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t shape, bool add) {
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.u32 p, %4, 0;\n\tmov.b64 da, {%1, " TIGA_DESC_HIGH "};\n\tmov.b64 db, {%2, " TIGA_DESC_HIGH "};\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "r"(b), "r"(shape), "r"((uint32_t)add) : "memory");
 }
 // A from tensor memory: two consecutive K elements per 32-bit column
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t shape, bool add) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-                 ::"r"(d), "r"(a), "l"(b), "r"(shape), "r"((uint32_t)add) : "memory");
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t shape, bool add) {
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 db;\n\tsetp.ne.u32 p, %4, 0;\n\tmov.b64 db, {%2, " TIGA_DESC_HIGH "};\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "r"(b), "r"(shape), "r"((uint32_t)add) : "memory");
 }
 // arrives on the barrier once all matrix instructions that this thread issued so far are done
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
-
-// ---- registers: warpgroups that need fewer leave them to those that need more (their sum is what the block was launched with)
-template <int N> __device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
-template <int N> __device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 
 // ---- arithmetic
 __device__ __forceinline__ float ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
