@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
         }
     } else if (warp == BWD_MMA) {
         // ---------------------------------------------------------------- matrix instructions
-        const bool lead = lane == 0;            // the warp goes its way together, one thread issues
+        // the warp goes its way together, one thread issues
         const uint32_t s_shape = mma_shape<T>(BWD_STEP, false), acc_shape = mma_shape<T>(DP, true);
         const uint32_t sign = p.scale < 0.f ? MMA_NEGATE_A : 0;
         uint32_t tile0 = 0, steps = 0, items = 0;
@@ -237,12 +237,12 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
             wait(b, parity);
             tmem_fence_after();
         };
-        auto commit = [&](unsigned long long& b) { if (lead) mma_commit(bar(b)); };
+        auto commit = [&](unsigned long long& b) { if (elected()) mma_commit(bar(b)); };
         auto release = [&](uint32_t tile) { commit(ctl.empty[tile % C::SLOTS]); };
         // d = X Y^T, features in pieces of 16
         auto inner = [&](uint32_t d, int second, uint32_t tile, uint32_t shape) {
             const uint32_t x = x_desc + second * (C::TILE / 16), y = inner_desc + slot(tile);
-            if (lead)
+            if (elected())
 #pragma unroll
                 for (int k = 0; k < DP / 16; ++k)
                     if (k * 16 < p.D) mma_ss(d, x + piece(k), y + piece(k), shape, k > 0);
@@ -251,7 +251,7 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
         // acc (+)= (16-bit weights at a: 32 of them in the first half of each 32 columns) Y
         auto outer = [&](uint32_t acc, uint32_t a, uint32_t tile, bool add) {
             const uint32_t y = outer_desc + slot(tile);
-            if (lead) {
+            if (elected()) {
                 mma_ts(acc, a, y, acc_shape, add);
 #pragma unroll
                 for (int k = 1; k < BWD_STEP / 16; ++k) mma_ts(acc, a + (k / 2) * 32 + (k % 2) * 8, y + k * (2048 / 16), acc_shape, true);

@@ -123,7 +123,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
         }
     } else if (warp == FWD_MMA) {
         // ---------------------------------------------------------------- matrix instructions
-        const bool lead = lane == 0;            // the warp goes its way together, one thread issues
+        // the warp goes its way together, one thread issues
         const uint32_t s_shape = mma_shape<T>(128, false) | (p.scale < 0.f ? MMA_NEGATE_A : 0), o_shape = mma_shape<T>(DP, true);
         uint32_t tile0 = 0, items = 0, done0 = 0, done1 = 0;     // done: p_full phases consumed
         bool ok = true;
@@ -136,10 +136,10 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
             wait(ctl.full[tile % C::SLOTS], tile / C::SLOTS);
             fence_async_proxy();
         };
-        auto release = [&](uint32_t tile) { if (lead) mma_commit(bar(ctl.empty[tile % C::SLOTS])); };
+        auto release = [&](uint32_t tile) { if (elected()) mma_commit(bar(ctl.empty[tile % C::SLOTS])); };
         auto scores = [&](int x, int half, uint32_t tile) {
             const uint32_t q = q_desc + half * (C::TILE / 16), k = k_desc + slot(tile);
-            if (lead) {
+            if (elected()) {
 #pragma unroll
                 for (int c = 0; c < DP / 16; ++c)
                     if (c * 16 < p.D) mma_ss(tmem + 128 * x, q + piece(c), k + piece(c), s_shape, c > 0);
@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
             tmem_fence_after();
             const uint32_t v = v_desc + slot(tile);
             const uint32_t o = tmem + 256 + DP * x, a = tmem + 128 * x;
-            if (lead) {
+            if (elected()) {
                 mma_ts(o, a, v, o_shape, add);
 #pragma unroll
                 for (int k = 1; k < 8; ++k) mma_ts(o, a + (k / 2) * 32 + (k % 2) * 8, v + k * (2048 / 16), o_shape, true);
@@ -188,10 +188,10 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
                 if (more_keys) release(k_next);
             }
             if (!ok) break;
-            if (lead) mma_commit(bar(ctl.q_empty));
+            if (elected()) mma_commit(bar(ctl.q_empty));
             tile0 += 2 * n;
         }
-        if (lead) mma_commit(bar(ctl.drain));
+        if (elected()) mma_commit(bar(ctl.drain));
         mbar_wait(bar(ctl.drain), 0, &ctl.never);
         __syncwarp();
     } else {

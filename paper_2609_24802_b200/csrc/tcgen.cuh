@@ -129,6 +129,13 @@ __device__ __forceinline__ constexpr uint32_t mma_shape(int N, bool b_mn_major) 
 }
 constexpr uint32_t MMA_NEGATE_A = 1u << 13;
 
+// One thread of a converged warp.  (Where the compiler sees this election, the operands of the instructions below stay in the warp's
+// uniform registers; behind a comparison of thread numbers each instruction paid about 80 cycles for their transfer.)
+__device__ __forceinline__ bool elected() {
+    uint32_t yes;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+    return yes;
+}
 __device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t shape, bool add) {
     asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.u32 p, %4, 0;\n\tmov.b64 da, {%1, " TIGA_DESC_HIGH "};\n\tmov.b64 db, {%2, " TIGA_DESC_HIGH "};\n\t"
                  "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}"
