@@ -21,25 +21,24 @@ typedef Cut<BWD_ROWS, BWD_STEP, true> KvCut;
 typedef Cut<BWD_ROWS, BWD_STEP, false> QCut;
 template <bool KV> struct CutOf { typedef QCut type; };
 template <> struct CutOf<true> { typedef KvCut type; };
-// What goes along with a step's rows.  A step's first tile waits for the place of the one SLOTS tiles before, of which SLOTS / 2
-// steps at most are behind: the steps in front of those are done with their entries.
-constexpr int BWD_AUX = 4;
-
 template <int DP> struct Bwd {
     static constexpr int TILE = 128 * DP * 2;
-    static constexpr int SLOTS = DP == 128 ? 4 : 8;         // tiles of the ring, in the order Y1 Y2 Y1 Y2 ...
-    static_assert(SLOTS / 2 <= BWD_AUX, "entries of steps in flight");
+    static constexpr int SLOTS = DP == 128 ? 5 : 8;         // tiles of the ring, in the order Y1 Y2 Y1 Y2 ...
+    // Entries of what goes along with a step's rows.  Step n's is written once there is room for its Y2, the tile 2 n + 1: then the tile
+    // 2 n + 1 - SLOTS is done with.  Of five slots that is Y1 of step n - 2, whose last product comes after all that its step reads: two
+    // entries do.  Of eight it is Y2 of step n - 4, so step n - 4 may still read: eight do.
+    static constexpr int AUX = DP == 128 ? 2 : 8;
     static constexpr int CONTROL = (2 + SLOTS) * TILE;
-    static constexpr int SMEM = CONTROL + 5120;
+    static constexpr int SMEM = CONTROL + (DP == 128 ? 3072 : 10240);
 };
 
-struct BwdControl {
-    unsigned long long full[8], empty[8], aux_full[BWD_AUX], x_full, x_empty, s_full, dp_full, p_full, ds_full, acc_full, acc_empty, drain;
+template <int AUX> struct BwdControl {
+    unsigned long long full[8], empty[8], aux_full[AUX], x_full, x_empty, s_full, dp_full, p_full, ds_full, acc_full, acc_empty, drain;
     uint32_t tmem, abort_word, never, pad;
-    alignas(16) float minus_lse[BWD_AUX][BWD_STEP], minus_delta[BWD_AUX][BWD_STEP];     // keys stationary: of the step's rows
-    uint32_t mask[BWD_AUX][4];                                                          // queries stationary: the step's keys
+    alignas(16) float minus_lse[AUX][BWD_STEP], minus_delta[AUX][BWD_STEP];     // keys stationary: of the step's rows
+    uint32_t mask[AUX][4];                                                      // queries stationary: the step's keys
 };
-static_assert(sizeof(BwdControl) <= 5120, "control block");
+static_assert(sizeof(BwdControl<2>) <= 3072 && sizeof(BwdControl<8>) <= 10240, "control block");
 
 struct BwdWork {
     long long *kv_start_unit, *q_start_unit;        // NULL: the blocks count for themselves
@@ -123,7 +122,7 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
     constexpr bool F16 = operand_type<T>() == 0;
     constexpr float BIAS = F16 ? 14.f : 0.f;
     extern __shared__ __align__(1024) unsigned char smem[];
-    BwdControl& ctl = *reinterpret_cast<BwdControl*>(smem + C::CONTROL);
+    BwdControl<C::AUX>& ctl = *reinterpret_cast<BwdControl<C::AUX>*>(smem + C::CONTROL);
     const uint32_t x_tile = smem_u32(smem), ring = x_tile + 2 * C::TILE;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     volatile uint32_t* abort_word = &ctl.abort_word;
@@ -137,7 +136,7 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < C::SLOTS; ++i) { mbar_init(bar(ctl.full[i]), 128); mbar_init(bar(ctl.empty[i]), 1); }
-        for (int i = 0; i < BWD_AUX; ++i) mbar_init(bar(ctl.aux_full[i]), 4);
+        for (int i = 0; i < C::AUX; ++i) mbar_init(bar(ctl.aux_full[i]), 4);
         mbar_init(bar(ctl.x_full), 256);
         mbar_init(bar(ctl.x_empty), 1);
         mbar_init(bar(ctl.s_full), 1);
@@ -194,8 +193,13 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
                 const Place here = at;
                 const bool wanted = on;
                 const float2 st = stat;
-                const int aux = steps % BWD_AUX;
+                const int aux = steps % C::AUX, r = i * BWD_STEP + 32 * pw + lane;
                 if (!slot_free()) break;
+                fetch(ring + (tiles % C::SLOTS) * C::TILE, bar(ctl.full[tiles % C::SLOTS]), !KV, false, here, wanted, r);
+                ++tiles;
+                if (!slot_free()) break;
+                fetch(ring + (tiles % C::SLOTS) * C::TILE, bar(ctl.full[tiles % C::SLOTS]), !KV, true, here, wanted, r);
+                ++tiles;
                 if (KV) {
                     ctl.minus_lse[aux][32 * pw + lane] = BIAS - st.x;
                     ctl.minus_delta[aux][32 * pw + lane] = -st.y;
@@ -205,12 +209,7 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(ctl.aux_full[aux]));
-                if (i + 1 < it.i1) look(!KV, (i + 1) * BWD_STEP + 32 * pw + lane);
-                for (int y = 0; y < 2; ++y, ++tiles) {
-                    if (y && !slot_free()) break;
-                    fetch(ring + (tiles % C::SLOTS) * C::TILE, bar(ctl.full[tiles % C::SLOTS]), !KV, y, here, wanted, i * BWD_STEP + 32 * pw + lane);
-                }
-                if (!ok) break;
+                if (i + 1 < it.i1) look(!KV, r + BWD_STEP);
             }
         }
         cp_async_wait_all();
@@ -337,8 +336,8 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
                 masked = st.x == INFINITY;
             }
             for (int i = 0; i < n; ++i, ++steps) {
-                const uint32_t aux = steps % BWD_AUX;
-                ok = ok && mbar_wait(bar(ctl.aux_full[aux]), (steps / BWD_AUX) & 1, abort_word) && mbar_wait(bar(ctl.s_full), steps & 1, abort_word);
+                const uint32_t aux = steps % C::AUX;
+                ok = ok && mbar_wait(bar(ctl.aux_full[aux]), (steps / C::AUX) & 1, abort_word) && mbar_wait(bar(ctl.s_full), steps & 1, abort_word);
                 ok = __all_sync(~0u, ok);
                 if (!ok) continue;
                 tmem_fence_after();
