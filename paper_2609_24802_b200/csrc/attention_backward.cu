@@ -15,8 +15,8 @@ namespace tiga {
 // grad_value and the next step's S.
 // fp16: P carries 2^14 and dS a power of two from the largest norms of the rows of grad_out and value, which bound |dP - delta|: the
 // largest value cannot overflow, the smallest keep as many digits as there are.
-constexpr int BWD_WEIGHT_WARPS = 16, BWD_PRODUCER = BWD_WEIGHT_WARPS, BWD_MMA = BWD_PRODUCER + 4;
-constexpr int BWD_THREADS = 32 * (BWD_MMA + 1), BWD_ROWS = 128, BWD_STEP = 128, BWD_LEAST = 2;
+constexpr int BWD_WEIGHT_WARPS = 16, BWD_PRODUCER = BWD_WEIGHT_WARPS, BWD_MMA = BWD_PRODUCER + 4, BWD_WALKER = BWD_MMA + 1;
+constexpr int BWD_THREADS = 32 * (BWD_WALKER + 1), BWD_ROWS = 128, BWD_STEP = 128, BWD_LEAST = 2;
 typedef Cut<BWD_ROWS, BWD_STEP, true> KvCut;
 typedef Cut<BWD_ROWS, BWD_STEP, false> QCut;
 template <bool KV> struct CutOf { typedef QCut type; };
@@ -34,6 +34,7 @@ template <int DP> struct Bwd {
 
 template <int AUX> struct BwdControl {
     unsigned long long full[8], empty[8], aux_full[AUX], x_full, x_empty, s_full, dp_full, p_full, ds_full, acc_full, acc_empty, drain;
+    ItemRing items;
     uint32_t tmem, abort_word, never, pad;
     alignas(16) float minus_lse[AUX][BWD_STEP], minus_delta[AUX][BWD_STEP];     // keys stationary: of the step's rows
     uint32_t mask[AUX][4];                                                      // queries stationary: the step's keys
@@ -130,11 +131,8 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
 
     wait_for_previous_kernel();
     let_next_kernel_start();
-    Walker<WorkCut> it;
-    bool more = it.begin(p, KV ? w.kv_start_unit : w.q_start_unit, blockIdx.x, gridDim.x, BWD_LEAST);
-    if (!more) return;
-
     if (threadIdx.x == 0) {
+        items_init(ctl.items, BWD_WALKER);
         for (int i = 0; i < C::SLOTS; ++i) { mbar_init(bar(ctl.full[i]), 128); mbar_init(bar(ctl.empty[i]), 1); }
         for (int i = 0; i < C::AUX; ++i) mbar_init(bar(ctl.aux_full[i]), 4);
         mbar_init(bar(ctl.x_full), 256);
@@ -149,6 +147,9 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
         ctl.abort_word = ctl.never = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    Walker<WorkCut> walk;
+    bool work_here = false;
+    if (warp == BWD_WALKER) work_here = walk.begin(p, KV ? w.kv_start_unit : w.q_start_unit, blockIdx.x, gridDim.x, BWD_LEAST);
     if (warp == BWD_MMA) tmem_alloc(smem_u32(&ctl.tmem), 512);
     tmem_fence_before();
     __syncthreads();
@@ -156,15 +157,21 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
     const uint32_t tmem = ctl.tmem;
     const uint32_t s_at = tmem, dp_at = tmem + 128, acc1 = tmem + 256, acc2 = tmem + 384;
 
-    if (warp >= BWD_PRODUCER && warp < BWD_MMA) {
+    if (warp == BWD_WALKER) {
+        if (lane == 0) items_hand_out(ctl.items, p, walk, work_here, &ctl.never);
+        __syncwarp();
+    } else if (warp >= BWD_PRODUCER && warp < BWD_MMA) {
         // ---------------------------------------------------------------- producers
         const int pw = warp - BWD_PRODUCER;
         uint32_t tiles = 0, steps = 0, items = 0;
         bool ok = true;
         auto wait = [&](unsigned long long& b, uint32_t parity) { return ok = __all_sync(~0u, mbar_wait(bar(b), parity & 1, abort_word)); };
         auto slot_free = [&]() { return tiles < (uint32_t)C::SLOTS || wait(ctl.empty[tiles % C::SLOTS], tiles / C::SLOTS + 1); };
-        for (; more && ok; more = it.next(p), ++items) {
-            const int packed_rows = it.g.nq * p.group;
+        for (uint32_t item = 0;; ++item) {
+            const Item& e = item_take(ctl.items, item, &ctl.never);
+            if (e.steps == 0) break;
+            const Segment g = e.segment();
+            const int packed_rows = g.nq * p.group, i0 = e.i0, i1 = ok ? e.i1 : e.i0, h = e.h;
             // a row of the other side, or of the tile itself: where key r lies, or whether packed row r is wanted
             Place at;
             bool on;
@@ -174,22 +181,26 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
                 on = false;
                 stat = make_float2(INFINITY, 0.f);
                 if (keys) {
-                    if (r < it.g.nk) at = key_place(p, it.g, it.s, r);
+                    if (r < g.nk) at = key_place(p, g, e.s, r);
                 } else if (r < packed_rows) {
-                    const PackedRow pr = packed_row(p, it.g, it.h, r);
+                    const PackedRow pr = packed_row(p, g, h, r);
                     stat = w.stats[(long long)pr.row * p.heads + pr.head];
                     on = stat.x != INFINITY;            // a row that reads nothing: whatever lies there stays out of the products
                 }
             };
             auto fetch = [&](uint32_t tile, uint32_t full, bool keys, bool second, Place a, bool wanted, int r) {
-                if (keys) fetch_keys<DP>(tile, 32 * pw, full, p, maps, second, a, it.h, w.stats);
-                else fetch_packed<DP>(tile, 32 * pw, full, p, it.g, maps, second, it.h, r, wanted, w.stats);
+                if (keys) fetch_keys<DP>(tile, 32 * pw, full, p, maps, second, a, h, w.stats);
+                else fetch_packed<DP>(tile, 32 * pw, full, p, g, maps, second, h, r, wanted, w.stats);
             };
-            if (items && !wait(ctl.x_empty, items - 1)) break;
-            look(KV, it.t * BWD_ROWS + 32 * pw + lane);
-            for (int y = 0; y < 2; ++y) fetch(x_tile + y * C::TILE, bar(ctl.x_full), KV, y, at, on, it.t * BWD_ROWS + 32 * pw + lane);
-            look(!KV, it.i0 * BWD_STEP + 32 * pw + lane);
-            for (int i = it.i0; i < it.i1; ++i, ++steps) {
+            if (ok && items) wait(ctl.x_empty, items - 1);
+            const int x_row = e.t * BWD_ROWS + 32 * pw + lane;
+            if (ok) {
+                look(KV, x_row);
+                for (int y = 0; y < 2; ++y) fetch(x_tile + y * C::TILE, bar(ctl.x_full), KV, y, at, on, x_row);
+                ++items;
+                look(!KV, i0 * BWD_STEP + 32 * pw + lane);
+            }
+            for (int i = i0; i < i1 && ok; ++i, ++steps) {
                 const Place here = at;
                 const bool wanted = on;
                 const float2 st = stat;
@@ -209,8 +220,9 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(ctl.aux_full[aux]));
-                if (i + 1 < it.i1) look(!KV, r + BWD_STEP);
+                if (i + 1 < i1) look(!KV, r + BWD_STEP);
             }
+            item_return(ctl.items, item);
         }
         cp_async_wait_all();
         if (*abort_word) {          // boxes may still be on their way: their tiles, as far as they were asked for
@@ -257,15 +269,18 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
             }
             __syncwarp();
         };
-        for (; more && ok; more = it.next(p), ++items) {
-            const int n = it.i1 - it.i0;
+        for (;; ++items) {
+            const Item& e = item_take(ctl.items, items, &ctl.never);
+            if (e.steps == 0) break;
+            const int n = e.i1 - e.i0;
+            item_return(ctl.items, items);
             wait(ctl.x_full, items);
             wait_tile(tile0);
-            if (!ok) break;
+            if (!ok) continue;
             inner(s_at, 0, tile0, s_shape | sign);
             commit(ctl.s_full);
             wait_tile(tile0 + 1);
-            if (!ok) break;
+            if (!ok) continue;
             inner(dp_at, 1, tile0 + 1, s_shape);
             commit(ctl.dp_full);
             if (!KV) release(tile0 + 1);
@@ -299,7 +314,7 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
                     if (i + 2 == n) commit(ctl.x_empty);
                 }
             }
-            if (!ok) break;
+            if (!ok) continue;
             commit(ctl.acc_full);
             tile0 += 2 * n;
         }
@@ -317,18 +332,20 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
         const f32x2 sc2 = dup2(scale2), ds2 = dup2(F16 ? factor * 0x1p-14f : 1.f);
         uint32_t steps = 0, items = 0;
         bool ok = true;
-        for (; more; more = it.next(p), ++items) {
-            const int n = it.i1 - it.i0, r = it.t * BWD_ROWS + row, n_rows = WorkCut::rows(p, it.g);
+        for (;; ++items) {
+            const Item& item = item_take(ctl.items, items, &ctl.never);
+            if (item.steps == 0) break;
+            const int n = item.i1 - item.i0, r = item.t * BWD_ROWS + row, n_rows = WorkCut::rows(p, item.segment());
             const bool valid = r < n_rows;
             const bool warp_on = (r & ~31) < n_rows;
             f32x2 my_lse = 0, my_delta = 0;
             long long out_row = 0;
             bool masked = false;
             if (KV) {
-                out_row = (long long)(it.g.k0 + r) * p.kv_heads + it.h;
-                masked = valid && key_place(p, it.g, it.s, r).at < 0;
+                out_row = (long long)(item.k0 + r) * p.kv_heads + item.h;
+                masked = valid && key_place(p, item.segment(), item.s, r).at < 0;
             } else if (valid) {
-                const PackedRow pr = packed_row(p, it.g, it.h, r);
+                const PackedRow pr = packed_row(p, item.segment(), item.h, r);
                 out_row = (long long)pr.row * p.heads + pr.head;
                 const float2 st = w.stats[out_row];
                 my_lse = dup2(BIAS - st.x);
@@ -399,14 +416,14 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
             ok = __all_sync(~0u, ok);
             tmem_fence_after();
             // keys stationary: warpgroups 0 and 1 write grad_key, 2 and 3 grad_value, a half of the features each; queries: a quarter each
-            const bool whole_tile = it.i0 == 0 && it.i1 == it.steps;
+            const bool whole_tile = n == item.steps;
             const int rows = KV ? w.kv_rows : w.q_rows;
             constexpr int SIDES = KV ? 2 : 1, PIECES = DP / 16 * SIDES / 4;        // pieces of 16 features a thread
             const int side = KV ? x / 2 : 0, c0 = (KV ? x % 2 : x) * PIECES;
             const uint32_t acc = side ? acc2 : acc1;
             const float finish = side ? (F16 ? 0x1p-14f : 1.f) : p.scale / factor;
             T* out = (T*)(KV ? (side ? p.gv : p.gk) : p.gq);
-            float* part = w.part + ((((2LL * blockIdx.x + (it.i0 == 0)) * rows + row) * SIDES) + side) * DP;
+            float* part = w.part + ((((2LL * blockIdx.x + (item.i0 == 0)) * rows + row) * SIDES) + side) * DP;
             if (warp_on)
                 for (int c = c0; c < c0 + PIECES; ++c) {
                     uint32_t v[16];
@@ -436,6 +453,7 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
                 }
             tmem_fence_before();
             mbar_arrive(bar(ctl.acc_empty));
+            item_return(ctl.items, items);
         }
     }
     tmem_fence_before();

@@ -16,8 +16,8 @@ namespace tiga {
 // and the mass carries the same factor.
 // What bounds it: the chain S -> maximum -> P -> O of a half.  A warp alone on its scheduler takes about 13 cycles a column for the
 // exponentials (8 are the unit's), so a row's two threads halve the chain; the exchange of their maxima costs about 100 cycles.
-constexpr int FWD_SOFTMAX_WARPS = 16, FWD_PRODUCER = FWD_SOFTMAX_WARPS, FWD_MMA = FWD_PRODUCER + 4;
-constexpr int FWD_THREADS = 32 * (FWD_MMA + 1), FWD_ROWS = 256, FWD_STEP = 128;
+constexpr int FWD_SOFTMAX_WARPS = 16, FWD_PRODUCER = FWD_SOFTMAX_WARPS, FWD_MMA = FWD_PRODUCER + 4, FWD_WALKER = FWD_MMA + 1;
+constexpr int FWD_THREADS = 32 * (FWD_WALKER + 1), FWD_ROWS = 256, FWD_STEP = 128;
 typedef Cut<FWD_ROWS, FWD_STEP, false> FwdCut;
 constexpr int FWD_LEAST = 2;            // units a block at least
 constexpr int MASK_RING = 8;            // the producers are at most 6 steps ahead of the softmax (ring of at most 10 tiles)
@@ -32,6 +32,7 @@ template <int DP> struct Fwd {
 
 struct FwdControl {
     unsigned long long full[10], empty[10], q_full, q_empty, s_full[2], p_full[2], o_full[2], mask_full[MASK_RING], drain;
+    ItemRing items;
     uint32_t tmem, abort_word, never, mask[MASK_RING][4];
     float share[2][2][128];             // what a row's threads tell each other
 };
@@ -58,11 +59,8 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
 
     wait_for_previous_kernel();
     let_next_kernel_start();
-    Walker<FwdCut> it;
-    bool more = it.begin(p, w.unit_start, blockIdx.x, gridDim.x, FWD_LEAST);
-    if (!more) return;
-
     if (threadIdx.x == 0) {
+        items_init(ctl.items, FWD_WALKER);
         for (int i = 0; i < C::SLOTS; ++i) { mbar_init(bar(ctl.full[i]), 128); mbar_init(bar(ctl.empty[i]), 1); }
         mbar_init(bar(ctl.q_full), 256);
         mbar_init(bar(ctl.q_empty), 1);
@@ -72,49 +70,61 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
         ctl.abort_word = ctl.never = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    Walker<FwdCut> walk;
+    bool work_here = false;
+    if (warp == FWD_WALKER) work_here = walk.begin(p, w.unit_start, blockIdx.x, gridDim.x, FWD_LEAST);
     if (warp == FWD_MMA) tmem_alloc(smem_u32(&ctl.tmem), 512);
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
     const uint32_t tmem = ctl.tmem;
-    const uint32_t s_at[2] = {tmem, tmem + 128}, o_at[2] = {tmem + 256, tmem + 256 + DP};
+    // tensor memory: S of half x at 128 x, O at 256 + DP x
 
-    if (warp >= FWD_PRODUCER && warp < FWD_MMA) {
+    if (warp == FWD_WALKER) {
+        if (lane == 0) items_hand_out(ctl.items, p, walk, work_here, &ctl.never);
+        __syncwarp();
+    } else if (warp >= FWD_PRODUCER && warp < FWD_MMA) {
         // ---------------------------------------------------------------- producers
         const int pw = warp - FWD_PRODUCER;
         uint32_t tiles = 0, steps = 0, items = 0;
         bool ok = true;
         auto wait = [&](unsigned long long& b, uint32_t parity) { return ok = __all_sync(~0u, mbar_wait(bar(b), parity & 1, abort_word)); };
         auto slot_free = [&]() { return tiles < (uint32_t)C::SLOTS || wait(ctl.empty[tiles % C::SLOTS], tiles / C::SLOTS + 1); };
-        for (; more && ok; more = it.next(p), ++items) {
-            const int rows = min(it.g.nq * p.group - it.t * FWD_ROWS, FWD_ROWS);
+        for (uint32_t item = 0;; ++item) {
+            const Item& e = item_take(ctl.items, item, &ctl.never);
+            if (e.steps == 0) break;
+            const Segment g = e.segment();
+            const int i0 = e.i0, i1 = e.i1, h = e.h;
             auto place = [&](int i) {
                 const int j = i * FWD_STEP + 32 * pw + lane;
-                return j < it.g.nk ? key_place(p, it.g, it.s, j) : Place{-1, 0};
+                return j < g.nk ? key_place(p, g, e.s, j) : Place{-1, 0};
             };
-            Place at = place(it.i0);
-            for (int i = it.i0; i < it.i1 && ok; ++i, ++steps) {
+            Place at = place(i0);
+            for (int i = i0; i < i1 && ok; ++i, ++steps) {
                 const Place here = at;
                 const uint32_t valid = __ballot_sync(~0u, here.at >= 0);
                 if (lane == 0) {
                     ctl.mask[steps % MASK_RING][pw] = valid;
                     mbar_arrive(bar(ctl.mask_full[steps % MASK_RING]));
                 }
-                if (i + 1 < it.i1) at = place(i + 1);
+                if (i + 1 < i1) at = place(i + 1);
                 for (int kv = 0; kv < 2; ++kv, ++tiles) {
                     if (!slot_free()) break;
-                    fetch_keys<DP>(ring + (tiles % C::SLOTS) * C::TILE, 32 * pw, bar(ctl.full[tiles % C::SLOTS]), p, maps, kv, here, it.h, p.q);
+                    fetch_keys<DP>(ring + (tiles % C::SLOTS) * C::TILE, 32 * pw, bar(ctl.full[tiles % C::SLOTS]), p, maps, kv, here, h, p.q);
                 }
-                if (i == it.i0 && ok) {         // the queries' tile may still be in use by the item before: its first keys are on their way
+                if (i == i0 && ok) {            // the queries' tile may still be in use by the item before: its first keys are on their way
                     if (items && !wait(ctl.q_empty, items - 1)) break;
+                    const int rows = min(g.nq * p.group - e.t * FWD_ROWS, FWD_ROWS);
                     for (int x = 0; x < 2; ++x) {
                         const int r = x * 128 + 32 * pw + lane;
                         if (x == 1 && rows <= 128) {
                             if (lane == 0) mbar_arrive(bar(ctl.q_full), 32);
-                        } else fetch_packed<DP>(q_tile + x * C::TILE, 32 * pw, bar(ctl.q_full), p, it.g, maps, false, it.h, it.t * FWD_ROWS + r, r < rows, p.q);
+                        } else fetch_packed<DP>(q_tile + x * C::TILE, 32 * pw, bar(ctl.q_full), p, g, maps, false, h, e.t * FWD_ROWS + r, r < rows, p.q);
                     }
+                    ++items;
                 }
             }
+            item_return(ctl.items, item);
         }
         cp_async_wait_all();
         if (*abort_word) {          // boxes may still be on their way: their tiles, as far as they were asked for
@@ -161,9 +171,13 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
             }
             __syncwarp();
         };
-        for (; more && ok; more = it.next(p), ++items) {
-            const int n = it.i1 - it.i0;
-            const bool two = it.g.nq * p.group - it.t * FWD_ROWS > 128;
+        for (;; ++items) {
+            const Item& e = item_take(ctl.items, items, &ctl.never);
+            if (e.steps == 0) break;
+            const int n = e.i1 - e.i0;
+            const bool two = e.nq * p.group - e.t * FWD_ROWS > 128;
+            item_return(ctl.items, items);
+            if (!ok) continue;
             const int ahead = two ? 1 : 2;              // steps between two of a half
             wait(ctl.q_full, items);
             // i: the step whose values are next; its half's (two: both halves') next scores follow
@@ -187,7 +201,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
                 if (two && more_keys) scores(1, 1, k_next);
                 if (more_keys) release(k_next);
             }
-            if (!ok) break;
+            if (!ok) continue;
             if (elected()) mma_commit(bar(ctl.q_empty));
             tile0 += 2 * n;
         }
@@ -199,23 +213,25 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
         const int x = warp / 8, y = warp / 4 % 2;           // half, and which of its columns
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const int row = threadIdx.x & 127;
-        const uint32_t S = s_at[x] + lanes + 64 * y;
+        const uint32_t S = tmem + 128 * x + lanes + 64 * y, O = tmem + 256 + lanes;
         const float scale2 = fmaxf(fabsf(p.scale) * LOG2E_F, 1e-30f);       // (not zero: masked scores are -inf)
         constexpr float BIAS = operand_type<T>() == 0 ? 7.f : 0.f;          // fp16: weights up to 2^15, so that small ones keep their digits
         // The threads of a half, and all of them, meet here; everyone comes the same number of times, after a failed wait too.
         auto meet_half = [&]() { if (x) asm volatile("bar.sync 2, 256;" ::: "memory"); else asm volatile("bar.sync 1, 256;" ::: "memory"); };
         auto meet_all = [&]() { asm volatile("bar.sync 3, 512;" ::: "memory"); };
-        uint32_t step0 = 0, s_done = 0, o_base[2] = {0, 0};
+        uint32_t step0 = 0, s_done = 0, o_done0 = 0, o_done1 = 0;       // steps, scores of this half, values of each half in the items before
         bool ok = true;
-        for (; more; more = it.next(p)) {
-            const int n = it.i1 - it.i0;
-            const int rows = min(it.g.nq * p.group - it.t * FWD_ROWS, FWD_ROWS);
+        for (uint32_t item = 0;; ++item) {
+            const Item& e = item_take(ctl.items, item, &ctl.never);
+            if (e.steps == 0) break;
+            const int n = e.i1 - e.i0;
+            const int rows = min(e.nq * p.group - e.t * FWD_ROWS, FWD_ROWS);
             const bool two = rows > 128;
             const int tile_row = two ? x * 128 + row : row;
             const bool valid = tile_row < rows;
             const bool warp_on = (tile_row & ~31) < rows;
-            const int packed = it.t * FWD_ROWS + tile_row;
-            const int limit = (p.causal && valid ? keys_of_row(p, it.g, packed / p.group) : it.g.nk) - it.i0 * FWD_STEP - 64 * y;
+            const int limit = (p.causal && valid ? keys_of_row(p, e.segment(), (e.t * FWD_ROWS + tile_row) / p.group) : e.nk) - e.i0 * FWD_STEP - 64 * y;
+            const uint32_t o_mine = x ? o_done1 : o_done0;
             float m = -INFINITY, l = 0.f;               // reference of the exponents (log2), this thread's mass relative to 2^(m - BIAS)
             uint32_t mine = 0;                          // steps of this half's threads in this item
             for (int i = two ? 0 : x; i < n; i += two ? 1 : 2, ++mine, ++s_done) {
@@ -263,13 +279,13 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
                         const float m_new = grown ? top : m;
                         const float fade = grown ? ex2(m - m_new) : 1.f;
                         if (mine) {
-                            ok = mbar_wait(bar(ctl.o_full[x]), (o_base[x] + mine - 1) & 1, abort_word);
+                            ok = mbar_wait(bar(ctl.o_full[x]), (o_mine + mine - 1) & 1, abort_word);
                             ok = __all_sync(~0u, ok);
                             tmem_fence_after();
                             if (ok)
 #pragma unroll 1
                                 for (int c = 0; c < DP / 16; ++c) {         // this thread's half of the features, eight at a time
-                                    const uint32_t at = o_at[x] + lanes + y * (DP / 2) + 8 * c;
+                                    const uint32_t at = O + DP * x + y * (DP / 2) + 8 * c;
                                     uint32_t o[8];
                                     tmem_ld8(at, o);
                                     tmem_wait_ld(o);
@@ -311,9 +327,9 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
                 mbar_arrive(bar(ctl.p_full[x]));
             }
             // ---- the item's end: the row's mass; a short tile's two states are joined; then the rows are finished or put aside
-            const uint32_t made[2] = {two ? (uint32_t)n : (uint32_t)(n + 1) / 2, two ? (uint32_t)n : (uint32_t)n / 2};
-            for (int z = 0; z < 2; ++z)
-                if (made[z] && ok && (!two || z == x)) ok = mbar_wait(bar(ctl.o_full[z]), (o_base[z] + made[z] - 1) & 1, abort_word);
+            const uint32_t made0 = two ? n : (n + 1) / 2, made1 = two ? n : n / 2;
+            if (ok && (!two || x == 0)) ok = mbar_wait(bar(ctl.o_full[0]), (o_done0 + made0 - 1) & 1, abort_word);
+            if (ok && made1 && (!two || x == 1)) ok = mbar_wait(bar(ctl.o_full[1]), (o_done1 + made1 - 1) & 1, abort_word);
             ok = __all_sync(~0u, ok);
             if (!ok) l = __int_as_float(0x7fffffff);
             tmem_fence_after();
@@ -334,23 +350,23 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
                 w1 = mb == -INFINITY ? 0.f : ex2(mb - m);
                 l = la * w0 + lb * w1;
             }
-            const bool whole_tile = it.i0 == 0 && it.i1 == it.steps;
-            const long long part = (2LL * blockIdx.x + (it.i0 == 0)) * w.rows + tile_row;
-            const PackedRow pr = packed_row(p, it.g, it.h, packed);
+            const bool whole_tile = n == e.steps;
+            const long long part = (2LL * blockIdx.x + (e.i0 == 0)) * w.rows + tile_row;
+            const PackedRow pr = packed_row(p, e.segment(), e.h, e.t * FWD_ROWS + tile_row);
             const long long out_row = (long long)pr.row * p.heads + pr.head;
             const float finish = l > 0.f || l != l ? 1.f / l : 0.f;
             const int c0 = two ? y * (DP / 32) : (2 * x + y) * (DP / 64), c1 = c0 + (two ? DP / 32 : DP / 64);      // pieces of 16 features
             if (warp_on)
                 for (int c = c0; c < c1; ++c) {
                     uint32_t v[16], u[16];
-                    tmem_ld16(o_at[two ? x : 0] + lanes + 16 * c, v);
-                    tmem_ld16(o_at[1] + lanes + 16 * c, u);         // (read in short tiles with a second state only)
+                    tmem_ld16(O + (two ? DP * x : 0) + 16 * c, v);
+                    tmem_ld16(O + DP + 16 * c, u);         // (read in short tiles with a second state only)
                     tmem_wait_ld(v);
                     tmem_wait_ld(u);
                     if (!two)
 #pragma unroll
                         for (int k = 0; k < 16; ++k)
-                            v[k] = __float_as_uint(__uint_as_float(v[k]) * w0 + (made[1] ? __uint_as_float(u[k]) * w1 : 0.f));
+                            v[k] = __float_as_uint(__uint_as_float(v[k]) * w0 + (made1 ? __uint_as_float(u[k]) * w1 : 0.f));
                     if (!valid) continue;
                     if (whole_tile) {
                         uint4* out = reinterpret_cast<uint4*>((T*)p.out + out_row * p.D + 16 * c);
@@ -378,8 +394,9 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
             if (two) meet_half();
             else meet_all();
             step0 += n;
-            o_base[0] += made[0];
-            o_base[1] += made[1];
+            o_done0 += made0;
+            o_done1 += made1;
+            item_return(ctl.items, item);
         }
     }
     tmem_fence_before();

@@ -34,6 +34,41 @@ __device__ __forceinline__ void copy_rows(uint32_t tile, int first_row, const vo
 // distance of a tile's piece of 16 features from its beginning, in the descriptors' unit
 __device__ __forceinline__ constexpr uint32_t piece(int k) { return ((k / 4) * (128 * 128) + (k % 4) * 32) / 16; }
 
+// ---- The items of a block (a tile, or a part of one) are found by a warp of their own and handed to the others through shared memory, a few
+// ahead: where a segment lies comes from global memory, and the kernels' shared memory leaves no first-level cache, so every warp that
+// looked for itself (or kept the walk's state in spilled registers) stood still for thousands of cycles between items.
+constexpr int ITEMS = 4;
+struct Item {
+    int q0, nq, k0, nk, s, h, t, steps, i0, i1;         // as in Walker; steps 0: there are no more
+    __device__ __forceinline__ Segment segment() const { return {q0, nq, k0, nk}; }
+};
+struct ItemRing {
+    unsigned long long full[ITEMS], empty[ITEMS];
+    Item item[ITEMS];
+};
+__device__ __forceinline__ void items_init(ItemRing& r, int consumer_warps) {
+    for (int i = 0; i < ITEMS; ++i) { mbar_init(smem_u32(&r.full[i]), 1); mbar_init(smem_u32(&r.empty[i]), consumer_warps); }
+}
+template <typename C>
+__device__ __forceinline__ void items_hand_out(ItemRing& r, const AttnParams& p, Walker<C>& it, bool more, volatile uint32_t* never) {
+    for (uint32_t n = 0;; ++n) {
+        if (n >= (uint32_t)ITEMS) mbar_wait(smem_u32(&r.empty[n % ITEMS]), (n / ITEMS + 1) & 1, never);
+        r.item[n % ITEMS] = {it.g.q0, it.g.nq, it.g.k0, it.g.nk, it.s, it.h, it.t, more ? it.steps : 0, it.i0, it.i1};
+        mbar_arrive(smem_u32(&r.full[n % ITEMS]));
+        if (!more) return;
+        more = it.next(p);
+    }
+}
+// The n-th item, for a whole warp, and its return.  Neither looks at the abort word: every warp goes through all items.
+__device__ __forceinline__ const Item& item_take(ItemRing& r, uint32_t n, volatile uint32_t* never) {
+    mbar_wait(smem_u32(&r.full[n % ITEMS]), (n / ITEMS) & 1, never);
+    return r.item[n % ITEMS];
+}
+__device__ __forceinline__ void item_return(ItemRing& r, uint32_t n) {
+    __syncwarp();
+    if (threadIdx.x % 32 == 0) mbar_arrive(smem_u32(&r.empty[n % ITEMS]));
+}
+
 // Tensor maps of the arrays: q and grad_out as [rows][heads][D], boxes of 32 packed rows of a kv head (32 / group rows of its group
 // heads: one box where group divides 32); key and value as [heads][rows][D] or [pages][heads][slots][D], boxes of kv_box rows of a head.
 struct TileMaps { CUtensorMap q, go, k, v; };
