@@ -45,6 +45,7 @@ struct BwdWork {
     long long *kv_start_unit, *q_start_unit;        // NULL: the blocks count for themselves
     float2* stats;                  // [n_q, heads]: lse in log2 (+inf: the row reads nothing), delta
     uint32_t* norms;                // largest squared norms of grad_out and value rows, as bits
+    Joint* joints;                  // [grid], the key kernel's, then the query kernel's
     float* part;                    // [2 * grid][rows][sides][DP]
     int kv_rows, q_rows;            // rows that a partial state holds at most
 };
@@ -56,54 +57,70 @@ __device__ __forceinline__ float gradient_factor(const uint32_t* norms) {
     return exp2f(14.f - (float)(ilogbf(largest) + 1));
 }
 
-// delta, lse in log2, and the norms behind gradient_factor: 16 lanes a row
+// delta, lse in log2, and the norms behind gradient_factor: a row by LANES threads, 8 features each.  Bound by memory: grad_out and out
+// are read once (fp16: value too).
 constexpr int PREP_THREADS = 256;
-template <typename T>
+template <typename T, int LANES>
 __global__ void __launch_bounds__(PREP_THREADS) attention_prepare_kernel(const AttnParams p, const BwdWork w) {
     constexpr bool NORMS = operand_type<T>() == 0;
+    constexpr int ROWS = PREP_THREADS / LANES;
     wait_for_previous_kernel();
     let_next_kernel_start();
-    const int lane = threadIdx.x % 16;
+    const int lane = threadIdx.x % LANES;
+    const bool in_width = lane * 8 < p.D;
     const int q_first = clamp_to(p.q_start[0], p.n_q), q_end = max(clamp_to(p.q_start[p.n_seg], p.n_q), q_first);
-    const int k_first = clamp_to(p.kv_start[0], p.n_kv), k_end = max(clamp_to(p.kv_start[p.n_seg], p.n_kv), k_first);
-    const long long q_rows = (long long)(q_end - q_first) * p.heads, rows = q_rows + (NORMS ? (long long)(k_end - k_first) * p.kv_heads : 0);
+    const long long q_rows = (long long)(q_end - q_first) * p.heads, stride = (long long)gridDim.x * ROWS;
+    auto fold = [&](float v) {
+#pragma unroll
+        for (int d = LANES / 2; d; d >>= 1) v += __shfl_xor_sync(~0u, v, d);
+        return v;
+    };
     float top_go = 0.f, top_v = 0.f;
-    const long long stride = (long long)gridDim.x * (PREP_THREADS / 16);
-    for (long long r0 = (long long)blockIdx.x * (PREP_THREADS / 16); r0 < rows; r0 += stride) {      // whole warps stay together
-        const long long r = r0 + threadIdx.x / 16;
-        float dot = 0.f, norm = 0.f;
-        const bool is_q = r < q_rows, on = r < rows && lane * 8 < p.D;
-        const long long row = is_q ? q_first + r / p.heads : k_first + (r - q_rows) / p.kv_heads;
-        const int head = (int)(is_q ? r % p.heads : (r - q_rows) % p.kv_heads);
+    for (long long r0 = (long long)blockIdx.x * ROWS; r0 < q_rows; r0 += stride) {      // whole warps stay together
+        const long long r = r0 + threadIdx.x / LANES, row = quotient(r, p.heads), at = (q_first + row) * p.heads + (r - row * p.heads);
         uint4 a = make_uint4(0, 0, 0, 0), b = a;
-        const T* src = is_q ? (const T*)p.go + row * p.go_row + head * p.go_head : (const T*)p.v + row * p.v_row + head * p.v_head;
-        if (on) {
-            if (is_q) b = *reinterpret_cast<const uint4*>((const T*)p.o + (row * p.heads + head) * p.D + lane * 8);
-            if (is_q || !p.mask || p.mask[row]) a = *reinterpret_cast<const uint4*>(src + lane * 8);
+        float lse = 0.f;
+        if (r < q_rows) {
+            if (in_width) {
+                a = *reinterpret_cast<const uint4*>((const T*)p.go + (q_first + row) * p.go_row + (r - row * p.heads) * p.go_head + lane * 8);
+                b = *reinterpret_cast<const uint4*>((const T*)p.o + at * p.D + lane * 8);
+            }
+            lse = p.lse_in[at];
         }
         const T* ea = reinterpret_cast<const T*>(&a);
         const T* eb = reinterpret_cast<const T*>(&b);
+        float dot = 0.f, norm = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float x = Half<T>::to(ea[e]);
             dot += x * Half<T>::to(eb[e]);
             if (NORMS) norm += x * x;
         }
-#pragma unroll
-        for (int d = 8; d; d >>= 1) {
-            dot += __shfl_xor_sync(~0u, dot, d);
-            if (NORMS) norm += __shfl_xor_sync(~0u, norm, d);
-        }
-        if (r >= rows) continue;
-        if (is_q) {
-            const long long at = row * p.heads + head;
-            const float lse = p.lse_in[at];
-            const bool reads = lse != -INFINITY;
-            if (lane == 0) w.stats[at] = make_float2(reads ? lse * LOG2E_F : INFINITY, reads ? dot : 0.f);
-            if (NORMS && reads) top_go = norm == norm ? fmaxf(top_go, norm) : INFINITY;
-        } else if (NORMS) top_v = norm == norm ? fmaxf(top_v, norm) : INFINITY;
+        dot = fold(dot);
+        if (NORMS) norm = fold(norm);
+        if (r >= q_rows) continue;
+        const bool reads = lse != -INFINITY;
+        if (lane == 0) w.stats[at] = make_float2(reads ? lse * LOG2E_F : INFINITY, reads ? dot : 0.f);
+        if (NORMS && reads) top_go = norm == norm ? fmaxf(top_go, norm) : INFINITY;
     }
     if (NORMS) {
+        const int k_first = clamp_to(p.kv_start[0], p.n_kv), k_end = max(clamp_to(p.kv_start[p.n_seg], p.n_kv), k_first);
+        const long long v_rows = (long long)(k_end - k_first) * p.kv_heads;
+        for (long long r0 = (long long)blockIdx.x * ROWS; r0 < v_rows; r0 += stride) {
+            const long long r = r0 + threadIdx.x / LANES, row = quotient(r, p.kv_heads);
+            uint4 a = make_uint4(0, 0, 0, 0);
+            if (r < v_rows && in_width && (!p.mask || p.mask[k_first + row]))
+                a = *reinterpret_cast<const uint4*>((const T*)p.v + (k_first + row) * p.v_row + (r - row * p.kv_heads) * p.v_head + lane * 8);
+            const T* ea = reinterpret_cast<const T*>(&a);
+            float norm = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float x = Half<T>::to(ea[e]);
+                norm += x * x;
+            }
+            norm = fold(norm);
+            top_v = norm == norm ? fmaxf(top_v, norm) : INFINITY;
+        }
 #pragma unroll
         for (int d = 16; d; d >>= 1) {
             top_go = fmaxf(top_go, __shfl_xor_sync(~0u, top_go, d));
@@ -158,7 +175,10 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
     const uint32_t s_at = tmem, dp_at = tmem + 128, acc1 = tmem + 256, acc2 = tmem + 384;
 
     if (warp == BWD_WALKER) {
-        if (lane == 0) items_hand_out(ctl.items, p, walk, work_here, &ctl.never);
+        if (lane == 0) {
+            w.joints[blockIdx.x] = joint_of(walk, work_here, blockIdx.x);
+            items_hand_out(ctl.items, p, walk, work_here, &ctl.never);
+        }
         __syncwarp();
     } else if (warp >= BWD_PRODUCER && warp < BWD_MMA) {
         // ---------------------------------------------------------------- producers
@@ -472,11 +492,12 @@ __global__ void __launch_bounds__(SUM_WARPS * 32) attention_sum_kernel(const Att
     constexpr bool F16 = operand_type<T>() == 0;
     wait_for_previous_kernel();
     let_next_kernel_start();
-    Walker<WorkCut> it;
-    if (!it.begin(p, KV ? w.kv_start_unit : w.q_start_unit, blockIdx.x, gridDim.x, BWD_LEAST) || it.i0 == 0 || it.i1 < it.steps) return;
-    const int first = it.first_block(blockIdx.x);
-    const int parts = (int)blockIdx.x - first + 1;
-    const int rows = min(WorkCut::rows(p, it.g) - it.t * BWD_ROWS, BWD_ROWS), cap = KV ? w.kv_rows : w.q_rows;
+    const Joint& j = w.joints[blockIdx.x];
+    const int parts = j.parts;
+    if (parts == 0) return;
+    const Item it = j.item;
+    const Segment g = it.segment();
+    const int first = j.first, rows = min(WorkCut::rows(p, g) - it.t * BWD_ROWS, BWD_ROWS), cap = KV ? w.kv_rows : w.q_rows;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const float factor = F16 ? gradient_factor(w.norms) : 1.f;
     __shared__ float sh[SUM_WARPS][DP];
@@ -510,10 +531,10 @@ __global__ void __launch_bounds__(SUM_WARPS * 32) attention_sum_kernel(const Att
             long long out_row;
             bool masked;
             if (KV) {
-                out_row = (long long)(it.g.k0 + n) * p.kv_heads + it.h;
-                masked = key_place(p, it.g, it.s, n).at < 0;
+                out_row = (long long)(g.k0 + n) * p.kv_heads + it.h;
+                masked = key_place(p, g, it.s, n).at < 0;
             } else {
-                const PackedRow pr = packed_row(p, it.g, it.h, n);
+                const PackedRow pr = packed_row(p, g, it.h, n);
                 out_row = (long long)pr.row * p.heads + pr.head;
                 masked = w.stats[out_row].x == INFINITY;
             }
@@ -544,6 +565,7 @@ static size_t backward_carve(const AttnParams& p, void* ws, BwdWork* w) {
     const bool counted_there = counts_itself(p, BWD_ROWS);
     w->kv_start_unit = counted_there ? nullptr : cv.take<long long>((size_t)p.n_seg + 1);
     w->q_start_unit = counted_there ? nullptr : cv.take<long long>((size_t)p.n_seg + 1);
+    w->joints = cv.take<Joint>(MAX_SMS);
     w->norms = cv.take<uint32_t>(2);
     w->stats = cv.take<float2>((size_t)p.n_q * p.heads);
     w->part = cv.take<float>(slots * floats * dp);          // the key kernel's, then the query kernel's
@@ -567,8 +589,8 @@ static tiga_status launch_backward(AttnParams p, const BwdWork& w, cudaStream_t 
     if (sms <= 0) return TIGA_ERR_CUDA;
     backward_plan_kernel<<<counted(2), PLAN_THREADS, 0, s>>>(p, w);
     const long long rows = (long long)p.n_q * p.heads + (long long)p.n_kv * p.kv_heads;
-    const long long grid = (rows * 16 + PREP_THREADS - 1) / PREP_THREADS;
-    TIGA_CUDA_TRY(launch_after(attention_prepare_kernel<T>, dim3((unsigned)(grid < 8 * sms ? grid : 8 * sms)), PREP_THREADS, 0, s, p, w));
+    const long long grid = (rows * (DP / 8) + PREP_THREADS - 1) / PREP_THREADS;
+    TIGA_CUDA_TRY(launch_after(attention_prepare_kernel<T, DP / 8>, dim3((unsigned)(grid < 8 * sms ? grid : 8 * sms)), PREP_THREADS, 0, s, p, w));
     tiga_status st = TIGA_OK;
     if ((p.gk || p.gv) && p.n_kv) st = launch_side<T, DP, true>(p, w, maps, sms, s);
     if (st == TIGA_OK && p.gq && p.n_q) st = launch_side<T, DP, false>(p, w, maps, sms, s);

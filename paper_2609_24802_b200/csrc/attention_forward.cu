@@ -42,6 +42,7 @@ struct FwdWork {
     long long* unit_start;          // NULL: the blocks count for themselves
     float2* part_ml;                // [2 * grid][rows]: reference of the exponents (log2), mass
     float* part_o;                  // [2 * grid][rows][DP]: unnormalised
+    Joint* joints;                  // [grid]
     int rows;                       // packed rows that a partial state holds at most
 };
 
@@ -81,7 +82,10 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
     // tensor memory: S of half x at 128 x, O at 256 + DP x
 
     if (warp == FWD_WALKER) {
-        if (lane == 0) items_hand_out(ctl.items, p, walk, work_here, &ctl.never);
+        if (lane == 0) {
+            w.joints[blockIdx.x] = joint_of(walk, work_here, blockIdx.x);
+            items_hand_out(ctl.items, p, walk, work_here, &ctl.never);
+        }
         __syncwarp();
     } else if (warp >= FWD_PRODUCER && warp < FWD_MMA) {
         // ---------------------------------------------------------------- producers
@@ -412,11 +416,11 @@ constexpr int JOIN_WARPS = 8, JOIN_Y = 16, JOIN_FEW = 8;
 template <typename T, int DP>
 __global__ void __launch_bounds__(JOIN_WARPS * 32) attention_join_kernel(const AttnParams p, const FwdWork w) {
     wait_for_previous_kernel();
-    Walker<FwdCut> it;
-    if (!it.begin(p, w.unit_start, blockIdx.x, gridDim.x, FWD_LEAST) || it.i0 == 0 || it.i1 < it.steps) return;
-    const int first = it.first_block(blockIdx.x);
-    const int parts = (int)blockIdx.x - first + 1;
-    const int rows = min(it.g.nq * p.group - it.t * FWD_ROWS, FWD_ROWS);
+    const Joint& j = w.joints[blockIdx.x];
+    const int parts = j.parts;
+    if (parts == 0) return;
+    const Item it = j.item;
+    const int first = j.first, rows = min(it.nq * p.group - it.t * FWD_ROWS, FWD_ROWS);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     constexpr int E = DP / 32;
     __shared__ float sh_m[JOIN_WARPS], sh_l[JOIN_WARPS], sh_o[JOIN_WARPS][DP];
@@ -445,11 +449,11 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) attention_join_kernel(const A
             m = top;
             const int here = min(32, b - k0);
 #pragma unroll 8
-            for (int j = 0; j < here; ++j) {
-                const float fj = __shfl_sync(~0u, f, j);
-                const float* src = w.part_o + ((2LL * (first + k0 + j) + (k0 + j == 0)) * w.rows + r) * DP;
+            for (int n = 0; n < here; ++n) {
+                const float fn = __shfl_sync(~0u, f, n);
+                const float* src = w.part_o + ((2LL * (first + k0 + n) + (k0 + n == 0)) * w.rows + r) * DP;
 #pragma unroll
-                for (int e = 0; e < E; ++e) o[e] += fj * src[lane + 32 * e];
+                for (int e = 0; e < E; ++e) o[e] += fn * src[lane + 32 * e];
             }
         }
         if (!few) {
@@ -474,7 +478,7 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) attention_join_kernel(const A
             __syncthreads();
         }
         if (few || warp == 0) {
-            const PackedRow pr = packed_row(p, it.g, it.h, it.t * FWD_ROWS + r);
+            const PackedRow pr = packed_row(p, it.segment(), it.h, it.t * FWD_ROWS + r);
             const long long out_row = (long long)pr.row * p.heads + pr.head;
             const float finish = l > 0.f || l != l ? 1.f / l : 0.f;
 #pragma unroll
@@ -491,6 +495,7 @@ size_t attention_forward_carve(const AttnParams& p, void* ws, FwdWork* w) {
     w->rows = (int)(packed < FWD_ROWS ? packed : FWD_ROWS);
     Carver cv(ws);
     w->unit_start = counts_itself(p, FWD_ROWS) ? nullptr : cv.take<long long>((size_t)p.n_seg + 1);
+    w->joints = cv.take<Joint>(MAX_SMS);
     w->part_ml = cv.take<float2>(slots * w->rows);
     w->part_o = cv.take<float>(slots * w->rows * (p.D > 64 ? 128 : 64));
     return cv.off;

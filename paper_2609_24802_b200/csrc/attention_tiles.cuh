@@ -59,6 +59,20 @@ __device__ __forceinline__ void items_hand_out(ItemRing& r, const AttnParams& p,
         more = it.next(p);
     }
 }
+// What a block leaves for the kernel that joins: the tile that ends in its first item and began in an earlier block's (parts 0: none).
+struct Joint {
+    Item item;
+    int first, parts;           // the block in which the tile begins; how many share it
+};
+template <typename C>
+__device__ __forceinline__ Joint joint_of(const Walker<C>& it, bool any, int block) {
+    Joint j;
+    j.item = {it.g.q0, it.g.nq, it.g.k0, it.g.nk, it.s, it.h, it.t, it.steps, it.i0, it.i1};
+    const bool ends = any && it.i0 > 0 && it.i1 == it.steps;
+    j.first = ends ? it.first_block(block) : 0;
+    j.parts = ends ? block - j.first + 1 : 0;
+    return j;
+}
 // The n-th item, for a whole warp, and its return.  Neither looks at the abort word: every warp goes through all items.
 __device__ __forceinline__ const Item& item_take(ItemRing& r, uint32_t n, volatile uint32_t* never) {
     mbar_wait(smem_u32(&r.full[n % ITEMS]), (n / ITEMS) & 1, never);
