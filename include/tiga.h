@@ -463,7 +463,7 @@ tiga_status tiga_rotary_frequencies(int32_t turned, double base, int32_t scaling
  * transpose (t -> -t, the same magnitude): the gradient of the call.
  *   x, y : dtype TIGA_F32, TIGA_F16 or TIGA_BF16, [n, heads, D], strided as above but without the rule on alignment (bases aligned to
  *          their element); y == x with equal strides rotates in place, other overlaps are not allowed;
- *   turned even, 0 < turned <= D;  positions: device int32 or int64 [n]. */
+ *   turned even, 0 < turned <= D (TIGA_ERR_UNSUPPORTED above 8192);  positions: device int32 or int64 [n]. */
 typedef struct {
     const double* freq;         /* device, fp64 [turned / 2] */
     int32_t turned, layout;

@@ -611,8 +611,9 @@ def _on(like, stream):
 
 
 def _same(like, *arrays):
+    device = like.device
     for t in arrays:
-        if t is not None and t.device != like.device:
+        if t is not None and t.device != device:
             raise ValueError("all arrays of a call must lie on one device")
 
 
@@ -628,17 +629,32 @@ def _step(t, d):
 
 def _stride_of(t, shape, dtype, name):
     """(row, head) strides of an array [rows, heads, D] whose features are contiguous."""
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+    if t.dtype is not dtype or t.shape != shape:
         raise ValueError(f"{name} must be {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
-    if t.shape[2] > 1 and t.stride(2) != 1:
+    row, head, one = t.stride()
+    if one != 1 and shape[2] > 1:
         raise ValueError(f"the features of {name} must be contiguous")
-    return _Stride(_step(t, 0), _step(t, 1))
+    return (row if shape[0] > 1 else 0), (head if shape[1] > 1 else 0)
 
 
 def _dense_out(t, shape, dtype, name):
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} array {tuple(shape)}")
     return t.data_ptr()
+
+
+# the descriptors' fields packed at once: a ctypes structure filled field by field costs several times as much
+_HEADS_BYTES, _HEADS_OF, _NO_STRIDE = struct.Struct("=4if4x8q"), _Heads.from_buffer_copy, (0, 0)
+_DENSE_BYTES, _DENSE_OF = struct.Struct("=6q"), _Dense.from_buffer_copy
+_STRIDE_BYTES, _STRIDE_OF = struct.Struct("=2q"), _Stride.from_buffer_copy
+assert _HEADS_BYTES.size == ctypes.sizeof(_Heads) and _DENSE_BYTES.size == ctypes.sizeof(_Dense)
+
+
+def _heads_of(dt, heads, kv_heads, D, scale, q, key=_NO_STRIDE, value=_NO_STRIDE, grad_out=_NO_STRIDE):
+    try:
+        return _HEADS_OF(_HEADS_BYTES.pack(dt, heads, kv_heads, D, scale, *q, *key, *value, *grad_out))
+    except (struct.error, OverflowError):          # a number that int32 or fp32 does not hold, another kind of number: as ctypes converts them
+        return _Heads(dt, heads, kv_heads, D, float(scale), _Stride(*q), _Stride(*key), _Stride(*value), _Stride(*grad_out))
 
 
 def _type_of(t, types):
@@ -662,22 +678,23 @@ class DenseRelation:
             raise ValueError("mask must be a contiguous bool or uint8 array")
         _same(q_start, kv_start, mask)
         self.q_start, self.kv_start, self.mask = q_start, kv_start, mask
+        self.q_ptr, self.kv_ptr, self.mask_ptr = q_start.data_ptr(), kv_start.data_ptr(), 0 if mask is None else mask.data_ptr()
         self.n_seg = q_start.numel() - 1
 
 
 def _dense_args(g, q, key, value, scale, grad_out=None):
-    dt = _type_of(q, _HALF)
-    n_q, heads, D = q.shape
+    dt, dtype, shape = _type_of(q, _HALF), q.dtype, q.shape
+    n_q, heads, D = shape
     if key.dim() != 3:
         raise ValueError("arrays with heads have three dimensions: [rows, heads, D]")
-    n_kv, kv_heads = key.shape[:2]
+    n_kv, kv_heads, _ = key.shape
     _same(q, key, value, grad_out, g.q_start)
     if g.mask is not None and g.mask.numel() != n_kv:
         raise ValueError("the mask has one entry per key")
-    h = _Heads(dt, heads, kv_heads, D, scale, _stride_of(q, (n_q, heads, D), q.dtype, "q"),
-               _stride_of(key, (n_kv, kv_heads, D), q.dtype, "key"), _stride_of(value, (n_kv, kv_heads, D), q.dtype, "value"),
-               _Stride() if grad_out is None else _stride_of(grad_out, (n_q, heads, D), q.dtype, "grad_out"))
-    return _Dense(g.q_start.data_ptr(), g.kv_start.data_ptr(), 0 if g.mask is None else g.mask.data_ptr(), g.n_seg, n_q, n_kv), h
+    keys = (n_kv, kv_heads, D)
+    h = _heads_of(dt, heads, kv_heads, D, scale, _stride_of(q, shape, dtype, "q"), _stride_of(key, keys, dtype, "key"),
+                  _stride_of(value, keys, dtype, "value"), _NO_STRIDE if grad_out is None else _stride_of(grad_out, shape, dtype, "grad_out"))
+    return _DENSE_OF(_DENSE_BYTES.pack(g.q_ptr, g.kv_ptr, g.mask_ptr, g.n_seg, n_q, n_kv)), h
 
 
 def tiga_dense_attention_workspace_bytes(g: DenseRelation, q, key, value, backward: bool = False) -> int:
@@ -752,7 +769,7 @@ def _paged_heads(cache, q, scale):
     if _type_of(q, _HALF) != _HALF[cache.key.dtype] or q.shape[2] != cache.key.shape[3]:
         raise ValueError("queries and cache must have one storage type and width")
     _same(q, cache.key)
-    return _Heads(_HALF[q.dtype], q.shape[1], cache.key.shape[2], q.shape[2], scale, _stride_of(q, q.shape, q.dtype, "q"))
+    return _heads_of(_HALF[q.dtype], q.shape[1], cache.key.shape[2], q.shape[2], scale, _stride_of(q, q.shape, q.dtype, "q"))
 
 
 def tiga_paged_attention_workspace_bytes(cache: PagedCache, q) -> int:
@@ -811,7 +828,7 @@ def tiga_apply_rotary(rotary: Rotary, x, positions, out=None, inverse=False, str
         if out is None:
             out = x.new_empty(x.shape)
         _same(x, positions, out, rotary.freq)
-        xs, ys = _stride_of(x, x.shape, x.dtype, "x"), _stride_of(out, x.shape, x.dtype, "out")
+        xs, ys = (_STRIDE_OF(_STRIDE_BYTES.pack(*_stride_of(t, x.shape, x.dtype, n))) for t, n in ((x, "x"), (out, "out")))
         _ok(_L.tiga_apply_rotary(rotary.ref, x.data_ptr(), ctypes.byref(xs), out.data_ptr(), ctypes.byref(ys), dt, x.shape[0], x.shape[1],
                                  x.shape[2], positions.data_ptr(), I32 if positions.dtype == torch.int32 else I64, int(bool(inverse)),
                                  _stream(stream)), "tiga_apply_rotary")
@@ -827,6 +844,6 @@ def tiga_paged_append(cache: PagedCache, key, value, start, rotary: Rotary = Non
             raise ValueError("the rows must have the cache's storage type, heads and width")
         _same(key, value, start, cache.key, None if rotary is None else rotary.freq)
         n, heads, D = key.shape
-        h = _Heads(dt, heads, heads, D, 1.0, _Stride(), _stride_of(key, key.shape, key.dtype, "key"), _stride_of(value, key.shape, key.dtype, "value"))
+        h = _heads_of(dt, heads, heads, D, 1.0, _NO_STRIDE, _stride_of(key, key.shape, key.dtype, "key"), _stride_of(value, key.shape, key.dtype, "value"))
         _ok(_L.tiga_paged_append(cache.ref, ctypes.byref(h), key.data_ptr(), value.data_ptr(), _ints(start, cache.c.n_seg + 1, "start"), n,
                                  None if rotary is None else rotary.ref, _stream(stream)), "tiga_paged_append")

@@ -3,14 +3,16 @@
 // A pair (a, b) of features at position n is turned by t = n f: (a cos t - b sin t, a sin t + b cos t).  The work is bound by
 // memory: every element is read and written once, the turn costs six operations per pair, its sine and cosine once per
 // (row, pair) and thread, kept in registers for the thread's heads.
-// t is formed in 64 bits as a number of turns, n (f / 2 pi); whole turns are taken off there, so position 2^22 keeps an error of
-// 2^22 2^-53 turns, and the remaining half turn at most enters sincospif in fp32.  (In fp32 the product alone is off by
-// 2^22 2^-24 / 2 turns: the angle would mean nothing.)
+// t is a number of turns in 64-bit fixed point: f / 2 pi without its whole turns, times the position, modulo 2^64.  Whole turns drop
+// out by themselves, and position 2^22 keeps an error of 2^22 2^-54 turns; the upper 32 bits, at most half a turn either way, enter
+// sincospif in fp32.  (In fp32 the product alone is off by 2^22 2^-24 / 2 turns: the angle would mean nothing.  Formed once per row and
+// pair of a block: formed again for every few heads they took as long as the memory.)
 #include "attention_shared.cuh"
 
 namespace tiga {
 
-constexpr int ROT_THREADS = 256, BATCH = 4;       // heads whose loads are under way at a time
+constexpr int ROT_THREADS = 256;
+constexpr int ROT_ROWS = 8, ROT_PAIRS_MAX = 4096;
 
 struct RotParams {
     const void *x, *value;          // value: append only
@@ -20,11 +22,17 @@ struct RotParams {
     const int32_t *start, *kv_len, *table;
     long long x_row, x_head, v_row, v_head, y_row, y_head, slot_stride, page_size, max_pages, table_stride, n_pages;
     long long n;
-    int pos64, n_seg, heads, D, turned, pairs, splits, rot_units, tail_units, val_units, in_place;
+    int pos64, n_seg, heads, D, turned, pairs, rows, rot_units, tail_units, val_units, in_place;
     float magnitude;
     int inverse;
 };
 
+// f / 2 pi modulo a turn, in units of 2^-64 turns
+__device__ __forceinline__ unsigned long long turns_of(double f) {
+    double t = f * 0.15915494309189533577;
+    t -= floor(t);
+    return t < 1.0 ? (unsigned long long)(t * 18446744073709551616.0) : 0ull;
+}
 template <typename T, int VEC, bool ALIGNED>
 struct alignas(ALIGNED ? sizeof(T) * VEC : sizeof(T)) Pack { T e[VEC]; };
 
@@ -58,115 +66,93 @@ __device__ __forceinline__ int last_start_at_or_before(const int32_t* start, int
     return lo - 1;
 }
 
-// A thread has one unit of a row (VEC pairs as two vectors of the halves; or VEC / 2 pairs as one vector; or a vector of
-// what is copied) and every `splits`-th head.
+// A block has up to ROT_ROWS rows.  It looks up where they lie, forms the sines and cosines of their pairs once, and then passes over
+// the rows' heads in the order of memory.  A unit is VEC pairs as two vectors of the halves, VEC / 2 pairs as one vector, or one vector
+// of what is copied.  Many threads hide the
+// loads, not batches of them: two and four units a thread at a time cost registers and 14 and 67 %.
 template <typename T, int VEC, bool ALIGNED, bool APPEND>
 __global__ void __launch_bounds__(ROT_THREADS) rotary_kernel(const RotParams p) {
-    const int units = p.rot_units + p.tail_units + (APPEND ? p.val_units : 0);
-    const long long idx = (long long)blockIdx.x * ROT_THREADS + threadIdx.x;
-    const long long row_split = quotient(idx, units);
-    const int u = (int)(idx - row_split * units);
-    const long long i = quotient(row_split, p.splits);
-    const int split = (int)(row_split - i * p.splits);
-    if (i >= p.n) return;
-
-    long long pos, y0;
-    if (APPEND) {
-        const int s = last_start_at_or_before(p.start, p.n_seg, (int)p.n, (int)i);
-        if (s < 0) return;
-        const int first = clamp_to(p.start[s], (int)p.n), end = clamp_to(p.start[s + 1], (int)p.n);
-        pos = (long long)max(p.kv_len[s], 0) - (end - i);
-        if (pos < 0 || pos >= p.max_pages * p.page_size || first > i) return;
-        const long long page = quotient(pos, p.page_size);
-        const int id = p.table[s * p.table_stride + page];
-        if (id < 0 || id >= p.n_pages) return;
-        y0 = id * p.y_row + (pos - page * p.page_size) * p.slot_stride;
-    } else {
-        pos = p.pos64 ? ((const long long*)p.positions)[i] : ((const int*)p.positions)[i];
-        y0 = i * p.y_row;
-    }
-    const T* x = (const T*)p.x + i * p.x_row;
-    T* y = (T*)p.y + y0;
-    typedef Pack<T, VEC, ALIGNED> V;
-
-    if (u < p.rot_units) {
-        const int np = p.pairs ? VEC / 2 : VEC;             // pairs of this unit
-        const int first = u * np, half = p.turned / 2;
-        const int a0 = p.pairs ? 2 * first : first;
-        const int left = p.pairs ? p.turned - a0 : half - first;
-        float c[VEC], s[VEC];
-#pragma unroll
-        for (int k = 0; k < VEC; ++k)
-            if (k < np && first + k < half) {
-                double t = (double)pos * (p.freq[first + k] * 0.15915494309189533577);
-                t -= rint(t);
-                sincospif(2.f * (float)t, &s[k], &c[k]);
-                c[k] *= p.magnitude;
-                s[k] *= p.inverse ? -p.magnitude : p.magnitude;
-            }
-        // heads in batches whose loads are all on their way before the first is used (in place, loads and stores of one pointer would
-        // otherwise take turns: 16384 rows of 40 heads of 128 took 37 us a pass instead of 30)
-        if (p.pairs) {
-            for (int h0 = split; h0 < p.heads; h0 += BATCH * p.splits) {
-                V a[BATCH];
-#pragma unroll
-                for (int j = 0; j < BATCH; ++j)
-                    if (h0 + j * p.splits < p.heads) a[j] = load_pack<T, VEC, ALIGNED>(x + (h0 + j * p.splits) * p.x_head + a0, left);
-#pragma unroll
-                for (int j = 0; j < BATCH; ++j) {
-                    if (h0 + j * p.splits >= p.heads) continue;
-#pragma unroll
-                    for (int k = 0; k < VEC / 2; ++k) {
-                        const float e = Half<T>::to(a[j].e[2 * k]), f = Half<T>::to(a[j].e[2 * k + 1]);
-                        a[j].e[2 * k] = Half<T>::from(e * c[k] - f * s[k]);
-                        a[j].e[2 * k + 1] = Half<T>::from(e * s[k] + f * c[k]);
-                    }
-                    store_pack<T, VEC, ALIGNED>(y + (h0 + j * p.splits) * p.y_head + a0, a[j], left);
+    extern __shared__ float2 turn[];            // [rows][pairs]: cosine, sine
+    __shared__ long long position[ROT_ROWS], target[ROT_ROWS];      // target: the row's offset in y, -1: it goes nowhere
+    const long long first_row = (long long)blockIdx.x * p.rows;
+    const int rows = (int)min((long long)p.rows, p.n - first_row), n_pairs = p.turned / 2;
+    if (threadIdx.x < rows) {
+        const long long i = first_row + threadIdx.x;
+        long long pos = 0, y0 = -1;
+        if (APPEND) {
+            const int s = last_start_at_or_before(p.start, p.n_seg, (int)p.n, (int)i);
+            if (s >= 0) {
+                const int first = clamp_to(p.start[s], (int)p.n), end = clamp_to(p.start[s + 1], (int)p.n);
+                pos = (long long)max(p.kv_len[s], 0) - (end - i);
+                if (pos >= 0 && pos < p.max_pages * p.page_size && first <= i) {
+                    const long long page = quotient(pos, p.page_size);
+                    const int id = p.table[s * p.table_stride + page];
+                    if (id >= 0 && id < p.n_pages) y0 = id * p.y_row + (pos - page * p.page_size) * p.slot_stride;
                 }
             }
         } else {
-            for (int h0 = split; h0 < p.heads; h0 += BATCH * p.splits) {
-                V a[BATCH], b[BATCH];
-#pragma unroll
-                for (int j = 0; j < BATCH; ++j)
-                    if (h0 + j * p.splits < p.heads) {
-                        const T* src = x + (h0 + j * p.splits) * p.x_head + a0;
-                        a[j] = load_pack<T, VEC, ALIGNED>(src, left);
-                        b[j] = load_pack<T, VEC, ALIGNED>(src + half, left);
-                    }
-#pragma unroll
-                for (int j = 0; j < BATCH; ++j) {
-                    if (h0 + j * p.splits >= p.heads) continue;
-#pragma unroll
-                    for (int k = 0; k < VEC; ++k) {
-                        const float e = Half<T>::to(a[j].e[k]), f = Half<T>::to(b[j].e[k]);
-                        a[j].e[k] = Half<T>::from(e * c[k] - f * s[k]);
-                        b[j].e[k] = Half<T>::from(e * s[k] + f * c[k]);
-                    }
-                    T* dst = y + (h0 + j * p.splits) * p.y_head + a0;
-                    store_pack<T, VEC, ALIGNED>(dst, a[j], left);
-                    store_pack<T, VEC, ALIGNED>(dst + half, b[j], left);
-                }
-            }
+            pos = p.pos64 ? ((const long long*)p.positions)[i] : ((const int*)p.positions)[i];
+            y0 = i * p.y_row;
         }
-        return;
+        position[threadIdx.x] = pos;
+        target[threadIdx.x] = y0;
     }
-    long long xh = p.x_head;
-    int at = p.turned + (u - p.rot_units) * VEC;
-    if (APPEND && u >= p.rot_units + p.tail_units) {
-        at = (u - p.rot_units - p.tail_units) * VEC;
-        x = (const T*)p.value + i * p.v_row;
-        xh = p.v_head;
-        y = (T*)p.vy + y0;
-    } else if (p.in_place) return;
-    for (int h0 = split; h0 < p.heads; h0 += BATCH * p.splits) {
-        V a[BATCH];
+    __syncthreads();
+    for (int k = threadIdx.x; k < rows * n_pairs; k += ROT_THREADS) {
+        const int r = k / n_pairs;
+        const unsigned long long t = (unsigned long long)position[r] * turns_of(p.freq[k - r * n_pairs]);
+        float c, s;
+        sincospif((float)(int)(t >> 32) * 0x1p-31f, &s, &c);
+        turn[k] = make_float2(c * p.magnitude, p.inverse ? -s * p.magnitude : s * p.magnitude);
+    }
+    __syncthreads();
+
+    // A thread has one unit of every step-th (row, head); rows wider than a block are cut into parts of its threads.
+    typedef Pack<T, VEC, ALIGNED> V;
+    const int units = p.rot_units + (p.in_place ? 0 : p.tail_units) + (APPEND ? p.val_units : 0);
+    const int part = min(units, ROT_THREADS), step = ROT_THREADS / part;
+    const int lane = threadIdx.x % part, begin = threadIdx.x / part;
+    if (begin >= step) return;
+    for (int u = lane; u < units; u += part) {
+        const bool turned = u < p.rot_units, value = APPEND && u >= p.rot_units + p.tail_units;
+        const int at = turned ? u * VEC : value ? (u - p.rot_units - p.tail_units) * VEC : p.turned + (u - p.rot_units) * VEC;
+        const int left = turned ? (p.pairs ? p.turned : n_pairs) - at : p.D - at;
+        const T* src = (const T*)(value ? p.value : p.x) + at;
+        T* dst = (T*)(value ? p.vy : p.y) + at;
+        const long long src_row = value ? p.v_row : p.x_row, src_head = value ? p.v_head : p.x_head;
+        for (int r = begin / p.heads, h = begin - r * p.heads; r < rows;) {
+            if (target[r] >= 0) {
+                const T* from = src + (first_row + r) * src_row + h * src_head;
+                T* to = dst + target[r] + h * p.y_head;
+                V a = load_pack<T, VEC, ALIGNED>(from, left);
+                if (turned) {
+                    const float2* cs = turn + r * n_pairs + (p.pairs ? at / 2 : at);
+                    if (p.pairs) {
 #pragma unroll
-        for (int j = 0; j < BATCH; ++j)
-            if (h0 + j * p.splits < p.heads) a[j] = load_pack<T, VEC, ALIGNED>(x + (h0 + j * p.splits) * xh + at, p.D - at);
+                        for (int k = 0; k < VEC / 2; ++k) {
+                            const float e = Half<T>::to(a.e[2 * k]), f = Half<T>::to(a.e[2 * k + 1]);
+                            const float2 t = cs[k];
+                            a.e[2 * k] = Half<T>::from(e * t.x - f * t.y);
+                            a.e[2 * k + 1] = Half<T>::from(e * t.y + f * t.x);
+                        }
+                    } else {
+                        V b = load_pack<T, VEC, ALIGNED>(from + n_pairs, left);
 #pragma unroll
-        for (int j = 0; j < BATCH; ++j)
-            if (h0 + j * p.splits < p.heads) store_pack<T, VEC, ALIGNED>(y + (h0 + j * p.splits) * p.y_head + at, a[j], p.D - at);
+                        for (int k = 0; k < VEC; ++k) {
+                            if (!ALIGNED && k >= left) continue;
+                            const float e = Half<T>::to(a.e[k]), f = Half<T>::to(b.e[k]);
+                            const float2 t = cs[k];
+                            a.e[k] = Half<T>::from(e * t.x - f * t.y);
+                            b.e[k] = Half<T>::from(e * t.y + f * t.x);
+                        }
+                        store_pack<T, VEC, ALIGNED>(to + n_pairs, b, left);
+                    }
+                }
+                store_pack<T, VEC, ALIGNED>(to, a, left);
+            }
+            h += step;
+            while (h >= p.heads) { h -= p.heads; ++r; }
+        }
     }
 }
 
@@ -176,14 +162,15 @@ static tiga_status launch_rotary_t(RotParams p, cudaStream_t s) {
     p.rot_units = (p.turned / 2 + np - 1) / np;
     p.tail_units = (p.D - p.turned + VEC - 1) / VEC;
     p.val_units = (p.D + VEC - 1) / VEC;
-    const long long per_row = p.rot_units + p.tail_units + (APPEND ? p.val_units : 0);
-    // A thread keeps its sines and cosines for as many heads as leave a wave of 4 blocks an SM; few rows are spread over all heads.
-    const long long wave = 148LL * 4 * ROT_THREADS;
-    long long splits = (wave + p.n * per_row - 1) / (p.n * per_row);
-    p.splits = (int)(splits < 1 ? 1 : splits > p.heads ? p.heads : splits);
-    const long long blocks = (p.n * per_row * p.splits + ROT_THREADS - 1) / ROT_THREADS;
-    if (blocks > 0x7fffffffLL) return TIGA_ERR_UNSUPPORTED;
-    rotary_kernel<T, VEC, ALIGNED, APPEND><<<counted((unsigned)blocks), ROT_THREADS, 0, s>>>(p);
+    if (APPEND == false && p.in_place && p.rot_units == 0) return TIGA_OK;
+    // rows of a block: as many as leave four blocks an SM and their sines and cosines room (32 KB)
+    long long rows = p.n / (148 * 4);
+    const int room = p.turned ? ROT_PAIRS_MAX / (p.turned / 2) : ROT_ROWS;
+    rows = rows < 1 ? 1 : rows > ROT_ROWS ? ROT_ROWS : rows;
+    p.rows = (int)(rows > room ? room : rows);
+    const long long blocks = (p.n + p.rows - 1) / p.rows;
+    if (blocks > 0x7fffffffLL || (long long)p.rows * p.heads * (p.rot_units + p.tail_units + p.val_units) > 0x7fffffffLL) return TIGA_ERR_UNSUPPORTED;
+    rotary_kernel<T, VEC, ALIGNED, APPEND><<<counted((unsigned)blocks), ROT_THREADS, (size_t)p.rows * (p.turned / 2) * sizeof(float2), s>>>(p);
     return launch_status();
 }
 
@@ -247,7 +234,7 @@ extern "C" tiga_status tiga_apply_rotary(const tiga_rotary* r, const void* x, co
     if (x == y && (xs->row != ys->row || xs->head != ys->head)) return TIGA_ERR_INVALID_ARG;
     // rows or heads of y that share storage would be written twice
     if ((n > 1 && ys->row == 0) || (heads > 1 && ys->head == 0)) return TIGA_ERR_INVALID_ARG;
-    if (n > (1LL << 40)) return TIGA_ERR_UNSUPPORTED;
+    if (n > (1LL << 40) || r->turned > 2 * ROT_PAIRS_MAX) return TIGA_ERR_UNSUPPORTED;
     RotParams p{};
     p.x = x; p.y = y; p.x_row = xs->row; p.x_head = xs->head; p.y_row = ys->row; p.y_head = ys->head; p.in_place = x == y;
     p.freq = r->freq; p.turned = r->turned; p.pairs = r->layout == TIGA_ROT_PAIRS; p.magnitude = r->magnitude; p.inverse = inverse != 0;
