@@ -3,7 +3,7 @@
 
 namespace tiga {
 
-// Two kernels of one form.  A block keeps a stationary tile of 128 rows of two arrays, X1 and X2, and goes through the other side in
+// Two passes of one form, by blocks of their own in one launch (keys first; a pass's blocks share its work).  A block keeps a stationary tile of 128 rows of two arrays, X1 and X2, and goes through the other side in
 // steps of 128 rows of Y1 and Y2:
 //     keys and values:  X = (key, value), Y = (q, grad_out):   S = X1 Y1^T, dP = X2 Y2^T (both transposed), grad_value += P Y2,
 //                                                               grad_key += dS Y1;      all heads of a group pass by: their sum
@@ -45,8 +45,8 @@ struct BwdWork {
     long long *kv_start_unit, *q_start_unit;        // NULL: the blocks count for themselves
     float2* stats;                  // [n_q, heads]: lse in log2 (+inf: the row reads nothing), delta
     uint32_t* norms;                // largest squared norms of grad_out and value rows, as bits
-    Joint* joints;                  // [grid], the key kernel's, then the query kernel's
-    float* part;                    // [2 * grid][rows][sides][DP]
+    Joint *kv_joints, *q_joints;    // [blocks of the side]
+    float *kv_part, *q_part;        // [2 * blocks of the side][rows][gradients of the side][DP]
     int kv_rows, q_rows;            // rows that a partial state holds at most
 };
 
@@ -59,7 +59,7 @@ __device__ __forceinline__ float gradient_factor(const uint32_t* norms) {
 
 // delta, lse in log2, and the norms behind gradient_factor: a row by LANES threads, 8 features each.  Bound by memory: grad_out and out
 // are read once (fp16: value too).
-constexpr int PREP_THREADS = 256;
+constexpr int PREP_THREADS = 256, PREP_ALONE = 16;     // blocks of work that one block does alone
 template <typename T, int LANES>
 __global__ void __launch_bounds__(PREP_THREADS) attention_prepare_kernel(const AttnParams p, const BwdWork w) {
     constexpr bool NORMS = operand_type<T>() == 0;
@@ -126,15 +126,20 @@ __global__ void __launch_bounds__(PREP_THREADS) attention_prepare_kernel(const A
             top_go = fmaxf(top_go, __shfl_xor_sync(~0u, top_go, d));
             top_v = fmaxf(top_v, __shfl_xor_sync(~0u, top_v, d));
         }
-        if (threadIdx.x % 32 == 0) {        // a maximum does not depend on the order
-            atomicMax(&w.norms[0], __float_as_uint(top_go));
-            atomicMax(&w.norms[1], __float_as_uint(top_v));
+        __shared__ float tops[2][PREP_THREADS / 32];
+        if (threadIdx.x % 32 == 0) { tops[0][threadIdx.x / 32] = top_go; tops[1][threadIdx.x / 32] = top_v; }
+        __syncthreads();
+        if (threadIdx.x < 2) {              // a maximum does not depend on the order
+            float top = 0.f;
+            for (int k = 0; k < PREP_THREADS / 32; ++k) top = fmaxf(top, tops[threadIdx.x][k]);
+            if (gridDim.x == 1) w.norms[threadIdx.x] = __float_as_uint(top);
+            else atomicMax(&w.norms[threadIdx.x], __float_as_uint(top));
         }
     }
 }
 
 template <typename T, int DP, bool KV>
-__global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(const AttnParams p, const BwdWork w, const __grid_constant__ TileMaps maps) {
+__device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork& w, const TileMaps& maps, const int block, const int blocks) {
     typedef Bwd<DP> C;
     typedef typename CutOf<KV>::type WorkCut;
     constexpr bool F16 = operand_type<T>() == 0;
@@ -166,7 +171,7 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
     }
     Walker<WorkCut> walk;
     bool work_here = false;
-    if (warp == BWD_WALKER) work_here = walk.begin(p, KV ? w.kv_start_unit : w.q_start_unit, blockIdx.x, gridDim.x, BWD_LEAST);
+    if (warp == BWD_WALKER) work_here = walk.begin(p, KV ? w.kv_start_unit : w.q_start_unit, block, blocks, BWD_LEAST);
     if (warp == BWD_MMA) tmem_alloc(smem_u32(&ctl.tmem), 512);
     tmem_fence_before();
     __syncthreads();
@@ -176,7 +181,7 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
 
     if (warp == BWD_WALKER) {
         if (lane == 0) {
-            w.joints[blockIdx.x] = joint_of(walk, work_here, blockIdx.x);
+            (KV ? w.kv_joints : w.q_joints)[block] = joint_of(walk, work_here, block);
             items_hand_out(ctl.items, p, walk, work_here, &ctl.never);
         }
         __syncwarp();
@@ -443,7 +448,7 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
             const uint32_t acc = side ? acc2 : acc1;
             const float finish = side ? (F16 ? 0x1p-14f : 1.f) : p.scale / factor;
             T* out = (T*)(KV ? (side ? p.gv : p.gk) : p.gq);
-            float* part = w.part + ((((2LL * blockIdx.x + (item.i0 == 0)) * rows + row) * SIDES) + side) * DP;
+            float* part = (KV ? w.kv_part : w.q_part) + ((((2LL * block + (item.i0 == 0)) * rows + row) * SIDES) + side) * DP;
             if (warp_on)
                 for (int c = c0; c < c0 + PIECES; ++c) {
                     uint32_t v[16];
@@ -481,18 +486,22 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(cons
     if (warp == BWD_MMA) { tmem_fence_after(); tmem_free(tmem, 512); }
 }
 
+template <typename T, int DP>
+__global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(const AttnParams p, const BwdWork w, const __grid_constant__ TileMaps maps, const int kv_blocks) {
+    if ((int)blockIdx.x < kv_blocks) backward_pass<T, DP, true>(p, w, maps, blockIdx.x, kv_blocks);
+    else backward_pass<T, DP, false>(p, w, maps, (int)blockIdx.x - kv_blocks, (int)gridDim.x - kv_blocks);
+}
+
 // Adds up the partial sums of a tile that several blocks shared, in the order of its steps.  A warp has a row of one gradient; many parts
 // (few tiles, a long axis) are shared by the block's warps, whose sums are added in order.
 constexpr int SUM_WARPS = 8, SUM_Y = 16, SUM_FEW = 8;
 
 template <typename T, int DP, bool KV>
-__global__ void __launch_bounds__(SUM_WARPS * 32) attention_sum_kernel(const AttnParams p, const BwdWork w) {
+__device__ __forceinline__ void sum_pass(const AttnParams& p, const BwdWork& w, const int block) {
     typedef typename CutOf<KV>::type WorkCut;
     constexpr int SIDES = KV ? 2 : 1, E = DP / 32;
     constexpr bool F16 = operand_type<T>() == 0;
-    wait_for_previous_kernel();
-    let_next_kernel_start();
-    const Joint& j = w.joints[blockIdx.x];
+    const Joint& j = (KV ? w.kv_joints : w.q_joints)[block];
     const int parts = j.parts;
     if (parts == 0) return;
     const Item it = j.item;
@@ -510,7 +519,7 @@ __global__ void __launch_bounds__(SUM_WARPS * 32) attention_sum_kernel(const Att
         for (int e = 0; e < E; ++e) o[e] = 0.f;
 #pragma unroll 8
         for (int k = a; k < b; ++k) {
-            const float* src = w.part + (((2LL * (first + k) + (k == 0)) * cap + r) * SIDES + side) * DP;
+            const float* src = (KV ? w.kv_part : w.q_part) + (((2LL * (first + k) + (k == 0)) * cap + r) * SIDES + side) * DP;
 #pragma unroll
             for (int e = 0; e < E; ++e) o[e] += src[lane + 32 * e];
         }
@@ -547,6 +556,13 @@ __global__ void __launch_bounds__(SUM_WARPS * 32) attention_sum_kernel(const Att
     }
 }
 
+template <typename T, int DP>
+__global__ void __launch_bounds__(SUM_WARPS * 32) attention_sum_kernel(const AttnParams p, const BwdWork w, const int kv_blocks) {
+    wait_for_previous_kernel();
+    if ((int)blockIdx.x < kv_blocks) sum_pass<T, DP, true>(p, w, blockIdx.x);
+    else sum_pass<T, DP, false>(p, w, (int)blockIdx.x - kv_blocks);
+}
+
 // clears the norms; counts the units of every segment where the blocks do not
 static __global__ void __launch_bounds__(PLAN_THREADS) backward_plan_kernel(const AttnParams p, const BwdWork w) {
     let_next_kernel_start();
@@ -560,26 +576,19 @@ static size_t backward_carve(const AttnParams& p, void* ws, BwdWork* w) {
     const long long packed = (long long)p.n_q * p.group;
     w->kv_rows = p.n_kv < BWD_ROWS ? p.n_kv : BWD_ROWS;
     w->q_rows = (int)(packed < BWD_ROWS ? packed : BWD_ROWS);
-    const size_t floats = (size_t)w->kv_rows * 2 > (size_t)w->q_rows ? (size_t)w->kv_rows * 2 : (size_t)w->q_rows;
     Carver cv(ws);
     const bool counted_there = counts_itself(p, BWD_ROWS);
     w->kv_start_unit = counted_there ? nullptr : cv.take<long long>((size_t)p.n_seg + 1);
     w->q_start_unit = counted_there ? nullptr : cv.take<long long>((size_t)p.n_seg + 1);
-    w->joints = cv.take<Joint>(MAX_SMS);
+    w->kv_joints = cv.take<Joint>(MAX_SMS);
+    w->q_joints = cv.take<Joint>(MAX_SMS);
     w->norms = cv.take<uint32_t>(2);
     w->stats = cv.take<float2>((size_t)p.n_q * p.heads);
-    w->part = cv.take<float>(slots * floats * dp);          // the key kernel's, then the query kernel's
+    w->kv_part = cv.take<float>(slots * w->kv_rows * 2 * dp);
+    w->q_part = cv.take<float>(slots * w->q_rows * dp);
     return cv.off;
 }
 size_t attention_backward_bytes(const AttnParams& p) { BwdWork w; return backward_carve(p, nullptr, &w); }
-
-template <typename T, int DP, bool KV>
-static tiga_status launch_side(const AttnParams& p, const BwdWork& w, const TileMaps& maps, int sms, cudaStream_t s) {
-    TIGA_CUDA_TRY(cudaFuncSetAttribute(attention_backward_kernel<T, DP, KV>, cudaFuncAttributeMaxDynamicSharedMemorySize, Bwd<DP>::SMEM));
-    TIGA_CUDA_TRY(launch_after(attention_backward_kernel<T, DP, KV>, dim3(sms), BWD_THREADS, Bwd<DP>::SMEM, s, p, w, maps));
-    TIGA_CUDA_TRY(launch_after(attention_sum_kernel<T, DP, KV>, dim3(sms, SUM_Y), SUM_WARPS * 32, 0, s, p, w));
-    return TIGA_OK;
-}
 
 template <typename T, int DP>
 static tiga_status launch_backward(AttnParams p, const BwdWork& w, cudaStream_t s) {
@@ -587,14 +596,23 @@ static tiga_status launch_backward(AttnParams p, const BwdWork& w, cudaStream_t 
     make_tile_maps(&p, operand_type<T>() == 1, &maps);
     const int sms = attention_grid();
     if (sms <= 0) return TIGA_ERR_CUDA;
-    backward_plan_kernel<<<counted(2), PLAN_THREADS, 0, s>>>(p, w);
-    const long long rows = (long long)p.n_q * p.heads + (long long)p.n_kv * p.kv_heads;
-    const long long grid = (rows * (DP / 8) + PREP_THREADS - 1) / PREP_THREADS;
-    TIGA_CUDA_TRY(launch_after(attention_prepare_kernel<T, DP / 8>, dim3((unsigned)(grid < 8 * sms ? grid : 8 * sms)), PREP_THREADS, 0, s, p, w));
-    tiga_status st = TIGA_OK;
-    if ((p.gk || p.gv) && p.n_kv) st = launch_side<T, DP, true>(p, w, maps, sms, s);
-    if (st == TIGA_OK && p.gq && p.n_q) st = launch_side<T, DP, false>(p, w, maps, sms, s);
-    return st == TIGA_OK ? launch_status() : st;
+    const int kv_blocks = (p.gk || p.gv) && p.n_kv ? sms : 0, q_blocks = p.gq && p.n_q ? sms : 0;
+    if (kv_blocks + q_blocks == 0) return TIGA_OK;
+    TIGA_CUDA_TRY(cudaFuncSetAttribute(attention_backward_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, Bwd<DP>::SMEM));
+    const long long rows = (long long)p.n_q * p.heads + (operand_type<T>() == 0 ? (long long)p.n_kv * p.kv_heads : 0);
+    long long grid = (rows * (DP / 8) + PREP_THREADS - 1) / PREP_THREADS;
+    grid = grid < 1 ? 1 : grid < 8 * sms ? grid : 8 * sms;
+    // Little work is prepared by one block, which needs no cleared words to put its maxima into: a launch less (about 8 us of the
+    // host's time against 1 us for each 256 rows of 64 features).
+    if (grid <= PREP_ALONE) grid = 1;
+    const bool plan = w.kv_start_unit || (operand_type<T>() == 0 && grid > 1);
+    if (plan) {
+        backward_plan_kernel<<<counted(2), PLAN_THREADS, 0, s>>>(p, w);
+        TIGA_CUDA_TRY(launch_after(attention_prepare_kernel<T, DP / 8>, dim3((unsigned)grid), PREP_THREADS, 0, s, p, w));
+    } else attention_prepare_kernel<T, DP / 8><<<counted((unsigned)grid), PREP_THREADS, 0, s>>>(p, w);
+    TIGA_CUDA_TRY(launch_after(attention_backward_kernel<T, DP>, dim3(kv_blocks + q_blocks), BWD_THREADS, Bwd<DP>::SMEM, s, p, w, maps, kv_blocks));
+    TIGA_CUDA_TRY(launch_after(attention_sum_kernel<T, DP>, dim3(kv_blocks + q_blocks, SUM_Y), SUM_WARPS * 32, 0, s, p, w, kv_blocks));
+    return launch_status();
 }
 
 tiga_status attention_backward(const AttnParams& p, bool bf16, void* ws, cudaStream_t s) {
