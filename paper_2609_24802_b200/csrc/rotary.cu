@@ -71,7 +71,7 @@ __device__ __forceinline__ int last_start_at_or_before(const int32_t* start, int
 // of what is copied.  Many threads hide the
 // loads, not batches of them: two and four units a thread at a time cost registers and 14 and 67 %.
 template <typename T, int VEC, bool ALIGNED, bool APPEND>
-__global__ void __launch_bounds__(ROT_THREADS) rotary_kernel(const RotParams p) {
+__global__ void __launch_bounds__(ROT_THREADS, APPEND ? 6 : 8) rotary_kernel(const RotParams p) {
     extern __shared__ float2 turn[];            // [rows][pairs]: cosine, sine
     __shared__ long long position[ROT_ROWS], target[ROT_ROWS];      // target: the row's offset in y, -1: it goes nowhere
     const long long first_row = (long long)blockIdx.x * p.rows;
