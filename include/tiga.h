@@ -374,7 +374,9 @@ tiga_status tiga_apply_csr_attention(const tiga_csr* g, const float* q, const fl
  * lengths.  Bounds are clamped to the arrays, so no bound leads outside of them.  A row that reads no key yields the zero vector
  * and lse = -inf, and zero gradients.  Rows outside of every segment (in front of start[0], behind start[n_seg]) are not
  * touched, in outputs and gradients alike.  What lies in keys that no row of the segment reads (masked keys, places behind
- * the last key of a page), NaN and infinities included, has no influence.  No atomics on results: they are reproducible. */
+ * the last key of a page), NaN and infinities included, has no influence.  No atomics on results: they are reproducible.
+ * A workspace belongs to one call at a time.  A block that waits about two seconds for one of its own copies or products in vain
+ * leaves NaN in the rows that it did not finish. */
 typedef struct { int64_t row, head; } tiga_stride;
 
 typedef struct {
@@ -392,7 +394,8 @@ typedef struct {
     const int32_t* kv_start;    /* device, int32 [n_seg + 1], ascending */
     const uint8_t* kv_mask;     /* device [n_kv], 0: the key is not read; NULL: all are */
     int64_t n_seg;
-    int64_t n_q, n_kv;          /* rows of q / out, and of key / value; below 2^31 */
+    int64_t n_q, n_kv;          /* rows of q / out, and of key / value; heads / kv_heads * n_q and n_kv at most
+                                 * 2^31 - 2^16 (TIGA_ERR_UNSUPPORTED above) */
 } tiga_dense;
 
 /* out [n_q, heads, D], lse [n_q, heads] or NULL.  ws: tiga_dense_attention_workspace_bytes(g, h, 0) bytes. */
@@ -424,14 +427,15 @@ typedef struct {
     const int32_t* kv_len;      /* device, int32 [n_seg]: tokens in the cache, those of the current chunk included */
     int64_t n_seg, n_pages, page_size;
     int64_t table_stride;       /* entries from one sequence's row to the next */
-    int64_t max_pages;          /* entries of a sequence's row; positions from max_pages * page_size on do not exist */
+    int64_t max_pages;          /* entries of a sequence's row; positions from max_pages * page_size on (and from
+                                 * 2^31 - 2^16 on) do not exist */
     int64_t page_stride, slot_stride, head_stride;
 } tiga_pages;
 
 /* Attention of a chunk of new tokens over a paged cache (the triangular relation, its sources in pages): rows
  * [q_start[s], q_start[s+1]) are the last n tokens of sequence s, their keys and values are in the cache already.
  * Token t of them reads the positions up to kv_len[s] - n + t (causal != 0), or all kv_len[s].
- *   q [n_q, heads, D] strided (h->q);  out [n_q, heads, D];  lse [n_q, heads] or NULL;  n_q below 2^31.
+ *   q [n_q, heads, D] strided (h->q);  out [n_q, heads, D];  lse [n_q, heads] or NULL;  heads / kv_heads * n_q at most 2^31 - 2^16.
  *   ws: tiga_paged_attention_workspace_bytes(c, h, n_q) bytes. */
 size_t tiga_paged_attention_workspace_bytes(const tiga_pages* c, const tiga_heads* h, int64_t n_q);
 tiga_status tiga_apply_paged_attention(const tiga_pages* c, const tiga_heads* h, const void* q, const int32_t* q_start, int64_t n_q,

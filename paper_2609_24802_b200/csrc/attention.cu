@@ -78,13 +78,13 @@ static AttnParams heads_params(const tiga_heads* h) {
 }
 
 // row numbers of a head group's packed rows (row * group + member) are 32-bit, and so are the counts of tiles
-static bool too_many_rows(int64_t n, const tiga_heads* h) { return n * (h->heads / h->kv_heads) > 0x7fff0000LL; }
+static bool too_many_rows(int64_t n, const tiga_heads* h) { return n * (h->heads / h->kv_heads) > MOST_ROWS; }
 
 static tiga_status dense_check(const tiga_dense* g, const tiga_heads* h, AttnParams* p) {
     tiga_status st = attention_heads_check(h);
     if (st != TIGA_OK) return st;
     if (!g || g->n_seg < 0 || g->n_q < 0 || g->n_kv < 0) return TIGA_ERR_INVALID_ARG;
-    if (g->n_seg > (1 << 24) || g->n_q > 0x7fffffffLL || g->n_kv > 0x7fffffffLL || too_many_rows(g->n_q, h)) return TIGA_ERR_UNSUPPORTED;
+    if (g->n_seg > (1 << 24) || g->n_q > 0x7fffffffLL || g->n_kv > MOST_ROWS || too_many_rows(g->n_q, h)) return TIGA_ERR_UNSUPPORTED;
     *p = heads_params(h);
     p->q_start = g->q_start; p->kv_start = g->kv_start; p->mask = g->kv_mask;
     p->n_seg = (int)g->n_seg; p->n_q = (int)g->n_q; p->n_kv = (int)g->n_kv;

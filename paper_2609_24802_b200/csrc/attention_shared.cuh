@@ -25,6 +25,9 @@ struct AttnParams {
 // A segment's rows [q0, q0 + nq) and its keys [k0, k0 + nk) (paged: k0 = 0), bounds clamped to the arrays.
 struct Segment { int q0, nq, k0, nk; };
 
+// Rows and positions end here, so that a tile's last row number fits 32 bits.
+constexpr long long MOST_ROWS = 0x7fff0000LL;
+
 __device__ __forceinline__ int clamp_to(int v, int hi) { return min(max(v, 0), hi); }
 
 __device__ __forceinline__ Segment segment_of(const AttnParams& p, int s) {
@@ -33,7 +36,7 @@ __device__ __forceinline__ Segment segment_of(const AttnParams& p, int s) {
     g.nq = max(clamp_to(p.q_start[s + 1], p.n_q) - g.q0, 0);
     if (p.table) {
         g.k0 = 0;
-        g.nk = (int)min((long long)max(p.kv_len[s], 0), p.max_pages * p.page_size);
+        g.nk = (int)min(min((long long)max(p.kv_len[s], 0), p.max_pages * p.page_size), MOST_ROWS);
     } else {
         g.k0 = clamp_to(p.kv_start[s], p.n_kv);
         g.nk = max(clamp_to(p.kv_start[s + 1], p.n_kv) - g.k0, 0);

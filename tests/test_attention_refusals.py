@@ -62,6 +62,7 @@ def test_dense_arguments(api):
     assert forward(api, dense(api, n_q=-1), h) == 1 and forward(api, dense(api, n_seg=-1), h) == 1
     assert forward(api, dense(api, n_q=1 << 31), h) == 2 and forward(api, dense(api, n_seg=1 << 25), h) == 2
     assert forward(api, dense(api, n_q=1 << 30), heads(api, h=64)) == 2                  # packed rows of a group beyond 32 bits
+    assert forward(api, dense(api, n_kv=(1 << 31) - 100), h) == 2                         # a tile's last row would not fit 32 bits
     assert forward(api, dense(api, q=0), h) == 1 and forward(api, dense(api, kv=258), h) == 1
     for name in ("q", "k", "v", "out"):
         assert forward(api, dense(api), h, **{name: None}) == 1 and forward(api, dense(api), h, **{name: 264}) == 1

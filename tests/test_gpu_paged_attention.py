@@ -119,6 +119,12 @@ def test_many_splits_and_batches(tiga):
     check(tiga, make([600, 1, 1, 250], [1500, 2000, 3, 250], 8, 4, 128, F16, 32, seed=8))
 
 
+def test_long_chunks_whose_tiles_are_counted_by_a_kernel_of_their_own(tiga):
+    """More than 64 tiles of 256 packed rows under the triangle: the workspace also holds the counts."""
+    check(tiga, make([4200, 90], [4300, 90], 4, 1, 64, BF16, 64, seed=15))
+    check(tiga, make([5000], [5000], 4, 1, 32, F16, 16, seed=16))
+
+
 def test_missing_pages_are_read_as_masked_keys(tiga):
     c = make([1, 30], [200, 150], 4, 2, 64, BF16, 16, seed=9)
     c["table"][0, 3], c["table"][1, 0], c["table"][1, 1] = -1, 2 ** 31 - 1, c["key_pages"].shape[0]
