@@ -13,6 +13,8 @@ namespace tiga {
 // P lies over S and dS over dP in 16 bits (tensor memory: 128 + 128 + 2 * 128 columns, all there is).  The products run in two
 // streams that take turns: while the threads turn S into P, dP and the last step's grad_key are formed; while they turn dP into dS,
 // grad_value and the next step's S.
+// A step of 128 lasts about 3480 cycles (products 2048 or 1536, exponentials 1024, the threads' two turns 2200): 4 segments of 4096 rows
+// and keys, 16/4 heads of 128, bf16: 1.70 ms for both passes.
 // fp16: P carries 2^14 and dS a power of two from the largest norms of the rows of grad_out and value, which bound |dP - delta|: the
 // largest value cannot overflow, the smallest keep as many digits as there are.
 constexpr int BWD_WEIGHT_WARPS = 16, BWD_PRODUCER = BWD_WEIGHT_WARPS, BWD_MMA = BWD_PRODUCER + 4, BWD_WALKER = BWD_MMA + 1;
@@ -602,7 +604,7 @@ static tiga_status launch_backward(AttnParams p, const BwdWork& w, cudaStream_t 
     const long long rows = (long long)p.n_q * p.heads + (operand_type<T>() == 0 ? (long long)p.n_kv * p.kv_heads : 0);
     long long grid = (rows * (DP / 8) + PREP_THREADS - 1) / PREP_THREADS;
     grid = grid < 1 ? 1 : grid < 8 * sms ? grid : 8 * sms;
-    // Little work is prepared by one block, which needs no cleared words to put its maxima into: a launch less (about 8 us of the
+    // Little work is prepared by one block, which needs no cleared words to put its maxima into: a launch less (about 5 us of the
     // host's time against 1 us for each 256 rows of 64 features).
     if (grid <= PREP_ALONE) grid = 1;
     const bool plan = w.kv_start_unit || (operand_type<T>() == 0 && grid > 1);
