@@ -31,7 +31,7 @@ template <int DP> struct Bwd {
     // entries do.  Of eight it is Y2 of step n - 4, so step n - 4 may still read: eight do.
     static constexpr int AUX = DP == 128 ? 2 : 8;
     static constexpr int CONTROL = (2 + SLOTS) * TILE;
-    static constexpr int SMEM = CONTROL + (DP == 128 ? 3072 : 10240);
+    static constexpr int SMEM = CONTROL + (DP == 128 ? 3 : 10) * 1024;
 };
 
 template <int AUX> struct BwdControl {
@@ -41,7 +41,7 @@ template <int AUX> struct BwdControl {
     alignas(16) float minus_lse[AUX][BWD_STEP], minus_delta[AUX][BWD_STEP];     // keys stationary: of the step's rows
     uint32_t mask[AUX][4];                                                      // queries stationary: the step's keys
 };
-static_assert(sizeof(BwdControl<2>) <= 3072 && sizeof(BwdControl<8>) <= 10240, "control block");
+static_assert(sizeof(BwdControl<2>) <= 3 * 1024 && sizeof(BwdControl<8>) <= 10 * 1024, "control block");
 
 struct BwdWork {
     long long *kv_start_unit, *q_start_unit;        // NULL: the blocks count for themselves

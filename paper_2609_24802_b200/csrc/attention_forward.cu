@@ -29,7 +29,7 @@ template <int DP> struct Fwd {
     static constexpr int TILE = 128 * DP * 2;
     static constexpr int SLOTS = DP == 128 ? 5 : 10;
     static constexpr int CONTROL = 2 * TILE + SLOTS * TILE;
-    static constexpr int SMEM = CONTROL + 3072;
+    static constexpr int SMEM = CONTROL + 3 * 1024;
 };
 
 struct FwdControl {
@@ -38,7 +38,7 @@ struct FwdControl {
     uint32_t tmem, abort_word, never, mask[MASK_RING][4];
     float share[2][2][128];             // what a row's threads tell each other
 };
-static_assert(sizeof(FwdControl) <= 3072, "control block");
+static_assert(sizeof(FwdControl) <= 3 * 1024, "control block");
 
 struct FwdWork {
     long long* unit_start;          // NULL: the blocks count for themselves
@@ -206,9 +206,8 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
                 }
                 if (two && more_keys) scores(1, 1, k_next);
                 if (more_keys) release(k_next);
+                if (i + ahead == n - 1 && elected()) mma_commit(bar(ctl.q_empty));      // the last scores: the next item's queries may come
             }
-            if (!ok) continue;
-            if (elected()) mma_commit(bar(ctl.q_empty));
             tile0 += 2 * n;
         }
         if (elected()) mma_commit(bar(ctl.drain));

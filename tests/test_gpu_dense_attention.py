@@ -227,6 +227,27 @@ def test_only_the_wanted_gradients(tiga):
     assert torch.equal(gv, want["grad_value"])
 
 
+def test_nothing_on_one_side(tiga):
+    """No rows at all, no keys at all, no segments: zeros where something is left to write."""
+    c = case([0, 0], [5, 3], 2, 2, 64, F16, seed=32)
+    got = run(tiga, c)
+    assert torch.all(got["grad_key"] == 0) and torch.all(got["grad_value"] == 0) and got["out"].shape == (0, 2, 64)
+    c = case([5], [0], 2, 2, 64, BF16, seed=33)
+    got = run(tiga, c)
+    assert torch.all(got["out"] == 0) and torch.all(got["lse"] == -float("inf")) and torch.all(got["grad_q"] == 0)
+    g = tiga.DenseRelation(starts([]), starts([]))
+    out = torch.full_like(c["q"], 7.0)
+    tiga.tiga_apply_dense_attention(g, c["q"], c["k"], c["v"], 1.0, out=out)
+    assert torch.all(out == 7)
+
+
+def test_without_lse(tiga):
+    c = case([70, 300], [90, 513], 4, 2, 64, BF16, seed=34)
+    g = tiga.DenseRelation(starts(c["q_len"]), starts(c["kv_len"]))
+    out, lse, _ = tiga.tiga_apply_dense_attention(g, c["q"], c["k"], c["v"], c["scale"], want_lse=False)
+    assert lse is None and torch.equal(out, run(tiga, c, backward=False)["out"])
+
+
 def test_graph_replays_with_other_lengths(tiga):
     """Bounds are read on the device: one captured step serves other lengths and other data."""
     a, b = case([60, 70], [200, 150], 4, 2, 64, BF16, seed=26), case([100, 30], [9, 341], 4, 2, 64, BF16, seed=27)

@@ -125,6 +125,28 @@ def test_long_chunks_whose_tiles_are_counted_by_a_kernel_of_their_own(tiga):
     check(tiga, make([5000], [5000], 4, 1, 32, F16, 16, seed=16))
 
 
+def test_more_sequences_than_the_blocks_count_themselves(tiga):
+    check(tiga, make([1 + i % 3 for i in range(300)], [4 + (i * 37) % 400 for i in range(300)], 4, 2, 64, BF16, 16, seed=17))
+
+
+def test_on_another_stream(tiga):
+    """Rotate, append and attend on a stream that is not the current one; outputs and workspaces are allocated for it."""
+    c = make([3, 40], [100, 77], 4, 2, 64, F16, 16, seed=18)
+    want = run(tiga, c)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    cache = tiga.PagedCache(c["key_pages"], c["value_pages"], c["table"], c["lens"])
+    freq, _ = tiga.tiga_rotary_frequencies(64)
+    rot = tiga.Rotary(freq.cuda())
+    side.wait_stream(torch.cuda.current_stream())
+    start = starts(c["q_len"])
+    side.wait_stream(torch.cuda.current_stream())
+    same = tiga.tiga_apply_rotary(rot, c["q"], torch.zeros(43, dtype=torch.int64, device="cuda"), stream=side)
+    out, lse, ws = tiga.tiga_apply_paged_attention(cache, same, start, c["scale"], stream=side)
+    side.synchronize()
+    assert torch.equal(same, c["q"]) and torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
 def test_missing_pages_are_read_as_masked_keys(tiga):
     c = make([1, 30], [200, 150], 4, 2, 64, BF16, 16, seed=9)
     c["table"][0, 3], c["table"][1, 0], c["table"][1, 1] = -1, 2 ** 31 - 1, c["key_pages"].shape[0]
