@@ -360,32 +360,33 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
             const PackedRow pr = packed_row(p, e.segment(), e.h, e.t * FWD_ROWS + tile_row);
             const long long out_row = (long long)pr.row * p.heads + pr.head;
             const float finish = l > 0.f || l != l ? 1.f / l : 0.f;
-            const int c0 = two ? y * (DP / 32) : (2 * x + y) * (DP / 64), c1 = c0 + (two ? DP / 32 : DP / 64);      // pieces of 16 features
+            // this thread's half of the row's features, or its quarter of both states, 16 at a time
+            const int f0 = two ? y * (DP / 2) : (2 * x + y) * (DP / 4), f1 = f0 + (two ? DP / 2 : DP / 4);
             if (warp_on)
-                for (int c = c0; c < c1; ++c) {
+#pragma unroll 1
+                for (int f = f0; f < f1; f += 16) {
                     uint32_t v[16], u[16];
-                    tmem_ld16(O + (two ? DP * x : 0) + 16 * c, v);
-                    tmem_ld16(O + DP + 16 * c, u);         // (read in short tiles with a second state only)
+                    tmem_ld16(O + (two ? DP * x : 0) + f, v);
+                    tmem_ld16(O + DP + f, u);           // (wanted in short tiles with a second state only)
                     tmem_wait_ld(v);
                     tmem_wait_ld(u);
                     if (!two)
 #pragma unroll
                         for (int k = 0; k < 16; ++k)
                             v[k] = __float_as_uint(__uint_as_float(v[k]) * w0 + (made1 ? __uint_as_float(u[k]) * w1 : 0.f));
-                    if (!valid) continue;
                     if (whole_tile) {
-                        uint4* out = reinterpret_cast<uint4*>((T*)p.out + out_row * p.D + 16 * c);
+                        uint4 o[2];
 #pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            if (16 * c + 8 * k >= p.D) continue;
-                            uint32_t o[4];
+                        for (int c = 0; c < 2; ++c) {
+                            uint32_t h[4];
 #pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                o[e] = finish == 0.f ? 0u : pack_half<T>(__uint_as_float(v[8 * k + 2 * e]) * finish, __uint_as_float(v[8 * k + 2 * e + 1]) * finish);
-                            out[k] = make_uint4(o[0], o[1], o[2], o[3]);
+                            for (int k = 0; k < 4; ++k)
+                                h[k] = finish == 0.f ? 0u : pack_half<T>(__uint_as_float(v[8 * c + 2 * k]) * finish, __uint_as_float(v[8 * c + 2 * k + 1]) * finish);
+                            o[c] = make_uint4(h[0], h[1], h[2], h[3]);
                         }
-                    } else {
-                        uint4* out = reinterpret_cast<uint4*>(w.part_o + part * DP + 16 * c);
+                        store_rows<2>(o, (T*)p.out + out_row * p.D + f, valid, (p.D - f) / 8);
+                    } else if (valid) {
+                        uint4* out = reinterpret_cast<uint4*>(w.part_o + part * DP + f);
 #pragma unroll
                         for (int k = 0; k < 4; ++k) out[k] = make_uint4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
                     }
