@@ -607,14 +607,18 @@ def _on(like, stream):
             raise ValueError("the stream belongs to another device than the arrays")
         return torch.cuda.stream(stream)
     current = _current_device() if _current_device else torch.cuda.current_device()
-    return _NO_CONTEXT if like.device.index == current else torch.cuda.device(like.device)
+    return _NO_CONTEXT if like.get_device() == current else torch.cuda.device(like.device)
 
 
 def _same(like, *arrays):
-    device = like.device
+    device = like.get_device()         # (-1: on the host)
     for t in arrays:
-        if t is not None and t.device != device:
+        if t is not None and t.get_device() != device:
             raise ValueError("all arrays of a call must lie on one device")
+
+
+def _scratch(nbytes, like):
+    return like.new_empty(nbytes if nbytes > 256 else 256, dtype=torch.uint8)
 
 
 def _ints(t, n, name):
@@ -647,6 +651,8 @@ def _dense_out(t, shape, dtype, name):
 _HEADS_BYTES, _HEADS_OF, _NO_STRIDE = struct.Struct("=4if4x8q"), _Heads.from_buffer_copy, (0, 0)
 _DENSE_BYTES, _DENSE_OF = struct.Struct("=6q"), _Dense.from_buffer_copy
 _STRIDE_BYTES, _STRIDE_OF = struct.Struct("=2q"), _Stride.from_buffer_copy
+_PAGES_BYTES, _PAGES_OF = struct.Struct("=12q"), _Pages.from_buffer_copy
+assert _PAGES_BYTES.size == ctypes.sizeof(_Pages)
 assert _HEADS_BYTES.size == ctypes.sizeof(_Heads) and _DENSE_BYTES.size == ctypes.sizeof(_Dense)
 
 
@@ -713,7 +719,7 @@ def tiga_apply_dense_attention(g: DenseRelation, q, key, value, scale: float, ou
             lse = q.new_empty(q.shape[:2], dtype=torch.float32)
         _same(q, out, lse, ws)
         if ws is None:
-            ws = _ws(_L.tiga_dense_attention_workspace_bytes(ctypes.byref(c), ctypes.byref(h), 0), q)
+            ws = _scratch(_L.tiga_dense_attention_workspace_bytes(ctypes.byref(c), ctypes.byref(h), 0), q)
         _ok(_L.tiga_apply_dense_attention(ctypes.byref(c), ctypes.byref(h), q.data_ptr(), key.data_ptr(), value.data_ptr(),
                                           _dense_out(out, q.shape, q.dtype, "out"),
                                           None if lse is None else _dense_out(lse, q.shape[:2], torch.float32, "lse"),
@@ -735,7 +741,7 @@ def tiga_apply_dense_attention_backward(g: DenseRelation, q, key, value, out, ls
             grad_value = q.new_empty(key.shape)
         _same(q, out, lse, grad_q, grad_key, grad_value, ws)
         if ws is None:
-            ws = _ws(_L.tiga_dense_attention_workspace_bytes(ctypes.byref(c), ctypes.byref(h), 1), q)
+            ws = _scratch(_L.tiga_dense_attention_workspace_bytes(ctypes.byref(c), ctypes.byref(h), 1), q)
         grads = [None if t is None else _dense_out(t, like.shape, q.dtype, name)
                  for t, like, name in ((grad_q, q, "grad_q"), (grad_key, key, "grad_key"), (grad_value, key, "grad_value"))]
         _ok(_L.tiga_apply_dense_attention_backward(ctypes.byref(c), ctypes.byref(h), q.data_ptr(), key.data_ptr(), value.data_ptr(),
@@ -752,16 +758,19 @@ class PagedCache:
     def __init__(self, key, value, table, kv_len):
         if key.dim() != 4 or key.shape != value.shape or key.dtype != value.dtype or key.dtype not in _HALF:
             raise ValueError("key and value must be fp16 or bf16 arrays [n_pages, page_size, kv_heads, D] of one shape")
-        step = [_step(key, d) for d in range(3)]
-        if step != [_step(value, d) for d in range(3)] or (key.shape[3] > 1 and (key.stride(3) != 1 or value.stride(3) != 1)):
+        shape, steps = key.shape, key.stride()
+        step = [s if n > 1 else 0 for s, n in zip(steps, shape)]                 # (the stride of a single entry means nothing)
+        if (steps != value.stride() and step != [s if n > 1 else 0 for s, n in zip(value.stride(), shape)]) or step[3] > 1:
             raise ValueError("key and value must have the same strides and contiguous features")
-        if table.dtype != torch.int32 or table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
+        if table.dtype is not torch.int32 or table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
             raise ValueError("table must be an int32 array [n_seg, max_pages] with contiguous rows")
-        _ints(kv_len, table.shape[0], "kv_len")
+        n_seg, max_pages = table.shape
+        _ints(kv_len, n_seg, "kv_len")
         _same(key, value, table, kv_len)
         self.key, self.value, self.table, self.kv_len = key, value, table, kv_len
-        self.c = _Pages(key.data_ptr(), value.data_ptr(), table.data_ptr(), kv_len.data_ptr(), table.shape[0], key.shape[0], key.shape[1],
-                        _step(table, 0), table.shape[1], *step)
+        self.n_seg = n_seg
+        self.c = _PAGES_OF(_PAGES_BYTES.pack(key.data_ptr(), value.data_ptr(), table.data_ptr(), kv_len.data_ptr(), n_seg, shape[0], shape[1],
+                                             _step(table, 0), max_pages, step[0], step[1], step[2]))
         self.ref = ctypes.byref(self.c)
 
 
@@ -782,13 +791,13 @@ def tiga_apply_paged_attention(cache: PagedCache, q, q_start, scale: float, caus
     with _on(q, stream):
         h = _paged_heads(cache, q, scale)
         _same(q, q_start, out, lse, ws)
-        start = _ints(q_start, cache.c.n_seg + 1, "q_start")
+        start = _ints(q_start, cache.n_seg + 1, "q_start")
         if out is None:
             out = q.new_empty(q.shape)
         if want_lse and lse is None:
             lse = q.new_empty(q.shape[:2], dtype=torch.float32)
         if ws is None:
-            ws = _ws(_L.tiga_paged_attention_workspace_bytes(cache.ref, ctypes.byref(h), q.shape[0]), q)
+            ws = _scratch(_L.tiga_paged_attention_workspace_bytes(cache.ref, ctypes.byref(h), q.shape[0]), q)
         _ok(_L.tiga_apply_paged_attention(cache.ref, ctypes.byref(h), q.data_ptr(), start, q.shape[0], int(bool(causal)),
                                           _dense_out(out, q.shape, q.dtype, "out"),
                                           None if lse is None else _dense_out(lse, q.shape[:2], torch.float32, "lse"),
@@ -825,13 +834,14 @@ def tiga_apply_rotary(rotary: Rotary, x, positions, out=None, inverse=False, str
         dt = _type_of(x, _REAL)
         if positions.dtype not in (torch.int32, torch.int64) or positions.shape != x.shape[:1] or not positions.is_contiguous():
             raise ValueError("positions must be a contiguous int32 or int64 array with one entry per row")
+        shape, dtype = x.shape, x.dtype
         if out is None:
-            out = x.new_empty(x.shape)
+            out = x.new_empty(shape)
         _same(x, positions, out, rotary.freq)
-        xs, ys = (_STRIDE_OF(_STRIDE_BYTES.pack(*_stride_of(t, x.shape, x.dtype, n))) for t, n in ((x, "x"), (out, "out")))
-        _ok(_L.tiga_apply_rotary(rotary.ref, x.data_ptr(), ctypes.byref(xs), out.data_ptr(), ctypes.byref(ys), dt, x.shape[0], x.shape[1],
-                                 x.shape[2], positions.data_ptr(), I32 if positions.dtype == torch.int32 else I64, int(bool(inverse)),
-                                 _stream(stream)), "tiga_apply_rotary")
+        xs = _STRIDE_OF(_STRIDE_BYTES.pack(*_stride_of(x, shape, dtype, "x")))
+        ys = _STRIDE_OF(_STRIDE_BYTES.pack(*_stride_of(out, shape, dtype, "out")))
+        _ok(_L.tiga_apply_rotary(rotary.ref, x.data_ptr(), ctypes.byref(xs), out.data_ptr(), ctypes.byref(ys), dt, *shape, positions.data_ptr(),
+                                 I32 if positions.dtype is torch.int32 else I64, 1 if inverse else 0, _stream(stream)), "tiga_apply_rotary")
     return out
 
 
@@ -845,5 +855,5 @@ def tiga_paged_append(cache: PagedCache, key, value, start, rotary: Rotary = Non
         _same(key, value, start, cache.key, None if rotary is None else rotary.freq)
         n, heads, D = key.shape
         h = _heads_of(dt, heads, heads, D, 1.0, _NO_STRIDE, _stride_of(key, key.shape, key.dtype, "key"), _stride_of(value, key.shape, key.dtype, "value"))
-        _ok(_L.tiga_paged_append(cache.ref, ctypes.byref(h), key.data_ptr(), value.data_ptr(), _ints(start, cache.c.n_seg + 1, "start"), n,
+        _ok(_L.tiga_paged_append(cache.ref, ctypes.byref(h), key.data_ptr(), value.data_ptr(), _ints(start, cache.n_seg + 1, "start"), n,
                                  None if rotary is None else rotary.ref, _stream(stream)), "tiga_paged_append")

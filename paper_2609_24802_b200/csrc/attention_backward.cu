@@ -445,7 +445,7 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
             // keys stationary: warpgroups 0 and 1 write grad_key, 2 and 3 grad_value, a half of the features each; queries: a quarter each
             const bool whole_tile = n == item.steps;
             const int rows = KV ? w.kv_rows : w.q_rows;
-            constexpr int SIDES = KV ? 2 : 1, MINE = DP * SIDES / 4, AT_ONCE = MINE < 32 ? MINE : 32;     // this thread's features of a row
+            constexpr int SIDES = KV ? 2 : 1, MINE = DP * SIDES / 4;        // this thread's features of a row
             const int side = KV ? x / 2 : 0, f0 = (KV ? x % 2 : x) * MINE;
             const uint32_t acc = (side ? acc2 : acc1) + lanes;
             const float finish = side ? (F16 ? 0x1p-14f : 1.f) : p.scale / factor;
@@ -453,27 +453,27 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
             float* part = (KV ? w.kv_part : w.q_part) + ((((2LL * block + (item.i0 == 0)) * rows + row) * SIDES) + side) * DP;
             if (warp_on)
 #pragma unroll 1
-                for (int f = f0; f < f0 + MINE; f += AT_ONCE) {
-                    uint32_t v[AT_ONCE];
-                    if constexpr (AT_ONCE == 32) tmem_ld32(acc + f, v); else tmem_ld16(acc + f, v);
+                for (int f = f0; f < f0 + MINE; f += 16) {
+                    uint32_t v[16];
+                    tmem_ld16(acc + f, v);
                     tmem_wait_ld(v);
                     if (!ok)
 #pragma unroll
-                        for (int k = 0; k < AT_ONCE; ++k) v[k] = 0x7fffffffu;
+                        for (int k = 0; k < 16; ++k) v[k] = 0x7fffffffu;
                     if (whole_tile) {
-                        uint4 o[AT_ONCE / 8];
+                        uint4 o[2];
 #pragma unroll
-                        for (int c = 0; c < AT_ONCE / 8; ++c) {
+                        for (int c = 0; c < 2; ++c) {
                             uint32_t h[4];
 #pragma unroll
                             for (int k = 0; k < 4; ++k)
                                 h[k] = masked && ok ? 0u : pack_half<T>(__uint_as_float(v[8 * c + 2 * k]) * finish, __uint_as_float(v[8 * c + 2 * k + 1]) * finish);
                             o[c] = make_uint4(h[0], h[1], h[2], h[3]);
                         }
-                        store_rows<AT_ONCE / 8>(o, out + out_row * p.D + f, valid && out, (p.D - f) / 8);
+                        store_rows<2>(o, out + out_row * p.D + f, valid && out, (p.D - f) / 8);
                     } else if (valid) {
 #pragma unroll
-                        for (int k = 0; k < AT_ONCE / 4; ++k) reinterpret_cast<uint4*>(part + f)[k] = make_uint4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+                        for (int k = 0; k < 4; ++k) reinterpret_cast<uint4*>(part + f)[k] = make_uint4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
                     }
                 }
             tmem_fence_before();
