@@ -18,7 +18,7 @@ namespace tiga {
 // fp16: P carries 2^14 and dS a power of two from the largest norms of the rows of grad_out and value, which bound |dP - delta|: the
 // largest value cannot overflow, the smallest keep as many digits as there are.
 constexpr int BWD_WEIGHT_WARPS = 16, BWD_PRODUCER = BWD_WEIGHT_WARPS, BWD_MMA = BWD_PRODUCER + 4, BWD_WALKER = BWD_MMA + 1;
-constexpr int BWD_THREADS = 32 * (BWD_WALKER + 1), BWD_ROWS = 128, BWD_STEP = 128, BWD_LEAST = 2;
+constexpr int BWD_THREADS = 32 * (BWD_WALKER + 1), BWD_ROWS = 128, BWD_STEP = 128;
 typedef Cut<BWD_ROWS, BWD_STEP, true> KvCut;
 typedef Cut<BWD_ROWS, BWD_STEP, false> QCut;
 template <bool KV> struct CutOf { typedef QCut type; };
@@ -60,7 +60,18 @@ __device__ __forceinline__ float gradient_factor(const uint32_t* norms) {
 }
 
 // delta, lse in log2, and the norms behind gradient_factor: a row by LANES threads, 8 features each.  Bound by memory: grad_out and out
-// are read once (fp16: value too).
+// are read once (fp16: value too).  Of few keys delta is summed as sum p dP: out is then as large as the values, and its rounding would
+// show in dP - delta (over n keys it is smaller by the root of n).
+constexpr int FEW_KEYS = 16;
+template <typename T>
+__device__ __forceinline__ float dot8(const uint4& a, const uint4& b) {
+    const T* x = reinterpret_cast<const T*>(&a);
+    const T* y = reinterpret_cast<const T*>(&b);
+    float d = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) d += Half<T>::to(x[e]) * Half<T>::to(y[e]);
+    return d;
+}
 constexpr int PREP_THREADS = 256, PREP_ALONE = 16;     // blocks of work that one block does alone
 template <typename T, int LANES>
 __global__ void __launch_bounds__(PREP_THREADS) attention_prepare_kernel(const AttnParams p, const BwdWork w) {
@@ -77,6 +88,10 @@ __global__ void __launch_bounds__(PREP_THREADS) attention_prepare_kernel(const A
         for (int d = LANES / 2; d; d >>= 1) v += __shfl_xor_sync(~0u, v, d);
         return v;
     };
+    // are there such segments at all?  (Looking for every row's segment cost 20 us of 262144 rows.)
+    bool few_here = false;
+    for (int s = threadIdx.x; s < p.n_seg; s += PREP_THREADS) few_here = few_here || segment_of(p, s).nk <= FEW_KEYS;
+    const bool any_few = __syncthreads_or(few_here);
     float top_go = 0.f, top_v = 0.f;
     for (long long r0 = (long long)blockIdx.x * ROWS; r0 < q_rows; r0 += stride) {      // whole warps stay together
         const long long r = r0 + threadIdx.x / LANES, row = quotient(r, p.heads), at = (q_first + row) * p.heads + (r - row * p.heads);
@@ -89,17 +104,32 @@ __global__ void __launch_bounds__(PREP_THREADS) attention_prepare_kernel(const A
             }
             lse = p.lse_in[at];
         }
-        const T* ea = reinterpret_cast<const T*>(&a);
-        const T* eb = reinterpret_cast<const T*>(&b);
-        float dot = 0.f, norm = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float x = Half<T>::to(ea[e]);
-            dot += x * Half<T>::to(eb[e]);
-            if (NORMS) norm += x * x;
+        float dot = fold(dot8<T>(a, b));
+        const float norm = NORMS ? fold(dot8<T>(a, a)) : 0.f;
+        Segment g{};
+        int s = -1, few = 0;
+        if (any_few && r < q_rows && lse != -INFINITY && (s = segment_of_row(p.q_start, p.n_seg, p.n_q, (int)(q_first + row))) >= 0) {
+            g = segment_of(p, s);
+            if (g.nk <= FEW_KEYS) few = g.nk;
         }
-        dot = fold(dot);
-        if (NORMS) norm = fold(norm);
+        const int most = __reduce_max_sync(~0u, few);
+        if (most) {                         // (whole warps: rows of other segments take part with nothing)
+            const int head = (int)(r - row * p.heads), kv_head = head / p.group;
+            uint4 q = make_uint4(0, 0, 0, 0);
+            if (few && in_width) q = *reinterpret_cast<const uint4*>((const T*)p.q + (q_first + row) * p.q_row + head * p.q_head + lane * 8);
+            float sum = 0.f;
+            for (int j = 0; j < most; ++j) {
+                const Place at_key = j < few ? key_place(p, g, s, j) : Place{-1, 0};
+                uint4 k = make_uint4(0, 0, 0, 0), v = k;
+                if (at_key.at >= 0 && in_width) {
+                    k = *reinterpret_cast<const uint4*>((const T*)p.k + key_offset(p, at_key, kv_head) + lane * 8);
+                    v = *reinterpret_cast<const uint4*>((const T*)p.v + value_offset(p, at_key, kv_head) + lane * 8);
+                }
+                const float score = fold(dot8<T>(q, k)), dp = fold(dot8<T>(a, v));
+                if (at_key.at >= 0) sum += ex2((score * p.scale - lse) * LOG2E_F) * dp;
+            }
+            if (few) dot = sum;
+        }
         if (r >= q_rows) continue;
         const bool reads = lse != -INFINITY;
         if (lane == 0) w.stats[at] = make_float2(reads ? lse * LOG2E_F : INFINITY, reads ? dot : 0.f);
@@ -113,14 +143,7 @@ __global__ void __launch_bounds__(PREP_THREADS) attention_prepare_kernel(const A
             uint4 a = make_uint4(0, 0, 0, 0);
             if (r < v_rows && in_width && (!p.mask || p.mask[k_first + row]))
                 a = *reinterpret_cast<const uint4*>((const T*)p.v + (k_first + row) * p.v_row + (r - row * p.kv_heads) * p.v_head + lane * 8);
-            const T* ea = reinterpret_cast<const T*>(&a);
-            float norm = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float x = Half<T>::to(ea[e]);
-                norm += x * x;
-            }
-            norm = fold(norm);
+            const float norm = fold(dot8<T>(a, a));
             top_v = norm == norm ? fmaxf(top_v, norm) : INFINITY;
         }
 #pragma unroll
@@ -173,7 +196,7 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
     }
     Walker<WorkCut> walk;
     bool work_here = false;
-    if (warp == BWD_WALKER) work_here = walk.begin(p, KV ? w.kv_start_unit : w.q_start_unit, block, blocks, BWD_LEAST);
+    if (warp == BWD_WALKER) work_here = walk.begin(p, KV ? w.kv_start_unit : w.q_start_unit, block, blocks);
     if (warp == BWD_MMA) tmem_alloc(smem_u32(&ctl.tmem), 512);
     tmem_fence_before();
     __syncthreads();
@@ -447,6 +470,7 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
             const int rows = KV ? w.kv_rows : w.q_rows;
             constexpr int SIDES = KV ? 2 : 1, MINE = DP * SIDES / 4;        // this thread's features of a row
             const int side = KV ? x / 2 : 0, f0 = (KV ? x % 2 : x) * MINE;
+            const bool zero = masked || (side == 0 && reads_one_key(p, item.segment()));
             const uint32_t acc = (side ? acc2 : acc1) + lanes;
             const float finish = side ? (F16 ? 0x1p-14f : 1.f) : p.scale / factor;
             T* out = (T*)(KV ? (side ? p.gv : p.gk) : p.gq);
@@ -467,7 +491,7 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
                             uint32_t h[4];
 #pragma unroll
                             for (int k = 0; k < 4; ++k)
-                                h[k] = masked && ok ? 0u : pack_half<T>(__uint_as_float(v[8 * c + 2 * k]) * finish, __uint_as_float(v[8 * c + 2 * k + 1]) * finish);
+                                h[k] = zero && ok ? 0u : pack_half<T>(__uint_as_float(v[8 * c + 2 * k]) * finish, __uint_as_float(v[8 * c + 2 * k + 1]) * finish);
                             o[c] = make_uint4(h[0], h[1], h[2], h[3]);
                         }
                         store_rows<2>(o, out + out_row * p.D + f, valid && out, (p.D - f) / 8);
@@ -547,6 +571,7 @@ __device__ __forceinline__ void sum_pass(const AttnParams& p, const BwdWork& w, 
                 out_row = (long long)pr.row * p.heads + pr.head;
                 masked = w.stats[out_row].x == INFINITY;
             }
+            masked = masked || (side == 0 && reads_one_key(p, g));
             const float finish = KV && side ? (F16 ? 0x1p-14f : 1.f) : p.scale / factor;
             T* out = (T*)(KV ? (side ? p.gv : p.gk) : p.gq);
 #pragma unroll

@@ -21,7 +21,6 @@ namespace tiga {
 constexpr int FWD_SOFTMAX_WARPS = 16, FWD_PRODUCER = FWD_SOFTMAX_WARPS, FWD_MMA = FWD_PRODUCER + 4, FWD_WALKER = FWD_MMA + 1;
 constexpr int FWD_THREADS = 32 * (FWD_WALKER + 1), FWD_ROWS = 256, FWD_STEP = 128;
 typedef Cut<FWD_ROWS, FWD_STEP, false> FwdCut;
-constexpr int FWD_LEAST = 2;            // units a block at least
 constexpr int MASK_RING = 8;            // the producers are at most 6 steps ahead of the softmax (ring of at most 10 tiles)
 constexpr float RESCALE_AT = 8.f;
 
@@ -75,7 +74,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
     }
     Walker<FwdCut> walk;
     bool work_here = false;
-    if (warp == FWD_WALKER) work_here = walk.begin(p, w.unit_start, blockIdx.x, gridDim.x, FWD_LEAST);
+    if (warp == FWD_WALKER) work_here = walk.begin(p, w.unit_start, blockIdx.x, gridDim.x);
     if (warp == FWD_MMA) tmem_alloc(smem_u32(&ctl.tmem), 512);
     tmem_fence_before();
     __syncthreads();

@@ -67,6 +67,26 @@ __device__ __forceinline__ long long value_offset(const AttnParams& p, Place a, 
     return a.at < 0 ? -1 : p.table ? a.at * p.page_stride + a.slot * p.slot_stride + h * p.v_head : a.at * p.v_row + h * p.v_head;
 }
 
+// Whether the rows of a dense segment read one key: its weight is 1 whatever the score, so scores have no gradient.  (Masks of up to
+// 32 keys are counted; where a longer one leaves a single key the gradient is what is left of dP - delta, a few 2^-23 of either.)
+__device__ __forceinline__ bool reads_one_key(const AttnParams& p, const Segment& g) {
+    if (!p.mask || g.nk > 32) return g.nk == 1;
+    int n = 0;
+    for (int j = 0; j < g.nk; ++j) n += p.mask[g.k0 + j] != 0;
+    return n == 1;
+}
+
+// the segment that holds row i (the last one that starts at or before it), or -1
+__device__ __forceinline__ int segment_of_row(const int32_t* start, int n_seg, int n_rows, int i) {
+    int lo = 0, hi = n_seg;
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (start[mid] <= i) lo = mid + 1; else hi = mid;
+    }
+    if (lo == 0 || i >= clamp_to(start[lo], n_rows)) return -1;
+    return lo - 1;
+}
+
 // ---- How the work is cut.  A segment's heads share keys, so the rows of a group's heads are packed: packed row r of a kv head is row
 // r / group, head kv_head * group + r % group.  A tile of stationary rows (packed rows, or keys for their gradients) meets the other
 // side in steps; a unit is one step of one tile of one kv head.  All units of a call stand in one line (segment, kv head, tile,
@@ -134,10 +154,10 @@ struct Walker {
     }
     __device__ __forceinline__ long long first_unit(long long block) const { return quotient(block * units, blocks); }
 
-    // The piece of block `block` of `grid`, which takes part only if there are `least` units a block.  Every warp of a block calls it
-    // with all its lanes.  unit_start: units in front of every segment; NULL (few segments, few tiles): they are counted here.
+    // The piece of block `block` of `grid`, by a warp with all its lanes; of few units every one has a block of its own (two units a block:
+    // a single token on 777 keys 14.2 us on the device instead of 11.0).  unit_start: units in front of every segment; NULL (few segments, few tiles): they are counted here.
     // false: nothing to do.
-    __device__ __forceinline__ bool begin(const AttnParams& p, const long long* unit_start, int block, int grid, int least) {
+    __device__ __forceinline__ bool begin(const AttnParams& p, const long long* unit_start, int block, int grid) {
         const int lane = threadIdx.x % 32;
         if (unit_start) units = unit_start[p.n_seg];
         else {
@@ -145,7 +165,7 @@ struct Walker {
             for (int k = 0; k < p.n_seg; k += 32) units += k + lane < p.n_seg ? C::units(p, segment_of(p, k + lane)) * p.kv_heads : 0;
             units = warp_total(units);
         }
-        blocks = min((long long)grid, max(quotient(units + least - 1, least), 1LL));
+        blocks = min((long long)grid, max(units, 1LL));
         if (block >= blocks || units == 0) return false;
         long long off = first_unit(block), mine = 0;
         left = first_unit(block + 1) - off;

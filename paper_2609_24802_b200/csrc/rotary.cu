@@ -57,16 +57,6 @@ __device__ __forceinline__ void store_pack(T* p, const Pack<T, VEC, ALIGNED>& r,
     }
 }
 
-__device__ __forceinline__ int last_start_at_or_before(const int32_t* start, int n_seg, int n_rows, int i) {
-    int lo = 0, hi = n_seg;
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (start[mid] <= i) lo = mid + 1; else hi = mid;
-    }
-    if (lo == 0 || i >= clamp_to(start[lo], n_rows)) return -1;
-    return lo - 1;
-}
-
 // A block has up to ROT_ROWS rows.  It looks up where they lie, forms the sines and cosines of their pairs once, and then passes over
 // the rows' heads in the order of memory.  A unit is VEC pairs as two vectors of the halves, VEC / 2 pairs as one vector, or one vector
 // of what is copied.  Many threads hide the
@@ -81,7 +71,7 @@ __global__ void __launch_bounds__(ROT_THREADS, APPEND ? 6 : 8) rotary_kernel(con
         const long long i = first_row + threadIdx.x;
         long long pos = 0, y0 = -1;
         if (APPEND) {
-            const int s = last_start_at_or_before(p.start, p.n_seg, (int)p.n, (int)i);
+            const int s = segment_of_row(p.start, p.n_seg, (int)p.n, (int)i);
             if (s >= 0) {
                 const int first = clamp_to(p.start[s], (int)p.n), end = clamp_to(p.start[s + 1], (int)p.n);
                 pos = (long long)max(p.kv_len[s], 0) - (end - i);

@@ -159,6 +159,28 @@ def test_single_key_has_weight_one(tiga):
     assert torch.all(got["grad_q"].abs() <= 1.01 * ds * k.abs()) and torch.all(got["grad_key"].abs() <= 1.01 * (ds * q.abs()).sum(0, keepdim=True))
 
 
+def test_scores_of_a_single_key_have_no_gradient(tiga):
+    """One key, or one that the mask leaves: exact zeros, in whole tiles and in tiles that several blocks share."""
+    for q_len, kv_len, left in (([50], [1], None), ([20000, 7], [1, 1], None), ([300, 40], [9, 30], (4, 20))):
+        c = case(q_len, kv_len, 4, 2, 64, BF16, seed=35)
+        if left:
+            c["mask"] = torch.zeros(sum(kv_len), dtype=torch.bool, device="cuda")
+            c["mask"][left[0]] = c["mask"][kv_len[0] + left[1]] = True
+        got = check(tiga, c)
+        assert torch.all(got["grad_q"] == 0) and torch.all(got["grad_key"] == 0) and torch.any(got["grad_value"] != 0)
+
+
+@pytest.mark.parametrize("dtype,D", [(F16, 64), (BF16, 128), (BF16, 40)])
+@pytest.mark.parametrize("n", [2, 3, 7, 16, 17])
+def test_few_keys(tiga, n, dtype, D):
+    """delta is summed over the keys themselves: dS is rounded once and the result once, as over many keys (2 u + u^2, no share of out's
+    rounding; seventeen keys and more have that share)."""
+    c = case([70, 3, 200], [n, 1, n], 4, 2, D, dtype, seed=36 + n)
+    want, got = reference(c), run(tiga, c)
+    for name in got:
+        close(got[name], want[name], want[name + "_tol"] * (0.7 if name in ("grad_q", "grad_key") and n <= 16 else 1.0) + torch.finfo(dtype).smallest_normal, name)
+
+
 def test_rows_outside_of_the_segments_stay(tiga):
     c = case([10, 20], [30, 40], 2, 2, 64, BF16, seed=21)
     want = run(tiga, c)
