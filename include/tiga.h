@@ -407,7 +407,8 @@ tiga_status tiga_apply_dense_attention(const tiga_dense* g, const tiga_heads* h,
  *     grad_q_i = scale sum_j dS_ij key_j,   grad_key_j = scale sum_i dS_ij q_i,   grad_value_j = sum_i p_ij grad_out_i,
  * key and value gradients summed over the heads of their group.  p is recomputed from lse; nothing of size rows x keys is
  * stored.  out and lse are the forward's outputs for these inputs.  Gradients have the storage type and are dense,
- * [n_q, heads, D] and [n_kv, kv_heads, D]; any of them may be NULL (skipped).  Masked keys have zero gradients.
+ * [n_q, heads, D] and [n_kv, kv_heads, D]; any of them may be NULL (skipped).  Masked keys have zero gradients, and so have
+ * the scores of rows that read a single key.  Of up to 16 keys delta is summed as sum_j p_ij dP_ij.
  * TIGA_F16: p and dS are scaled by powers of two before they are rounded (dS by one that all segments of a call
  * share, from the largest row norms of grad_out and value), so that small weights and small gradients keep their digits.
  * ws: tiga_dense_attention_workspace_bytes(g, h, 1) bytes. */
