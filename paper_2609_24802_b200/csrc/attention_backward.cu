@@ -37,7 +37,7 @@ template <int DP> struct Bwd {
 template <int AUX> struct BwdControl {
     unsigned long long full[8], empty[8], aux_full[AUX], x_full, x_empty, s_full, dp_full, p_full, ds_full, acc_full, acc_empty, drain;
     ItemRing items;
-    uint32_t tmem, abort_word, never, pad;
+    uint32_t tmem, abort_word;
     alignas(16) float minus_lse[AUX][BWD_STEP], minus_delta[AUX][BWD_STEP];     // keys stationary: of the step's rows
     uint32_t mask[AUX][4];                                                      // queries stationary: the step's keys
 };
@@ -191,7 +191,7 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
         mbar_init(bar(ctl.acc_full), 1);
         mbar_init(bar(ctl.acc_empty), 32 * BWD_WEIGHT_WARPS);
         mbar_init(bar(ctl.drain), 1);
-        ctl.abort_word = ctl.never = 0;
+        ctl.abort_word = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     Walker<WorkCut> walk;
@@ -207,7 +207,7 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
     if (warp == BWD_WALKER) {
         if (lane == 0) {
             (KV ? w.kv_joints : w.q_joints)[block] = joint_of(walk, work_here, block);
-            items_hand_out(ctl.items, p, walk, work_here, &ctl.never);
+            items_hand_out(ctl.items, p, walk, work_here);
         }
         __syncwarp();
     } else if (warp >= BWD_PRODUCER && warp < BWD_MMA) {
@@ -218,7 +218,7 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
         auto wait = [&](unsigned long long& b, uint32_t parity) { return ok = __all_sync(~0u, mbar_wait(bar(b), parity & 1, abort_word)); };
         auto slot_free = [&]() { return tiles < (uint32_t)C::SLOTS || wait(ctl.empty[tiles % C::SLOTS], tiles / C::SLOTS + 1); };
         for (uint32_t item = 0;; ++item) {
-            const Item& e = item_take(ctl.items, item, &ctl.never);
+            const Item& e = item_take(ctl.items, item);
             if (e.steps == 0) break;
             const Segment g = e.segment();
             const int packed_rows = g.nq * p.group, i0 = e.i0, i1 = ok ? e.i1 : e.i0, h = e.h;
@@ -276,8 +276,8 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
         }
         cp_async_wait_all();
         if (*abort_word) {          // boxes may still be on their way: their tiles, as far as they were asked for
-            for (uint32_t k = tiles < (uint32_t)C::SLOTS ? 0 : tiles - C::SLOTS; k < tiles; ++k) mbar_wait(bar(ctl.full[k % C::SLOTS]), (k / C::SLOTS) & 1, &ctl.never);
-            if (items) mbar_wait(bar(ctl.x_full), (items - 1) & 1, &ctl.never);
+            for (uint32_t k = tiles < (uint32_t)C::SLOTS ? 0 : tiles - C::SLOTS; k < tiles; ++k) mbar_wait_for(bar(ctl.full[k % C::SLOTS]), (k / C::SLOTS) & 1, HALF_A_SECOND);
+            if (items) mbar_wait_for(bar(ctl.x_full), (items - 1) & 1, HALF_A_SECOND);
         }
     } else if (warp == BWD_MMA) {
         // ---------------------------------------------------------------- matrix instructions
@@ -320,7 +320,7 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
             __syncwarp();
         };
         for (;; ++items) {
-            const Item& e = item_take(ctl.items, items, &ctl.never);
+            const Item& e = item_take(ctl.items, items);
             if (e.steps == 0) break;
             const int n = e.i1 - e.i0;
             item_return(ctl.items, items);
@@ -369,7 +369,7 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
             tile0 += 2 * n;
         }
         commit(ctl.drain);
-        mbar_wait(bar(ctl.drain), 0, &ctl.never);
+        mbar_wait_for(bar(ctl.drain), 0, HALF_A_SECOND);
         __syncwarp();
     } else {
         // ---------------------------------------------------------------- weights: warpgroup x has 32 of a step's 128 columns
@@ -383,7 +383,7 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
         uint32_t steps = 0, items = 0;
         bool ok = true;
         for (;; ++items) {
-            const Item& item = item_take(ctl.items, items, &ctl.never);
+            const Item& item = item_take(ctl.items, items);
             if (item.steps == 0) break;
             const int n = item.i1 - item.i0, r = item.t * BWD_ROWS + row, n_rows = WorkCut::rows(p, item.segment());
             const bool valid = r < n_rows;

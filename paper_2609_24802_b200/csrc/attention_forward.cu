@@ -34,7 +34,7 @@ template <int DP> struct Fwd {
 struct FwdControl {
     unsigned long long full[10], empty[10], q_full, q_empty, s_full[2], p_full[2], o_full[2], mask_full[MASK_RING], drain;
     ItemRing items;
-    uint32_t tmem, abort_word, never, mask[MASK_RING][4];
+    uint32_t tmem, abort_word, mask[MASK_RING][4];
     float share[2][2][128];             // what a row's threads tell each other
 };
 static_assert(sizeof(FwdControl) <= 3 * 1024, "control block");
@@ -69,7 +69,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
         for (int x = 0; x < 2; ++x) { mbar_init(bar(ctl.s_full[x]), 1); mbar_init(bar(ctl.p_full[x]), 256); mbar_init(bar(ctl.o_full[x]), 1); }
         for (int i = 0; i < MASK_RING; ++i) mbar_init(bar(ctl.mask_full[i]), 4);
         mbar_init(bar(ctl.drain), 1);
-        ctl.abort_word = ctl.never = 0;
+        ctl.abort_word = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     Walker<FwdCut> walk;
@@ -85,7 +85,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
     if (warp == FWD_WALKER) {
         if (lane == 0) {
             w.joints[blockIdx.x] = joint_of(walk, work_here, blockIdx.x);
-            items_hand_out(ctl.items, p, walk, work_here, &ctl.never);
+            items_hand_out(ctl.items, p, walk, work_here);
         }
         __syncwarp();
     } else if (warp >= FWD_PRODUCER && warp < FWD_MMA) {
@@ -96,7 +96,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
         auto wait = [&](unsigned long long& b, uint32_t parity) { return ok = __all_sync(~0u, mbar_wait(bar(b), parity & 1, abort_word)); };
         auto slot_free = [&]() { return tiles < (uint32_t)C::SLOTS || wait(ctl.empty[tiles % C::SLOTS], tiles / C::SLOTS + 1); };
         for (uint32_t item = 0;; ++item) {
-            const Item& e = item_take(ctl.items, item, &ctl.never);
+            const Item& e = item_take(ctl.items, item);
             if (e.steps == 0) break;
             const Segment g = e.segment();
             const int i0 = e.i0, i1 = e.i1, h = e.h;
@@ -133,8 +133,8 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
         }
         cp_async_wait_all();
         if (*abort_word) {          // boxes may still be on their way: their tiles, as far as they were asked for
-            for (uint32_t k = tiles < (uint32_t)C::SLOTS ? 0 : tiles - C::SLOTS; k < tiles; ++k) mbar_wait(bar(ctl.full[k % C::SLOTS]), (k / C::SLOTS) & 1, &ctl.never);
-            if (items) mbar_wait(bar(ctl.q_full), (items - 1) & 1, &ctl.never);
+            for (uint32_t k = tiles < (uint32_t)C::SLOTS ? 0 : tiles - C::SLOTS; k < tiles; ++k) mbar_wait_for(bar(ctl.full[k % C::SLOTS]), (k / C::SLOTS) & 1, HALF_A_SECOND);
+            if (items) mbar_wait_for(bar(ctl.q_full), (items - 1) & 1, HALF_A_SECOND);
         }
     } else if (warp == FWD_MMA) {
         // ---------------------------------------------------------------- matrix instructions
@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
             __syncwarp();
         };
         for (;; ++items) {
-            const Item& e = item_take(ctl.items, items, &ctl.never);
+            const Item& e = item_take(ctl.items, items);
             if (e.steps == 0) break;
             const int n = e.i1 - e.i0;
             const bool two = e.nq * p.group - e.t * FWD_ROWS > 128;
@@ -210,7 +210,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
             tile0 += 2 * n;
         }
         if (elected()) mma_commit(bar(ctl.drain));
-        mbar_wait(bar(ctl.drain), 0, &ctl.never);
+        mbar_wait_for(bar(ctl.drain), 0, HALF_A_SECOND);
         __syncwarp();
     } else {
         // ---------------------------------------------------------------- softmax
@@ -226,7 +226,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
         uint32_t step0 = 0, s_done = 0, o_done0 = 0, o_done1 = 0;       // steps, scores of this half, values of each half in the items before
         bool ok = true;
         for (uint32_t item = 0;; ++item) {
-            const Item& e = item_take(ctl.items, item, &ctl.never);
+            const Item& e = item_take(ctl.items, item);
             if (e.steps == 0) break;
             const int n = e.i1 - e.i0;
             const int rows = min(e.nq * p.group - e.t * FWD_ROWS, FWD_ROWS);

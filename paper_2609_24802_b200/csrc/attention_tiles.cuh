@@ -44,15 +44,16 @@ struct Item {
 };
 struct ItemRing {
     unsigned long long full[ITEMS], empty[ITEMS];
-    Item item[ITEMS];
+    Item item[ITEMS], none;         // none: for a warp to which no item came
 };
 __device__ __forceinline__ void items_init(ItemRing& r, int consumer_warps) {
+    r.none.steps = 0;
     for (int i = 0; i < ITEMS; ++i) { mbar_init(smem_u32(&r.full[i]), 1); mbar_init(smem_u32(&r.empty[i]), consumer_warps); }
 }
 template <typename C>
-__device__ __forceinline__ void items_hand_out(ItemRing& r, const AttnParams& p, Walker<C>& it, bool more, volatile uint32_t* never) {
+__device__ __forceinline__ void items_hand_out(ItemRing& r, const AttnParams& p, Walker<C>& it, bool more) {
     for (uint32_t n = 0;; ++n) {
-        if (n >= (uint32_t)ITEMS) mbar_wait(smem_u32(&r.empty[n % ITEMS]), (n / ITEMS + 1) & 1, never);
+        if (n >= (uint32_t)ITEMS && !mbar_wait_for(smem_u32(&r.empty[n % ITEMS]), (n / ITEMS + 1) & 1, A_MINUTE)) return;
         r.item[n % ITEMS] = {it.g.q0, it.g.nq, it.g.k0, it.g.nk, it.s, it.h, it.t, more ? it.steps : 0, it.i0, it.i1};
         mbar_arrive(smem_u32(&r.full[n % ITEMS]));
         if (!more) return;
@@ -74,9 +75,9 @@ __device__ __forceinline__ Joint joint_of(const Walker<C>& it, bool any, int blo
     return j;
 }
 // The n-th item, for a whole warp, and its return.  Neither looks at the abort word: every warp goes through all items.
-__device__ __forceinline__ const Item& item_take(ItemRing& r, uint32_t n, volatile uint32_t* never) {
-    mbar_wait(smem_u32(&r.full[n % ITEMS]), (n / ITEMS) & 1, never);
-    return r.item[n % ITEMS];
+__device__ __forceinline__ const Item& item_take(ItemRing& r, uint32_t n) {
+    const bool came = __all_sync(~0u, mbar_wait_for(smem_u32(&r.full[n % ITEMS]), (n / ITEMS) & 1, A_MINUTE));
+    return came ? r.item[n % ITEMS] : r.none;
 }
 __device__ __forceinline__ void item_return(ItemRing& r, uint32_t n) {
     __syncwarp();

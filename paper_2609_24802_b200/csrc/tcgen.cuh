@@ -43,6 +43,14 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
         }
     }
 }
+// Without the abort word: waits for other warps of the block, whose own waits all end (a minute), or for what is still on its way.
+constexpr long long A_MINUTE = 1LL << 37, HALF_A_SECOND = 1LL << 30;
+__device__ __forceinline__ bool mbar_wait_for(uint32_t bar, uint32_t parity, long long cycles) {
+    const long long t0 = clock64();
+    while (!mbar_try(bar, parity))
+        if (clock64() - t0 > cycles) return false;
+    return true;
+}
 
 // ---- asynchronous copies (generic proxy) and the fence in front of their use by the matrix instructions
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool on) {
@@ -100,11 +108,6 @@ __device__ __forceinline__ void tmem_ld8(uint32_t at, uint32_t (&r)[8]) {
 }
 __device__ __forceinline__ void tmem_st8(uint32_t at, const uint32_t (&r)[8]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(at), TIGA_W8(r, 0) : "memory");
-}
-__device__ __forceinline__ void tmem_st32(uint32_t at, const uint32_t (&r)[32]) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-                 "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
-                 ::"r"(at), TIGA_W8(r, 0), TIGA_W8(r, 8), TIGA_W8(r, 16), TIGA_W8(r, 24) : "memory");
 }
 template <int N>
 __device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&r)[N]) {          // the first 16
