@@ -760,7 +760,7 @@ class PagedCache:
             raise ValueError("key and value must be fp16 or bf16 arrays [n_pages, page_size, kv_heads, D] of one shape")
         shape, steps = key.shape, key.stride()
         step = [s if n > 1 else 0 for s, n in zip(steps, shape)]                 # (the stride of a single entry means nothing)
-        if (steps != value.stride() and step != [s if n > 1 else 0 for s, n in zip(value.stride(), shape)]) or step[3] > 1:
+        if (steps != value.stride() and step != [s if n > 1 else 0 for s, n in zip(value.stride(), shape)]) or (step[3] != 1 and shape[3] > 1):
             raise ValueError("key and value must have the same strides and contiguous features")
         if table.dtype is not torch.int32 or table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
             raise ValueError("table must be an int32 array [n_seg, max_pages] with contiguous rows")

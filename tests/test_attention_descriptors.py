@@ -1,0 +1,37 @@
+"""Descriptors of dense and paged relations: what they refuse when they are made, without a device."""
+import pytest
+import torch
+
+
+@pytest.fixture(scope="module")
+def api():
+    from paper_2609_24802_b200 import build
+    build.build_library()
+    from paper_2609_24802_b200 import api
+    return api
+
+
+def pages(n_pages=3, page=16, heads=2, D=64, dtype=torch.float16):
+    return torch.zeros(n_pages, page, heads, D, dtype=dtype)
+
+
+def places(n_seg=1, max_pages=2):
+    return torch.zeros(n_seg, max_pages, dtype=torch.int32), torch.zeros(n_seg, dtype=torch.int32)
+
+
+def test_pages_whose_features_share_storage_are_refused(api):
+    """One element seen as D features: the kernels would read, and write, D elements per slot."""
+    thin = pages(D=8)[..., :1].expand(3, 16, 2, 64)
+    assert thin.stride() == (256, 16, 8, 0)
+    for key, value in ((thin, thin), (thin, pages()), (pages(), thin)):
+        with pytest.raises(ValueError):
+            api.PagedCache(key, value, *places())
+    apart = pages(D=128)[..., ::2]
+    with pytest.raises(ValueError):
+        api.PagedCache(apart, apart, *places())
+
+
+def test_pages_in_any_order_of_slots_and_heads_are_taken(api):
+    for t in (pages(), pages(page=2, heads=16).transpose(1, 2), pages(D=128)[..., 64:], pages(n_pages=1), pages(page=1), pages(heads=1), pages(n_pages=0)):
+        cache = api.PagedCache(t, t, *places())
+        assert (cache.c.n_pages, cache.c.page_size) == t.shape[:2]
