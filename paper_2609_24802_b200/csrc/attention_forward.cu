@@ -332,8 +332,10 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
             }
             // ---- the item's end: the row's mass; a short tile's two states are joined; then the rows are finished or put aside
             const uint32_t made0 = two ? n : (n + 1) / 2, made1 = two ? n : n / 2;
-            if (ok && (!two || x == 0)) ok = mbar_wait(bar(ctl.o_full[0]), (o_done0 + made0 - 1) & 1, abort_word);
-            if (ok && made1 && (!two || x == 1)) ok = mbar_wait(bar(ctl.o_full[1]), (o_done1 + made1 - 1) & 1, abort_word);
+            // Each half waits for its own products alone: the scores of its last step came behind the products of the step before, so the
+            // phase that it waits for is the one under way.  (The other half's may lag by more than a phase, which a parity cannot tell.)
+            const uint32_t made = x ? made1 : made0;
+            if (ok && made) ok = mbar_wait(bar(ctl.o_full[x]), (o_mine + made - 1) & 1, abort_word);
             ok = __all_sync(~0u, ok);
             if (!ok) l = __int_as_float(0x7fffffff);
             tmem_fence_after();
@@ -343,7 +345,9 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
                 meet_half();
                 l += ctl.share[x][1 - y][row];
             } else {
-                meet_all();
+                tmem_fence_before();
+                meet_all();                     // both accumulators are complete, and may be read
+                tmem_fence_after();
                 const float la = ctl.share[0][0][row] + ctl.share[0][1][row], lb = ctl.share[1][0][row] + ctl.share[1][1][row];
                 meet_all();
                 if (y == 0) ctl.share[x][0][row] = m;
