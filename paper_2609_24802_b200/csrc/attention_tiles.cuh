@@ -44,16 +44,23 @@ struct Item {
 };
 struct ItemRing {
     unsigned long long full[ITEMS], empty[ITEMS];
-    Item item[ITEMS], none;         // none: for a warp to which no item came
+    Item item[ITEMS], none;         // none: in place of the items that were not handed out
+    uint32_t given_up;              // the first of these
 };
 __device__ __forceinline__ void items_init(ItemRing& r, int consumer_warps) {
     r.none.steps = 0;
+    r.given_up = ~0u;
     for (int i = 0; i < ITEMS; ++i) { mbar_init(smem_u32(&r.full[i]), 1); mbar_init(smem_u32(&r.empty[i]), consumer_warps); }
 }
-template <typename C>
-__device__ __forceinline__ void items_hand_out(ItemRing& r, const AttnParams& p, Walker<C>& it, bool more) {
+// Waits at most `limit` cycles for the return of an item; then there are no more, and every warp learns from which one on.
+template <typename W>
+__device__ __forceinline__ void items_hand_out(ItemRing& r, const AttnParams& p, W& it, bool more, long long limit = A_MINUTE) {
     for (uint32_t n = 0;; ++n) {
-        if (n >= (uint32_t)ITEMS && !mbar_wait_for(smem_u32(&r.empty[n % ITEMS]), (n / ITEMS + 1) & 1, A_MINUTE)) return;
+        if (n >= (uint32_t)ITEMS && !mbar_wait_for(smem_u32(&r.empty[n % ITEMS]), (n / ITEMS + 1) & 1, limit)) {
+            __threadfence_block();
+            *(volatile uint32_t*)&r.given_up = n;
+            return;
+        }
         r.item[n % ITEMS] = {it.g.q0, it.g.nq, it.g.k0, it.g.nk, it.s, it.h, it.t, more ? it.steps : 0, it.i0, it.i1};
         mbar_arrive(smem_u32(&r.full[n % ITEMS]));
         if (!more) return;
@@ -74,9 +81,19 @@ __device__ __forceinline__ Joint joint_of(const Walker<C>& it, bool any, int blo
     j.parts = ends ? block - j.first + 1 : 0;
     return j;
 }
-// The n-th item, for a whole warp, and its return.  Neither looks at the abort word: every warp goes through all items.
+// The n-th item, for a whole warp, and its return.  Neither looks at the abort word: every warp goes through all items.  A warp does not
+// give up by itself: warps that meet at a barrier have to leave at the same item.  The warp that hands out does so for all of them after a
+// minute at most, so this wait ends as well (a bound of its own, four minutes, lies behind that): items in front of given_up are there.
 __device__ __forceinline__ const Item& item_take(ItemRing& r, uint32_t n) {
-    const bool came = __all_sync(~0u, mbar_wait_for(smem_u32(&r.full[n % ITEMS]), (n / ITEMS) & 1, A_MINUTE));
+    const long long t0 = clock64();
+    uint32_t end = ~0u;
+    while (!mbar_try(smem_u32(&r.full[n % ITEMS]), (n / ITEMS) & 1)) {
+        end = *(volatile uint32_t*)&r.given_up;
+        if (end == ~0u && clock64() - t0 > 4 * A_MINUTE) end = 0;
+        if (end != ~0u) break;
+    }
+    __threadfence_block();
+    const bool came = __all_sync(~0u, n < end);
     return came ? r.item[n % ITEMS] : r.none;
 }
 __device__ __forceinline__ void item_return(ItemRing& r, uint32_t n) {
