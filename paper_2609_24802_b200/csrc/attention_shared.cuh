@@ -22,8 +22,9 @@ struct AttnParams {
     int kv_box, q_box;              // rows that a box of the tensor maps brings (0: rows are copied one by one)
 };
 
-// A segment's rows [q0, q0 + nq) and its keys [k0, k0 + nk) (paged: k0 = 0), bounds clamped to the arrays.
-struct Segment { int q0, nq, k0, nk; };
+// A segment's rows [q0, q0 + nq) and its keys [k0, k0 + nk) (paged: k0 = 0), bounds clamped to the arrays.  length: its tokens, of which a
+// cache may hold fewer (the rows' positions count from its end, not from that of the table).
+struct Segment { int q0, nq, k0, nk, length; };
 
 // Rows and positions end here, so that a tile's last row number fits 32 bits.
 constexpr long long MOST_ROWS = 0x7fff0000LL;
@@ -36,17 +37,18 @@ __device__ __forceinline__ Segment segment_of(const AttnParams& p, int s) {
     g.nq = max(clamp_to(p.q_start[s + 1], p.n_q) - g.q0, 0);
     if (p.table) {
         g.k0 = 0;
-        g.nk = (int)min(min((long long)max(p.kv_len[s], 0), p.max_pages * p.page_size), MOST_ROWS);
+        g.length = max(p.kv_len[s], 0);
+        g.nk = (int)min(min((long long)g.length, p.max_pages * p.page_size), MOST_ROWS);
     } else {
         g.k0 = clamp_to(p.kv_start[s], p.n_kv);
-        g.nk = max(clamp_to(p.kv_start[s + 1], p.n_kv) - g.k0, 0);
+        g.length = g.nk = max(clamp_to(p.kv_start[s + 1], p.n_kv) - g.k0, 0);
     }
     return g;
 }
 
 // keys that row t of the segment's nq rows reads: [0, this)
 __device__ __forceinline__ int keys_of_row(const AttnParams& p, const Segment& g, int t) {
-    return p.causal ? min(max(g.nk - g.nq + t + 1, 0), g.nk) : g.nk;
+    return p.causal ? min(max(g.length - g.nq + t + 1, 0), g.nk) : g.nk;
 }
 
 // Where key j of segment s (0 <= j < g.nk) lies: paged, its page and slot; dense, its row and 0.  at < 0: it is masked, or has no page.
