@@ -90,9 +90,11 @@ __device__ __forceinline__ const Item& item_take(ItemRing& r, uint32_t n) {
     while (!mbar_try(smem_u32(&r.full[n % ITEMS]), (n / ITEMS) & 1)) {
         end = *(volatile uint32_t*)&r.given_up;
         if (end == ~0u && clock64() - t0 > 4 * A_MINUTE) end = 0;
-        if (end != ~0u) break;
+        if (end != ~0u) {
+            __threadfence_block();
+            break;
+        }
     }
-    __threadfence_block();
     const bool came = __all_sync(~0u, n < end);
     return came ? r.item[n % ITEMS] : r.none;
 }
