@@ -177,9 +177,10 @@ extern "C" tiga_status tiga_apply_paged_attention(const tiga_pages* c, const tig
     if (attention_bad_stride(h->q)) return TIGA_ERR_INVALID_ARG;
     if (c->n_seg == 0 || n_q == 0) return TIGA_OK;
     if (bad_ints(q_start) || bad_ints(c->kv_len) || bad_array(q) || bad_array(out)) return TIGA_ERR_INVALID_ARG;
-    if (bad_ints(c->table) || (c->n_pages > 0 && (bad_array(c->key) || bad_array(c->value)))) return TIGA_ERR_INVALID_ARG;
+    if ((c->max_pages > 0 && bad_ints(c->table)) || (c->n_pages > 0 && (bad_array(c->key) || bad_array(c->value)))) return TIGA_ERR_INVALID_ARG;
     if (lse && !aligned16(lse)) return TIGA_ERR_INVALID_ARG;
     if (!ws || !aligned16(ws) || ws_bytes < tiga_paged_attention_workspace_bytes(c, h, n_q)) return TIGA_ERR_WORKSPACE;
+    if (c->max_pages == 0) p.table = c->kv_len;         // an empty table may have no address; any says that the relation is paged, and none of it is read
     p.q = q; p.q_start = q_start; p.causal = causal != 0; p.out = out; p.lse = lse;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     return attention_forward(p, h->dtype == TIGA_BF16, ws, s);

@@ -1,4 +1,6 @@
 """Descriptors of dense and paged relations: what they refuse when they are made, without a device."""
+import ctypes
+
 import pytest
 import torch
 
@@ -35,3 +37,15 @@ def test_pages_in_any_order_of_slots_and_heads_are_taken(api):
     for t in (pages(), pages(page=2, heads=16).transpose(1, 2), pages(D=128)[..., 64:], pages(n_pages=1), pages(page=1), pages(heads=1), pages(n_pages=0)):
         cache = api.PagedCache(t, t, *places())
         assert (cache.c.n_pages, cache.c.page_size) == t.shape[:2]
+
+
+def test_a_table_with_entries_needs_an_address(api):
+    """(Without entries it may have none: nothing of it is read.)"""
+    L, s, ref = api.load_library(), api._Stride, ctypes.byref
+    h = api._Heads(1, 4, 2, 64, 1.0, s(256, 64), s(128, 64), s(128, 64), s(256, 64))
+
+    def call(max_pages, table, size):
+        c = api._Pages(256, 256, table, 256, 2, 8, 16, 4, max_pages, 2048, 128, 64)
+        return L.tiga_apply_paged_attention(ref(c), ref(h), 256, 256, 10, 1, 256, 256, 256, size, None)
+    assert call(4, None, 1 << 40) == 1 and call(4, 258, 1 << 40) == 1
+    assert call(0, None, 16) == 3               # goes on to the next check: the workspace is too small

@@ -53,3 +53,16 @@ def test_appended_tokens_read_themselves_beyond_the_table(tiga):
     tiga.tiga_paged_append(cache, q * 64, v, starts([n]))           # a token's own score is far above all others
     out, _, _ = tiga.tiga_apply_paged_attention(cache, q, starts([n]), 1.0)
     assert torch.equal(out[:4], v[:4])
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_a_table_without_entries_holds_nothing(tiga, causal):
+    """No place at all: rows read nothing and are written, as where every entry names no page."""
+    c = make([5, 1], [12, 3], 4, 2, 64, F16, 16, seed=46)
+    c["table"] = c["table"][:, :0].contiguous()
+    out, lse = run(tiga, c, causal)
+    assert torch.all(out == 0) and torch.all(lse == -float("inf"))
+    before = c["key_pages"].clone()
+    new = normal((6, 2, 64), F16, 3)
+    tiga.tiga_paged_append(tiga.PagedCache(c["key_pages"], c["value_pages"], c["table"], c["lens"]), new, new, starts([5, 1]))
+    assert torch.equal(c["key_pages"].nan_to_num(nan=9.0), before.nan_to_num(nan=9.0))
