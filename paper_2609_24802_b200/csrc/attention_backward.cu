@@ -231,7 +231,7 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
                 on = false;
                 stat = make_float2(INFINITY, 0.f);
                 if (keys) {
-                    if (r < g.nk) at = key_place(p, g, e.s, r);
+                    if (r < g.nk && g.nq) at = key_place(p, g, e.s, r);     // (keys that no row reads stay out of the products as masked ones do)
                 } else if (r < packed_rows) {
                     const PackedRow pr = packed_row(p, g, h, r);
                     stat = w.stats[(long long)pr.row * p.heads + pr.head];
@@ -393,7 +393,7 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
             bool masked = false;
             if (KV) {
                 out_row = (long long)(item.k0 + r) * p.kv_heads + item.h;
-                masked = valid && key_place(p, item.segment(), item.s, r).at < 0;
+                masked = valid && (item.nq == 0 || key_place(p, item.segment(), item.s, r).at < 0);
             } else if (valid) {
                 const PackedRow pr = packed_row(p, item.segment(), item.h, r);
                 out_row = (long long)pr.row * p.heads + pr.head;
