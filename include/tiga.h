@@ -409,8 +409,8 @@ tiga_status tiga_apply_dense_attention(const tiga_dense* g, const tiga_heads* h,
  * stored.  out and lse are the forward's outputs for these inputs.  Gradients have the storage type and are dense,
  * [n_q, heads, D] and [n_kv, kv_heads, D]; any of them may be NULL (skipped).  Masked keys have zero gradients, and so have
  * the scores of rows that read a single key.  Of up to 16 keys delta is summed as sum_j p_ij dP_ij.
- * TIGA_F16: p and dS are scaled by powers of two before they are rounded (dS by one that all segments of a call
- * share, from the largest row norms of grad_out and value), so that small weights and small gradients keep their digits.
+ * TIGA_F16: p and dS are scaled by powers of two before they are rounded (dS by one of each segment, from the largest norms
+ * of its rows of grad_out and value), so that small weights and small gradients keep their digits.
  * ws: tiga_dense_attention_workspace_bytes(g, h, 1) bytes. */
 tiga_status tiga_apply_dense_attention_backward(const tiga_dense* g, const tiga_heads* h, const void* q, const void* key,
                                                 const void* value, const void* out, const float* lse, const void* grad_out,

@@ -15,8 +15,8 @@ namespace tiga {
 // grad_value and the next step's S.
 // A step of 128 lasts about 3480 cycles (products 2048 or 1536, exponentials 1024, the threads' two turns 2200): 4 segments of 4096 rows
 // and keys, 16/4 heads of 128, bf16: 1.70 ms for both passes.
-// fp16: P carries 2^14 and dS a power of two from the largest norms of the rows of grad_out and value, which bound |dP - delta|: the
-// largest value cannot overflow, the smallest keep as many digits as there are.
+// fp16: P carries 2^14 and dS a power of two from the largest norms of the segment's rows of grad_out and value, which bound |dP - delta|:
+// the largest value cannot overflow, the smallest keep as many digits as there are.
 constexpr int BWD_WEIGHT_WARPS = 16, BWD_PRODUCER = BWD_WEIGHT_WARPS, BWD_MMA = BWD_PRODUCER + 4, BWD_WALKER = BWD_MMA + 1;
 constexpr int BWD_THREADS = 32 * (BWD_WALKER + 1), BWD_ROWS = 128, BWD_STEP = 128;
 typedef Cut<BWD_ROWS, BWD_STEP, true> KvCut;
@@ -46,22 +46,24 @@ static_assert(sizeof(BwdControl<2>) <= 3 * 1024 && sizeof(BwdControl<8>) <= 10 *
 struct BwdWork {
     long long *kv_start_unit, *q_start_unit;        // NULL: the blocks count for themselves
     float2* stats;                  // [n_q, heads]: lse in log2 (+inf: the row reads nothing), delta
-    uint32_t* norms;                // largest squared norms of grad_out and value rows, as bits
+    uint32_t* norms;                // [n_seg][2], fp16: largest squared norms of a segment's rows of grad_out and value, as bits
     Joint *kv_joints, *q_joints;    // [blocks of the side]
     float *kv_part, *q_part;        // [2 * blocks of the side][rows][gradients of the side][DP]
     int kv_rows, q_rows;            // rows that a partial state holds at most
 };
 
-// the power of two that dS carries (fp16)
-__device__ __forceinline__ float gradient_factor(const uint32_t* norms) {
-    const float largest = 2.f * sqrtf(__uint_as_float(norms[0])) * sqrtf(__uint_as_float(norms[1]));
+// the power of two that dS of segment s carries (fp16)
+__device__ __forceinline__ float gradient_factor(const uint32_t* norms, int s) {
+    const uint2 n = reinterpret_cast<const uint2*>(norms)[s];
+    const float largest = 2.f * sqrtf(__uint_as_float(n.x)) * sqrtf(__uint_as_float(n.y));
     if (!(largest > 1e-30f && largest < 1e30f)) return 1.f;
     return exp2f(14.f - (float)(ilogbf(largest) + 1));
 }
 
 // delta, lse in log2, and the norms behind gradient_factor: a row by LANES threads, 8 features each.  Bound by memory: grad_out and out
-// are read once (fp16: value too).  Of few keys delta is summed as sum p dP: out is then as large as the values, and its rounding would
-// show in dP - delta (over n keys it is smaller by the root of n).
+// are read once (fp16: value too).  A block has rows that follow one another, so that it passes through their segments in order.  Of few
+// keys delta is summed as sum p dP: out is then as large as the values, and its rounding would show in dP - delta (over n keys it is
+// smaller by the root of n).
 constexpr int FEW_KEYS = 16;
 template <typename T>
 __device__ __forceinline__ float dot8(const uint4& a, const uint4& b) {
@@ -72,93 +74,145 @@ __device__ __forceinline__ float dot8(const uint4& a, const uint4& b) {
     for (int e = 0; e < 8; ++e) d += Half<T>::to(x[e]) * Half<T>::to(y[e]);
     return d;
 }
-constexpr int PREP_THREADS = 256, PREP_ALONE = 16;     // blocks of work that one block does alone
+constexpr int PREP_THREADS = 256, PREP_BLOCKS = 4;      // of an SM
+constexpr int PREP_ALONE = 16;                          // blocks of work that one block does alone
+// The largest norm of a segment, as far as this thread's rows go, to memory: a maximum does not depend on the order.
+__device__ __forceinline__ void put_norm(uint32_t* norm, float top) {
+    const uint32_t bits = __float_as_uint(top);
+    if (bits > *(volatile uint32_t*)norm) atomicMax(norm, bits);
+}
+// ... at the end of a block's rows: once for all of them where they lie in one segment
+template <int LANES>
+__device__ __forceinline__ void put_last_norms(uint32_t* norms, int s, int first_s, float top) {
+    __shared__ uint32_t tops[PREP_THREADS / 32];
+    if (__syncthreads_and(s == first_s)) {
+        const uint32_t bits = __reduce_max_sync(~0u, __float_as_uint(top));
+        if (threadIdx.x % 32 == 0) tops[threadIdx.x / 32] = bits;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            uint32_t most = 0;
+            for (int k = 0; k < PREP_THREADS / 32; ++k) most = max(most, tops[k]);
+            put_norm(norms + 2LL * s, __uint_as_float(most));
+        }
+    } else if (threadIdx.x % LANES == 0) put_norm(norms + 2LL * s, top);
+}
 template <typename T, int LANES>
-__global__ void __launch_bounds__(PREP_THREADS) attention_prepare_kernel(const AttnParams p, const BwdWork w) {
+__global__ void __launch_bounds__(PREP_THREADS, PREP_BLOCKS) attention_prepare_kernel(const AttnParams p, const BwdWork w, const int q_blocks, const int v_blocks) {
     constexpr bool NORMS = operand_type<T>() == 0;
     constexpr int ROWS = PREP_THREADS / LANES;
     wait_for_previous_kernel();
     let_next_kernel_start();
+    if (NORMS && gridDim.x == 1) {
+        for (int i = threadIdx.x; i < 2 * p.n_seg; i += PREP_THREADS) w.norms[i] = 0;
+        __syncthreads();
+    }
+    // the bounds of few segments at once, so that no look-up waits for the one before it
+    __shared__ int32_t bounds[2][PREP_THREADS];
+    const int32_t *q_start = p.q_start, *kv_start = p.kv_start;
+    if (p.n_seg < PREP_THREADS) {
+        if ((int)threadIdx.x <= p.n_seg) { bounds[0][threadIdx.x] = q_start[threadIdx.x]; bounds[1][threadIdx.x] = kv_start[threadIdx.x]; }
+        __syncthreads();
+        q_start = bounds[0];
+        kv_start = bounds[1];
+    }
     const int lane = threadIdx.x % LANES;
     const bool in_width = lane * 8 < p.D;
-    const int q_first = clamp_to(p.q_start[0], p.n_q), q_end = max(clamp_to(p.q_start[p.n_seg], p.n_q), q_first);
-    const long long q_rows = (long long)(q_end - q_first) * p.heads, stride = (long long)gridDim.x * ROWS;
     auto fold = [&](float v) {
 #pragma unroll
         for (int d = LANES / 2; d; d >>= 1) v += __shfl_xor_sync(~0u, v, d);
         return v;
     };
-    // are there such segments at all?  (Looking for every row's segment cost 20 us of 262144 rows.)
-    bool few_here = false;
-    for (int s = threadIdx.x; s < p.n_seg; s += PREP_THREADS) few_here = few_here || segment_of(p, s).nk <= FEW_KEYS;
-    const bool any_few = __syncthreads_or(few_here);
-    float top_go = 0.f, top_v = 0.f;
-    for (long long r0 = (long long)blockIdx.x * ROWS; r0 < q_rows; r0 += stride) {      // whole warps stay together
-        const long long r = r0 + threadIdx.x / LANES, row = quotient(r, p.heads), at = (q_first + row) * p.heads + (r - row * p.heads);
-        uint4 a = make_uint4(0, 0, 0, 0), b = a;
-        float lse = 0.f;
-        if (r < q_rows) {
-            if (in_width) {
-                a = *reinterpret_cast<const uint4*>((const T*)p.go + (q_first + row) * p.go_row + (r - row * p.heads) * p.go_head + lane * 8);
-                b = *reinterpret_cast<const uint4*>((const T*)p.o + at * p.D + lane * 8);
-            }
-            lse = p.lse_in[at];
-        }
-        float dot = fold(dot8<T>(a, b));
-        const float norm = NORMS ? fold(dot8<T>(a, a)) : 0.f;
-        Segment g{};
-        int s = -1, few = 0;
-        if (any_few && r < q_rows && lse != -INFINITY && (s = segment_of_row(p.q_start, p.n_seg, p.n_q, (int)(q_first + row))) >= 0) {
-            g = segment_of(p, s);
-            if (g.nk <= FEW_KEYS) few = g.nk;
-        }
-        const int most = __reduce_max_sync(~0u, few);
-        if (most) {                         // (whole warps: rows of other segments take part with nothing)
-            const int head = (int)(r - row * p.heads), kv_head = head / p.group;
-            uint4 q = make_uint4(0, 0, 0, 0);
-            if (few && in_width) q = *reinterpret_cast<const uint4*>((const T*)p.q + (q_first + row) * p.q_row + head * p.q_head + lane * 8);
-            float sum = 0.f;
-            for (int j = 0; j < most; ++j) {
-                const Place at_key = j < few ? key_place(p, g, s, j) : Place{-1, 0};
-                uint4 k = make_uint4(0, 0, 0, 0), v = k;
-                if (at_key.at >= 0 && in_width) {
-                    k = *reinterpret_cast<const uint4*>((const T*)p.k + key_offset(p, at_key, kv_head) + lane * 8);
-                    v = *reinterpret_cast<const uint4*>((const T*)p.v + value_offset(p, at_key, kv_head) + lane * 8);
+    // the first blocks have rows of queries, the last ones of values (one block: both); where those of a block among `blocks` begin
+    const int v_block = (int)blockIdx.x - ((int)gridDim.x - v_blocks);
+    auto piece_begin = [&](long long n, int block, int blocks) { return min(quotient(n + (long long)blocks * ROWS - 1, (long long)blocks * ROWS) * ROWS * block, n); };
+    const int q_first = clamp_to(q_start[0], p.n_q), q_end = max(clamp_to(q_start[p.n_seg], p.n_q), q_first);
+    const long long q_rows = (long long)(q_end - q_first) * p.heads, q_from = piece_begin(q_rows, blockIdx.x, q_blocks), q_to = piece_begin(q_rows, blockIdx.x + 1, q_blocks);
+    if (q_from < q_to) {
+        Along at_seg;
+        at_seg.open(q_start, p.n_seg, q_first + (int)quotient(q_from, p.heads));
+        const int first_s = at_seg.s;
+        Segment g = segment_of(p, first_s, q_start, kv_start);
+        float top = 0.f;
+        for (long long r0 = q_from; r0 < q_to; r0 += ROWS) {        // whole warps stay together
+            const long long r = r0 + threadIdx.x / LANES, row = quotient(r, p.heads), at = (q_first + row) * p.heads + (r - row * p.heads);
+            uint4 a = make_uint4(0, 0, 0, 0), b = a;
+            float lse = 0.f;
+            int few = 0;
+            if (r < q_to) {
+                if (in_width) {
+                    a = *reinterpret_cast<const uint4*>((const T*)p.go + (q_first + row) * p.go_row + (r - row * p.heads) * p.go_head + lane * 8);
+                    b = *reinterpret_cast<const uint4*>((const T*)p.o + at * p.D + lane * 8);
                 }
-                const float score = fold(dot8<T>(q, k)), dp = fold(dot8<T>(a, v));
-                if (at_key.at >= 0) sum += ex2((score * p.scale - lse) * LOG2E_F) * dp;
+                lse = p.lse_in[at];
+                const int before = at_seg.s;
+                if (at_seg.go_on(q_start, p.n_seg, q_first + (int)row)) {
+                    if (NORMS && lane == 0) put_norm(w.norms + 2LL * before, top);
+                    top = 0.f;
+                    g = segment_of(p, at_seg.s, q_start, kv_start);
+                }
+                if (g.nk <= FEW_KEYS && lse != -INFINITY) few = g.nk;
             }
-            if (few) dot = sum;
+            float dot = fold(dot8<T>(a, b));
+            const float norm = NORMS ? fold(dot8<T>(a, a)) : 0.f;
+            const int most = __reduce_max_sync(~0u, few);
+            if (most) {                     // (whole warps: rows of other segments take part with nothing)
+                const int head = (int)(r - row * p.heads), kv_head = head / p.group;
+                uint4 q = make_uint4(0, 0, 0, 0);
+                if (few && in_width) q = *reinterpret_cast<const uint4*>((const T*)p.q + (q_first + row) * p.q_row + head * p.q_head + lane * 8);
+                float sum = 0.f;
+                for (int j = 0; j < most; ++j) {
+                    const Place at_key = j < few ? key_place(p, g, at_seg.s, j) : Place{-1, 0};
+                    uint4 k = make_uint4(0, 0, 0, 0), v = k;
+                    if (at_key.at >= 0 && in_width) {
+                        k = *reinterpret_cast<const uint4*>((const T*)p.k + key_offset(p, at_key, kv_head) + lane * 8);
+                        v = *reinterpret_cast<const uint4*>((const T*)p.v + value_offset(p, at_key, kv_head) + lane * 8);
+                    }
+                    const float score = fold(dot8<T>(q, k)), dp = fold(dot8<T>(a, v));
+                    if (at_key.at >= 0) sum += ex2((score * p.scale - lse) * LOG2E_F) * dp;
+                }
+                if (few) dot = sum;
+            }
+            if (r >= q_to) continue;
+            const bool reads = lse != -INFINITY;
+            if (lane == 0) w.stats[at] = make_float2(reads ? lse * LOG2E_F : INFINITY, reads ? dot : 0.f);
+            if (NORMS && reads) top = norm == norm ? fmaxf(top, norm) : INFINITY;
         }
-        if (r >= q_rows) continue;
-        const bool reads = lse != -INFINITY;
-        if (lane == 0) w.stats[at] = make_float2(reads ? lse * LOG2E_F : INFINITY, reads ? dot : 0.f);
-        if (NORMS && reads) top_go = norm == norm ? fmaxf(top_go, norm) : INFINITY;
+        if (NORMS) put_last_norms<LANES>(w.norms, at_seg.s, first_s, top);
     }
-    if (NORMS) {
-        const int k_first = clamp_to(p.kv_start[0], p.n_kv), k_end = max(clamp_to(p.kv_start[p.n_seg], p.n_kv), k_first);
-        const long long v_rows = (long long)(k_end - k_first) * p.kv_heads;
-        for (long long r0 = (long long)blockIdx.x * ROWS; r0 < v_rows; r0 += stride) {
-            const long long r = r0 + threadIdx.x / LANES, row = quotient(r, p.kv_heads);
-            uint4 a = make_uint4(0, 0, 0, 0);
-            if (r < v_rows && in_width && (!p.mask || p.mask[k_first + row]))
-                a = *reinterpret_cast<const uint4*>((const T*)p.v + (k_first + row) * p.v_row + (r - row * p.kv_heads) * p.v_head + lane * 8);
-            const float norm = fold(dot8<T>(a, a));
-            top_v = norm == norm ? fmaxf(top_v, norm) : INFINITY;
-        }
-#pragma unroll
-        for (int d = 16; d; d >>= 1) {
-            top_go = fmaxf(top_go, __shfl_xor_sync(~0u, top_go, d));
-            top_v = fmaxf(top_v, __shfl_xor_sync(~0u, top_v, d));
-        }
-        __shared__ float tops[2][PREP_THREADS / 32];
-        if (threadIdx.x % 32 == 0) { tops[0][threadIdx.x / 32] = top_go; tops[1][threadIdx.x / 32] = top_v; }
-        __syncthreads();
-        if (threadIdx.x < 2) {              // a maximum does not depend on the order
+    if (NORMS && v_block >= 0) {
+        const int k_first = clamp_to(kv_start[0], p.n_kv), k_end = max(clamp_to(kv_start[p.n_seg], p.n_kv), k_first);
+        const long long v_rows = (long long)(k_end - k_first) * p.kv_heads, v_from = piece_begin(v_rows, v_block, v_blocks), v_to = piece_begin(v_rows, v_block + 1, v_blocks);
+        if (v_from < v_to) {
+            Along at_seg;
+            at_seg.open(kv_start, p.n_seg, k_first + (int)quotient(v_from, p.kv_heads));
+            const int first_s = at_seg.s;
+            bool read = segment_of(p, first_s, q_start, kv_start).nq > 0;       // (what no row reads sets no scale)
             float top = 0.f;
-            for (int k = 0; k < PREP_THREADS / 32; ++k) top = fmaxf(top, tops[threadIdx.x][k]);
-            if (gridDim.x == 1) w.norms[threadIdx.x] = __float_as_uint(top);
-            else atomicMax(&w.norms[threadIdx.x], __float_as_uint(top));
+            constexpr int AHEAD = 4;            // rows of a thread under way (one: the kernel 33 us instead of 31, of 163840 rows of queries and 240000 of values, width 64)
+            for (long long r0 = v_from + threadIdx.x / LANES; r0 - threadIdx.x / LANES < v_to; r0 += AHEAD * ROWS) {
+                uint4 a[AHEAD];
+#pragma unroll
+                for (int k = 0; k < AHEAD; ++k) {
+                    const long long r = r0 + k * ROWS, row = quotient(r, p.kv_heads);
+                    a[k] = make_uint4(0, 0, 0, 0);
+                    if (r < v_to && in_width && (!p.mask || p.mask[k_first + row]))
+                        a[k] = *reinterpret_cast<const uint4*>((const T*)p.v + (k_first + row) * p.v_row + (r - row * p.kv_heads) * p.v_head + lane * 8);
+                }
+#pragma unroll
+                for (int k = 0; k < AHEAD; ++k) {
+                    const long long r = r0 + k * ROWS;
+                    const float norm = fold(dot8<T>(a[k], a[k]));
+                    if (r >= v_to) continue;
+                    const int before = at_seg.s;
+                    if (at_seg.go_on(kv_start, p.n_seg, k_first + (int)quotient(r, p.kv_heads))) {
+                        if (lane == 0) put_norm(w.norms + 2LL * before + 1, top);
+                        top = 0.f;
+                        read = segment_of(p, at_seg.s, q_start, kv_start).nq > 0;
+                    }
+                    if (read) top = norm == norm ? fmaxf(top, norm) : INFINITY;
+                }
+            }
+            put_last_norms<LANES>(w.norms + 1, at_seg.s, first_s, top);
         }
     }
 }
@@ -207,7 +261,13 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
     if (warp == BWD_WALKER) {
         if (lane == 0) {
             (KV ? w.kv_joints : w.q_joints)[block] = joint_of(walk, work_here, block);
-            items_hand_out(ctl.items, p, walk, work_here);
+            int of = -1;
+            float factor = 1.f;
+            auto factor_of = [&](int s) {
+                if (F16 && s != of) factor = gradient_factor(w.norms, of = s);
+                return factor;
+            };
+            items_hand_out(ctl.items, p, walk, work_here, A_MINUTE, factor_of);
         }
         __syncwarp();
     } else if (warp >= BWD_PRODUCER && warp < BWD_MMA) {
@@ -378,8 +438,7 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
         const int row = threadIdx.x & 127;
         const uint32_t S = s_at + lanes + 32 * x, dP = dp_at + lanes + 32 * x;
         const float scale2 = fmaxf(fabsf(p.scale) * LOG2E_F, 1e-30f);
-        const float factor = F16 ? gradient_factor(w.norms) : 1.f;
-        const f32x2 sc2 = dup2(scale2), ds2 = dup2(F16 ? factor * 0x1p-14f : 1.f);
+        const f32x2 sc2 = dup2(scale2);
         uint32_t steps = 0, items = 0;
         bool ok = true;
         for (;; ++items) {
@@ -388,6 +447,8 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
             const int n = item.i1 - item.i0, r = item.t * BWD_ROWS + row, n_rows = WorkCut::rows(p, item.segment());
             const bool valid = r < n_rows;
             const bool warp_on = (r & ~31) < n_rows;
+            const float factor = F16 ? item.factor : 1.f;
+            const f32x2 ds2 = dup2(F16 ? factor * 0x1p-14f : 1.f);
             f32x2 my_lse = 0, my_delta = 0;
             long long out_row = 0;
             bool masked = false;
@@ -532,7 +593,7 @@ __device__ __forceinline__ void sum_pass(const AttnParams& p, const BwdWork& w, 
     const Segment g = it.segment();
     const int first = j.first, rows = min(WorkCut::rows(p, g) - it.t * BWD_ROWS, BWD_ROWS), cap = KV ? w.kv_rows : w.q_rows;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const float factor = F16 ? gradient_factor(w.norms) : 1.f;
+    const float factor = F16 ? gradient_factor(w.norms, it.s) : 1.f;
     __shared__ float sh[SUM_WARPS][DP];
     const bool few = parts <= SUM_FEW;
     for (int rs = few ? blockIdx.y * SUM_WARPS + warp : blockIdx.y; rs < rows * SIDES; rs += few ? SUM_Y * SUM_WARPS : SUM_Y) {
@@ -588,10 +649,10 @@ __global__ void __launch_bounds__(SUM_WARPS * 32) attention_sum_kernel(const Att
     else sum_pass<T, DP, false>(p, w, (int)blockIdx.x - kv_blocks);
 }
 
-// clears the norms; counts the units of every segment where the blocks do not
-static __global__ void __launch_bounds__(PLAN_THREADS) backward_plan_kernel(const AttnParams p, const BwdWork w) {
+// clears the norms (fp16); counts the units of every segment where the blocks do not
+static __global__ void __launch_bounds__(PLAN_THREADS) backward_plan_kernel(const AttnParams p, const BwdWork w, const bool norms) {
     let_next_kernel_start();
-    if (blockIdx.x == 0 && threadIdx.x < 2) w.norms[threadIdx.x] = 0;
+    if (norms) for (int i = blockIdx.x * PLAN_THREADS + threadIdx.x; i < 2 * p.n_seg; i += 2 * PLAN_THREADS) w.norms[i] = 0;
     if (blockIdx.x == 0) { if (w.kv_start_unit) plan_units<KvCut>(p, w.kv_start_unit); }
     else if (w.q_start_unit) plan_units<QCut>(p, w.q_start_unit);
 }
@@ -607,7 +668,7 @@ static size_t backward_carve(const AttnParams& p, void* ws, BwdWork* w) {
     w->q_start_unit = counted_there ? nullptr : cv.take<long long>((size_t)p.n_seg + 1);
     w->kv_joints = cv.take<Joint>(MAX_SMS);
     w->q_joints = cv.take<Joint>(MAX_SMS);
-    w->norms = cv.take<uint32_t>(2);
+    w->norms = cv.take<uint32_t>(2 * (size_t)p.n_seg);
     w->stats = cv.take<float2>((size_t)p.n_q * p.heads);
     w->kv_part = cv.take<float>(slots * w->kv_rows * 2 * dp);
     w->q_part = cv.take<float>(slots * w->q_rows * dp);
@@ -624,17 +685,19 @@ static tiga_status launch_backward(AttnParams p, const BwdWork& w, cudaStream_t 
     const int kv_blocks = (p.gk || p.gv) && p.n_kv ? sms : 0, q_blocks = p.gq && p.n_q ? sms : 0;
     if (kv_blocks + q_blocks == 0) return TIGA_OK;
     TIGA_CUDA_TRY(cudaFuncSetAttribute(attention_backward_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, Bwd<DP>::SMEM));
-    const long long rows = (long long)p.n_q * p.heads + (operand_type<T>() == 0 ? (long long)p.n_kv * p.kv_heads : 0);
-    long long grid = (rows * (DP / 8) + PREP_THREADS - 1) / PREP_THREADS;
-    grid = grid < 1 ? 1 : grid < 8 * sms ? grid : 8 * sms;
-    // Little work is prepared by one block, which needs no cleared words to put its maxima into: a launch less (about 5 us of the
+    // blocks by the work there may be
+    const long long q_work = (long long)p.n_q * p.heads, v_work = operand_type<T>() == 0 ? (long long)p.n_kv * p.kv_heads / 2 : 0;
+    long long grid = ((q_work + v_work) * (DP / 8) + PREP_THREADS - 1) / PREP_THREADS;
+    // Little work is prepared by one block, which clears the words for its maxima itself: a launch less (about 5 us of the
     // host's time against 1 us for each 256 rows of 64 features).
-    if (grid <= PREP_ALONE) grid = 1;
+    grid = grid <= PREP_ALONE ? 1 : grid < PREP_BLOCKS * sms ? grid : PREP_BLOCKS * sms;
+    const int prep_v = !v_work ? 0 : grid == 1 ? 1 : (int)min(max(grid * v_work / (q_work + v_work), 1LL), grid - 1);
+    const int prep_q = grid == 1 ? 1 : (int)grid - prep_v;
     const bool plan = w.kv_start_unit || (operand_type<T>() == 0 && grid > 1);
     if (plan) {
-        backward_plan_kernel<<<counted(2), PLAN_THREADS, 0, s>>>(p, w);
-        TIGA_CUDA_TRY(launch_after(attention_prepare_kernel<T, DP / 8>, dim3((unsigned)grid), PREP_THREADS, 0, s, p, w));
-    } else attention_prepare_kernel<T, DP / 8><<<counted((unsigned)grid), PREP_THREADS, 0, s>>>(p, w);
+        backward_plan_kernel<<<counted(2), PLAN_THREADS, 0, s>>>(p, w, operand_type<T>() == 0);
+        TIGA_CUDA_TRY(launch_after(attention_prepare_kernel<T, DP / 8>, dim3((unsigned)grid), PREP_THREADS, 0, s, p, w, prep_q, prep_v));
+    } else attention_prepare_kernel<T, DP / 8><<<counted((unsigned)grid), PREP_THREADS, 0, s>>>(p, w, prep_q, prep_v);
     TIGA_CUDA_TRY(launch_after(attention_backward_kernel<T, DP>, dim3(kv_blocks + q_blocks), BWD_THREADS, Bwd<DP>::SMEM, s, p, w, maps, kv_blocks));
     TIGA_CUDA_TRY(launch_after(attention_sum_kernel<T, DP>, dim3(kv_blocks + q_blocks, SUM_Y), SUM_WARPS * 32, 0, s, p, w, kv_blocks));
     return launch_status();

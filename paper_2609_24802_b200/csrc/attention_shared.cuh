@@ -31,20 +31,22 @@ constexpr long long MOST_ROWS = 0x7fff0000LL;
 
 __device__ __forceinline__ int clamp_to(int v, int hi) { return min(max(v, 0), hi); }
 
-__device__ __forceinline__ Segment segment_of(const AttnParams& p, int s) {
+// (the bounds of rows and of dense keys: p.q_start and p.kv_start, or a copy of them)
+__device__ __forceinline__ Segment segment_of(const AttnParams& p, int s, const int32_t* q_start, const int32_t* kv_start) {
     Segment g;
-    g.q0 = clamp_to(p.q_start[s], p.n_q);
-    g.nq = max(clamp_to(p.q_start[s + 1], p.n_q) - g.q0, 0);
+    g.q0 = clamp_to(q_start[s], p.n_q);
+    g.nq = max(clamp_to(q_start[s + 1], p.n_q) - g.q0, 0);
     if (p.table) {
         g.k0 = 0;
         g.length = max(p.kv_len[s], 0);
         g.nk = (int)min(min((long long)g.length, p.max_pages * p.page_size), MOST_ROWS);
     } else {
-        g.k0 = clamp_to(p.kv_start[s], p.n_kv);
-        g.length = g.nk = max(clamp_to(p.kv_start[s + 1], p.n_kv) - g.k0, 0);
+        g.k0 = clamp_to(kv_start[s], p.n_kv);
+        g.length = g.nk = max(clamp_to(kv_start[s + 1], p.n_kv) - g.k0, 0);
     }
     return g;
 }
+__device__ __forceinline__ Segment segment_of(const AttnParams& p, int s) { return segment_of(p, s, p.q_start, p.kv_start); }
 
 // keys that row t of the segment's nq rows reads: [0, this)
 __device__ __forceinline__ int keys_of_row(const AttnParams& p, const Segment& g, int t) {
@@ -88,6 +90,42 @@ __device__ __forceinline__ int segment_of_row(const int32_t* start, int n_seg, i
     if (lo == 0 || i >= clamp_to(start[lo], n_rows)) return -1;
     return lo - 1;
 }
+
+// The last of n ascending places that is at most `v`, which start[0] is: by a warp with all its lanes, 32 places a round.
+template <typename V>
+__device__ __forceinline__ int last_place(const V* start, int n, V v) {
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int gap = (hi - lo + 31) / 32, at = lo + (int)(threadIdx.x % 32) * gap;
+        const unsigned before = __ballot_sync(~0u, at < hi && start[at] <= v) | 1u;
+        lo += (31 - __clz(before)) * gap;
+        hi = min(hi, lo + gap);
+    }
+    return lo;
+}
+
+// The segment of rows that come one behind the other.  A segment's end is kept; behind it the next one is sought in growing strides (there
+// may be many without rows in between).
+struct Along {
+    int s, end;
+    __device__ __forceinline__ void open(const int32_t* start, int n_seg, int row) {            // by a whole warp
+        s = last_place(start, n_seg, row);
+        end = s + 1 < n_seg ? start[s + 1] : INT32_MAX;
+    }
+    __device__ __forceinline__ bool go_on(const int32_t* start, int n_seg, int row) {           // true: to another segment
+        if (row < end) return false;
+        int lo = s + 1, hi = lo + 1;                // start[lo] <= row
+        while (hi < n_seg && start[hi] <= row) { const int step = 2 * (hi - lo); lo = hi; hi = lo + step; }
+        hi = min(hi, n_seg);
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (start[mid] <= row) lo = mid; else hi = mid;
+        }
+        s = lo;
+        end = s + 1 < n_seg ? start[s + 1] : INT32_MAX;
+        return true;
+    }
+};
 
 // ---- How the work is cut.  A segment's heads share keys, so the rows of a group's heads are packed: packed row r of a kv head is row
 // r / group, head kv_head * group + r % group.  A tile of stationary rows (packed rows, or keys for their gradients) meets the other
@@ -172,14 +210,7 @@ struct Walker {
         long long off = first_unit(block), mine = 0;
         left = first_unit(block + 1) - off;
         if (unit_start) {
-            int lo = 0, hi = p.n_seg;               // the last segment that begins at or before this unit: 32 places a round
-            while (hi - lo > 1) {
-                const int gap = (hi - lo + 31) / 32, at = lo + lane * gap;
-                const unsigned before = __ballot_sync(~0u, at < hi && unit_start[at] <= off);
-                lo += (31 - __clz(before)) * gap;
-                hi = min(hi, lo + gap);
-            }
-            s = lo;
+            s = last_place(unit_start, p.n_seg, off);           // the last segment that begins at or before this unit
             off -= unit_start[s];
             mine = unit_start[s + 1] - unit_start[s];
         } else {

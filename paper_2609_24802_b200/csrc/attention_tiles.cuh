@@ -40,6 +40,7 @@ __device__ __forceinline__ constexpr uint32_t piece(int k) { return ((k / 4) * (
 constexpr int ITEMS = 4;
 struct Item {
     int q0, nq, k0, nk, length, s, h, t, steps, i0, i1;     // as in Walker; steps 0: there are no more
+    float factor;                   // what the kernel says of its segment
     __device__ __forceinline__ Segment segment() const { return {q0, nq, k0, nk, length}; }
 };
 struct ItemRing {
@@ -53,15 +54,18 @@ __device__ __forceinline__ void items_init(ItemRing& r, int consumer_warps) {
     for (int i = 0; i < ITEMS; ++i) { mbar_init(smem_u32(&r.full[i]), 1); mbar_init(smem_u32(&r.empty[i]), consumer_warps); }
 }
 // Waits at most `limit` cycles for the return of an item; then there are no more, and every warp learns from which one on.
-template <typename W>
-__device__ __forceinline__ void items_hand_out(ItemRing& r, const AttnParams& p, W& it, bool more, long long limit = A_MINUTE) {
+struct NoFactor {
+    __device__ __forceinline__ float operator()(int) const { return 1.f; }
+};
+template <typename W, typename F = NoFactor>
+__device__ __forceinline__ void items_hand_out(ItemRing& r, const AttnParams& p, W& it, bool more, long long limit = A_MINUTE, F factor = F()) {
     for (uint32_t n = 0;; ++n) {
         if (n >= (uint32_t)ITEMS && !mbar_wait_for(smem_u32(&r.empty[n % ITEMS]), (n / ITEMS + 1) & 1, limit)) {
             __threadfence_block();
             *(volatile uint32_t*)&r.given_up = n;
             return;
         }
-        r.item[n % ITEMS] = {it.g.q0, it.g.nq, it.g.k0, it.g.nk, it.g.length, it.s, it.h, it.t, more ? it.steps : 0, it.i0, it.i1};
+        r.item[n % ITEMS] = {it.g.q0, it.g.nq, it.g.k0, it.g.nk, it.g.length, it.s, it.h, it.t, more ? it.steps : 0, it.i0, it.i1, more ? factor(it.s) : 1.f};
         mbar_arrive(smem_u32(&r.full[n % ITEMS]));
         if (!more) return;
         more = it.next(p);
@@ -75,7 +79,7 @@ struct Joint {
 template <typename C>
 __device__ __forceinline__ Joint joint_of(const Walker<C>& it, bool any, int block) {
     Joint j;
-    j.item = {it.g.q0, it.g.nq, it.g.k0, it.g.nk, it.g.length, it.s, it.h, it.t, it.steps, it.i0, it.i1};
+    j.item = {it.g.q0, it.g.nq, it.g.k0, it.g.nk, it.g.length, it.s, it.h, it.t, it.steps, it.i0, it.i1, 1.f};
     const bool ends = any && it.i0 > 0 && it.i1 == it.steps;
     j.first = ends ? it.first_block(block) : 0;
     j.parts = ends ? block - j.first + 1 : 0;
