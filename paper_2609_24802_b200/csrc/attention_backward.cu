@@ -96,6 +96,22 @@ __device__ __forceinline__ void put_last_norms(uint32_t* norms, int s, int first
         }
     } else if (threadIdx.x % LANES == 0) put_norm(norms + 2LL * s, top);
 }
+// Row and head of numbers that grow by one step after the other.  (With divisions for each of them the kernel took 33 us of 163840 rows of
+// queries and 240000 of values, fp16, width 64; now 22.)
+struct RowHead {
+    int row, head, rows, heads, of;         // rows, heads: of a step
+    __device__ __forceinline__ RowHead(long long r, int step, int n) : of(n) {
+        row = (int)quotient(r, n);
+        head = (int)(r - (long long)row * n);
+        rows = step / n;
+        heads = step - rows * n;
+    }
+    __device__ __forceinline__ void go_on() {
+        row += rows;
+        head += heads;
+        if (head >= of) { head -= of; ++row; }
+    }
+};
 template <typename T, int LANES>
 __global__ void __launch_bounds__(PREP_THREADS, PREP_BLOCKS) attention_prepare_kernel(const AttnParams p, const BwdWork w, const int q_blocks, const int v_blocks) {
     constexpr bool NORMS = operand_type<T>() == 0;
@@ -133,19 +149,20 @@ __global__ void __launch_bounds__(PREP_THREADS, PREP_BLOCKS) attention_prepare_k
         const int first_s = at_seg.s;
         Segment g = segment_of(p, first_s, q_start, kv_start);
         float top = 0.f;
-        for (long long r0 = q_from; r0 < q_to; r0 += ROWS) {        // whole warps stay together
-            const long long r = r0 + threadIdx.x / LANES, row = quotient(r, p.heads), at = (q_first + row) * p.heads + (r - row * p.heads);
+        RowHead here(q_from + threadIdx.x / LANES, ROWS, p.heads);
+        for (long long r0 = q_from; r0 < q_to; r0 += ROWS, here.go_on()) {          // whole warps stay together
+            const long long r = r0 + threadIdx.x / LANES, row = q_first + here.row, at = row * p.heads + here.head;
             uint4 a = make_uint4(0, 0, 0, 0), b = a;
             float lse = 0.f;
             int few = 0;
             if (r < q_to) {
                 if (in_width) {
-                    a = *reinterpret_cast<const uint4*>((const T*)p.go + (q_first + row) * p.go_row + (r - row * p.heads) * p.go_head + lane * 8);
+                    a = *reinterpret_cast<const uint4*>((const T*)p.go + row * p.go_row + here.head * p.go_head + lane * 8);
                     b = *reinterpret_cast<const uint4*>((const T*)p.o + at * p.D + lane * 8);
                 }
                 lse = p.lse_in[at];
                 const int before = at_seg.s;
-                if (at_seg.go_on(q_start, p.n_seg, q_first + (int)row)) {
+                if (at_seg.go_on(q_start, p.n_seg, (int)row)) {
                     if (NORMS && lane == 0) put_norm(w.norms + 2LL * before, top);
                     top = 0.f;
                     g = segment_of(p, at_seg.s, q_start, kv_start);
@@ -156,9 +173,9 @@ __global__ void __launch_bounds__(PREP_THREADS, PREP_BLOCKS) attention_prepare_k
             const float norm = NORMS ? fold(dot8<T>(a, a)) : 0.f;
             const int most = __reduce_max_sync(~0u, few);
             if (most) {                     // (whole warps: rows of other segments take part with nothing)
-                const int head = (int)(r - row * p.heads), kv_head = head / p.group;
+                const int kv_head = here.head / p.group;
                 uint4 q = make_uint4(0, 0, 0, 0);
-                if (few && in_width) q = *reinterpret_cast<const uint4*>((const T*)p.q + (q_first + row) * p.q_row + head * p.q_head + lane * 8);
+                if (few && in_width) q = *reinterpret_cast<const uint4*>((const T*)p.q + row * p.q_row + here.head * p.q_head + lane * 8);
                 float sum = 0.f;
                 for (int j = 0; j < most; ++j) {
                     const Place at_key = j < few ? key_place(p, g, at_seg.s, j) : Place{-1, 0};
@@ -188,23 +205,24 @@ __global__ void __launch_bounds__(PREP_THREADS, PREP_BLOCKS) attention_prepare_k
             const int first_s = at_seg.s;
             bool read = segment_of(p, first_s, q_start, kv_start).nq > 0;       // (what no row reads sets no scale)
             float top = 0.f;
-            constexpr int AHEAD = 4;            // rows of a thread under way (one: the kernel 33 us instead of 31, of 163840 rows of queries and 240000 of values, width 64)
-            for (long long r0 = v_from + threadIdx.x / LANES; r0 - threadIdx.x / LANES < v_to; r0 += AHEAD * ROWS) {
+            constexpr int AHEAD = 4;            // rows of a thread under way
+            RowHead here(v_from + threadIdx.x / LANES, ROWS, p.kv_heads);
+            for (long long r0 = v_from; r0 < v_to; r0 += AHEAD * ROWS) {
                 uint4 a[AHEAD];
+                int rows[AHEAD];
 #pragma unroll
-                for (int k = 0; k < AHEAD; ++k) {
-                    const long long r = r0 + k * ROWS, row = quotient(r, p.kv_heads);
+                for (int k = 0; k < AHEAD; ++k, here.go_on()) {
+                    rows[k] = r0 + k * ROWS + threadIdx.x / LANES < v_to ? k_first + here.row : -1;
                     a[k] = make_uint4(0, 0, 0, 0);
-                    if (r < v_to && in_width && (!p.mask || p.mask[k_first + row]))
-                        a[k] = *reinterpret_cast<const uint4*>((const T*)p.v + (k_first + row) * p.v_row + (r - row * p.kv_heads) * p.v_head + lane * 8);
+                    if (rows[k] >= 0 && in_width && (!p.mask || p.mask[rows[k]]))
+                        a[k] = *reinterpret_cast<const uint4*>((const T*)p.v + rows[k] * p.v_row + here.head * p.v_head + lane * 8);
                 }
 #pragma unroll
                 for (int k = 0; k < AHEAD; ++k) {
-                    const long long r = r0 + k * ROWS;
                     const float norm = fold(dot8<T>(a[k], a[k]));
-                    if (r >= v_to) continue;
+                    if (rows[k] < 0) continue;
                     const int before = at_seg.s;
-                    if (at_seg.go_on(kv_start, p.n_seg, k_first + (int)quotient(r, p.kv_heads))) {
+                    if (at_seg.go_on(kv_start, p.n_seg, rows[k])) {
                         if (lane == 0) put_norm(w.norms + 2LL * before + 1, top);
                         top = 0.f;
                         read = segment_of(p, at_seg.s, q_start, kv_start).nq > 0;
@@ -447,7 +465,7 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
             const int n = item.i1 - item.i0, r = item.t * BWD_ROWS + row, n_rows = WorkCut::rows(p, item.segment());
             const bool valid = r < n_rows;
             const bool warp_on = (r & ~31) < n_rows;
-            const float factor = F16 ? item.factor : 1.f;
+            const float factor = F16 ? ctl.items.factor[items % ITEMS] : 1.f;
             const f32x2 ds2 = dup2(F16 ? factor * 0x1p-14f : 1.f);
             f32x2 my_lse = 0, my_delta = 0;
             long long out_row = 0;
@@ -685,7 +703,7 @@ static tiga_status launch_backward(AttnParams p, const BwdWork& w, cudaStream_t 
     const int kv_blocks = (p.gk || p.gv) && p.n_kv ? sms : 0, q_blocks = p.gq && p.n_q ? sms : 0;
     if (kv_blocks + q_blocks == 0) return TIGA_OK;
     TIGA_CUDA_TRY(cudaFuncSetAttribute(attention_backward_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, Bwd<DP>::SMEM));
-    // blocks by the work there may be
+    // blocks by the work there may be: a row of values costs about half of one of queries
     const long long q_work = (long long)p.n_q * p.heads, v_work = operand_type<T>() == 0 ? (long long)p.n_kv * p.kv_heads / 2 : 0;
     long long grid = ((q_work + v_work) * (DP / 8) + PREP_THREADS - 1) / PREP_THREADS;
     // Little work is prepared by one block, which clears the words for its maxima itself: a launch less (about 5 us of the

@@ -40,13 +40,13 @@ __device__ __forceinline__ constexpr uint32_t piece(int k) { return ((k / 4) * (
 constexpr int ITEMS = 4;
 struct Item {
     int q0, nq, k0, nk, length, s, h, t, steps, i0, i1;     // as in Walker; steps 0: there are no more
-    float factor;                   // what the kernel says of its segment
     __device__ __forceinline__ Segment segment() const { return {q0, nq, k0, nk, length}; }
 };
 struct ItemRing {
     unsigned long long full[ITEMS], empty[ITEMS];
     Item item[ITEMS], none;         // none: in place of the items that were not handed out
     uint32_t given_up;              // the first of these
+    float factor[ITEMS];            // what the kernel says of an item's segment (apart from the items, whose twelfth word would change how all warps load them)
 };
 __device__ __forceinline__ void items_init(ItemRing& r, int consumer_warps) {
     r.none.steps = 0;
@@ -65,7 +65,8 @@ __device__ __forceinline__ void items_hand_out(ItemRing& r, const AttnParams& p,
             *(volatile uint32_t*)&r.given_up = n;
             return;
         }
-        r.item[n % ITEMS] = {it.g.q0, it.g.nq, it.g.k0, it.g.nk, it.g.length, it.s, it.h, it.t, more ? it.steps : 0, it.i0, it.i1, more ? factor(it.s) : 1.f};
+        r.item[n % ITEMS] = {it.g.q0, it.g.nq, it.g.k0, it.g.nk, it.g.length, it.s, it.h, it.t, more ? it.steps : 0, it.i0, it.i1};
+        if (more) r.factor[n % ITEMS] = factor(it.s);
         mbar_arrive(smem_u32(&r.full[n % ITEMS]));
         if (!more) return;
         more = it.next(p);
@@ -79,7 +80,7 @@ struct Joint {
 template <typename C>
 __device__ __forceinline__ Joint joint_of(const Walker<C>& it, bool any, int block) {
     Joint j;
-    j.item = {it.g.q0, it.g.nq, it.g.k0, it.g.nk, it.g.length, it.s, it.h, it.t, it.steps, it.i0, it.i1, 1.f};
+    j.item = {it.g.q0, it.g.nq, it.g.k0, it.g.nk, it.g.length, it.s, it.h, it.t, it.steps, it.i0, it.i1};
     const bool ends = any && it.i0 > 0 && it.i1 == it.steps;
     j.first = ends ? it.first_block(block) : 0;
     j.parts = ends ? block - j.first + 1 : 0;
