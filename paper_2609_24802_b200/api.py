@@ -671,9 +671,21 @@ def _type_of(t, types):
     return types[t.dtype]
 
 
-class DenseRelation:
+class _Held:
+    """A descriptor holds the addresses of the arrays that it was made of.  They may be written into; another array in the place of one
+    would leave the old address behind, so it takes a new descriptor."""
+    _held = ()
+
+    def __setattr__(self, name, value):
+        if name in self._held and value is not self.__dict__.get(name):
+            raise AttributeError(f"{type(self).__name__}.{name} is what the descriptor was made of: write into it, or make another {type(self).__name__}")
+        self.__dict__[name] = value
+
+
+class DenseRelation(_Held):
     """Block-diagonal dense relation: the rows [q_start[s], q_start[s+1]) read the keys [kv_start[s], kv_start[s+1]) of their
     segment, those that `mask` (bool or uint8 [n_kv], optional) leaves."""
+    _held = ("q_start", "kv_start", "mask")
 
     def __init__(self, q_start, kv_start, mask=None):
         _ints(q_start, None, "q_start")
@@ -683,9 +695,8 @@ class DenseRelation:
         if mask is not None and (mask.dtype not in (torch.bool, torch.uint8) or mask.dim() != 1 or not mask.is_contiguous()):
             raise ValueError("mask must be a contiguous bool or uint8 array")
         _same(q_start, kv_start, mask)
-        self.q_start, self.kv_start, self.mask = q_start, kv_start, mask
-        self.q_ptr, self.kv_ptr, self.mask_ptr = q_start.data_ptr(), kv_start.data_ptr(), 0 if mask is None else mask.data_ptr()
-        self.n_seg = q_start.numel() - 1
+        self.__dict__.update(q_start=q_start, kv_start=kv_start, mask=mask, q_ptr=q_start.data_ptr(), kv_ptr=kv_start.data_ptr(),
+                             mask_ptr=0 if mask is None else mask.data_ptr(), n_seg=q_start.numel() - 1)
 
 
 def _dense_args(g, q, key, value, scale, grad_out=None):
@@ -751,9 +762,10 @@ def tiga_apply_dense_attention_backward(g: DenseRelation, q, key, value, out, ls
     return grad_q, grad_key, grad_value, ws
 
 
-class PagedCache:
+class PagedCache(_Held):
     """Keys and values in pages: key and value [n_pages, page_size, kv_heads, D] with equal strides, table int32 [n_seg, max_pages]
     (entries outside [0, n_pages) name no page), kv_len int32 [n_seg]: tokens in the cache, the current chunk's included."""
+    _held = ("key", "value", "table", "kv_len")
 
     def __init__(self, key, value, table, kv_len):
         if key.dim() != 4 or key.shape != value.shape or key.dtype != value.dtype or key.dtype not in _HALF:
@@ -767,11 +779,9 @@ class PagedCache:
         n_seg, max_pages = table.shape
         _ints(kv_len, n_seg, "kv_len")
         _same(key, value, table, kv_len)
-        self.key, self.value, self.table, self.kv_len = key, value, table, kv_len
-        self.n_seg = n_seg
-        self.c = _PAGES_OF(_PAGES_BYTES.pack(key.data_ptr(), value.data_ptr(), table.data_ptr(), kv_len.data_ptr(), n_seg, shape[0], shape[1],
-                                             _step(table, 0), max_pages, step[0], step[1], step[2]))
-        self.ref = ctypes.byref(self.c)
+        c = _PAGES_OF(_PAGES_BYTES.pack(key.data_ptr(), value.data_ptr(), table.data_ptr(), kv_len.data_ptr(), n_seg, shape[0], shape[1],
+                                        _step(table, 0), max_pages, step[0], step[1], step[2]))
+        self.__dict__.update(key=key, value=value, table=table, kv_len=kv_len, n_seg=n_seg, c=c, ref=ctypes.byref(c))
 
 
 def _paged_heads(cache, q, scale):
@@ -815,14 +825,15 @@ def tiga_rotary_frequencies(turned: int, base: float = 10000.0, scaling: int = R
     return freq, m.value
 
 
-class Rotary:
+class Rotary(_Held):
     """Descriptor of rotary positions: freq float64 [turned / 2] on the device, the layout of the pairs (halves, or interleaved with
     pairs=True) and the magnitude."""
+    _held = ("freq",)
 
     def __init__(self, freq, pairs=False, magnitude=1.0):
         if freq.dtype != torch.float64 or freq.dim() != 1 or not freq.is_cuda or not freq.is_contiguous():
             raise ValueError("freq must be a contiguous float64 CUDA array")
-        self.freq = freq
+        self.__dict__["freq"] = freq
         self.c = _Rotary(freq.data_ptr(), 2 * freq.numel(), ROT_PAIRS if pairs else ROT_HALVES, magnitude)
         self.ref = ctypes.byref(self.c)
 

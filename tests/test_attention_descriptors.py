@@ -49,3 +49,22 @@ def test_a_table_with_entries_needs_an_address(api):
         return L.tiga_apply_paged_attention(ref(c), ref(h), 256, 256, 10, 1, 256, 256, 256, size, None)
     assert call(4, None, 1 << 40) == 1 and call(4, 258, 1 << 40) == 1
     assert call(0, None, 16) == 3               # goes on to the next check: the workspace is too small
+
+
+def test_arrays_of_a_descriptor_are_written_into_not_replaced(api):
+    """The descriptor keeps addresses: with another array in its place it would go on reading the old one."""
+    cache = api.PagedCache(pages(), pages(), *places())
+    for name in ("key", "value", "table", "kv_len"):
+        with pytest.raises(AttributeError):
+            setattr(cache, name, getattr(cache, name).clone())
+    kv_len = cache.kv_len
+    cache.kv_len += 3
+    cache.kv_len[0] += 1
+    assert cache.kv_len is kv_len and kv_len.tolist() == [4] and cache.c.kv_len == kv_len.data_ptr()
+    start = torch.tensor([0, 4], dtype=torch.int32)
+    relation = api.DenseRelation(start, start.clone())
+    for name, other in (("q_start", start.clone()), ("kv_start", start), ("mask", torch.ones(4, dtype=torch.bool))):
+        with pytest.raises(AttributeError):
+            setattr(relation, name, other)
+    relation.note = cache.note = "anything else may be kept here"
+    assert relation.q_start is start and relation.mask is None
