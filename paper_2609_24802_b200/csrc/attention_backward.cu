@@ -704,7 +704,7 @@ static tiga_status launch_backward(AttnParams p, const BwdWork& w, cudaStream_t 
     if (kv_blocks + q_blocks == 0) return TIGA_OK;
     TIGA_CUDA_TRY(cudaFuncSetAttribute(attention_backward_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, Bwd<DP>::SMEM));
     // blocks by the work there may be: a row of values costs about half of one of queries
-    const long long q_work = (long long)p.n_q * p.heads, v_work = operand_type<T>() == 0 ? (long long)p.n_kv * p.kv_heads / 2 : 0;
+    const long long q_work = (long long)p.n_q * p.heads, v_work = operand_type<T>() == 0 ? ((long long)p.n_kv * p.kv_heads + 1) / 2 : 0;
     long long grid = ((q_work + v_work) * (DP / 8) + PREP_THREADS - 1) / PREP_THREADS;
     // Little work is prepared by one block, which clears the words for its maxima itself: a launch less (about 5 us of the
     // host's time against 1 us for each 256 rows of 64 features).
