@@ -374,7 +374,9 @@ tiga_status tiga_apply_csr_attention(const tiga_csr* g, const float* q, const fl
  * lengths.  Bounds are clamped to the arrays, so no bound leads outside of them.  A row that reads no key yields the zero vector
  * and lse = -inf, and zero gradients.  Rows outside of every segment (in front of start[0], behind start[n_seg]) are not
  * touched, in outputs and gradients alike.  What lies in keys that no row of the segment reads (masked keys, places behind
- * the last key of a page), NaN and infinities included, has no influence.  No atomics on results: they are reproducible.
+ * the last key of a page, all keys of a segment without rows), NaN and infinities included, has no influence.  (An infinity or
+ * NaN in a key or value that some rows of a segment read may also reach those of its rows that do not: a weight of zero times
+ * it is NaN.)  No atomics on results: they are reproducible.
  * A workspace belongs to one call at a time.  A block that waits about two seconds for one of its own copies or products in vain
  * leaves NaN in the rows that it did not finish. */
 typedef struct { int64_t row, head; } tiga_stride;

@@ -14,7 +14,7 @@ namespace tiga {
 // streams that take turns: while the threads turn S into P, dP and the last step's grad_key are formed; while they turn dP into dS,
 // grad_value and the next step's S.
 // A step of 128 lasts about 3480 cycles (products 2048 or 1536, exponentials 1024, the threads' two turns 2200): 4 segments of 4096 rows
-// and keys, 16/4 heads of 128, bf16: 1.70 ms for both passes.
+// and keys, 16/4 heads of 128, bf16: 1.70 ms alone for both passes.
 // fp16: P carries 2^14 and dS a power of two from the largest norms of the segment's rows of grad_out and value, which bound |dP - delta|:
 // the largest value cannot overflow, the smallest keep as many digits as there are.
 constexpr int BWD_WEIGHT_WARPS = 16, BWD_PRODUCER = BWD_WEIGHT_WARPS, BWD_MMA = BWD_PRODUCER + 4, BWD_WALKER = BWD_MMA + 1;

@@ -16,8 +16,8 @@ namespace tiga {
 // and the mass carries the same factor.
 // What bounds it: the chain S -> maximum -> P -> O of a half, 4050 cycles a step of 128 keys at a width of 128 where its products take
 // 1024 and its 16384 exponentials another 1024.  Two threads a row halve what one would take (a warp alone on its scheduler needs
-// about 13 cycles a column); the exchange of their maxima costs 100.  4 segments of 4096 rows and keys, 16/4 heads of 128, bf16: 543 us,
-// 1.0 PFLOP/s; single tokens read their cache at 6.3 TB/s between the ends of items.
+// about 13 cycles a column); the exchange of their maxima costs 100.  4 segments of 4096 rows and keys, 16/4 heads of 128, bf16: 543 us
+// alone, 1.0 PFLOP/s; single tokens read their cache at 6.3 TB/s between the ends of items.
 constexpr int FWD_SOFTMAX_WARPS = 16, FWD_PRODUCER = FWD_SOFTMAX_WARPS, FWD_MMA = FWD_PRODUCER + 4, FWD_WALKER = FWD_MMA + 1;
 constexpr int FWD_THREADS = 32 * (FWD_WALKER + 1), FWD_ROWS = 256, FWD_STEP = 128;
 typedef Cut<FWD_ROWS, FWD_STEP, false> FwdCut;

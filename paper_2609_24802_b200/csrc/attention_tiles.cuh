@@ -53,10 +53,10 @@ __device__ __forceinline__ void items_init(ItemRing& r, int consumer_warps) {
     r.given_up = ~0u;
     for (int i = 0; i < ITEMS; ++i) { mbar_init(smem_u32(&r.full[i]), 1); mbar_init(smem_u32(&r.empty[i]), consumer_warps); }
 }
-// Waits at most `limit` cycles for the return of an item; then there are no more, and every warp learns from which one on.
 struct NoFactor {
     __device__ __forceinline__ float operator()(int) const { return 1.f; }
 };
+// Waits at most `limit` cycles for the return of an item; then there are no more, and every warp learns from which one on.
 template <typename W, typename F = NoFactor>
 __device__ __forceinline__ void items_hand_out(ItemRing& r, const AttnParams& p, W& it, bool more, long long limit = A_MINUTE, F factor = F()) {
     for (uint32_t n = 0;; ++n) {

@@ -1,8 +1,8 @@
 // Rotary positions, on their own and on the way into the pages of a cache.
 //
 // A pair (a, b) of features at position n is turned by t = n f: (a cos t - b sin t, a sin t + b cos t).  The work is bound by
-// memory: every element is read and written once, the turn costs six operations per pair, its sine and cosine once per
-// (row, pair) and thread, kept in registers for the thread's heads.
+// memory: every element is read and written once, the turn costs six operations per pair, its sine and cosine are formed once per
+// (row, pair) of a block and lie in shared memory for the row's heads.
 // t is a number of turns in 64-bit fixed point: f / 2 pi without its whole turns, times the position, modulo 2^64.  Whole turns drop
 // out by themselves, and position 2^22 keeps an error of 2^22 2^-54 turns; the upper 32 bits, at most half a turn either way, enter
 // sincospif in fp32.  (In fp32 the product alone is off by 2^22 2^-24 / 2 turns: the angle would mean nothing.  Formed once per row and
