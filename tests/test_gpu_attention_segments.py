@@ -132,3 +132,33 @@ def test_many_segments_of_many_sizes_in_f16(tiga, n):
             for name, (i, j) in (("grad_q", (q0, q0 + a)), ("grad_key", (k0, k0 + b)), ("grad_value", (k0, k0 + b))):
                 close(got[name][i:j], want[name], want[name + "_tol"], f"{name} of segment {s}")
         k0 += b
+
+
+@pytest.mark.parametrize("rows,keys,heads", [(60, 90, 2), (700, 900, 4)])
+def test_graph_replays_start_from_no_norms_in_f16(tiga, rows, keys, heads):
+    """One captured step, replayed with large gradients and then with small ones, bit for bit as eager calls: in one block, and where a
+    kernel in front clears the norms."""
+    a = case([rows, rows], [keys, keys], heads, heads, 64, F16, seed=51)
+    b = case([rows + 30, rows - 30], [keys - 11, keys + 11], heads, heads, 64, F16, seed=52)
+    b["go"] = (b["go"].float() * 2.0 ** -12).to(F16)
+    qs, ks = starts(a["q_len"]), starts(a["kv_len"])
+    x = {n: a[n].clone() for n in ("q", "k", "v", "go")}
+    g = tiga.DenseRelation(qs, ks)
+
+    def step():
+        out, lse, ws = tiga.tiga_apply_dense_attention(g, x["q"], x["k"], x["v"], a["scale"])
+        return out, lse, *tiga.tiga_apply_dense_attention_backward(g, x["q"], x["k"], x["v"], out, lse, x["go"], a["scale"]), ws
+    step()
+    torch.cuda.synchronize()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=side):
+        got = step()
+    for c in (a, b, a, b):
+        qs.copy_(starts(c["q_len"]))
+        ks.copy_(starts(c["kv_len"]))
+        for n in x:
+            x[n].copy_(c[n])
+        graph.replay()
+        want = run(tiga, c)
+        for t, name in zip(got, ("out", "lse", "grad_q", "grad_key", "grad_value")):
+            assert torch.equal(t, want[name]), name
