@@ -419,6 +419,18 @@ tiga_status tiga_apply_dense_attention_backward(const tiga_dense* g, const tiga_
                                                 void* grad_q, void* grad_key, void* grad_value,
                                                 void* ws, size_t ws_bytes, void* stream);
 
+/* The same reducer over a triangular relation (causal attention): row t of the n rows of segment s reads, of its m keys, those up to
+ * m - n + t (the rows are the segment's last ones: with as many keys as rows each reads up to its own place), of which kv_mask leaves
+ * out more.  Rows in front of the first key (n > m) read nothing.  Packed sequences of different lengths are segments.  Arguments,
+ * outputs, gradients and workspace as above; scores of rows that read a single key have no gradient in grad_q. */
+size_t tiga_triangular_attention_workspace_bytes(const tiga_dense* g, const tiga_heads* h, int backward);
+tiga_status tiga_apply_triangular_attention(const tiga_dense* g, const tiga_heads* h, const void* q, const void* key, const void* value,
+                                            void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+tiga_status tiga_apply_triangular_attention_backward(const tiga_dense* g, const tiga_heads* h, const void* q, const void* key,
+                                                     const void* value, const void* out, const float* lse, const void* grad_out,
+                                                     void* grad_q, void* grad_key, void* grad_value,
+                                                     void* ws, size_t ws_bytes, void* stream);
+
 /* Keys and values in the pages of a cache: position p of sequence s lies in slot p % page_size of page
  * table[s * table_stride + p / page_size].  Element (page, slot, head, d) of either array lies at
  * page * page_stride + slot * slot_stride + head * head_stride + d, in elements.  A table entry outside [0, n_pages)

@@ -24,7 +24,8 @@ __all__ = [
     "tiga_apply_radius_mlp_backward", "tiga_knn_workspace_bytes", "tiga_apply_knn",
     "tiga_csr_attention_workspace_bytes", "tiga_apply_csr_attention", "launch_count",
     "BF16", "DenseRelation", "tiga_dense_attention_workspace_bytes", "tiga_apply_dense_attention",
-    "tiga_apply_dense_attention_backward", "PagedCache", "tiga_paged_attention_workspace_bytes", "tiga_apply_paged_attention",
+    "tiga_apply_dense_attention_backward", "TriangularRelation", "tiga_triangular_attention_workspace_bytes",
+    "tiga_apply_triangular_attention", "tiga_apply_triangular_attention_backward", "PagedCache", "tiga_paged_attention_workspace_bytes", "tiga_apply_paged_attention",
     "tiga_paged_append", "ROT_PLAIN", "ROT_LINEAR", "ROT_BASE", "ROT_BANDS", "tiga_rotary_frequencies", "Rotary", "tiga_apply_rotary",
 ]
 
@@ -44,6 +45,7 @@ EXPORTS = [
     "tiga_apply_radius_backward", "tiga_apply_radius_mlp", "tiga_apply_radius_mlp_backward",
     "tiga_knn_workspace_bytes", "tiga_apply_knn", "tiga_csr_attention_workspace_bytes", "tiga_apply_csr_attention",
     "tiga_dense_attention_workspace_bytes", "tiga_apply_dense_attention", "tiga_apply_dense_attention_backward",
+    "tiga_triangular_attention_workspace_bytes", "tiga_apply_triangular_attention", "tiga_apply_triangular_attention_backward",
     "tiga_paged_attention_workspace_bytes", "tiga_apply_paged_attention", "tiga_paged_append", "tiga_rotary_frequencies", "tiga_apply_rotary",
 ]
 
@@ -183,6 +185,12 @@ def load_library() -> ctypes.CDLL:
     lib.tiga_apply_dense_attention.argtypes = [ref(_Dense), ref(_Heads), vp, vp, vp, vp, vp, vp, sz, vp]
     lib.tiga_apply_dense_attention_backward.restype = ctypes.c_int
     lib.tiga_apply_dense_attention_backward.argtypes = [ref(_Dense), ref(_Heads), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.tiga_triangular_attention_workspace_bytes.restype = sz
+    lib.tiga_triangular_attention_workspace_bytes.argtypes = lib.tiga_dense_attention_workspace_bytes.argtypes
+    lib.tiga_apply_triangular_attention.restype = ctypes.c_int
+    lib.tiga_apply_triangular_attention.argtypes = lib.tiga_apply_dense_attention.argtypes
+    lib.tiga_apply_triangular_attention_backward.restype = ctypes.c_int
+    lib.tiga_apply_triangular_attention_backward.argtypes = lib.tiga_apply_dense_attention_backward.argtypes
     lib.tiga_paged_attention_workspace_bytes.restype = sz
     lib.tiga_paged_attention_workspace_bytes.argtypes = [ref(_Pages), ref(_Heads), i64]
     lib.tiga_apply_paged_attention.restype = ctypes.c_int
@@ -682,9 +690,7 @@ class _Held:
         self.__dict__[name] = value
 
 
-class DenseRelation(_Held):
-    """Block-diagonal dense relation: the rows [q_start[s], q_start[s+1]) read the keys [kv_start[s], kv_start[s+1]) of their
-    segment, those that `mask` (bool or uint8 [n_kv], optional) leaves."""
+class _Segments(_Held):
     _held = ("q_start", "kv_start", "mask")
 
     def __init__(self, q_start, kv_start, mask=None):
@@ -699,7 +705,23 @@ class DenseRelation(_Held):
                              mask_ptr=0 if mask is None else mask.data_ptr(), n_seg=q_start.numel() - 1)
 
 
-def _dense_args(g, q, key, value, scale, grad_out=None):
+class DenseRelation(_Segments):
+    """Block-diagonal dense relation: the rows [q_start[s], q_start[s+1]) read the keys [kv_start[s], kv_start[s+1]) of their
+    segment, those that `mask` (bool or uint8 [n_kv], optional) leaves."""
+
+
+class TriangularRelation(_Segments):
+    """Block-diagonal triangular relation (causal attention of packed sequences): row t of the n rows [q_start[s], q_start[s+1]) reads, of
+    the m keys [kv_start[s], kv_start[s+1]), those up to m - n + t that `mask` leaves.  Without kv_start rows and keys have the same
+    segments."""
+
+    def __init__(self, q_start, kv_start=None, mask=None):
+        super().__init__(q_start, q_start if kv_start is None else kv_start, mask)
+
+
+def _dense_args(g, q, key, value, scale, grad_out=None, kind=DenseRelation):
+    if type(g) is not kind and not isinstance(g, kind):
+        raise TypeError(f"the relation must be a {kind.__name__}")
     dt, dtype, shape = _type_of(q, _HALF), q.dtype, q.shape
     n_q, heads, D = shape
     if key.dim() != 3:
@@ -714,36 +736,24 @@ def _dense_args(g, q, key, value, scale, grad_out=None):
     return _DENSE_OF(_DENSE_BYTES.pack(g.q_ptr, g.kv_ptr, g.mask_ptr, g.n_seg, n_q, n_kv)), h
 
 
-def tiga_dense_attention_workspace_bytes(g: DenseRelation, q, key, value, backward: bool = False) -> int:
-    c, h = _dense_args(g, q, key, value, 1.0)
-    return int(_L.tiga_dense_attention_workspace_bytes(ctypes.byref(c), ctypes.byref(h), int(backward)))
-
-
-def tiga_apply_dense_attention(g: DenseRelation, q, key, value, scale: float, out=None, lse=None, want_lse=True, ws=None, stream=None):
-    """out[i,h] = sum_j softmax_j(scale <q[i,h], key[j,h']>) value[j,h'] over the keys of the row's segment, h' the head of h's
-    group.  q [n_q, heads, D], key and value [n_kv, kv_heads, D], fp16 or bf16, rows and heads strided.  Returns (out, lse, ws)."""
+def _segments_forward(name, size, call, kind, g, q, key, value, scale, out, lse, want_lse, ws, stream):
     with _on(q, stream):
-        c, h = _dense_args(g, q, key, value, scale)
+        c, h = _dense_args(g, q, key, value, scale, None, kind)
         if out is None:
             out = q.new_empty(q.shape)
         if want_lse and lse is None:
             lse = q.new_empty(q.shape[:2], dtype=torch.float32)
         _same(q, out, lse, ws)
         if ws is None:
-            ws = _scratch(_L.tiga_dense_attention_workspace_bytes(ctypes.byref(c), ctypes.byref(h), 0), q)
-        _ok(_L.tiga_apply_dense_attention(ctypes.byref(c), ctypes.byref(h), q.data_ptr(), key.data_ptr(), value.data_ptr(),
-                                          _dense_out(out, q.shape, q.dtype, "out"),
-                                          None if lse is None else _dense_out(lse, q.shape[:2], torch.float32, "lse"),
-                                          _ptr(ws), ws.numel(), _stream(stream)), "tiga_apply_dense_attention")
+            ws = _scratch(size(ctypes.byref(c), ctypes.byref(h), 0), q)
+        _ok(call(ctypes.byref(c), ctypes.byref(h), q.data_ptr(), key.data_ptr(), value.data_ptr(), _dense_out(out, q.shape, q.dtype, "out"),
+                 None if lse is None else _dense_out(lse, q.shape[:2], torch.float32, "lse"), _ptr(ws), ws.numel(), _stream(stream)), name)
     return out, lse, ws
 
 
-def tiga_apply_dense_attention_backward(g: DenseRelation, q, key, value, out, lse, grad_out, scale: float, grad_q=None, grad_key=None,
-                                        grad_value=None, want_q=True, want_kv=True, ws=None, stream=None):
-    """Reverse mode of tiga_apply_dense_attention; out and lse are its outputs.  Returns (grad_q, grad_key, grad_value, ws); a
-    gradient is None where it is not wanted."""
+def _segments_backward(name, size, call, kind, g, q, key, value, out, lse, grad_out, scale, grad_q, grad_key, grad_value, want_q, want_kv, ws, stream):
     with _on(q, stream):
-        c, h = _dense_args(g, q, key, value, scale, grad_out)
+        c, h = _dense_args(g, q, key, value, scale, grad_out, kind)
         if want_q and grad_q is None:
             grad_q = q.new_empty(q.shape)
         if want_kv and grad_key is None:
@@ -752,14 +762,52 @@ def tiga_apply_dense_attention_backward(g: DenseRelation, q, key, value, out, ls
             grad_value = q.new_empty(key.shape)
         _same(q, out, lse, grad_q, grad_key, grad_value, ws)
         if ws is None:
-            ws = _scratch(_L.tiga_dense_attention_workspace_bytes(ctypes.byref(c), ctypes.byref(h), 1), q)
-        grads = [None if t is None else _dense_out(t, like.shape, q.dtype, name)
-                 for t, like, name in ((grad_q, q, "grad_q"), (grad_key, key, "grad_key"), (grad_value, key, "grad_value"))]
-        _ok(_L.tiga_apply_dense_attention_backward(ctypes.byref(c), ctypes.byref(h), q.data_ptr(), key.data_ptr(), value.data_ptr(),
-                                                   _dense_out(out, q.shape, q.dtype, "out"),
-                                                   _dense_out(lse, q.shape[:2], torch.float32, "lse"), grad_out.data_ptr(), *grads,
-                                                   _ptr(ws), ws.numel(), _stream(stream)), "tiga_apply_dense_attention_backward")
+            ws = _scratch(size(ctypes.byref(c), ctypes.byref(h), 1), q)
+        grads = [None if t is None else _dense_out(t, like.shape, q.dtype, what)
+                 for t, like, what in ((grad_q, q, "grad_q"), (grad_key, key, "grad_key"), (grad_value, key, "grad_value"))]
+        _ok(call(ctypes.byref(c), ctypes.byref(h), q.data_ptr(), key.data_ptr(), value.data_ptr(), _dense_out(out, q.shape, q.dtype, "out"),
+                 _dense_out(lse, q.shape[:2], torch.float32, "lse"), grad_out.data_ptr(), *grads, _ptr(ws), ws.numel(), _stream(stream)), name)
     return grad_q, grad_key, grad_value, ws
+
+
+def tiga_dense_attention_workspace_bytes(g: DenseRelation, q, key, value, backward: bool = False) -> int:
+    c, h = _dense_args(g, q, key, value, 1.0)
+    return int(_L.tiga_dense_attention_workspace_bytes(ctypes.byref(c), ctypes.byref(h), int(backward)))
+
+
+def tiga_apply_dense_attention(g: DenseRelation, q, key, value, scale: float, out=None, lse=None, want_lse=True, ws=None, stream=None):
+    """out[i,h] = sum_j softmax_j(scale <q[i,h], key[j,h']>) value[j,h'] over the keys of the row's segment, h' the head of h's
+    group.  q [n_q, heads, D], key and value [n_kv, kv_heads, D], fp16 or bf16, rows and heads strided.  Returns (out, lse, ws)."""
+    return _segments_forward("tiga_apply_dense_attention", _L.tiga_dense_attention_workspace_bytes, _L.tiga_apply_dense_attention, DenseRelation,
+                             g, q, key, value, scale, out, lse, want_lse, ws, stream)
+
+
+def tiga_apply_dense_attention_backward(g: DenseRelation, q, key, value, out, lse, grad_out, scale: float, grad_q=None, grad_key=None,
+                                        grad_value=None, want_q=True, want_kv=True, ws=None, stream=None):
+    """Reverse mode of tiga_apply_dense_attention; out and lse are its outputs.  Returns (grad_q, grad_key, grad_value, ws); a
+    gradient is None where it is not wanted."""
+    return _segments_backward("tiga_apply_dense_attention_backward", _L.tiga_dense_attention_workspace_bytes, _L.tiga_apply_dense_attention_backward,
+                              DenseRelation, g, q, key, value, out, lse, grad_out, scale, grad_q, grad_key, grad_value, want_q, want_kv, ws, stream)
+
+
+def tiga_triangular_attention_workspace_bytes(g: TriangularRelation, q, key, value, backward: bool = False) -> int:
+    c, h = _dense_args(g, q, key, value, 1.0, None, TriangularRelation)
+    return int(_L.tiga_triangular_attention_workspace_bytes(ctypes.byref(c), ctypes.byref(h), int(backward)))
+
+
+def tiga_apply_triangular_attention(g: TriangularRelation, q, key, value, scale: float, out=None, lse=None, want_lse=True, ws=None, stream=None):
+    """tiga_apply_dense_attention over a triangular relation (causal attention of packed sequences).  Returns (out, lse, ws)."""
+    return _segments_forward("tiga_apply_triangular_attention", _L.tiga_triangular_attention_workspace_bytes, _L.tiga_apply_triangular_attention,
+                             TriangularRelation, g, q, key, value, scale, out, lse, want_lse, ws, stream)
+
+
+def tiga_apply_triangular_attention_backward(g: TriangularRelation, q, key, value, out, lse, grad_out, scale: float, grad_q=None, grad_key=None,
+                                             grad_value=None, want_q=True, want_kv=True, ws=None, stream=None):
+    """Reverse mode of tiga_apply_triangular_attention; out and lse are its outputs.  Returns (grad_q, grad_key, grad_value, ws); a
+    gradient is None where it is not wanted."""
+    return _segments_backward("tiga_apply_triangular_attention_backward", _L.tiga_triangular_attention_workspace_bytes,
+                              _L.tiga_apply_triangular_attention_backward, TriangularRelation, g, q, key, value, out, lse, grad_out, scale,
+                              grad_q, grad_key, grad_value, want_q, want_kv, ws, stream)
 
 
 class PagedCache(_Held):

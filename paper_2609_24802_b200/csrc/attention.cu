@@ -120,14 +120,15 @@ static bool bad_ints(const void* p) { return !p || (reinterpret_cast<uintptr_t>(
 
 using namespace tiga;
 
-extern "C" size_t tiga_dense_attention_workspace_bytes(const tiga_dense* g, const tiga_heads* h, int backward) {
+// dense and triangular relations: one descriptor, whose rows read all keys of their segment or those up to their own place
+static size_t blocks_bytes(const tiga_dense* g, const tiga_heads* h, int backward) {
     AttnParams p;
     if (dense_check(g, h, &p) != TIGA_OK) return 0;
     return (backward ? attention_backward_bytes(p) : attention_forward_bytes(p)) + 256;
 }
 
-extern "C" tiga_status tiga_apply_dense_attention(const tiga_dense* g, const tiga_heads* h, const void* q, const void* key, const void* value,
-                                                  void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+static tiga_status blocks_forward(const tiga_dense* g, const tiga_heads* h, int causal, const void* q, const void* key, const void* value,
+                                  void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
     AttnParams p;
     tiga_status st = dense_check(g, h, &p);
     if (st != TIGA_OK) return st;
@@ -136,16 +137,15 @@ extern "C" tiga_status tiga_apply_dense_attention(const tiga_dense* g, const tig
     if (bad_ints(g->q_start) || bad_ints(g->kv_start) || bad_array(q) || bad_array(out)) return TIGA_ERR_INVALID_ARG;
     if (g->n_kv > 0 && (bad_array(key) || bad_array(value))) return TIGA_ERR_INVALID_ARG;
     if (lse && !aligned16(lse)) return TIGA_ERR_INVALID_ARG;
-    if (!ws || !aligned16(ws) || ws_bytes < tiga_dense_attention_workspace_bytes(g, h, 0)) return TIGA_ERR_WORKSPACE;
-    p.q = q; p.k = key; p.v = value; p.out = out; p.lse = lse;
+    if (!ws || !aligned16(ws) || ws_bytes < blocks_bytes(g, h, 0)) return TIGA_ERR_WORKSPACE;
+    p.q = q; p.k = key; p.v = value; p.causal = causal; p.out = out; p.lse = lse;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     return attention_forward(p, h->dtype == TIGA_BF16, ws, s);
 }
 
-extern "C" tiga_status tiga_apply_dense_attention_backward(const tiga_dense* g, const tiga_heads* h, const void* q, const void* key,
-                                                           const void* value, const void* out, const float* lse, const void* grad_out,
-                                                           void* grad_q, void* grad_key, void* grad_value,
-                                                           void* ws, size_t ws_bytes, void* stream) {
+static tiga_status blocks_backward(const tiga_dense* g, const tiga_heads* h, int causal, const void* q, const void* key,
+                                   const void* value, const void* out, const float* lse, const void* grad_out,
+                                   void* grad_q, void* grad_key, void* grad_value, void* ws, size_t ws_bytes, void* stream) {
     AttnParams p;
     tiga_status st = dense_check(g, h, &p);
     if (st != TIGA_OK) return st;
@@ -156,11 +156,35 @@ extern "C" tiga_status tiga_apply_dense_attention_backward(const tiga_dense* g, 
     if (g->n_q > 0 && (bad_array(q) || bad_array(out) || bad_array(lse) || bad_array(grad_out))) return TIGA_ERR_INVALID_ARG;
     if (g->n_kv > 0 && (bad_array(key) || bad_array(value))) return TIGA_ERR_INVALID_ARG;
     if (!aligned16(grad_q) || !aligned16(grad_key) || !aligned16(grad_value)) return TIGA_ERR_INVALID_ARG;
-    if (!ws || !aligned16(ws) || ws_bytes < tiga_dense_attention_workspace_bytes(g, h, 1)) return TIGA_ERR_WORKSPACE;
-    p.q = q; p.k = key; p.v = value; p.o = out; p.lse_in = lse; p.go = grad_out;
+    if (!ws || !aligned16(ws) || ws_bytes < blocks_bytes(g, h, 1)) return TIGA_ERR_WORKSPACE;
+    p.q = q; p.k = key; p.v = value; p.causal = causal; p.o = out; p.lse_in = lse; p.go = grad_out;
     p.gq = grad_q; p.gk = grad_key; p.gv = grad_value;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     return attention_backward(p, h->dtype == TIGA_BF16, ws, s);
+}
+
+extern "C" size_t tiga_dense_attention_workspace_bytes(const tiga_dense* g, const tiga_heads* h, int backward) { return blocks_bytes(g, h, backward); }
+extern "C" tiga_status tiga_apply_dense_attention(const tiga_dense* g, const tiga_heads* h, const void* q, const void* key, const void* value,
+                                                  void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+    return blocks_forward(g, h, 0, q, key, value, out, lse, ws, ws_bytes, stream);
+}
+extern "C" tiga_status tiga_apply_dense_attention_backward(const tiga_dense* g, const tiga_heads* h, const void* q, const void* key,
+                                                           const void* value, const void* out, const float* lse, const void* grad_out,
+                                                           void* grad_q, void* grad_key, void* grad_value,
+                                                           void* ws, size_t ws_bytes, void* stream) {
+    return blocks_backward(g, h, 0, q, key, value, out, lse, grad_out, grad_q, grad_key, grad_value, ws, ws_bytes, stream);
+}
+
+extern "C" size_t tiga_triangular_attention_workspace_bytes(const tiga_dense* g, const tiga_heads* h, int backward) { return blocks_bytes(g, h, backward); }
+extern "C" tiga_status tiga_apply_triangular_attention(const tiga_dense* g, const tiga_heads* h, const void* q, const void* key, const void* value,
+                                                       void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+    return blocks_forward(g, h, 1, q, key, value, out, lse, ws, ws_bytes, stream);
+}
+extern "C" tiga_status tiga_apply_triangular_attention_backward(const tiga_dense* g, const tiga_heads* h, const void* q, const void* key,
+                                                                const void* value, const void* out, const float* lse, const void* grad_out,
+                                                                void* grad_q, void* grad_key, void* grad_value,
+                                                                void* ws, size_t ws_bytes, void* stream) {
+    return blocks_backward(g, h, 1, q, key, value, out, lse, grad_out, grad_q, grad_key, grad_value, ws, ws_bytes, stream);
 }
 
 extern "C" size_t tiga_paged_attention_workspace_bytes(const tiga_pages* c, const tiga_heads* h, int64_t n_q) {

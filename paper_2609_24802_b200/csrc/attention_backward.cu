@@ -167,7 +167,8 @@ __global__ void __launch_bounds__(PREP_THREADS, PREP_BLOCKS) attention_prepare_k
                     top = 0.f;
                     g = segment_of(p, at_seg.s, q_start, kv_start);
                 }
-                if (g.nk <= FEW_KEYS && lse != -INFINITY) few = g.nk;
+                const int n = keys_of_row(p, g, (int)row - g.q0);
+                if (n <= FEW_KEYS && lse != -INFINITY) few = n;
             }
             float dot = fold(dot8<T>(a, b));
             const float norm = NORMS ? fold(dot8<T>(a, a)) : 0.f;
@@ -299,7 +300,7 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
             const Item& e = item_take(ctl.items, item);
             if (e.steps == 0) break;
             const Segment g = e.segment();
-            const int packed_rows = g.nq * p.group, i0 = e.i0, i1 = ok ? e.i1 : e.i0, h = e.h;
+            const int packed_rows = g.nq * p.group, skip = WorkCut::skipped(p, g, e.t), i0 = e.i0 + skip, i1 = ok ? e.i1 + skip : i0, h = e.h;
             // a row of the other side, or of the tile itself: where key r lies, or whether packed row r is wanted
             Place at;
             bool on;
@@ -470,11 +471,18 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
             f32x2 my_lse = 0, my_delta = 0;
             long long out_row = 0;
             bool masked = false;
+            int keys = item.nk;             // queries stationary: keys that the row reads
+            // under the triangle: how many of the item's columns, from this thread's first one on, are left out (keys stationary: rows in
+            // front of the first one that reads the key) or read (queries stationary)
+            int edge = KV ? 0 : INT32_MAX;
             if (KV) {
                 out_row = (long long)(item.k0 + r) * p.kv_heads + item.h;
                 masked = valid && (item.nq == 0 || key_place(p, item.segment(), item.s, r).at < 0);
+                if (p.causal && valid) edge = (min(max(r - (item.length - item.nq), 0), item.nq) * p.group) - (item.i0 + WorkCut::skipped(p, item.segment(), item.t)) * BWD_STEP - 32 * x;
             } else if (valid) {
                 const PackedRow pr = packed_row(p, item.segment(), item.h, r);
+                keys = keys_of_row(p, item.segment(), pr.row - item.q0);
+                if (p.causal) edge = keys - item.i0 * BWD_STEP - 32 * x;
                 out_row = (long long)pr.row * p.heads + pr.head;
                 const float2 st = w.stats[out_row];
                 my_lse = dup2(BIAS - st.x);
@@ -492,7 +500,9 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
                     uint32_t v[32];
                     tmem_ld32(S, v);
                     const float4* nl = reinterpret_cast<const float4*>(ctl.minus_lse[aux] + 32 * x);
-                    const uint32_t keep = KV ? ~0u : ctl.mask[aux][x];
+                    const int at = edge - i * BWD_STEP;
+                    const uint32_t keep = KV ? (at <= 0 ? ~0u : at >= 32 ? 0u : ~0u << at) : ctl.mask[aux][x] & (at >= 32 ? ~0u : at <= 0 ? 0u : (1u << at) - 1);
+                    const bool whole = __all_sync(~0u, keep == ~0u);
                     tmem_wait_ld(v);
 #pragma unroll
                     for (int k = 0; k < 16; ++k) {
@@ -502,7 +512,7 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
                         unpack2(fma2(pack2(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1])), sc2, lse), a, b);
                         a = ex2(a);
                         b = ex2(b);
-                        if (!KV && keep != ~0u) {
+                        if (!whole) {
                             if (!(keep >> (2 * k) & 1)) a = 0.f;
                             if (!(keep >> (2 * k + 1) & 1)) b = 0.f;
                         }
@@ -549,7 +559,7 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
             const int rows = KV ? w.kv_rows : w.q_rows;
             constexpr int SIDES = KV ? 2 : 1, MINE = DP * SIDES / 4;        // this thread's features of a row
             const int side = KV ? x / 2 : 0, f0 = (KV ? x % 2 : x) * MINE;
-            const bool zero = masked || (side == 0 && reads_one_key(p, item.segment()));
+            const bool zero = masked || (side == 0 && reads_one_key(p, item.segment(), keys));
             const uint32_t acc = (side ? acc2 : acc1) + lanes;
             const float finish = side ? (F16 ? 0x1p-14f : 1.f) : p.scale / factor;
             T* out = (T*)(KV ? (side ? p.gv : p.gk) : p.gq);
@@ -642,15 +652,17 @@ __device__ __forceinline__ void sum_pass(const AttnParams& p, const BwdWork& w, 
             const int n = it.t * BWD_ROWS + r;
             long long out_row;
             bool masked;
+            int keys = g.nk;
             if (KV) {
                 out_row = (long long)(g.k0 + n) * p.kv_heads + it.h;
                 masked = key_place(p, g, it.s, n).at < 0;
             } else {
                 const PackedRow pr = packed_row(p, g, it.h, n);
+                keys = keys_of_row(p, g, pr.row - g.q0);
                 out_row = (long long)pr.row * p.heads + pr.head;
                 masked = w.stats[out_row].x == INFINITY;
             }
-            masked = masked || (side == 0 && reads_one_key(p, g));
+            masked = masked || (side == 0 && reads_one_key(p, g, keys));
             const float finish = KV && side ? (F16 ? 0x1p-14f : 1.f) : p.scale / factor;
             T* out = (T*)(KV ? (side ? p.gv : p.gk) : p.gq);
 #pragma unroll
@@ -681,7 +693,7 @@ static size_t backward_carve(const AttnParams& p, void* ws, BwdWork* w) {
     w->kv_rows = p.n_kv < BWD_ROWS ? p.n_kv : BWD_ROWS;
     w->q_rows = (int)(packed < BWD_ROWS ? packed : BWD_ROWS);
     Carver cv(ws);
-    const bool counted_there = counts_itself(p, BWD_ROWS);
+    const bool counted_there = counts_itself(p);
     w->kv_start_unit = counted_there ? nullptr : cv.take<long long>((size_t)p.n_seg + 1);
     w->q_start_unit = counted_there ? nullptr : cv.take<long long>((size_t)p.n_seg + 1);
     w->kv_joints = cv.take<Joint>(MAX_SMS);

@@ -499,8 +499,8 @@ size_t attention_forward_carve(const AttnParams& p, void* ws, FwdWork* w) {
     const long long packed = (long long)p.n_q * p.group;
     w->rows = (int)(packed < FWD_ROWS ? packed : FWD_ROWS);
     Carver cv(ws);
-    w->unit_start = cv.take<long long>((size_t)p.n_seg + 1);       // (room for it whether or not this call needs it: its size is asked for without `causal`)
-    if (counts_itself(p, FWD_ROWS)) w->unit_start = nullptr;
+    w->unit_start = cv.take<long long>((size_t)p.n_seg + 1);       // (room for it whether or not this call needs it)
+    if (counts_itself(p)) w->unit_start = nullptr;
     w->joints = cv.take<Joint>(MAX_SMS);
     w->part_ml = cv.take<float2>(slots * w->rows);
     w->part_o = cv.take<float>(slots * w->rows * (p.D > 64 ? 128 : 64));

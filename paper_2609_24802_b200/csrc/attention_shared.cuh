@@ -49,8 +49,10 @@ __device__ __forceinline__ Segment segment_of(const AttnParams& p, int s, const 
 __device__ __forceinline__ Segment segment_of(const AttnParams& p, int s) { return segment_of(p, s, p.q_start, p.kv_start); }
 
 // keys that row t of the segment's nq rows reads: [0, this)
-__device__ __forceinline__ int keys_of_row(const AttnParams& p, const Segment& g, int t) {
-    return p.causal ? min(max(g.length - g.nq + t + 1, 0), g.nk) : g.nk;
+__host__ __device__ __forceinline__ int keys_of_row(const AttnParams& p, const Segment& g, int t) {
+    if (!p.causal) return g.nk;
+    const int n = g.length - g.nq + t + 1;
+    return n < 0 ? 0 : n < g.nk ? n : g.nk;
 }
 
 // Where key j of segment s (0 <= j < g.nk) lies: paged, its page and slot; dense, its row and 0.  at < 0: it is masked, or has no page.
@@ -71,12 +73,13 @@ __device__ __forceinline__ long long value_offset(const AttnParams& p, Place a, 
     return a.at < 0 ? -1 : p.table ? a.at * p.page_stride + a.slot * p.slot_stride + h * p.v_head : a.at * p.v_row + h * p.v_head;
 }
 
-// Whether the rows of a dense segment read one key: its weight is 1 whatever the score, so scores have no gradient.  (Masks of up to
-// 32 keys are counted; where a longer one leaves a single key the gradient is what is left of dP - delta, a few 2^-23 of either.)
-__device__ __forceinline__ bool reads_one_key(const AttnParams& p, const Segment& g) {
-    if (!p.mask || g.nk > 32) return g.nk == 1;
+// Whether a row of a dense segment reads one key of the first `most` (the segment's rows under the triangle: whether the last of them does,
+// then none reads more): its weight is 1 whatever the score, so scores have no gradient.  (Masks of up to 32 keys are counted; where a
+// longer one leaves a single key the gradient is what is left of dP - delta, a few 2^-23 of either.)
+__device__ __forceinline__ bool reads_one_key(const AttnParams& p, const Segment& g, int most) {
+    if (!p.mask || most > 32) return most == 1;
     int n = 0;
-    for (int j = 0; j < g.nk; ++j) n += p.mask[g.k0 + j] != 0;
+    for (int j = 0; j < most; ++j) n += p.mask[g.k0 + j] != 0;
     return n == 1;
 }
 
@@ -127,6 +130,37 @@ struct Along {
     }
 };
 
+// a / b for 0 <= a, 0 < b; the short division where both are short
+__host__ __device__ __forceinline__ long long quotient(long long a, long long b) {
+    return (a | b) >> 32 ? a / b : (long long)((unsigned)a / (unsigned)b);
+}
+// the same towards minus infinity, for any a, and towards plus infinity
+__host__ __device__ __forceinline__ long long floor_quotient(long long a, long long b) { return a >= 0 ? quotient(a, b) : -quotient(b - 1 - a, b); }
+__host__ __device__ __forceinline__ long long ceil_quotient(long long a, long long b) { return -floor_quotient(-a, b); }
+
+// Sum of floor((a k + b) / m) over k in [0, n), for 0 <= a, b: whole multiples of m leave a and b; what remains counts the lattice points
+// below a line, which are counted again along the other axis, with a and m exchanged, as in Euclid's algorithm.
+__host__ __device__ __forceinline__ long long lattice_points(long long n, long long a, long long b, long long m) {
+    long long sum = 0, sign = 1;
+    while (n > 0) {
+        const long long qa = quotient(a, m), qb = quotient(b, m);
+        a -= qa * m;
+        b -= qb * m;
+        sum += sign * (qa * (n * (n - 1) / 2) + qb * n);
+        const long long top = quotient(a * (n - 1) + b, m);         // the value of the last k; value v is reached from k = ceil((v m - b) / a) on
+        if (top == 0) break;
+        // sum over v in [1, top] of n - ceil((v m - b) / a), with v = w + 1
+        sum += sign * n * top;
+        sign = -sign;
+        const long long nb = m - b + a - 1, nm = a;
+        a = m;
+        b = nb;
+        m = nm;
+        n = top;
+    }
+    return sum;
+}
+
 // ---- How the work is cut.  A segment's heads share keys, so the rows of a group's heads are packed: packed row r of a kv head is row
 // r / group, head kv_head * group + r % group.  A tile of stationary rows (packed rows, or keys for their gradients) meets the other
 // side in steps; a unit is one step of one tile of one kv head.  All units of a call stand in one line (segment, kv head, tile,
@@ -137,27 +171,54 @@ struct Cut {
     static constexpr int TILE = TILE_, STEP = STEP_;      // stationary rows of a tile, rows of a step: powers of two
     static constexpr bool KEYS = KEYS_;                   // the keys are stationary
 
-    static __device__ __forceinline__ int rows(const AttnParams& p, const Segment& g) { return KEYS ? g.nk : g.nq * p.group; }
-    static __device__ __forceinline__ int tiles(const AttnParams& p, const Segment& g) {
+    static __host__ __device__ __forceinline__ int rows(const AttnParams& p, const Segment& g) { return KEYS ? g.nk : g.nq * p.group; }
+    static __host__ __device__ __forceinline__ int tiles(const AttnParams& p, const Segment& g) {
         const int n = rows(p, g);
         return n / TILE + (n % TILE != 0);
     }
+    // steps in front of a tile's first one (keys stationary, under the triangle: packed rows that read none of its keys)
+    static __host__ __device__ __forceinline__ int skipped(const AttnParams& p, const Segment& g, int t) {
+        if (!KEYS || !p.causal) return 0;
+        const long long first = (long long)t * TILE - (g.length - g.nq);        // the first row that reads the tile's first key
+        const int packed = g.nq * p.group;
+        return first <= 0 ? 0 : first >= g.nq ? packed / STEP : (int)first * p.group / STEP;
+    }
     // steps of tile t; one (in which nothing is read) where there is nothing on the other side, so that empty rows are written
-    static __device__ __forceinline__ int steps(const AttnParams& p, const Segment& g, int t) {
+    static __host__ __device__ __forceinline__ int steps(const AttnParams& p, const Segment& g, int t) {
         int n;
         if (KEYS) n = g.nq * p.group;
         else if (!p.causal) n = g.nk;
-        else n = keys_of_row(p, g, (min((t + 1) * TILE, g.nq * p.group) - 1) / p.group);
-        return max(n / STEP + (n % STEP != 0), 1);
+        else {
+            const int packed = g.nq * p.group, end = packed - t * TILE > TILE ? (t + 1) * TILE : packed;
+            n = keys_of_row(p, g, (end - 1) / p.group);
+        }
+        n = n / STEP + (n % STEP != 0) - skipped(p, g, t);
+        return n > 1 ? n : 1;
+    }
+    // Units of the first t tiles (t <= tiles()).  Under the triangle steps(k) is max(1, floor((x k + y) / z)), cut off at the segment's
+    // keys or rows: a sum of floors in the middle.
+    static __host__ __device__ __forceinline__ long long before(const AttnParams& p, const Segment& g, int t) {
+        if (t == 0) return 0;
+        if (!p.causal) return (long long)t * steps(p, g, 0);
+        const long long c = (long long)g.length - g.nq;
+        if (KEYS) {
+            if (g.nq == 0) return t;
+            static_assert(!KEYS || TILE == STEP, "a tile of keys skips `group` steps more than the one in front of it");
+            // skipped(k) = k group + floor(-c group / STEP) from the first tile k0 on that skips any rows; none is skipped in front of it
+            const long long total = ceil_quotient((long long)g.nq * p.group, STEP), k0 = c <= 0 ? 0 : ceil_quotient(c, TILE);
+            if (t <= k0) return t * total;
+            return t * total - p.group * ((t - 1LL) * t / 2 - (k0 - 1) * k0 / 2) - (t - k0) * floor_quotient(-c * p.group, STEP);
+        }
+        // the last tile apart: its rows may end early.  The others: floor((TILE k + b) / m), the last row of tile k being (TILE k + TILE - 1) / group
+        const int last = tiles(p, g) - 1;
+        const long long m = (long long)STEP * p.group, b = TILE - 1 + p.group * (c + STEP), most = g.nk ? ceil_quotient(g.nk, STEP) : 1;
+        const long long n = t <= last ? t : last;
+        const long long lo = ceil_quotient(2 * m - b, TILE), hi = ceil_quotient(most * m - b, TILE);          // from where on there are 2 steps, all steps
+        const long long k1 = lo < 0 ? 0 : lo < n ? lo : n, k2 = hi < k1 ? k1 : hi < n ? hi : n;
+        return k1 + (k1 < k2 ? lattice_points(k2 - k1, TILE, TILE * k1 + b, m) : 0) + (n - k2) * most + (t > last ? steps(p, g, last) : 0);
     }
     // units of a kv head
-    static __device__ __forceinline__ long long units(const AttnParams& p, const Segment& g) {
-        const int n = tiles(p, g);
-        if (KEYS || !p.causal) return n ? (long long)n * steps(p, g, 0) : 0;
-        long long sum = 0;
-        for (int t = 0; t < n; ++t) sum += steps(p, g, t);
-        return sum;
-    }
+    static __host__ __device__ __forceinline__ long long units(const AttnParams& p, const Segment& g) { return before(p, g, tiles(p, g)); }
 };
 
 __device__ __forceinline__ long long warp_total(long long v) {
@@ -173,11 +234,6 @@ __device__ __forceinline__ long long warp_running(long long v) {
     }
     return v;
 }
-// a / b for 0 <= a, 0 < b; the short division where both are short
-__device__ __forceinline__ long long quotient(long long a, long long b) {
-    return (a | b) >> 32 ? a / b : (long long)((unsigned)a / (unsigned)b);
-}
-
 // A block's way through its piece of the line: one tile, or a part of one, after the other.
 template <typename C>
 struct Walker {
@@ -232,24 +288,20 @@ struct Walker {
         const long long per_head = quotient(mine, p.kv_heads);
         h = (int)quotient(off, per_head);
         off -= h * per_head;
-        if (C::KEYS || !p.causal) {
+        if (!p.causal) {
             const int n = C::steps(p, g, 0);
             t = (int)quotient(off, n);
             i0 = (int)(off - (long long)t * n);
-        } else {
-            const int tiles = C::tiles(p, g);
-            for (t = 0;; t += 32) {
-                const long long run = warp_running(t + lane < tiles ? C::steps(p, g, t + lane) : 0);
-                const unsigned beyond = __ballot_sync(~0u, run > off);
-                if (beyond) {
-                    const int at = __ffs(beyond) - 1;
-                    if (at) off -= __shfl_sync(~0u, run, at - 1);
-                    t += at;
-                    break;
-                }
-                off -= __shfl_sync(~0u, run, 31);
+        } else {            // the last tile that begins at or before this unit, 32 places a round
+            int hi = C::tiles(p, g);
+            t = 0;
+            while (hi - t > 1) {
+                const int gap = (hi - t + 31) / 32, at = t + lane * gap;
+                const unsigned before = __ballot_sync(~0u, at < hi && C::before(p, g, at) <= off) | 1u;
+                t += (31 - __clz(before)) * gap;
+                hi = min(hi, t + gap);
             }
-            i0 = (int)off;
+            i0 = (int)(off - C::before(p, g, t));
         }
         open(p);
         return true;
@@ -296,10 +348,8 @@ static __device__ void plan_units(const AttnParams& p, long long* unit_start) {
     if (threadIdx.x == 0) unit_start[0] = 0;
 }
 // Whether the blocks count the units themselves: a launch less, for a few hundred instructions in every warp.
-constexpr int COUNT_SEGMENTS = 256, COUNT_TILES = 64;
-static inline bool counts_itself(const AttnParams& p, int tile) {
-    return p.n_seg <= COUNT_SEGMENTS && (!p.causal || (long long)p.n_q * p.group <= (long long)COUNT_TILES * tile);
-}
+constexpr int COUNT_SEGMENTS = 256;
+static inline bool counts_itself(const AttnParams& p) { return p.n_seg <= COUNT_SEGMENTS; }
 
 // A kernel may start before the one in front of it in the stream has ended; it waits where it first reads what that one wrote.
 __device__ __forceinline__ void wait_for_previous_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
