@@ -331,7 +331,7 @@ def _own(s):
         weights, _ = T.tiga_paged_attention_weights(cache, s["q"], s["q_start"], s["lse"], s["scale"], before=s["before"], weights=s["weights"])
         return {"weights": weights}
     to = T.PagedCache(s["to_key"], s["to_value"], s["to_table"], s["to_len"])
-    kept, weights, _ = T.tiga_paged_evict(cache, to, s["weights"], c["keep"], c["recent"])
+    kept, weights = T.tiga_paged_evict(cache, to, s["weights"], c["keep"], c["recent"])
     return {"key_pages": s["to_key"], "value_pages": s["to_value"], "kv_len": s["to_len"], "kept": kept, "weights": weights}
 
 
