@@ -456,6 +456,38 @@ size_t tiga_paged_attention_workspace_bytes(const tiga_pages* c, const tiga_head
 tiga_status tiga_apply_paged_attention(const tiga_pages* c, const tiga_heads* h, const void* q, const int32_t* q_start, int64_t n_q,
                                        int causal, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
 
+/* A number for every position of every (sequence, kv head): entry (s, h, j) lies at data + s * seg + h * head + j, strides in
+ * elements, j < length.  fp32, the base 16-byte aligned; lists of an output share no entries. */
+typedef struct { float* data; int64_t seg, head, length; } tiga_weights;
+
+/* How much attention the cached positions have received: with lse of tiga_apply_paged_attention for the same chunk,
+ *     weights[s, h', j] = before[s, h', j] + sum over the chunk's rows i of s that read position j, and the heads h of group h', of
+ *                         exp(scale <q[i,h,:], key[j,h',:]> - lse[i,h]),          for j < kv_len[s].
+ * Entries behind a sequence's end are left as they were; positions from weights->length on are not counted, positions without a page
+ * receive nothing, and neither do rows whose lse is -inf give anything.  before == NULL: zeros; it may be the same array (with equal strides)
+ * as weights, and is otherwise apart from it; before->length >= weights->length.  Values are not read (c->value may be NULL).  Sums are
+ * fp32, in one order.
+ * ws: tiga_paged_weights_workspace_bytes(c, h, n_q) bytes. */
+size_t tiga_paged_weights_workspace_bytes(const tiga_pages* c, const tiga_heads* h, int64_t n_q);
+tiga_status tiga_paged_attention_weights(const tiga_pages* c, const tiga_heads* h, const void* q, const int32_t* q_start, int64_t n_q,
+                                         const float* lse, int causal, const tiga_weights* before, const tiga_weights* weights,
+                                         void* ws, size_t ws_bytes, void* stream);
+
+/* Cuts a cache to a budget: every kv head of sequence s keeps, of the positions that have a page, the last ones (from
+ * kv_len[s] - recent on) and those with the largest weights, `keep` in all, or all of them where there are no more.  Of equal weights
+ * the lower position stays; NaN counts as less than any number, and positions from weights->length on as zero.  What stays moves, in
+ * the order of its positions, to the first places of sequence s in `to`:
+ *     to->key, to->value   the kept rows (places of which the table of `to` names no page are not written)
+ *     to_len[s]            how many they are (device, int32 [n_seg]; may be to->kv_len, which is not read; not from->kv_len)
+ *     kept                 device, int32 [n_seg, kv_heads, keep]: their positions, -1 behind them
+ *     to_weights           their weights, zeros behind them (a new token's count begins there); NULL: not wanted
+ * Keys keep the rotation of their positions: the next token is rotated by its own position (tiga_apply_rotary) and appended without
+ * one.  Pages that are written must be apart from those that sequences of `from` name, and belong to one sequence alone; both caches
+ * may lie in the same arrays.
+ *   h : dtype, kv_heads, D;  1 <= keep <= to->max_pages * to->page_size;  0 <= recent <= keep. */
+tiga_status tiga_paged_evict(const tiga_pages* from, const tiga_pages* to, const tiga_heads* h, const tiga_weights* weights,
+                             int64_t keep, int64_t recent, const tiga_weights* to_weights, int32_t* to_len, int32_t* kept, void* stream);
+
 /* ----------------------------------------------------------------- rotary positions */
 
 typedef enum {

@@ -26,6 +26,7 @@ __all__ = [
     "BF16", "DenseRelation", "tiga_dense_attention_workspace_bytes", "tiga_apply_dense_attention",
     "tiga_apply_dense_attention_backward", "TriangularRelation", "tiga_triangular_attention_workspace_bytes",
     "tiga_apply_triangular_attention", "tiga_apply_triangular_attention_backward", "PagedCache", "tiga_paged_attention_workspace_bytes", "tiga_apply_paged_attention",
+    "tiga_paged_weights_workspace_bytes", "tiga_paged_attention_weights", "tiga_paged_evict",
     "tiga_paged_append", "ROT_PLAIN", "ROT_LINEAR", "ROT_BASE", "ROT_BANDS", "tiga_rotary_frequencies", "Rotary", "tiga_apply_rotary",
 ]
 
@@ -47,6 +48,7 @@ EXPORTS = [
     "tiga_dense_attention_workspace_bytes", "tiga_apply_dense_attention", "tiga_apply_dense_attention_backward",
     "tiga_triangular_attention_workspace_bytes", "tiga_apply_triangular_attention", "tiga_apply_triangular_attention_backward",
     "tiga_paged_attention_workspace_bytes", "tiga_apply_paged_attention", "tiga_paged_append", "tiga_rotary_frequencies", "tiga_apply_rotary",
+    "tiga_paged_weights_workspace_bytes", "tiga_paged_attention_weights", "tiga_paged_evict",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -103,6 +105,10 @@ class _Pages(ctypes.Structure):
     _fields_ = [("key", ctypes.c_void_p), ("value", ctypes.c_void_p), ("table", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
                 ("n_seg", ctypes.c_int64), ("n_pages", ctypes.c_int64), ("page_size", ctypes.c_int64), ("table_stride", ctypes.c_int64),
                 ("max_pages", ctypes.c_int64), ("page_stride", ctypes.c_int64), ("slot_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class _Weights(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("seg", ctypes.c_int64), ("head", ctypes.c_int64), ("length", ctypes.c_int64)]
 
 
 class _Rotary(ctypes.Structure):
@@ -195,6 +201,12 @@ def load_library() -> ctypes.CDLL:
     lib.tiga_paged_attention_workspace_bytes.argtypes = [ref(_Pages), ref(_Heads), i64]
     lib.tiga_apply_paged_attention.restype = ctypes.c_int
     lib.tiga_apply_paged_attention.argtypes = [ref(_Pages), ref(_Heads), vp, vp, i64, ctypes.c_int, vp, vp, vp, sz, vp]
+    lib.tiga_paged_weights_workspace_bytes.restype = sz
+    lib.tiga_paged_weights_workspace_bytes.argtypes = [ref(_Pages), ref(_Heads), i64]
+    lib.tiga_paged_attention_weights.restype = ctypes.c_int
+    lib.tiga_paged_attention_weights.argtypes = [ref(_Pages), ref(_Heads), vp, vp, i64, vp, ctypes.c_int, ref(_Weights), ref(_Weights), vp, sz, vp]
+    lib.tiga_paged_evict.restype = ctypes.c_int
+    lib.tiga_paged_evict.argtypes = [ref(_Pages), ref(_Pages), ref(_Heads), ref(_Weights), i64, i64, ref(_Weights), vp, vp, vp]
     lib.tiga_paged_append.restype = ctypes.c_int
     lib.tiga_paged_append.argtypes = [ref(_Pages), ref(_Heads), vp, vp, vp, i64, ref(_Rotary), vp]
     lib.tiga_rotary_frequencies.restype = ctypes.c_int
@@ -660,6 +672,7 @@ _HEADS_BYTES, _HEADS_OF, _NO_STRIDE = struct.Struct("=4if4x8q"), _Heads.from_buf
 _DENSE_BYTES, _DENSE_OF = struct.Struct("=6q"), _Dense.from_buffer_copy
 _STRIDE_BYTES, _STRIDE_OF = struct.Struct("=2q"), _Stride.from_buffer_copy
 _PAGES_BYTES, _PAGES_OF = struct.Struct("=12q"), _Pages.from_buffer_copy
+_WEIGHTS_BYTES, _WEIGHTS_OF = struct.Struct("=4q"), _Weights.from_buffer_copy
 assert _PAGES_BYTES.size == ctypes.sizeof(_Pages)
 assert _HEADS_BYTES.size == ctypes.sizeof(_Heads) and _DENSE_BYTES.size == ctypes.sizeof(_Dense)
 
@@ -861,6 +874,58 @@ def tiga_apply_paged_attention(cache: PagedCache, q, q_start, scale: float, caus
                                           None if lse is None else _dense_out(lse, q.shape[:2], torch.float32, "lse"),
                                           _ptr(ws), ws.numel(), _stream(stream)), "tiga_apply_paged_attention")
     return out, lse, ws
+
+
+def _weights_of(t, cache, name):
+    if t.dtype is not torch.float32 or t.dim() != 3 or t.shape[:2] != (cache.n_seg, cache.key.shape[2]) or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError(f"{name} must be an fp32 array [n_seg, kv_heads, positions] whose positions are contiguous")
+    _same(t, cache.key)
+    return ctypes.byref(_WEIGHTS_OF(_WEIGHTS_BYTES.pack(t.data_ptr(), _step(t, 0), _step(t, 1), t.shape[2])))
+
+
+def tiga_paged_weights_workspace_bytes(cache: PagedCache, q) -> int:
+    return int(_L.tiga_paged_weights_workspace_bytes(cache.ref, ctypes.byref(_paged_heads(cache, q, 1.0)), q.shape[0]))
+
+
+def tiga_paged_attention_weights(cache: PagedCache, q, q_start, lse, scale: float, causal=True, before=None, weights=None, ws=None, stream=None):
+    """weights[s,h',j] = before[s,h',j] + the softmax weights that position j of sequence s receives from the chunk's rows and the heads of
+    group h'; q, q_start, scale, causal and lse as in, and from, tiga_apply_paged_attention.  weights and before fp32 [n_seg, kv_heads,
+    positions]; weights may be before (the sums are kept in place).  Entries behind a sequence's end are left alone (zeros where weights is
+    allocated here).  Returns (weights, ws)."""
+    with _on(q, stream):
+        h = _paged_heads(cache, q, scale)
+        start = _ints(q_start, cache.n_seg + 1, "q_start")
+        if weights is None:
+            like = (cache.n_seg, cache.key.shape[2], cache.table.shape[1] * cache.key.shape[1] if before is None else before.shape[2])
+            weights = q.new_zeros(like, dtype=torch.float32)
+        b, o = None if before is None else _weights_of(before, cache, "before"), _weights_of(weights, cache, "weights")
+        _same(q, q_start, lse, ws)
+        if ws is None:
+            ws = _scratch(_L.tiga_paged_weights_workspace_bytes(cache.ref, ctypes.byref(h), q.shape[0]), q)
+        _ok(_L.tiga_paged_attention_weights(cache.ref, ctypes.byref(h), q.data_ptr(), start, q.shape[0], _dense_out(lse, q.shape[:2], torch.float32, "lse"),
+                                            int(bool(causal)), b, o, _ptr(ws), ws.numel(), _stream(stream)), "tiga_paged_attention_weights")
+    return weights, ws
+
+
+def tiga_paged_evict(cache: PagedCache, to: PagedCache, weights, keep: int, recent: int = 0, to_weights=None, want_weights=True, kept=None, stream=None):
+    """Every kv head of a sequence keeps its last `recent` positions and those with the largest weights [n_seg, kv_heads, positions], `keep`
+    in all; their keys and values move in order to the first places of `to` (pages apart from those that `cache` names), to.kv_len is
+    written.  Returns (kept int32 [n_seg, kv_heads, keep]: their positions, -1 behind them; to_weights [n_seg, kv_heads, positions of
+    `to`]: their weights, zeros behind them, or None)."""
+    with _on(cache.key, stream):
+        _, _, kv_heads, D = cache.key.shape
+        if to.key.dtype is not cache.key.dtype or to.key.shape[2:] != cache.key.shape[2:] or to.n_seg != cache.n_seg:
+            raise ValueError("both caches must have one storage type, number of sequences and heads, and width")
+        _same(cache.key, to.key, kept)
+        if kept is None:
+            kept = cache.table.new_empty((cache.n_seg, kv_heads, max(int(keep), 0)))
+        if want_weights and to_weights is None:
+            to_weights = weights.new_empty((cache.n_seg, kv_heads, to.table.shape[1] * to.key.shape[1]))
+        h = _heads_of(_HALF[cache.key.dtype], kv_heads, kv_heads, D, 1.0, _NO_STRIDE)
+        _ok(_L.tiga_paged_evict(cache.ref, to.ref, ctypes.byref(h), _weights_of(weights, cache, "weights"), int(keep), int(recent),
+                                None if to_weights is None else _weights_of(to_weights, cache, "to_weights"), to.kv_len.data_ptr(),
+                                _dense_out(kept, (cache.n_seg, kv_heads, int(keep)), torch.int32, "kept"), _stream(stream)), "tiga_paged_evict")
+    return kept, to_weights
 
 
 def tiga_rotary_frequencies(turned: int, base: float = 10000.0, scaling: int = ROT_PLAIN, factor: float = 1.0, length: float = 0.0,

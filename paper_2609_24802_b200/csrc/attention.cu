@@ -98,7 +98,7 @@ tiga_status attention_pages_check(const tiga_pages* c) {
     return TIGA_OK;
 }
 
-static tiga_status paged_check(const tiga_pages* c, const tiga_heads* h, int64_t n_q, AttnParams* p) {
+tiga_status attention_paged_check(const tiga_pages* c, const tiga_heads* h, int64_t n_q, AttnParams* p) {
     tiga_status st = attention_heads_check(h);
     if (st != TIGA_OK) return st;
     if ((st = attention_pages_check(c)) != TIGA_OK) return st;
@@ -114,7 +114,16 @@ static tiga_status paged_check(const tiga_pages* c, const tiga_heads* h, int64_t
 }
 
 static bool bad_array(const void* p) { return !p || !aligned16(p); }
-static bool bad_ints(const void* p) { return !p || (reinterpret_cast<uintptr_t>(p) & 3); }
+bool attention_bad_ints(const void* p) { return !p || (reinterpret_cast<uintptr_t>(p) & 3); }
+static bool bad_ints(const void* p) { return attention_bad_ints(p); }
+// whether the lists of an output share entries: heads lie one behind the other in a sequence, or sequences in a head
+bool attention_weights_overlap(const tiga_weights* a, int64_t n_seg, int64_t kv_heads) {
+    if (a->length == 0) return false;
+    const bool heads_inside = (kv_heads < 2 || a->head >= a->length) && (n_seg < 2 || a->seg >= (kv_heads < 2 ? a->length : a->head * (kv_heads - 1) + a->length));
+    const bool seqs_inside = (n_seg < 2 || a->seg >= a->length) && (kv_heads < 2 || a->head >= (n_seg < 2 ? a->length : a->seg * (n_seg - 1) + a->length));
+    return !heads_inside && !seqs_inside;
+}
+bool attention_bad_weights(const tiga_weights* a) { return !a || a->seg < 0 || a->head < 0 || a->length < 0 || a->length > MOST_ROWS; }
 
 }  // namespace tiga
 
@@ -189,14 +198,14 @@ extern "C" tiga_status tiga_apply_triangular_attention_backward(const tiga_dense
 
 extern "C" size_t tiga_paged_attention_workspace_bytes(const tiga_pages* c, const tiga_heads* h, int64_t n_q) {
     AttnParams p;
-    if (paged_check(c, h, n_q, &p) != TIGA_OK) return 0;
+    if (attention_paged_check(c, h, n_q, &p) != TIGA_OK) return 0;
     return attention_forward_bytes(p) + 256;
 }
 
 extern "C" tiga_status tiga_apply_paged_attention(const tiga_pages* c, const tiga_heads* h, const void* q, const int32_t* q_start, int64_t n_q,
                                                   int causal, void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
     AttnParams p;
-    tiga_status st = paged_check(c, h, n_q, &p);
+    tiga_status st = attention_paged_check(c, h, n_q, &p);
     if (st != TIGA_OK) return st;
     if (attention_bad_stride(h->q)) return TIGA_ERR_INVALID_ARG;
     if (c->n_seg == 0 || n_q == 0) return TIGA_OK;

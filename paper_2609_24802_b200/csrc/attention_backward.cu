@@ -34,14 +34,15 @@ template <int DP> struct Bwd {
     static constexpr int SMEM = CONTROL + (DP == 128 ? 3 : 10) * 1024;
 };
 
-template <int AUX> struct BwdControl {
+template <int AUX, typename C> struct BwdControl {
     unsigned long long full[8], empty[8], aux_full[AUX], x_full, x_empty, s_full, dp_full, p_full, ds_full, acc_full, acc_empty, drain;
     ItemRing items;
+    Walker<C> walk;
     uint32_t tmem, abort_word;
     alignas(16) float minus_lse[AUX][BWD_STEP], minus_delta[AUX][BWD_STEP];     // keys stationary: of the step's rows
     uint32_t mask[AUX][4];                                                      // queries stationary: the step's keys
 };
-static_assert(sizeof(BwdControl<2>) <= 3 * 1024 && sizeof(BwdControl<8>) <= 10 * 1024, "control block");
+static_assert(sizeof(BwdControl<2, KvCut>) <= 3 * 1024 && sizeof(BwdControl<8, KvCut>) <= 10 * 1024, "control block");
 
 struct BwdWork {
     long long *kv_start_unit, *q_start_unit;        // NULL: the blocks count for themselves
@@ -236,14 +237,14 @@ __global__ void __launch_bounds__(PREP_THREADS, PREP_BLOCKS) attention_prepare_k
     }
 }
 
-template <typename T, int DP, bool KV>
+template <typename T, int DP, bool KV, bool CAUSAL>
 __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork& w, const TileMaps& maps, const int block, const int blocks) {
     typedef Bwd<DP> C;
     typedef typename CutOf<KV>::type WorkCut;
     constexpr bool F16 = operand_type<T>() == 0;
     constexpr float BIAS = F16 ? 14.f : 0.f;
     extern __shared__ __align__(1024) unsigned char smem[];
-    BwdControl<C::AUX>& ctl = *reinterpret_cast<BwdControl<C::AUX>*>(smem + C::CONTROL);
+    BwdControl<C::AUX, WorkCut>& ctl = *reinterpret_cast<BwdControl<C::AUX, WorkCut>*>(smem + C::CONTROL);
     const uint32_t x_tile = smem_u32(smem), ring = x_tile + 2 * C::TILE;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     volatile uint32_t* abort_word = &ctl.abort_word;
@@ -267,9 +268,7 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
         ctl.abort_word = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    Walker<WorkCut> walk;
-    bool work_here = false;
-    if (warp == BWD_WALKER) work_here = walk.begin(p, KV ? w.kv_start_unit : w.q_start_unit, block, blocks);
+    if (warp == BWD_WALKER) walk_begin(&ctl.walk, p, KV ? w.kv_start_unit : w.q_start_unit, block, blocks);
     if (warp == BWD_MMA) tmem_alloc(smem_u32(&ctl.tmem), 512);
     tmem_fence_before();
     __syncthreads();
@@ -279,14 +278,15 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
 
     if (warp == BWD_WALKER) {
         if (lane == 0) {
-            (KV ? w.kv_joints : w.q_joints)[block] = joint_of(walk, work_here, block);
+            Walker<WorkCut> walk = ctl.walk;
+            (KV ? w.kv_joints : w.q_joints)[block] = joint_of(walk, walk.here, block);
             int of = -1;
             float factor = 1.f;
             auto factor_of = [&](int s) {
                 if (F16 && s != of) factor = gradient_factor(w.norms, of = s);
                 return factor;
             };
-            items_hand_out(ctl.items, p, walk, work_here, A_MINUTE, factor_of);
+            items_hand_out(ctl.items, p, walk, walk.here, A_MINUTE, factor_of);
         }
         __syncwarp();
     } else if (warp >= BWD_PRODUCER && warp < BWD_MMA) {
@@ -300,7 +300,7 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
             const Item& e = item_take(ctl.items, item);
             if (e.steps == 0) break;
             const Segment g = e.segment();
-            const int packed_rows = g.nq * p.group, skip = WorkCut::skipped(p, g, e.t), i0 = e.i0 + skip, i1 = ok ? e.i1 + skip : i0, h = e.h;
+            const int packed_rows = g.nq * p.group, skip = CAUSAL ? WorkCut::skipped(p, g, e.t) : 0, i0 = e.i0 + skip, i1 = ok ? e.i1 + skip : i0, h = e.h;
             // a row of the other side, or of the tile itself: where key r lies, or whether packed row r is wanted
             Place at;
             bool on;
@@ -472,17 +472,17 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
             long long out_row = 0;
             bool masked = false;
             int keys = item.nk;             // queries stationary: keys that the row reads
-            // under the triangle: how many of the item's columns, from this thread's first one on, are left out (keys stationary: rows in
-            // front of the first one that reads the key) or read (queries stationary)
+            // under the triangle, from this thread's first column of the item on: columns that are left out (keys stationary: rows in front of
+            // the first one that reads the key), or columns that are read (queries stationary)
             int edge = KV ? 0 : INT32_MAX;
             if (KV) {
                 out_row = (long long)(item.k0 + r) * p.kv_heads + item.h;
                 masked = valid && (item.nq == 0 || key_place(p, item.segment(), item.s, r).at < 0);
-                if (p.causal && valid) edge = (min(max(r - (item.length - item.nq), 0), item.nq) * p.group) - (item.i0 + WorkCut::skipped(p, item.segment(), item.t)) * BWD_STEP - 32 * x;
+                if (CAUSAL && valid) edge = min(max(r - (item.length - item.nq), 0), item.nq) * p.group - (item.i0 + WorkCut::skipped(p, item.segment(), item.t)) * BWD_STEP - 32 * x;
             } else if (valid) {
                 const PackedRow pr = packed_row(p, item.segment(), item.h, r);
-                keys = keys_of_row(p, item.segment(), pr.row - item.q0);
-                if (p.causal) edge = keys - item.i0 * BWD_STEP - 32 * x;
+                if (CAUSAL) keys = keys_of_row(p, item.segment(), pr.row - item.q0);
+                if (CAUSAL) edge = keys - item.i0 * BWD_STEP - 32 * x;
                 out_row = (long long)pr.row * p.heads + pr.head;
                 const float2 st = w.stats[out_row];
                 my_lse = dup2(BIAS - st.x);
@@ -500,9 +500,12 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
                     uint32_t v[32];
                     tmem_ld32(S, v);
                     const float4* nl = reinterpret_cast<const float4*>(ctl.minus_lse[aux] + 32 * x);
-                    const int at = edge - i * BWD_STEP;
-                    const uint32_t keep = KV ? (at <= 0 ? ~0u : at >= 32 ? 0u : ~0u << at) : ctl.mask[aux][x] & (at >= 32 ? ~0u : at <= 0 ? 0u : (1u << at) - 1);
-                    const bool whole = __all_sync(~0u, keep == ~0u);
+                    uint32_t keep = KV ? ~0u : ctl.mask[aux][x];
+                    if (CAUSAL) {
+                        const int at = edge - i * BWD_STEP;
+                        keep &= KV ? (at <= 0 ? ~0u : at >= 32 ? 0u : ~0u << at) : at >= 32 ? ~0u : at <= 0 ? 0u : (1u << at) - 1;
+                    }
+                    const bool whole = CAUSAL ? __all_sync(~0u, keep == ~0u) : keep == ~0u;
                     tmem_wait_ld(v);
 #pragma unroll
                     for (int k = 0; k < 16; ++k) {
@@ -599,10 +602,10 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
     if (warp == BWD_MMA) { tmem_fence_after(); tmem_free(tmem, 512); }
 }
 
-template <typename T, int DP>
-__global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(const AttnParams p, const BwdWork w, const __grid_constant__ TileMaps maps, const int kv_blocks) {
-    if ((int)blockIdx.x < kv_blocks) backward_pass<T, DP, true>(p, w, maps, blockIdx.x, kv_blocks);
-    else backward_pass<T, DP, false>(p, w, maps, (int)blockIdx.x - kv_blocks, (int)gridDim.x - kv_blocks);
+template <typename T, int DP, bool CAUSAL>
+__global__ void __launch_bounds__(BWD_THREADS, 1) attention_backward_kernel(const __grid_constant__ AttnParams p, const BwdWork w, const __grid_constant__ TileMaps maps, const int kv_blocks) {
+    if ((int)blockIdx.x < kv_blocks) backward_pass<T, DP, true, CAUSAL>(p, w, maps, blockIdx.x, kv_blocks);
+    else backward_pass<T, DP, false, CAUSAL>(p, w, maps, (int)blockIdx.x - kv_blocks, (int)gridDim.x - kv_blocks);
 }
 
 // Adds up the partial sums of a tile that several blocks shared, in the order of its steps.  A warp has a row of one gradient; many parts
@@ -714,7 +717,8 @@ static tiga_status launch_backward(AttnParams p, const BwdWork& w, cudaStream_t 
     if (sms <= 0) return TIGA_ERR_CUDA;
     const int kv_blocks = (p.gk || p.gv) && p.n_kv ? sms : 0, q_blocks = p.gq && p.n_q ? sms : 0;
     if (kv_blocks + q_blocks == 0) return TIGA_OK;
-    TIGA_CUDA_TRY(cudaFuncSetAttribute(attention_backward_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, Bwd<DP>::SMEM));
+    const auto kernel = p.causal ? attention_backward_kernel<T, DP, true> : attention_backward_kernel<T, DP, false>;
+    TIGA_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Bwd<DP>::SMEM));
     // blocks by the work there may be: a row of values costs about half of one of queries
     const long long q_work = (long long)p.n_q * p.heads, v_work = operand_type<T>() == 0 ? ((long long)p.n_kv * p.kv_heads + 1) / 2 : 0;
     long long grid = ((q_work + v_work) * (DP / 8) + PREP_THREADS - 1) / PREP_THREADS;
@@ -728,7 +732,7 @@ static tiga_status launch_backward(AttnParams p, const BwdWork& w, cudaStream_t 
         backward_plan_kernel<<<counted(2), PLAN_THREADS, 0, s>>>(p, w, operand_type<T>() == 0);
         TIGA_CUDA_TRY(launch_after(attention_prepare_kernel<T, DP / 8>, dim3((unsigned)grid), PREP_THREADS, 0, s, p, w, prep_q, prep_v));
     } else attention_prepare_kernel<T, DP / 8><<<counted((unsigned)grid), PREP_THREADS, 0, s>>>(p, w, prep_q, prep_v);
-    TIGA_CUDA_TRY(launch_after(attention_backward_kernel<T, DP>, dim3(kv_blocks + q_blocks), BWD_THREADS, Bwd<DP>::SMEM, s, p, w, maps, kv_blocks));
+    TIGA_CUDA_TRY(launch_after(kernel, dim3(kv_blocks + q_blocks), BWD_THREADS, Bwd<DP>::SMEM, s, p, w, maps, kv_blocks));
     TIGA_CUDA_TRY(launch_after(attention_sum_kernel<T, DP>, dim3(kv_blocks + q_blocks, SUM_Y), SUM_WARPS * 32, 0, s, p, w, kv_blocks));
     return launch_status();
 }

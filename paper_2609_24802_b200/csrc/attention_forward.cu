@@ -34,6 +34,7 @@ template <int DP> struct Fwd {
 struct FwdControl {
     unsigned long long full[10], empty[10], q_full, q_empty, s_full[2], p_full[2], o_full[2], mask_full[MASK_RING], drain;
     ItemRing items;
+    Walker<FwdCut> walk;
     uint32_t tmem, abort_word, mask[MASK_RING][4];
     float share[2][2][128];             // what a row's threads tell each other
 };
@@ -50,7 +51,7 @@ struct FwdWork {
 static __global__ void __launch_bounds__(PLAN_THREADS) forward_plan_kernel(const AttnParams p, long long* unit_start) { plan_units<FwdCut>(p, unit_start); }
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const AttnParams p, const FwdWork w, const __grid_constant__ TileMaps maps) {
+__global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const __grid_constant__ AttnParams p, const FwdWork w, const __grid_constant__ TileMaps maps) {
     typedef Fwd<DP> C;
     extern __shared__ __align__(1024) unsigned char smem[];
     FwdControl& ctl = *reinterpret_cast<FwdControl*>(smem + C::CONTROL);
@@ -72,9 +73,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
         ctl.abort_word = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    Walker<FwdCut> walk;
-    bool work_here = false;
-    if (warp == FWD_WALKER) work_here = walk.begin(p, w.unit_start, blockIdx.x, gridDim.x);
+    if (warp == FWD_WALKER) walk_begin(&ctl.walk, p, w.unit_start, blockIdx.x, gridDim.x);
     if (warp == FWD_MMA) tmem_alloc(smem_u32(&ctl.tmem), 512);
     tmem_fence_before();
     __syncthreads();
@@ -84,8 +83,9 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
 
     if (warp == FWD_WALKER) {
         if (lane == 0) {
-            w.joints[blockIdx.x] = joint_of(walk, work_here, blockIdx.x);
-            items_hand_out(ctl.items, p, walk, work_here);
+            Walker<FwdCut> walk = ctl.walk;
+            w.joints[blockIdx.x] = joint_of(walk, walk.here, blockIdx.x);
+            items_hand_out(ctl.items, p, walk, walk.here);
         }
         __syncwarp();
     } else if (warp >= FWD_PRODUCER && warp < FWD_MMA) {

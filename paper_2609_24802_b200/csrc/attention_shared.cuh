@@ -242,6 +242,7 @@ struct Walker {
     int steps, i0, i1;          // steps of the tile, and which of them are this block's
     long long left;             // units behind this item
     long long units, blocks;    // of the whole line: units, and blocks that share them
+    bool here;                  // this block has any
 
     __device__ __forceinline__ void open(const AttnParams& p) {
         steps = C::steps(p, g, t);
@@ -325,6 +326,15 @@ struct Walker {
     }
 };
 
+// The beginning of a block's piece, out of line: the triangle's closed forms want many registers for a moment, which inlined were spilled from
+// the loops of the other warps (chunk of 2048 on 16384: 559 us instead of 510).
+template <typename C>
+static __device__ __noinline__ void walk_begin(Walker<C>* to, const AttnParams& p, const long long* unit_start, int block, int grid) {
+    Walker<C> w{};
+    w.here = w.begin(p, unit_start, block, grid);
+    if (threadIdx.x % 32 == 0) *to = w;
+}
+
 // unit_start[s]: units in front of segment s.  By one block.
 constexpr int PLAN_THREADS = 1024;
 template <typename C>
@@ -380,6 +390,10 @@ tiga_status attention_forward(const AttnParams& p, bool bf16, void* ws, cudaStre
 // host checks of the descriptors (attention.cu)
 tiga_status attention_heads_check(const tiga_heads* h);
 tiga_status attention_pages_check(const tiga_pages* c);
+tiga_status attention_paged_check(const tiga_pages* c, const tiga_heads* h, int64_t n_q, AttnParams* p);
+bool attention_bad_ints(const void* p);
+bool attention_bad_weights(const tiga_weights* a);
+bool attention_weights_overlap(const tiga_weights* a, int64_t n_seg, int64_t kv_heads);
 bool attention_bad_stride(const tiga_stride& s);
 
 template <typename T> struct Half;
