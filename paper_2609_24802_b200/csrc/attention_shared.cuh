@@ -19,6 +19,7 @@ struct AttnParams {
     int n_seg, n_q, n_kv, heads, kv_heads, group, D, causal;
     long long n_pages, page_size, table_stride, max_pages, page_stride, slot_stride;
     float scale;
+    int item_cost;                  // units that a tile costs beside its steps (0: none; see Cut)
     int kv_box, q_box;              // rows that a box of the tensor maps brings (0: rows are copied one by one)
 };
 
@@ -166,6 +167,10 @@ __host__ __device__ __forceinline__ long long lattice_points(long long n, long l
 // side in steps; a unit is one step of one tile of one kv head.  All units of a call stand in one line (segment, kv head, tile,
 // step), and the blocks take equal pieces of it: a piece that begins or ends inside a tile leaves a partial state in the
 // workspace, and a last kernel joins those in order.  So short and long, few and many rows are balanced by one rule.
+// Beginning and ending a tile takes a block as long as some steps do (about 15000 cycles forward, where a step takes 3700).  Where the
+// tiles of a line have all numbers of steps, as under a triangle, equal numbers of steps would give the blocks of its short tiles several
+// times the work, so a tile counts item_cost units more, in front of its steps.  Under them nothing is done: a piece that ends there has
+// none of the tile, one that begins there has its first step.
 template <int TILE_, int STEP_, bool KEYS_>
 struct Cut {
     static constexpr int TILE = TILE_, STEP = STEP_;      // stationary rows of a tile, rows of a step: powers of two
@@ -195,9 +200,9 @@ struct Cut {
         n = n / STEP + (n % STEP != 0) - skipped(p, g, t);
         return n > 1 ? n : 1;
     }
-    // Units of the first t tiles (t <= tiles()).  Under the triangle steps(k) is max(1, floor((x k + y) / z)), cut off at the segment's
+    // Steps of the first t tiles (t <= tiles()).  Under the triangle steps(k) is max(1, floor((x k + y) / z)), cut off at the segment's
     // keys or rows: a sum of floors in the middle.
-    static __host__ __device__ __forceinline__ long long before(const AttnParams& p, const Segment& g, int t) {
+    static __host__ __device__ __forceinline__ long long steps_before(const AttnParams& p, const Segment& g, int t) {
         if (t == 0) return 0;
         if (!p.causal) return (long long)t * steps(p, g, 0);
         const long long c = (long long)g.length - g.nq;
@@ -217,7 +222,8 @@ struct Cut {
         const long long k1 = lo < 0 ? 0 : lo < n ? lo : n, k2 = hi < k1 ? k1 : hi < n ? hi : n;
         return k1 + (k1 < k2 ? lattice_points(k2 - k1, TILE, TILE * k1 + b, m) : 0) + (n - k2) * most + (t > last ? steps(p, g, last) : 0);
     }
-    // units of a kv head
+    // units of the first t tiles, and of all tiles of a kv head
+    static __host__ __device__ __forceinline__ long long before(const AttnParams& p, const Segment& g, int t) { return steps_before(p, g, t) + (long long)t * p.item_cost; }
     static __host__ __device__ __forceinline__ long long units(const AttnParams& p, const Segment& g) { return before(p, g, tiles(p, g)); }
 };
 
@@ -244,10 +250,14 @@ struct Walker {
     long long units, blocks;    // of the whole line: units, and blocks that share them
     bool here;                  // this block has any
 
-    __device__ __forceinline__ void open(const AttnParams& p) {
+    // the tile's steps from its unit `off` on; false: the piece ends in front of the tile's first step
+    __device__ __forceinline__ bool open(const AttnParams& p, int off) {
         steps = C::steps(p, g, t);
-        i1 = (int)min((long long)steps, i0 + left);
-        left -= i1 - i0;
+        const int end = (int)min((long long)steps + p.item_cost, off + left);
+        left -= end - off;
+        i0 = max(off - p.item_cost, 0);
+        i1 = max(end - p.item_cost, 0);
+        return i1 > i0;
     }
     __device__ __forceinline__ long long first_unit(long long block) const { return quotient(block * units, blocks); }
 
@@ -290,9 +300,9 @@ struct Walker {
         h = (int)quotient(off, per_head);
         off -= h * per_head;
         if (!p.causal) {
-            const int n = C::steps(p, g, 0);
+            const int n = C::steps(p, g, 0) + p.item_cost;
             t = (int)quotient(off, n);
-            i0 = (int)(off - (long long)t * n);
+            off -= (long long)t * n;
         } else {            // the last tile that begins at or before this unit, 32 places a round
             int hi = C::tiles(p, g);
             t = 0;
@@ -302,14 +312,12 @@ struct Walker {
                 t += (31 - __clz(before)) * gap;
                 hi = min(hi, t + gap);
             }
-            i0 = (int)(off - C::before(p, g, t));
+            off -= C::before(p, g, t);
         }
-        open(p);
-        return true;
+        return open(p, (int)off);
     }
     __device__ __forceinline__ bool next(const AttnParams& p) {
         if (left <= 0) return false;
-        i0 = 0;
         if (++t >= C::tiles(p, g)) {
             t = 0;
             if (++h >= p.kv_heads) {
@@ -317,10 +325,9 @@ struct Walker {
                 do { g = segment_of(p, ++s); } while (C::rows(p, g) == 0);
             }
         }
-        open(p);
-        return true;
+        return open(p, 0);
     }
-    // after begin(): the block in which this item's tile begins
+    // after begin() inside of a tile's steps: the block in which its first step lies
     __device__ __forceinline__ int first_block(int block) const {
         return (int)quotient((first_unit(block) - i0 + 1) * blocks - 1, units);
     }

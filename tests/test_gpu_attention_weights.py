@@ -85,7 +85,7 @@ def reference(c, lse, causal, before, out):
         old = 0.0 if before is None else before[b, :, :w].double()
         want[b, :, :w] = (old + fold(p)[:, :w])
         rows = n * q.shape[1] // hk
-        tol[b, :, :w] = (fold(p * off) + (rows + 4) * 2.0 ** -24 * fold(p))[:, :w] + 2.0 ** -24 * want[b, :, :w].abs() + rows * 2.0 ** -125
+        tol[b, :, :w] = (fold(torch.where(reads, p * off, 0.0)) + (rows + 4) * 2.0 ** -24 * fold(p))[:, :w] + 2.0 ** -24 * want[b, :, :w].abs() + rows * 2.0 ** -125
         q0 += n
     return want, tol
 
