@@ -456,6 +456,23 @@ size_t tiga_paged_attention_workspace_bytes(const tiga_pages* c, const tiga_head
 tiga_status tiga_apply_paged_attention(const tiga_pages* c, const tiga_heads* h, const void* q, const int32_t* q_start, int64_t n_q,
                                        int causal, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
 
+/* Sequences whose caches begin alike: the sequences [group_start[g], group_start[g+1]) of group g find their positions [0, shared[g]) in
+ * the same pages (those that the table names for the group's first sequence are read).  Sequences in no group share nothing. */
+typedef struct {
+    const int32_t* group_start; /* device, int32 [n_groups + 1], ascending numbers of sequences */
+    const int32_t* shared;      /* device, int32 [n_groups] */
+    int64_t n_groups;           /* n_groups + n_seg at most 2^24 */
+} tiga_prefixes;
+
+/* tiga_apply_paged_attention for a batch whose sequences share prefixes: a group's rows meet the shared positions together, once, and
+ * each sequence's rows the positions behind them; the two states of a row are joined as partial states are.  The result is that of
+ * tiga_apply_paged_attention (in another order of the sums), whatever shared says: positions that some row of the group does not read
+ * are not taken as shared, and a group shares nothing where that saves no work.
+ *   ws: tiga_shared_attention_workspace_bytes(c, h, g, n_q) bytes. */
+size_t tiga_shared_attention_workspace_bytes(const tiga_pages* c, const tiga_heads* h, const tiga_prefixes* g, int64_t n_q);
+tiga_status tiga_apply_shared_attention(const tiga_pages* c, const tiga_heads* h, const tiga_prefixes* g, const void* q, const int32_t* q_start,
+                                        int64_t n_q, int causal, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
 /* A number for every position of every (sequence, kv head): entry (s, h, j) lies at data + s * seg + h * head + j, strides in
  * elements, j < length.  fp32, the base 16-byte aligned; lists of an output share no entries. */
 typedef struct { float* data; int64_t seg, head, length; } tiga_weights;

@@ -26,6 +26,7 @@ __all__ = [
     "BF16", "DenseRelation", "tiga_dense_attention_workspace_bytes", "tiga_apply_dense_attention",
     "tiga_apply_dense_attention_backward", "TriangularRelation", "tiga_triangular_attention_workspace_bytes",
     "tiga_apply_triangular_attention", "tiga_apply_triangular_attention_backward", "PagedCache", "tiga_paged_attention_workspace_bytes", "tiga_apply_paged_attention",
+    "SharedPrefixes", "tiga_shared_attention_workspace_bytes", "tiga_apply_shared_attention",
     "tiga_paged_weights_workspace_bytes", "tiga_paged_attention_weights", "tiga_paged_evict",
     "tiga_paged_append", "ROT_PLAIN", "ROT_LINEAR", "ROT_BASE", "ROT_BANDS", "tiga_rotary_frequencies", "Rotary", "tiga_apply_rotary",
 ]
@@ -48,6 +49,7 @@ EXPORTS = [
     "tiga_dense_attention_workspace_bytes", "tiga_apply_dense_attention", "tiga_apply_dense_attention_backward",
     "tiga_triangular_attention_workspace_bytes", "tiga_apply_triangular_attention", "tiga_apply_triangular_attention_backward",
     "tiga_paged_attention_workspace_bytes", "tiga_apply_paged_attention", "tiga_paged_append", "tiga_rotary_frequencies", "tiga_apply_rotary",
+    "tiga_shared_attention_workspace_bytes", "tiga_apply_shared_attention",
     "tiga_paged_weights_workspace_bytes", "tiga_paged_attention_weights", "tiga_paged_evict",
 ]
 
@@ -105,6 +107,10 @@ class _Pages(ctypes.Structure):
     _fields_ = [("key", ctypes.c_void_p), ("value", ctypes.c_void_p), ("table", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
                 ("n_seg", ctypes.c_int64), ("n_pages", ctypes.c_int64), ("page_size", ctypes.c_int64), ("table_stride", ctypes.c_int64),
                 ("max_pages", ctypes.c_int64), ("page_stride", ctypes.c_int64), ("slot_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class _Prefixes(ctypes.Structure):
+    _fields_ = [("group_start", ctypes.c_void_p), ("shared", ctypes.c_void_p), ("n_groups", ctypes.c_int64)]
 
 
 class _Weights(ctypes.Structure):
@@ -201,6 +207,10 @@ def load_library() -> ctypes.CDLL:
     lib.tiga_paged_attention_workspace_bytes.argtypes = [ref(_Pages), ref(_Heads), i64]
     lib.tiga_apply_paged_attention.restype = ctypes.c_int
     lib.tiga_apply_paged_attention.argtypes = [ref(_Pages), ref(_Heads), vp, vp, i64, ctypes.c_int, vp, vp, vp, sz, vp]
+    lib.tiga_shared_attention_workspace_bytes.restype = sz
+    lib.tiga_shared_attention_workspace_bytes.argtypes = [ref(_Pages), ref(_Heads), ref(_Prefixes), i64]
+    lib.tiga_apply_shared_attention.restype = ctypes.c_int
+    lib.tiga_apply_shared_attention.argtypes = [ref(_Pages), ref(_Heads), ref(_Prefixes), vp, vp, i64, ctypes.c_int, vp, vp, vp, sz, vp]
     lib.tiga_paged_weights_workspace_bytes.restype = sz
     lib.tiga_paged_weights_workspace_bytes.argtypes = [ref(_Pages), ref(_Heads), i64]
     lib.tiga_paged_attention_weights.restype = ctypes.c_int
@@ -873,6 +883,44 @@ def tiga_apply_paged_attention(cache: PagedCache, q, q_start, scale: float, caus
                                           _dense_out(out, q.shape, q.dtype, "out"),
                                           None if lse is None else _dense_out(lse, q.shape[:2], torch.float32, "lse"),
                                           _ptr(ws), ws.numel(), _stream(stream)), "tiga_apply_paged_attention")
+    return out, lse, ws
+
+
+class SharedPrefixes(_Held):
+    """Sequences whose caches begin with the same pages: those of group g, [group_start[g], group_start[g+1]), share their positions
+    [0, shared[g]); group_start int32 [n_groups + 1], shared int32 [n_groups], both on the device."""
+    _held = ("group_start", "shared")
+
+    def __init__(self, group_start, shared):
+        _ints(shared, None, "shared")
+        _ints(group_start, shared.numel() + 1, "group_start")
+        _same(group_start, shared)
+        self.c = _Prefixes(group_start.data_ptr(), shared.data_ptr(), shared.numel())
+        self.__dict__.update(group_start=group_start, shared=shared, ref=ctypes.byref(self.c))
+
+
+def tiga_shared_attention_workspace_bytes(cache: PagedCache, prefixes: SharedPrefixes, q) -> int:
+    return int(_L.tiga_shared_attention_workspace_bytes(cache.ref, ctypes.byref(_paged_heads(cache, q, 1.0)), prefixes.ref, q.shape[0]))
+
+
+def tiga_apply_shared_attention(cache: PagedCache, prefixes: SharedPrefixes, q, q_start, scale: float, causal=True, out=None, lse=None, want_lse=True,
+                                ws=None, stream=None):
+    """tiga_apply_paged_attention for sequences that share prefixes: what a group shares is read once for all of its rows.  Returns
+    (out, lse, ws)."""
+    with _on(q, stream):
+        h = _paged_heads(cache, q, scale)
+        _same(q, q_start, prefixes.shared, out, lse, ws)
+        start = _ints(q_start, cache.n_seg + 1, "q_start")
+        if out is None:
+            out = q.new_empty(q.shape)
+        if want_lse and lse is None:
+            lse = q.new_empty(q.shape[:2], dtype=torch.float32)
+        if ws is None:
+            ws = _scratch(_L.tiga_shared_attention_workspace_bytes(cache.ref, ctypes.byref(h), prefixes.ref, q.shape[0]), q)
+        _ok(_L.tiga_apply_shared_attention(cache.ref, ctypes.byref(h), prefixes.ref, q.data_ptr(), start, q.shape[0], int(bool(causal)),
+                                           _dense_out(out, q.shape, q.dtype, "out"),
+                                           None if lse is None else _dense_out(lse, q.shape[:2], torch.float32, "lse"),
+                                           _ptr(ws), ws.numel(), _stream(stream)), "tiga_apply_shared_attention")
     return out, lse, ws
 
 

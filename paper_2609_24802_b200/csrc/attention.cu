@@ -223,3 +223,35 @@ extern "C" tiga_status tiga_apply_paged_attention(const tiga_pages* c, const tig
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     return attention_forward(p, h->dtype == TIGA_BF16, ws, s);
 }
+
+static tiga_status prefixes_check(const tiga_pages* c, const tiga_heads* h, const tiga_prefixes* g, int64_t n_q, AttnParams* p) {
+    const tiga_status st = attention_paged_check(c, h, n_q, p);
+    if (st != TIGA_OK) return st;
+    if (!g || g->n_groups < 0) return TIGA_ERR_INVALID_ARG;
+    return g->n_groups + c->n_seg > (1 << 24) ? TIGA_ERR_UNSUPPORTED : TIGA_OK;
+}
+
+extern "C" size_t tiga_shared_attention_workspace_bytes(const tiga_pages* c, const tiga_heads* h, const tiga_prefixes* g, int64_t n_q) {
+    AttnParams p;
+    if (prefixes_check(c, h, g, n_q, &p) != TIGA_OK) return 0;
+    return attention_shared_bytes(p, (int)g->n_groups) + 256;
+}
+
+extern "C" tiga_status tiga_apply_shared_attention(const tiga_pages* c, const tiga_heads* h, const tiga_prefixes* g, const void* q, const int32_t* q_start,
+                                                   int64_t n_q, int causal, void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+    AttnParams p;
+    tiga_status st = prefixes_check(c, h, g, n_q, &p);
+    if (st != TIGA_OK) return st;
+    if (attention_bad_stride(h->q)) return TIGA_ERR_INVALID_ARG;
+    if (c->n_seg == 0 || n_q == 0) return TIGA_OK;
+    if (bad_ints(q_start) || bad_ints(c->kv_len) || bad_array(q) || bad_array(out)) return TIGA_ERR_INVALID_ARG;
+    if (bad_ints(g->group_start) || (g->n_groups > 0 && bad_ints(g->shared))) return TIGA_ERR_INVALID_ARG;
+    if ((c->max_pages > 0 && bad_ints(c->table)) || (c->n_pages > 0 && (bad_array(c->key) || bad_array(c->value)))) return TIGA_ERR_INVALID_ARG;
+    if (lse && !aligned16(lse)) return TIGA_ERR_INVALID_ARG;
+    if (!ws || !aligned16(ws) || ws_bytes < tiga_shared_attention_workspace_bytes(c, h, g, n_q)) return TIGA_ERR_WORKSPACE;
+    if (c->max_pages == 0) p.table = c->kv_len;         // (as above)
+    p.q = q; p.q_start = q_start; p.causal = causal != 0; p.out = out; p.lse = lse;
+    const Prefixes x = {g->group_start, g->shared, (int)g->n_groups};
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    return attention_shared(p, x, h->dtype == TIGA_BF16, ws, s);
+}

@@ -46,11 +46,22 @@ struct FwdWork {
     float* part_o;                  // [2 * grid][rows][DP]: unnormalised
     Joint* joints;                  // [grid]
     int rows;                       // packed rows that a partial state holds at most
+    // shared prefixes
+    int n_groups, n_seq;
+    long long state_rows;           // rows that there is room for
+    const int32_t* line_row;        // [n_groups + n_seq]: the row of the page table that a segment of the line reads
+    const long long* line_state;    // [n_groups + n_seq]: what is added to a row's number for its place among the states
+    const int32_t* first_member;    // [n_groups]
+    const long long* state_start;   // [n_groups + 1]: rows of the groups in front that share
+    float2* state_ml;               // [2][state_rows][heads]: as part_ml, of the shared and of the own keys
+    float* state_o;                 // [2][state_rows][heads][DP]
 };
+// Whether a segment of the line has the only state of its rows.
+__device__ __forceinline__ bool only_state(const FwdWork& w, int s, int k0) { return s >= w.n_groups && k0 == 0; }
 
 static __global__ void __launch_bounds__(PLAN_THREADS) forward_plan_kernel(const AttnParams p, long long* unit_start) { plan_units<FwdCut>(p, unit_start); }
 
-template <typename T, int DP>
+template <typename T, int DP, bool SHARED>
 __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const __grid_constant__ AttnParams p, const FwdWork w, const __grid_constant__ TileMaps maps) {
     typedef Fwd<DP> C;
     extern __shared__ __align__(1024) unsigned char smem[];
@@ -84,7 +95,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
     if (warp == FWD_WALKER) {
         if (lane == 0) {
             Walker<FwdCut> walk = ctl.walk;
-            w.joints[blockIdx.x] = joint_of(walk, walk.here, blockIdx.x);
+            w.joints[blockIdx.x] = joint_of(walk, walk.here && (!SHARED || only_state(w, walk.s, walk.g.k0)), blockIdx.x);
             items_hand_out(ctl.items, p, walk, walk.here);
         }
         __syncwarp();
@@ -99,10 +110,10 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
             const Item& e = item_take(ctl.items, item);
             if (e.steps == 0) break;
             const Segment g = e.segment();
-            const int i0 = e.i0, i1 = e.i1, h = e.h;
+            const int i0 = e.i0, i1 = e.i1, h = e.h, row = SHARED ? w.line_row[e.s] : e.s;
             auto place = [&](int i) {
                 const int j = i * FWD_STEP + 32 * pw + lane;
-                return j < g.nk ? key_place(p, g, e.s, j) : Place{-1, 0};
+                return j >= g.nk ? Place{-1, 0} : SHARED ? shared_place(p, g, row, j) : key_place(p, g, row, j);
             };
             Place at = place(i0);
             for (int i = i0; i < i1 && ok; ++i, ++steps) {
@@ -358,10 +369,18 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
                 w1 = mb == -INFINITY ? 0.f : ex2(mb - m);
                 l = la * w0 + lb * w1;
             }
-            const bool whole_tile = n == e.steps;
-            const long long part = (2LL * blockIdx.x + (e.i0 == 0)) * w.rows + tile_row;
             const PackedRow pr = packed_row(p, e.segment(), e.h, e.t * FWD_ROWS + tile_row);
             const long long out_row = (long long)pr.row * p.heads + pr.head;
+            // a state that is not the rows' only one, or not whole, is put aside
+            const bool all_steps = n == e.steps, whole_tile = all_steps && (!SHARED || only_state(w, e.s, e.k0));
+            long long part = (2LL * blockIdx.x + (e.i0 == 0)) * w.rows + tile_row;
+            float* put_aside = w.part_o;
+            float2* put_ml = w.part_ml;
+            if (SHARED && all_steps && !whole_tile) {
+                part = ((e.s < w.n_groups ? 0 : w.state_rows) + w.line_state[e.s] + pr.row) * p.heads + pr.head;
+                put_aside = w.state_o;
+                put_ml = w.state_ml;
+            }
             const float finish = l > 0.f || l != l ? 1.f / l : 0.f;
             // this thread's half of the row's features, or its quarter of both states, 16 at a time
             const int f0 = two ? y * (DP / 2) : (2 * x + y) * (DP / 4), f1 = f0 + (two ? DP / 2 : DP / 4);
@@ -389,13 +408,13 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
                         }
                         store_rows<2>(o, (T*)p.out + out_row * p.D + f, valid, (p.D - f) / 8);
                     } else if (valid) {
-                        uint4* out = reinterpret_cast<uint4*>(w.part_o + part * DP + f);
+                        uint4* out = reinterpret_cast<uint4*>(put_aside + part * DP + f);
 #pragma unroll
                         for (int k = 0; k < 4; ++k) out[k] = make_uint4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
                     }
                 }
             if (valid && y == 0 && (two || x == 0)) {
-                if (!whole_tile) w.part_ml[part] = make_float2(m - BIAS, l);
+                if (!whole_tile) put_ml[part] = make_float2(m - BIAS, l);
                 else if (p.lse) p.lse[out_row] = l == 0.f ? -INFINITY : (m - BIAS + log2f(l)) * LN2_F;
             }
             tmem_fence_before();
@@ -419,9 +438,8 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
 constexpr int JOIN_WARPS = 8, JOIN_Y = 16, JOIN_FEW = 8;
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(JOIN_WARPS * 32) attention_join_kernel(const AttnParams p, const FwdWork w) {
-    wait_for_previous_kernel();
-    const Joint& j = w.joints[blockIdx.x];
+__device__ __forceinline__ void join_block(const AttnParams& p, const FwdWork& w, const int block, const int slice) {
+    const Joint& j = w.joints[block];
     const int parts = j.parts;
     if (parts == 0) return;
     const Item it = j.item;
@@ -430,7 +448,7 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) attention_join_kernel(const A
     constexpr int E = DP / 32;
     __shared__ float sh_m[JOIN_WARPS], sh_l[JOIN_WARPS], sh_o[JOIN_WARPS][DP];
     const bool few = parts <= JOIN_FEW;
-    for (int r = few ? blockIdx.y * JOIN_WARPS + warp : blockIdx.y; r < rows; r += few ? JOIN_Y * JOIN_WARPS : JOIN_Y) {
+    for (int r = few ? slice * JOIN_WARPS + warp : slice; r < rows; r += few ? JOIN_Y * JOIN_WARPS : JOIN_Y) {
         const int a = few ? 0 : parts * warp / JOIN_WARPS, b = few ? parts : parts * (warp + 1) / JOIN_WARPS;
         float m = -INFINITY, l = 0.f, o[E];
 #pragma unroll
@@ -494,6 +512,12 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) attention_join_kernel(const A
     }
 }
 
+template <typename T, int DP>
+__global__ void __launch_bounds__(JOIN_WARPS * 32) attention_join_kernel(const AttnParams p, const FwdWork w) {
+    wait_for_previous_kernel();
+    join_block<T, DP>(p, w, blockIdx.x, blockIdx.y);
+}
+
 size_t attention_forward_carve(const AttnParams& p, void* ws, FwdWork* w) {
     const size_t slots = 2 * (size_t)MAX_SMS;
     const long long packed = (long long)p.n_q * p.group;
@@ -515,10 +539,10 @@ static tiga_status launch_forward(AttnParams p, const FwdWork& w, cudaStream_t s
     const int sms = attention_grid();
     if (sms <= 0) return TIGA_ERR_CUDA;
     // asked for on every call: the attribute belongs to the current device
-    TIGA_CUDA_TRY(cudaFuncSetAttribute(attention_forward_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, Fwd<DP>::SMEM));
+    TIGA_CUDA_TRY(cudaFuncSetAttribute(attention_forward_kernel<T, DP, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, Fwd<DP>::SMEM));
     if (w.unit_start) forward_plan_kernel<<<counted(1), PLAN_THREADS, 0, s>>>(p, w.unit_start);
-    if (w.unit_start) TIGA_CUDA_TRY(launch_after(attention_forward_kernel<T, DP>, dim3(sms), FWD_THREADS, Fwd<DP>::SMEM, s, p, w, maps));
-    else attention_forward_kernel<T, DP><<<counted((unsigned)sms), FWD_THREADS, Fwd<DP>::SMEM, s>>>(p, w, maps);
+    if (w.unit_start) TIGA_CUDA_TRY(launch_after(attention_forward_kernel<T, DP, false>, dim3(sms), FWD_THREADS, Fwd<DP>::SMEM, s, p, w, maps));
+    else attention_forward_kernel<T, DP, false><<<counted((unsigned)sms), FWD_THREADS, Fwd<DP>::SMEM, s>>>(p, w, maps);
     TIGA_CUDA_TRY(launch_after(attention_join_kernel<T, DP>, dim3(sms, JOIN_Y), JOIN_WARPS * 32, 0, s, p, w));
     return launch_status();
 }
@@ -528,6 +552,235 @@ tiga_status attention_forward(const AttnParams& p, bool bf16, void* ws, cudaStre
     attention_forward_carve(p, ws, &w);
     if (bf16) return p.D > 64 ? launch_forward<__nv_bfloat16, 128>(p, w, s) : launch_forward<__nv_bfloat16, 64>(p, w, s);
     return p.D > 64 ? launch_forward<__half, 128>(p, w, s) : launch_forward<__half, 64>(p, w, s);
+}
+
+// ------------------------------------------------------------------------------------------------ shared prefixes
+
+// Sequences of a group read their first P positions from the same pages.  Taken one by one, a new token's few rows fill little of a tile,
+// and every sequence reads the shared pages again.  So a group's rows, which lie one behind the other, are one segment over the shared
+// positions (a dense block: each of them reads all), and every sequence's rows another over the positions behind them; both kinds stand
+// in one line, shared ones first, and are cut as everything else.  A row then has two states (maximum, mass, accumulator), which a last
+// kernel joins.  The shared positions are a hint, not a part of the result: they are cut so that every row of the group reads all of
+// them, and a group shares nothing where that would not make fewer steps.
+//
+// What the group's sequences cost alone, in halves of a step for every 128 shared positions, against the group together.
+__device__ __forceinline__ int tile_halves(int packed) {            // of a segment's tiles; one of at most 128 rows costs half of a full one
+    const int rest = packed % FWD_ROWS;
+    return 2 * (packed / FWD_ROWS) + (rest == 0 ? 0 : rest <= 128 ? 1 : 2);
+}
+constexpr int SHARED_ITEM_COST = 4;         // of a tile, in steps (attention_shared.cuh)
+// Rows of a group that shares: up to a full tile for each member on average (longer chunks fill their tiles alone).
+__host__ __device__ __forceinline__ long long most_state_rows(long long n_seq, long long n_q, int group) {
+    const long long n = (n_seq * FWD_ROWS + group - 1) / group;
+    return n < n_q ? n : n_q;
+}
+
+struct SharedPlan {
+    Segment* line;
+    int32_t *line_row, *first_member;
+    long long *line_state, *state_start, *unit_start;
+};
+
+// One block: a warp for each group, a thread for each sequence, then the units.
+static __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(const AttnParams p, const Prefixes x, const SharedPlan plan, const long long state_rows) {
+    wait_for_previous_kernel();
+    let_next_kernel_start();
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, n_seq = p.n_seg;
+    const long long most = min(min(p.max_pages * p.page_size, MOST_ROWS), 1LL << 30);
+    for (int g = warp; g < x.n_groups; g += PLAN_THREADS / 32) {
+        const int a = clamp_to(x.group_start[g], n_seq), b = max(clamp_to(x.group_start[g + 1], n_seq), a);
+        long long shared = min((long long)max(x.shared[g], 0), most);
+        int halves = 0;
+        for (int s = a + lane; s < b; s += 32) {
+            const Segment e = segment_of(p, s);
+            if (e.nq == 0) continue;
+            shared = min(shared, (long long)(p.causal ? max(e.length - e.nq + 1, 0) : e.length));
+            halves += tile_halves(e.nq * p.group);
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) shared = min(shared, __shfl_xor_sync(~0u, shared, o));
+        halves = __reduce_add_sync(~0u, halves);
+        const int q0 = clamp_to(p.q_start[a], p.n_q), nq = max(clamp_to(p.q_start[b], p.n_q) - q0, 0);
+        const long long steps = quotient(shared + FWD_STEP - 1, FWD_STEP), tiles = quotient((long long)nq * p.group + FWD_ROWS - 1, FWD_ROWS);
+        const bool pays = (long long)nq * p.group <= (long long)(b - a) * FWD_ROWS && (halves - tile_halves(nq * p.group)) * steps > 2 * SHARED_ITEM_COST * tiles && nq < 1 << 30;
+        if (lane == 0) {
+            plan.first_member[g] = a;
+            plan.line_row[g] = a;
+            plan.line[g] = {q0, pays ? nq : 0, 0, pays ? (int)shared : 0, pays ? (int)shared + nq : 0};
+        }
+    }
+    __syncthreads();
+    if (warp == 0) {            // places of the groups' states; a group for which there is no room (bounds that overlap) shares nothing
+        long long base = 0;
+        for (int g0 = 0; g0 < x.n_groups; g0 += 32) {
+            const int g = g0 + lane;
+            const long long n = g < x.n_groups ? plan.line[g].nq : 0, run = warp_running(n);
+            if (g < x.n_groups) {
+                plan.state_start[g] = base + run - n;
+                plan.line_state[g] = base + run - n - plan.line[g].q0;
+                if (base + run > state_rows) plan.line[g] = {0, 0, 0, 0, 0};
+            }
+            base += __shfl_sync(~0u, run, 31);
+        }
+        if (lane == 0) plan.state_start[x.n_groups] = min(base, state_rows);
+    }
+    __syncthreads();
+    for (int s = threadIdx.x; s < n_seq; s += PLAN_THREADS) {
+        int lo = 0, hi = x.n_groups;                // the last group that begins at or before it
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (x.group_start[mid] <= s) lo = mid + 1; else hi = mid;
+        }
+        const int g = lo - 1;
+        Segment e = segment_of(p, s);
+        long long state = 0;
+        if (g >= 0 && s >= plan.first_member[g] && s < clamp_to(x.group_start[g + 1], n_seq) && plan.line[g].nk > 0 && e.nq > 0
+            && e.q0 >= plan.line[g].q0 && (long long)e.q0 + e.nq <= (long long)plan.line[g].q0 + plan.line[g].nq) {        // (bounds that do not ascend lead nowhere)
+            const int base = plan.line[g].nk & ~31;
+            e.k0 = plan.line[g].nk;
+            e.nk = max(e.nk - base, 0);
+            e.length -= base;
+            state = plan.line_state[g];
+        }
+        plan.line[x.n_groups + s] = e;
+        plan.line_row[x.n_groups + s] = s;
+        plan.line_state[x.n_groups + s] = state;
+    }
+    __syncthreads();
+    AttnParams of_line = p;
+    of_line.line = plan.line;
+    of_line.n_seg = x.n_groups + n_seq;
+    plan_units<FwdCut>(of_line, plan.unit_start);
+}
+
+// Joins the states of tiles that several blocks shared, as above (the first blocks), and the two states of every row that has two: a warp
+// has the heads of a group of a row.  A state lies among the states where one block had its tile, else in as many parts.
+template <typename T, int DP>
+__global__ void __launch_bounds__(JOIN_WARPS * 32) shared_join_kernel(const AttnParams p, const FwdWork w, const int sms) {
+    wait_for_previous_kernel();
+    if ((int)blockIdx.x < sms * JOIN_Y) return join_block<T, DP>(p, w, blockIdx.x / JOIN_Y, blockIdx.x % JOIN_Y);
+    constexpr int E = DP / 32;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const long long units = w.unit_start[p.n_seg], blocks = min((long long)sms, max(units, 1LL));
+    auto block_of = [&](long long unit) { return (int)quotient((unit + 1) * blocks - 1, units); };
+    const long long tasks = w.state_start[w.n_groups] * p.kv_heads, stride = (long long)(gridDim.x - sms * JOIN_Y) * JOIN_WARPS;
+    for (long long task = (long long)(blockIdx.x - sms * JOIN_Y) * JOIN_WARPS + warp; task < tasks; task += stride) {
+        const long long at = quotient(task, p.kv_heads);
+        const int h = (int)(task - at * p.kv_heads);
+        const int g = last_place(w.state_start, w.n_groups, at);
+        const Segment shared = p.line[g];
+        const long long row_ll = at - w.line_state[g];
+        if (shared.nq == 0 || row_ll < shared.q0 || row_ll >= (long long)shared.q0 + shared.nq) continue;
+        const int row = (int)row_ll;
+        const int a = w.first_member[g], s = a + last_place(p.q_start + a, w.n_seq - a, row);
+        const Segment own = p.line[w.n_groups + s];
+        if (own.k0 == 0) continue;
+        int tile[2] = {-1, -1}, first[2], parts[2];
+        for (int m = 0; m < p.group; ++m) {
+            float top = -INFINITY, mass = 0.f, o[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] = 0.f;
+            const long long out_row = (long long)row * p.heads + h * p.group + m;
+#pragma unroll
+            for (int kind = 0; kind < 2; ++kind) {
+                const Segment& seg = kind ? own : shared;
+                const int packed = (row - seg.q0) * p.group + m, t = packed / FWD_ROWS, r = packed % FWD_ROWS;
+                if (t != tile[kind]) {
+                    const long long start = w.unit_start[kind ? w.n_groups + s : g] + h * FwdCut::units(p, seg) + FwdCut::before(p, seg, t) + p.item_cost;
+                    tile[kind] = t;
+                    first[kind] = block_of(start);
+                    parts[kind] = block_of(start + FwdCut::steps(p, seg, t) - 1) - first[kind] + 1;
+                }
+                const bool whole = parts[kind] == 1;
+                auto place = [&](int k) -> long long {
+                    return whole ? (kind * w.state_rows + at) * p.heads + h * p.group + m : (2LL * (first[kind] + k) + (k == 0)) * w.rows + r;
+                };
+                const float2* from_ml = whole ? w.state_ml : w.part_ml;
+                const float* from_o = whole ? w.state_o : w.part_o;
+                for (int k0 = 0; k0 < parts[kind]; k0 += 32) {
+                    const int k = k0 + lane, here = min(32, parts[kind] - k0);
+                    float2 ml = make_float2(-INFINITY, 0.f);
+                    if (k < parts[kind]) ml = from_ml[place(k)];
+                    float most = ml.x != ml.x ? INFINITY : ml.x;
+#pragma unroll
+                    for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(~0u, most, d));
+                    most = fmaxf(most, top);
+                    const float fade = top == -INFINITY ? 0.f : ex2(top - most), f = ml.x == -INFINITY ? 0.f : ex2(ml.x - most);
+                    float sum = f * ml.y;
+#pragma unroll
+                    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
+                    mass = mass * fade + sum;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) o[e] *= fade;
+                    top = most;
+#pragma unroll 4
+                    for (int n = 0; n < here; ++n) {
+                        const float fn = __shfl_sync(~0u, f, n);
+                        const float* src = from_o + place(k0 + n) * DP;
+#pragma unroll
+                        for (int e = 0; e < E; ++e) o[e] += fn * src[lane + 32 * e];
+                    }
+                }
+            }
+            const float finish = mass > 0.f || mass != mass ? 1.f / mass : 0.f;
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (lane + 32 * e < p.D) ((T*)p.out)[out_row * p.D + lane + 32 * e] = Half<T>::from(finish == 0.f ? 0.f : o[e] * finish);
+            if (lane == 0 && p.lse) p.lse[out_row] = mass == 0.f ? -INFINITY : (top + log2f(mass)) * LN2_F;
+        }
+    }
+}
+
+static size_t shared_carve(const AttnParams& p, int n_groups, void* ws, FwdWork* w, SharedPlan* plan) {
+    const size_t slots = 2 * (size_t)MAX_SMS, dp = p.D > 64 ? 128 : 64, line = (size_t)n_groups + p.n_seg;
+    const long long packed = (long long)p.n_q * p.group;
+    w->rows = (int)(packed < FWD_ROWS ? packed : FWD_ROWS);
+    w->n_groups = n_groups;
+    w->n_seq = p.n_seg;
+    w->state_rows = most_state_rows(p.n_seg, p.n_q, p.group);
+    Carver cv(ws);
+    plan->unit_start = w->unit_start = cv.take<long long>(line + 1);
+    plan->line = cv.take<Segment>(line);
+    plan->line_row = cv.take<int32_t>(line);
+    plan->line_state = cv.take<long long>(line);
+    plan->first_member = cv.take<int32_t>(n_groups);
+    plan->state_start = cv.take<long long>((size_t)n_groups + 1);
+    w->line_row = plan->line_row;
+    w->line_state = plan->line_state;
+    w->first_member = plan->first_member;
+    w->state_start = plan->state_start;
+    w->joints = cv.take<Joint>(MAX_SMS);
+    w->part_ml = cv.take<float2>(slots * w->rows);
+    w->part_o = cv.take<float>(slots * w->rows * dp);
+    w->state_ml = cv.take<float2>(2 * (size_t)w->state_rows * p.heads);
+    w->state_o = cv.take<float>(2 * (size_t)w->state_rows * p.heads * dp);
+    return cv.off;
+}
+size_t attention_shared_bytes(const AttnParams& p, int n_groups) { FwdWork w; SharedPlan plan; return shared_carve(p, n_groups, nullptr, &w, &plan); }
+
+template <typename T, int DP>
+static tiga_status launch_shared(AttnParams p, const Prefixes& g, const FwdWork& w, const SharedPlan& plan, cudaStream_t s) {
+    TileMaps maps;
+    make_tile_maps(&p, operand_type<T>() == 1, &maps);
+    const int sms = attention_grid();
+    if (sms <= 0) return TIGA_ERR_CUDA;
+    TIGA_CUDA_TRY(cudaFuncSetAttribute(attention_forward_kernel<T, DP, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Fwd<DP>::SMEM));
+    p.item_cost = SHARED_ITEM_COST;
+    shared_plan_kernel<<<counted(1), PLAN_THREADS, 0, s>>>(p, g, plan, w.state_rows);
+    p.line = plan.line;
+    p.n_seg = w.n_groups + w.n_seq;
+    TIGA_CUDA_TRY(launch_after(attention_forward_kernel<T, DP, true>, dim3(sms), FWD_THREADS, Fwd<DP>::SMEM, s, p, w, maps));
+    const long long warps = w.state_rows * p.kv_heads, blocks = (warps + JOIN_WARPS - 1) / JOIN_WARPS, most = 8LL * sms;
+    TIGA_CUDA_TRY(launch_after(shared_join_kernel<T, DP>, dim3((unsigned)(sms * JOIN_Y + (blocks < most ? blocks : most))), JOIN_WARPS * 32, 0, s, p, w, sms));
+    return launch_status();
+}
+
+tiga_status attention_shared(const AttnParams& p, const Prefixes& g, bool bf16, void* ws, cudaStream_t s) {
+    FwdWork w;
+    SharedPlan plan;
+    shared_carve(p, g.n_groups, ws, &w, &plan);
+    if (bf16) return p.D > 64 ? launch_shared<__nv_bfloat16, 128>(p, g, w, plan, s) : launch_shared<__nv_bfloat16, 64>(p, g, w, plan, s);
+    return p.D > 64 ? launch_shared<__half, 128>(p, g, w, plan, s) : launch_shared<__half, 64>(p, g, w, plan, s);
 }
 
 }  // namespace tiga

@@ -16,6 +16,7 @@ struct AttnParams {
     long long q_row, q_head, k_row, k_head, v_row, v_head, go_row, go_head;
     const int32_t *q_start, *kv_start, *kv_len, *table;      // table: NULL for the dense relation
     const uint8_t* mask;
+    const struct Segment* line;     // shared prefixes: the segments of the line, n_seg of them (NULL: they follow from the arrays above)
     int n_seg, n_q, n_kv, heads, kv_heads, group, D, causal;
     long long n_pages, page_size, table_stride, max_pages, page_stride, slot_stride;
     float scale;
@@ -34,6 +35,7 @@ __device__ __forceinline__ int clamp_to(int v, int hi) { return min(max(v, 0), h
 
 // (the bounds of rows and of dense keys: p.q_start and p.kv_start, or a copy of them)
 __device__ __forceinline__ Segment segment_of(const AttnParams& p, int s, const int32_t* q_start, const int32_t* kv_start) {
+    if (p.line) return p.line[s];
     Segment g;
     g.q0 = clamp_to(q_start[s], p.n_q);
     g.nq = max(clamp_to(q_start[s + 1], p.n_q) - g.q0, 0);
@@ -93,6 +95,15 @@ __device__ __forceinline__ int segment_of_row(const int32_t* start, int n_seg, i
     }
     if (lo == 0 || i >= clamp_to(start[lo], n_rows)) return -1;
     return lo - 1;
+}
+
+// Shared prefixes: the keys of a line's segment begin at position g.k0, key j lies at position (g.k0 & ~31) + j of the sequence whose pages
+// row `row` of the table names, and those in front of g.k0 count as masked.  (So groups of 8 to 32 keys stay inside of a page.)
+__device__ __forceinline__ Place shared_place(const AttnParams& p, const Segment& g, int row, int j) {
+    const int at = (g.k0 & ~31) + j, page = at / (int)p.page_size;
+    if (at < g.k0) return {-1, 0};
+    const int id = p.table[(long long)row * p.table_stride + page];
+    return {id >= p.n_pages ? -1 : id, at - page * (int)p.page_size};
 }
 
 // The last of n ascending places that is at most `v`, which start[0] is: by a warp with all its lanes, 32 places a round.
@@ -389,6 +400,11 @@ static inline cudaError_t launch_after(void (*kernel)(A...), dim3 grid, int thre
 
 constexpr int MAX_SMS = 160;            // blocks that workspaces provide for
 
+// Sequences whose caches begin with the same pages: those of group g, [group_start[g], group_start[g + 1]), share positions [0, shared[g]).
+struct Prefixes { const int32_t *group_start, *shared; int n_groups; };
+
+size_t attention_shared_bytes(const AttnParams& p, int n_groups);
+tiga_status attention_shared(const AttnParams& p, const Prefixes& g, bool bf16, void* ws, cudaStream_t s);
 size_t attention_forward_bytes(const AttnParams& p);
 size_t attention_backward_bytes(const AttnParams& p);
 tiga_status attention_backward(const AttnParams& p, bool bf16, void* ws, cudaStream_t s);
