@@ -58,6 +58,13 @@ void make_tile_maps(AttnParams* p, bool bf16, TileMaps* m) {
     p->kv_box = ok ? box : 0;
 }
 
+// queries in boxes of `packed` packed rows, 64 features each
+bool make_row_map(const AttnParams& p, bool bf16, int packed, CUtensorMap* m) {
+    if (!encoder() || p.n_q < 1 || packed % p.group) return false;
+    const long long dim[4] = {p.D, p.heads, p.n_q, 1};
+    return encode(m, bf16, p.q, dim, {p.q_head, p.q_row, 64}, p.group, packed / p.group);
+}
+
 // ------------------------------------------------------------------------------------------------ host checks
 
 bool attention_bad_stride(const tiga_stride& s) { return s.row < 0 || s.head < 0 || (s.row & 7) || (s.head & 7); }

@@ -174,6 +174,7 @@ __device__ __forceinline__ void store_rows(uint4 (&v)[C], void* to, bool on, int
 
 // host: the maps, and the boxes that they allow (attention.cu)
 void make_tile_maps(AttnParams* p, bool bf16, TileMaps* m);
+bool make_row_map(const AttnParams& p, bool bf16, int packed, CUtensorMap* m);
 
 // blocks of the persistent kernels: one on every SM (their shared memory admits one), 0 if the device does not answer
 static inline int attention_grid() {
