@@ -279,7 +279,7 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
     if (warp == BWD_WALKER) {
         if (lane == 0) {
             Walker<WorkCut> walk = ctl.walk;
-            (KV ? w.kv_joints : w.q_joints)[block] = joint_of(walk, walk.here, block);
+            (KV ? w.kv_joints : w.q_joints)[block] = joint_of(p, walk, walk.here, block);
             int of = -1;
             float factor = 1.f;
             auto factor_of = [&](int s) {

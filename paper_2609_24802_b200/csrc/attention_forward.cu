@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
     if (warp == FWD_WALKER) {
         if (lane == 0) {
             Walker<FwdCut> walk = ctl.walk;
-            w.joints[blockIdx.x] = joint_of(walk, walk.here && (!SHARED || only_state(w, walk.s, walk.g.k0)), blockIdx.x);
+            w.joints[blockIdx.x] = joint_of(p, walk, walk.here && (!SHARED || only_state(w, walk.s, walk.g.k0)), blockIdx.x);
             items_hand_out(ctl.items, p, walk, walk.here);
         }
         __syncwarp();
@@ -135,7 +135,10 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
                         const int r = x * 128 + 32 * pw + lane;
                         if (x == 1 && rows <= 128) {
                             if (lane == 0) mbar_arrive(bar(ctl.q_full), 32);
-                        } else fetch_packed<DP>(q_tile + x * C::TILE, 32 * pw, bar(ctl.q_full), p, g, maps, false, h, e.t * FWD_ROWS + r, r < rows, p.q);
+                        } else {
+                            // whatever a row of the queries holds stays in that row: boxes bring it where there is no such row, too
+                            fetch_packed<DP>(q_tile + x * C::TILE, 32 * pw, bar(ctl.q_full), p, g, maps, false, h, e.t * FWD_ROWS + r, p.q_box || r < rows, p.q);
+                        }
                     }
                     ++items;
                 }
@@ -437,8 +440,9 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
 // axis): the block's warps share a row's parts.
 constexpr int JOIN_WARPS = 8, JOIN_Y = 16, JOIN_FEW = 8;
 
+// one of `slices` parts of a block's rows
 template <typename T, int DP>
-__device__ __forceinline__ void join_block(const AttnParams& p, const FwdWork& w, const int block, const int slice) {
+__device__ __forceinline__ void join_block(const AttnParams& p, const FwdWork& w, const int block, const int slice, const int slices) {
     const Joint& j = w.joints[block];
     const int parts = j.parts;
     if (parts == 0) return;
@@ -448,7 +452,7 @@ __device__ __forceinline__ void join_block(const AttnParams& p, const FwdWork& w
     constexpr int E = DP / 32;
     __shared__ float sh_m[JOIN_WARPS], sh_l[JOIN_WARPS], sh_o[JOIN_WARPS][DP];
     const bool few = parts <= JOIN_FEW;
-    for (int r = few ? slice * JOIN_WARPS + warp : slice; r < rows; r += few ? JOIN_Y * JOIN_WARPS : JOIN_Y) {
+    for (int r = few ? slice * JOIN_WARPS + warp : slice; r < rows; r += few ? slices * JOIN_WARPS : slices) {
         const int a = few ? 0 : parts * warp / JOIN_WARPS, b = few ? parts : parts * (warp + 1) / JOIN_WARPS;
         float m = -INFINITY, l = 0.f, o[E];
 #pragma unroll
@@ -515,7 +519,7 @@ __device__ __forceinline__ void join_block(const AttnParams& p, const FwdWork& w
 template <typename T, int DP>
 __global__ void __launch_bounds__(JOIN_WARPS * 32) attention_join_kernel(const AttnParams p, const FwdWork w) {
     wait_for_previous_kernel();
-    join_block<T, DP>(p, w, blockIdx.x, blockIdx.y);
+    join_block<T, DP>(p, w, blockIdx.x, blockIdx.y, JOIN_Y);
 }
 
 size_t attention_forward_carve(const AttnParams& p, void* ws, FwdWork* w) {
@@ -568,7 +572,7 @@ __device__ __forceinline__ int tile_halves(int packed) {            // of a segm
     const int rest = packed % FWD_ROWS;
     return 2 * (packed / FWD_ROWS) + (rest == 0 ? 0 : rest <= 128 ? 1 : 2);
 }
-constexpr int SHARED_ITEM_COST = 4;         // of a tile, in steps (attention_shared.cuh)
+constexpr int SHARED_ITEM_COST = 5;         // of a tile, in units of which a step has two or three (attention_shared.cuh)
 // Rows of a group that shares: up to a full tile for each member on average (longer chunks fill their tiles alone).
 __host__ __device__ __forceinline__ long long most_state_rows(long long n_seq, long long n_q, int group) {
     const long long n = (n_seq * FWD_ROWS + group - 1) / group;
@@ -581,44 +585,56 @@ struct SharedPlan {
     long long *line_state, *state_start, *unit_start;
 };
 
-// One block: a warp for each group, a thread for each sequence, then the units.
-static __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(const AttnParams p, const Prefixes x, const SharedPlan plan, const long long state_rows) {
+// One block: a warp for each group, a thread for each sequence, then the units.  What is looked up again and again lies in shared memory where
+// it fits: this kernel is a chain of latencies in front of everything else.
+constexpr int PLAN_HELD = 1024;
+static __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(AttnParams p, Prefixes x, const SharedPlan plan, const long long state_rows) {
+    __shared__ int32_t rows[PLAN_HELD], lengths[PLAN_HELD], members[PLAN_HELD];
+    __shared__ Segment held[PLAN_HELD];             // of the groups
     wait_for_previous_kernel();
     let_next_kernel_start();
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, n_seq = p.n_seg;
+    if (n_seq < PLAN_HELD) {
+        if ((int)threadIdx.x <= n_seq) rows[threadIdx.x] = p.q_start[threadIdx.x];
+        if ((int)threadIdx.x < n_seq) lengths[threadIdx.x] = p.kv_len[threadIdx.x];
+        p.q_start = rows;
+        p.kv_len = lengths;
+    }
+    if (x.n_groups < PLAN_HELD) {
+        if ((int)threadIdx.x <= x.n_groups) members[threadIdx.x] = x.group_start[threadIdx.x];
+        x.group_start = members;
+    }
+    Segment* groups = x.n_groups < PLAN_HELD ? held : plan.line;
+    __syncthreads();
     const long long most = min(min(p.max_pages * p.page_size, MOST_ROWS), 1LL << 30);
     for (int g = warp; g < x.n_groups; g += PLAN_THREADS / 32) {
         const int a = clamp_to(x.group_start[g], n_seq), b = max(clamp_to(x.group_start[g + 1], n_seq), a);
-        long long shared = min((long long)max(x.shared[g], 0), most);
-        int halves = 0;
+        int shared = (int)min((long long)max(x.shared[g], 0), most), halves = 0;
         for (int s = a + lane; s < b; s += 32) {
             const Segment e = segment_of(p, s);
             if (e.nq == 0) continue;
-            shared = min(shared, (long long)(p.causal ? max(e.length - e.nq + 1, 0) : e.length));
+            shared = min(shared, p.causal ? max(e.length - e.nq + 1, 0) : e.length);
             halves += tile_halves(e.nq * p.group);
         }
-#pragma unroll
-        for (int o = 16; o; o >>= 1) shared = min(shared, __shfl_xor_sync(~0u, shared, o));
+        shared = __reduce_min_sync(~0u, shared);
         halves = __reduce_add_sync(~0u, halves);
         const int q0 = clamp_to(p.q_start[a], p.n_q), nq = max(clamp_to(p.q_start[b], p.n_q) - q0, 0);
         const long long steps = quotient(shared + FWD_STEP - 1, FWD_STEP), tiles = quotient((long long)nq * p.group + FWD_ROWS - 1, FWD_ROWS);
-        const bool pays = (long long)nq * p.group <= (long long)(b - a) * FWD_ROWS && (halves - tile_halves(nq * p.group)) * steps > 2 * SHARED_ITEM_COST * tiles && nq < 1 << 30;
-        if (lane == 0) {
-            plan.first_member[g] = a;
-            plan.line_row[g] = a;
-            plan.line[g] = {q0, pays ? nq : 0, 0, pays ? (int)shared : 0, pays ? (int)shared + nq : 0};
-        }
+        const bool pays = (long long)nq * p.group <= (long long)(b - a) * FWD_ROWS && (halves - tile_halves(nq * p.group)) * steps > 8 * tiles && nq < 1 << 30;
+        if (lane == 0) groups[g] = {q0, pays ? nq : 0, 0, pays ? shared : 0, pays ? shared + nq : 0};
     }
     __syncthreads();
     if (warp == 0) {            // places of the groups' states; a group for which there is no room (bounds that overlap) shares nothing
         long long base = 0;
         for (int g0 = 0; g0 < x.n_groups; g0 += 32) {
             const int g = g0 + lane;
-            const long long n = g < x.n_groups ? plan.line[g].nq : 0, run = warp_running(n);
+            const long long n = g < x.n_groups ? groups[g].nq : 0, run = warp_running(n);
             if (g < x.n_groups) {
                 plan.state_start[g] = base + run - n;
-                plan.line_state[g] = base + run - n - plan.line[g].q0;
-                if (base + run > state_rows) plan.line[g] = {0, 0, 0, 0, 0};
+                plan.line_state[g] = base + run - n - groups[g].q0;
+                if (base + run > state_rows) groups[g] = {0, 0, 0, 0, 0};
+                plan.line[g] = groups[g];
+                plan.line_row[g] = plan.first_member[g] = clamp_to(x.group_start[g], n_seq);
             }
             base += __shfl_sync(~0u, run, 31);
         }
@@ -634,40 +650,43 @@ static __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(const 
         const int g = lo - 1;
         Segment e = segment_of(p, s);
         long long state = 0;
-        if (g >= 0 && s >= plan.first_member[g] && s < clamp_to(x.group_start[g + 1], n_seq) && plan.line[g].nk > 0 && e.nq > 0
-            && e.q0 >= plan.line[g].q0 && (long long)e.q0 + e.nq <= (long long)plan.line[g].q0 + plan.line[g].nq) {        // (bounds that do not ascend lead nowhere)
-            const int base = plan.line[g].nk & ~31;
-            e.k0 = plan.line[g].nk;
-            e.nk = max(e.nk - base, 0);
-            e.length -= base;
-            state = plan.line_state[g];
+        if (g >= 0 && s < clamp_to(x.group_start[g + 1], n_seq) && e.nq > 0) {
+            const Segment of = groups[g];
+            if (of.nk > 0 && e.q0 >= of.q0 && (long long)e.q0 + e.nq <= (long long)of.q0 + of.nq) {            // (bounds that do not ascend lead nowhere)
+                const int base = of.nk & ~31;
+                e.k0 = of.nk;
+                e.nk = max(e.nk - base, 0);
+                e.length -= base;
+                state = plan.line_state[g];
+            }
         }
         plan.line[x.n_groups + s] = e;
         plan.line_row[x.n_groups + s] = s;
         plan.line_state[x.n_groups + s] = state;
     }
     __syncthreads();
-    AttnParams of_line = p;
-    of_line.line = plan.line;
-    of_line.n_seg = x.n_groups + n_seq;
-    plan_units<FwdCut>(of_line, plan.unit_start);
+    p.line = plan.line;
+    p.n_seg = x.n_groups + n_seq;
+    plan_units<FwdCut>(p, plan.unit_start);
 }
 
-// Joins the states of tiles that several blocks shared, as above (the first blocks), and the two states of every row that has two: a warp
-// has the heads of a group of a row.  A state lies among the states where one block had its tile, else in as many parts.
+// Joins the two states of every row that has two (the first blocks): a warp has one head of a row.  A state lies among the states
+// where one block had its tile, else in as many parts; the parts of both are looked up at once.  The last blocks join the tiles of rows with one state that several blocks shared, as above.
+// (With 16 slices of each of these, which mostly have nothing to do, the kernel took 25 us whatever the size: eight rounds of blocks.)
+constexpr int SHARED_JOIN_SLICES = 4, SHARED_JOIN_BLOCKS = 3;           // ... and blocks of an SM
 template <typename T, int DP>
-__global__ void __launch_bounds__(JOIN_WARPS * 32) shared_join_kernel(const AttnParams p, const FwdWork w, const int sms) {
+__global__ void __launch_bounds__(JOIN_WARPS * 32, SHARED_JOIN_BLOCKS) shared_join_kernel(const AttnParams p, const FwdWork w, const int sms) {
     wait_for_previous_kernel();
-    if ((int)blockIdx.x < sms * JOIN_Y) return join_block<T, DP>(p, w, blockIdx.x / JOIN_Y, blockIdx.x % JOIN_Y);
+    const int state_blocks = (int)gridDim.x - sms * SHARED_JOIN_SLICES, behind = (int)blockIdx.x - state_blocks;
+    if (behind >= 0) return join_block<T, DP>(p, w, behind / SHARED_JOIN_SLICES, behind % SHARED_JOIN_SLICES, SHARED_JOIN_SLICES);
     constexpr int E = DP / 32;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const long long units = w.unit_start[p.n_seg], blocks = min((long long)sms, max(units, 1LL));
+    const long long units = w.unit_start[p.n_seg], blocks = Walker<FwdCut>::pieces(p, units, sms);
     auto block_of = [&](long long unit) { return (int)quotient((unit + 1) * blocks - 1, units); };
-    const long long tasks = w.state_start[w.n_groups] * p.kv_heads, stride = (long long)(gridDim.x - sms * JOIN_Y) * JOIN_WARPS;
-    for (long long task = (long long)(blockIdx.x - sms * JOIN_Y) * JOIN_WARPS + warp; task < tasks; task += stride) {
-        const long long at = quotient(task, p.kv_heads);
-        const int h = (int)(task - at * p.kv_heads);
-        const int g = last_place(w.state_start, w.n_groups, at);
+    const long long tasks = w.state_start[w.n_groups] * p.heads, stride = (long long)state_blocks * JOIN_WARPS;
+    for (long long task = (long long)blockIdx.x * JOIN_WARPS + warp; task < tasks; task += stride) {
+        const long long at = quotient(task, p.heads);
+        const int head = (int)(task - at * p.heads), h = head / p.group, g = last_place(w.state_start, w.n_groups, at);
         const Segment shared = p.line[g];
         const long long row_ll = at - w.line_state[g];
         if (shared.nq == 0 || row_ll < shared.q0 || row_ll >= (long long)shared.q0 + shared.nq) continue;
@@ -675,59 +694,63 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) shared_join_kernel(const Attn
         const int a = w.first_member[g], s = a + last_place(p.q_start + a, w.n_seq - a, row);
         const Segment own = p.line[w.n_groups + s];
         if (own.k0 == 0) continue;
-        int tile[2] = {-1, -1}, first[2], parts[2];
-        for (int m = 0; m < p.group; ++m) {
-            float top = -INFINITY, mass = 0.f, o[E];
+        int first0, first1, parts0, parts1, r0, r1;
+        auto find = [&](const Segment& seg, int line, int& first, int& parts, int& r) {
+            const int packed = (row - seg.q0) * p.group + head % p.group, t = packed / FWD_ROWS, cost = FwdCut::step_cost(p, seg);
+            const long long start = w.unit_start[line] + h * FwdCut::units(p, seg) + FwdCut::before(p, seg, t) + p.item_cost - 1;
+            r = packed % FWD_ROWS;
+            first = block_of(start + cost);                 // the blocks that have the last unit of the tile's first and last step
+            parts = block_of(start + (long long)cost * FwdCut::steps(p, seg, t)) - first + 1;
+        };
+        find(shared, g, first0, parts0, r0);
+        find(own, w.n_groups + s, first1, parts1, r1);
+        // part k of both: where its maximum and mass lie, and (times DP) its accumulator
+        auto place = [&](int k, const float2*& ml, const float*& o) -> long long {
+            const bool kind = k >= parts0, whole = (kind ? parts1 : parts0) == 1;
+            const int of = kind ? k - parts0 : k;
+            ml = whole ? w.state_ml : w.part_ml;
+            o = whole ? w.state_o : w.part_o;
+            return whole ? ((kind ? w.state_rows : 0) + at) * p.heads + head : (2LL * ((kind ? first1 : first0) + of) + (of == 0)) * w.rows + (kind ? r1 : r0);
+        };
+        const int n = parts0 + parts1;
+        float top = -INFINITY, mass = 0.f, o[E];
 #pragma unroll
-            for (int e = 0; e < E; ++e) o[e] = 0.f;
-            const long long out_row = (long long)row * p.heads + h * p.group + m;
-#pragma unroll
-            for (int kind = 0; kind < 2; ++kind) {
-                const Segment& seg = kind ? own : shared;
-                const int packed = (row - seg.q0) * p.group + m, t = packed / FWD_ROWS, r = packed % FWD_ROWS;
-                if (t != tile[kind]) {
-                    const long long start = w.unit_start[kind ? w.n_groups + s : g] + h * FwdCut::units(p, seg) + FwdCut::before(p, seg, t) + p.item_cost;
-                    tile[kind] = t;
-                    first[kind] = block_of(start);
-                    parts[kind] = block_of(start + FwdCut::steps(p, seg, t) - 1) - first[kind] + 1;
-                }
-                const bool whole = parts[kind] == 1;
-                auto place = [&](int k) -> long long {
-                    return whole ? (kind * w.state_rows + at) * p.heads + h * p.group + m : (2LL * (first[kind] + k) + (k == 0)) * w.rows + r;
-                };
-                const float2* from_ml = whole ? w.state_ml : w.part_ml;
-                const float* from_o = whole ? w.state_o : w.part_o;
-                for (int k0 = 0; k0 < parts[kind]; k0 += 32) {
-                    const int k = k0 + lane, here = min(32, parts[kind] - k0);
-                    float2 ml = make_float2(-INFINITY, 0.f);
-                    if (k < parts[kind]) ml = from_ml[place(k)];
-                    float most = ml.x != ml.x ? INFINITY : ml.x;
-#pragma unroll
-                    for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(~0u, most, d));
-                    most = fmaxf(most, top);
-                    const float fade = top == -INFINITY ? 0.f : ex2(top - most), f = ml.x == -INFINITY ? 0.f : ex2(ml.x - most);
-                    float sum = f * ml.y;
-#pragma unroll
-                    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
-                    mass = mass * fade + sum;
-#pragma unroll
-                    for (int e = 0; e < E; ++e) o[e] *= fade;
-                    top = most;
-#pragma unroll 4
-                    for (int n = 0; n < here; ++n) {
-                        const float fn = __shfl_sync(~0u, f, n);
-                        const float* src = from_o + place(k0 + n) * DP;
-#pragma unroll
-                        for (int e = 0; e < E; ++e) o[e] += fn * src[lane + 32 * e];
-                    }
-                }
+        for (int e = 0; e < E; ++e) o[e] = 0.f;
+        for (int k0 = 0; k0 < n; k0 += 32) {
+            const int here = min(32, n - k0);
+            const float2* from_ml;
+            const float* from_o;
+            float2 ml = make_float2(-INFINITY, 0.f);
+            if (k0 + lane < n) {
+                const long long i = place(k0 + lane, from_ml, from_o);
+                ml = from_ml[i];
             }
-            const float finish = mass > 0.f || mass != mass ? 1.f / mass : 0.f;
+            float most = ml.x != ml.x ? INFINITY : ml.x;
 #pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (lane + 32 * e < p.D) ((T*)p.out)[out_row * p.D + lane + 32 * e] = Half<T>::from(finish == 0.f ? 0.f : o[e] * finish);
-            if (lane == 0 && p.lse) p.lse[out_row] = mass == 0.f ? -INFINITY : (top + log2f(mass)) * LN2_F;
+            for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(~0u, most, d));
+            most = fmaxf(most, top);
+            const float fade = top == -INFINITY ? 0.f : ex2(top - most), f = ml.x == -INFINITY ? 0.f : ex2(ml.x - most);
+            float sum = f * ml.y;
+#pragma unroll
+            for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
+            mass = mass * fade + sum;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] *= fade;
+            top = most;
+#pragma unroll 4
+            for (int k = 0; k < here; ++k) {
+                const float fk = __shfl_sync(~0u, f, k);
+                const long long i = place(k0 + k, from_ml, from_o);
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[e] += fk * from_o[i * DP + lane + 32 * e];
+            }
         }
+        const long long out_row = (long long)row * p.heads + head;
+        const float finish = mass > 0.f || mass != mass ? 1.f / mass : 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (lane + 32 * e < p.D) ((T*)p.out)[out_row * p.D + lane + 32 * e] = Half<T>::from(finish == 0.f ? 0.f : o[e] * finish);
+        if (lane == 0 && p.lse) p.lse[out_row] = mass == 0.f ? -INFINITY : (top + log2f(mass)) * LN2_F;
     }
 }
 
@@ -766,12 +789,13 @@ static tiga_status launch_shared(AttnParams p, const Prefixes& g, const FwdWork&
     if (sms <= 0) return TIGA_ERR_CUDA;
     TIGA_CUDA_TRY(cudaFuncSetAttribute(attention_forward_kernel<T, DP, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Fwd<DP>::SMEM));
     p.item_cost = SHARED_ITEM_COST;
+    p.uneven = 1;
     shared_plan_kernel<<<counted(1), PLAN_THREADS, 0, s>>>(p, g, plan, w.state_rows);
     p.line = plan.line;
     p.n_seg = w.n_groups + w.n_seq;
     TIGA_CUDA_TRY(launch_after(attention_forward_kernel<T, DP, true>, dim3(sms), FWD_THREADS, Fwd<DP>::SMEM, s, p, w, maps));
-    const long long warps = w.state_rows * p.kv_heads, blocks = (warps + JOIN_WARPS - 1) / JOIN_WARPS, most = 8LL * sms;
-    TIGA_CUDA_TRY(launch_after(shared_join_kernel<T, DP>, dim3((unsigned)(sms * JOIN_Y + (blocks < most ? blocks : most))), JOIN_WARPS * 32, 0, s, p, w, sms));
+    const long long warps = w.state_rows * p.heads, blocks = (warps + JOIN_WARPS - 1) / JOIN_WARPS, most = 8LL * sms;
+    TIGA_CUDA_TRY(launch_after(shared_join_kernel<T, DP>, dim3((unsigned)(sms * SHARED_JOIN_SLICES + (blocks < most ? blocks : most))), JOIN_WARPS * 32, 0, s, p, w, sms));
     return launch_status();
 }
 

@@ -20,7 +20,7 @@ struct AttnParams {
     int n_seg, n_q, n_kv, heads, kv_heads, group, D, causal;
     long long n_pages, page_size, table_stride, max_pages, page_stride, slot_stride;
     float scale;
-    int item_cost;                  // units that a tile costs beside its steps (0: none; see Cut)
+    int item_cost, uneven;          // units that a tile costs beside its steps; whether steps cost several (see Cut)
     int kv_box, q_box;              // rows that a box of the tensor maps brings (0: rows are copied one by one)
 };
 
@@ -181,7 +181,8 @@ __host__ __device__ __forceinline__ long long lattice_points(long long n, long l
 // Beginning and ending a tile takes a block as long as some steps do (about 15000 cycles forward, where a step takes 3700).  Where the
 // tiles of a line have all numbers of steps, as under a triangle, equal numbers of steps would give the blocks of its short tiles several
 // times the work, so a tile counts item_cost units more, in front of its steps.  Under them nothing is done: a piece that ends there has
-// none of the tile, one that begins there has its first step.
+// none of the tile, one that begins there has its first step.  Where full tiles stand beside tiles of a few rows, whose steps wait for memory
+// (2500 cycles against 3750), a step costs two or three units; it is done by the piece that has its last one.
 template <int TILE_, int STEP_, bool KEYS_>
 struct Cut {
     static constexpr int TILE = TILE_, STEP = STEP_;      // stationary rows of a tile, rows of a step: powers of two
@@ -215,7 +216,7 @@ struct Cut {
     // keys or rows: a sum of floors in the middle.
     static __host__ __device__ __forceinline__ long long steps_before(const AttnParams& p, const Segment& g, int t) {
         if (t == 0) return 0;
-        if (!p.causal) return (long long)t * steps(p, g, 0);
+        if (t == 1 || !p.causal) return (long long)t * steps(p, g, 0);
         const long long c = (long long)g.length - g.nq;
         if (KEYS) {
             if (g.nq == 0) return t;
@@ -233,8 +234,11 @@ struct Cut {
         const long long k1 = lo < 0 ? 0 : lo < n ? lo : n, k2 = hi < k1 ? k1 : hi < n ? hi : n;
         return k1 + (k1 < k2 ? lattice_points(k2 - k1, TILE, TILE * k1 + b, m) : 0) + (n - k2) * most + (t > last ? steps(p, g, last) : 0);
     }
+    static __host__ __device__ __forceinline__ int step_cost(const AttnParams& p, const Segment& g) { return !p.uneven ? 1 : (long long)rows(p, g) <= 128 ? 2 : 3; }
     // units of the first t tiles, and of all tiles of a kv head
-    static __host__ __device__ __forceinline__ long long before(const AttnParams& p, const Segment& g, int t) { return steps_before(p, g, t) + (long long)t * p.item_cost; }
+    static __host__ __device__ __forceinline__ long long before(const AttnParams& p, const Segment& g, int t) {
+        return steps_before(p, g, t) * step_cost(p, g) + (long long)t * p.item_cost;
+    }
     static __host__ __device__ __forceinline__ long long units(const AttnParams& p, const Segment& g) { return before(p, g, tiles(p, g)); }
 };
 
@@ -259,16 +263,23 @@ struct Walker {
     int steps, i0, i1;          // steps of the tile, and which of them are this block's
     long long left;             // units behind this item
     long long units, blocks;    // of the whole line: units, and blocks that share them
+    long long start;            // the piece's first unit, counted from the beginning of its tile
     bool here;                  // this block has any
 
     // the tile's steps from its unit `off` on; false: the piece ends in front of the tile's first step
-    __device__ __forceinline__ bool open(const AttnParams& p, int off) {
+    __device__ __forceinline__ bool open(const AttnParams& p, long long off) {
         steps = C::steps(p, g, t);
-        const int end = (int)min((long long)steps + p.item_cost, off + left);
+        const int cost = C::step_cost(p, g);
+        const long long end = min((long long)steps * cost + p.item_cost, off + left);
         left -= end - off;
-        i0 = max(off - p.item_cost, 0);
-        i1 = max(end - p.item_cost, 0);
+        auto steps_of = [&](long long u) { return u <= 0 ? 0 : cost == 1 ? (int)u : (int)quotient(u, cost); };
+        i0 = steps_of(off - p.item_cost);
+        i1 = steps_of(end - p.item_cost);
         return i1 > i0;
+    }
+    // blocks that take part: every piece has a step's units, so that the blocks between a tile's first and last one all have steps of it
+    static __device__ __forceinline__ long long pieces(const AttnParams& p, long long units, int grid) {
+        return min((long long)grid, max(p.uneven ? units / 3 : units, 1LL));
     }
     __device__ __forceinline__ long long first_unit(long long block) const { return quotient(block * units, blocks); }
 
@@ -283,7 +294,7 @@ struct Walker {
             for (int k = 0; k < p.n_seg; k += 32) units += k + lane < p.n_seg ? C::units(p, segment_of(p, k + lane)) * p.kv_heads : 0;
             units = warp_total(units);
         }
-        blocks = min((long long)grid, max(units, 1LL));
+        blocks = pieces(p, units, grid);
         if (block >= blocks || units == 0) return false;
         long long off = first_unit(block), mine = 0;
         left = first_unit(block + 1) - off;
@@ -311,9 +322,9 @@ struct Walker {
         h = (int)quotient(off, per_head);
         off -= h * per_head;
         if (!p.causal) {
-            const int n = C::steps(p, g, 0) + p.item_cost;
+            const long long n = C::before(p, g, 1);
             t = (int)quotient(off, n);
-            off -= (long long)t * n;
+            off -= t * n;
         } else {            // the last tile that begins at or before this unit, 32 places a round
             int hi = C::tiles(p, g);
             t = 0;
@@ -325,7 +336,8 @@ struct Walker {
             }
             off -= C::before(p, g, t);
         }
-        return open(p, (int)off);
+        start = off;
+        return open(p, off);
     }
     __device__ __forceinline__ bool next(const AttnParams& p) {
         if (left <= 0) return false;
@@ -338,9 +350,9 @@ struct Walker {
         }
         return open(p, 0);
     }
-    // after begin() inside of a tile's steps: the block in which its first step lies
-    __device__ __forceinline__ int first_block(int block) const {
-        return (int)quotient((first_unit(block) - i0 + 1) * blocks - 1, units);
+    // after begin() inside of a tile's steps: the block that has its first step
+    __device__ __forceinline__ int first_block(const AttnParams& p, int block) const {
+        return (int)quotient((first_unit(block) - start + p.item_cost + C::step_cost(p, g)) * blocks - 1, units);
     }
 };
 

@@ -78,11 +78,11 @@ struct Joint {
     int first, parts;           // the block in which the tile begins; how many share it
 };
 template <typename C>
-__device__ __forceinline__ Joint joint_of(const Walker<C>& it, bool any, int block) {
+__device__ __forceinline__ Joint joint_of(const AttnParams& p, const Walker<C>& it, bool any, int block) {
     Joint j;
     j.item = {it.g.q0, it.g.nq, it.g.k0, it.g.nk, it.g.length, it.s, it.h, it.t, it.steps, it.i0, it.i1};
     const bool ends = any && it.i0 > 0 && it.i1 == it.steps;
-    j.first = ends ? it.first_block(block) : 0;
+    j.first = ends ? it.first_block(p, block) : 0;
     j.parts = ends ? block - j.first + 1 : 0;
     return j;
 }

@@ -24,6 +24,7 @@ struct WtCut {
     static __host__ __device__ __forceinline__ int tiles(const AttnParams& p, const Segment& g) { return narrow(p, g) ? g.nk > 0 : Wide::tiles(p, g); }
     static __host__ __device__ __forceinline__ int skipped(const AttnParams& p, const Segment& g, int t) { return narrow(p, g) ? 0 : Wide::skipped(p, g, t); }
     static __host__ __device__ __forceinline__ int steps(const AttnParams& p, const Segment& g, int t) { return narrow(p, g) ? Wide::tiles(p, g) : Wide::steps(p, g, t); }
+    static __host__ __device__ __forceinline__ int step_cost(const AttnParams&, const Segment&) { return 1; }
     static __host__ __device__ __forceinline__ long long before(const AttnParams& p, const Segment& g, int t) {
         return narrow(p, g) ? (long long)t * Wide::tiles(p, g) : Wide::before(p, g, t);
     }
@@ -157,7 +158,7 @@ __global__ void __launch_bounds__(WT_THREADS, 1) attention_weights_kernel(const 
     if (warp == WT_WALKER) {
         if (lane == 0) {
             Walker<WtCut> walk = ctl.walk;
-            w.joints[blockIdx.x] = joint_of(walk, walk.here && !WtCut::narrow(p, walk.g), blockIdx.x);
+            w.joints[blockIdx.x] = joint_of(p, walk, walk.here && !WtCut::narrow(p, walk.g), blockIdx.x);
             items_hand_out(ctl.items, p, walk, walk.here);
         }
         __syncwarp();

@@ -9,10 +9,10 @@ namespace tiga {
 // come out in the order of their positions.
 // The keep-th largest is found digit by digit (11 + 11 + 10 bits): counts of a digit among the numbers that agree with the digits found so
 // far, added up from the top.  Then every warp, whose positions follow one another, knows from the warps in front how many it puts where.
-// A list has one block, or a cluster of SELECT_CLUSTER that share its positions and read one another's counts.  What bounds it: the steps
-// one after the other (three counts, three sums over 2048 of them); the weights are read from memory once and lie in shared memory, where
-// they fit.
-constexpr int SELECT_THREADS = 1024, SELECT_WARPS = SELECT_THREADS / 32, SELECT_BINS = 2048, SELECT_CLUSTER = 8;
+// A list has one block, or a cluster of SELECT_CLUSTER that share its positions and read one another's counts.  What bounds it: many lists, the
+// instructions of five passes over numbers in shared memory; few lists, the steps one after the other.  So many lists have small blocks, of which
+// an SM holds several (512 lists of up to 8192: 62 us with 1024 threads each and the same passes, here 27).
+constexpr int SELECT_MANY = 256, SELECT_FEW = 1024, SELECT_BINS = 2048, SELECT_CLUSTER = 8;            // threads
 constexpr int SELECT_HELD = 40960;              // numbers that a block's shared memory holds
 
 struct EvictParams {
@@ -44,45 +44,55 @@ __device__ __forceinline__ uint32_t rank_of(float w) {
 }
 constexpr uint32_t LAST_POSITION = 0xffffffffu;
 
-template <int CLUSTER>
-__global__ void __launch_bounds__(SELECT_THREADS) evict_select_kernel(const EvictParams p) {
+template <int THREADS, int CLUSTER>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_select_kernel(const EvictParams p) {
     namespace cg = cooperative_groups;
+    constexpr int WARPS = THREADS / 32;
     extern __shared__ uint32_t numbers[];
-    __shared__ uint32_t bins[SELECT_BINS], warp_sum[SELECT_WARPS], found[2];        // found: digit, how many more of it are wanted
-    __shared__ uint32_t above[SELECT_WARPS], equal[SELECT_WARPS], totals[4];        // totals: positions there are, above, equal (of this block)
+    __shared__ uint32_t bins[SELECT_BINS], warp_sum[32], found[2];              // found: digit, how many more of it are wanted
+    __shared__ uint32_t above[32], equal[32], totals[4];                        // totals: positions there are, above, equal (of this block)
     let_next_kernel_start();
     const int list = blockIdx.x / CLUSTER, part = blockIdx.x % CLUSTER, s = list / p.kv_heads, h = list % p.kv_heads;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const long long length = max(p.kv_len[s], 0);
-    const long long n = min(min(length, p.max_pages * p.page_size), MOST_ROWS);
+    const int length = max(p.kv_len[s], 0), n = (int)min(min((long long)length, p.max_pages * p.page_size), MOST_ROWS);
+    const int recent = (int)max((long long)length - p.recent, 0LL), weighed = (int)min((long long)n, p.w_length);         // the last positions begin, the weights end
     // this block's positions, and the warp's (whole groups of 32)
-    const long long per_warp = ((n + CLUSTER * SELECT_WARPS - 1) / (CLUSTER * SELECT_WARPS) + 31) / 32 * 32, per_block = per_warp * SELECT_WARPS;
-    const long long begin = min(per_block * part, n), end = min(begin + per_block, n);
-    const long long w0 = min(begin + per_warp * warp, end), w1 = min(w0 + per_warp, end);
+    const int per_warp = ((n + CLUSTER * WARPS - 1) / (CLUSTER * WARPS) + 31) / 32 * 32;
+    const int begin = (int)min((long long)per_warp * WARPS * part, (long long)n), end = (int)min((long long)begin + per_warp * WARPS, (long long)n);
+    const int w0 = (int)min((long long)begin + (long long)per_warp * warp, (long long)end), w1 = (int)min((long long)w0 + per_warp, (long long)end);
     const bool held = end - begin <= p.held;
     const float* weights = p.weights + s * p.w_seg + h * p.w_head;
-    auto fresh = [&](long long j) -> uint32_t {
-        const float w = j < p.w_length ? weights[j] : 0.f;
-        const int page = page_of(p.table, p.table_stride, s, (uint32_t)j / (uint32_t)p.page_size, p.n_pages);
-        return page < 0 ? 0 : j >= length - p.recent ? LAST_POSITION : rank_of(w);
+    const uint32_t page_size = (uint32_t)p.page_size;
+    auto fresh = [&](int j) -> uint32_t {
+        const float w = j < weighed ? weights[j] : 0.f;
+        const int page = page_of(p.table, p.table_stride, s, (uint32_t)j / page_size, p.n_pages);
+        return page < 0 ? 0 : j >= recent ? LAST_POSITION : rank_of(w);
     };
-    auto number = [&](long long j) { return held ? numbers[j - begin] : fresh(j); };
+    auto number = [&](int j) { return held ? numbers[j - begin] : fresh(j); };
     auto meet = [&]() { if (CLUSTER > 1) cg::this_cluster().sync(); else __syncthreads(); };
     auto of_block = [&](uint32_t* a, int b) { return CLUSTER > 1 ? cg::this_cluster().map_shared_rank(a, b) : a; };
 
-    // ---- the numbers, and how many positions there are
-    uint32_t there = 0;
+    // ---- the numbers, how many positions there are, and the counts of the first digit (the last positions' apart: a crowd in one bin)
+    for (int k = threadIdx.x; k < SELECT_BINS; k += THREADS) bins[k] = 0;
+    __syncthreads();
+    uint32_t there = 0, last = 0;
 #pragma unroll 4
-    for (long long j = w0 + lane; j < w1; j += 32) {
+    for (int j = w0 + lane; j < w1; j += 32) {
         const uint32_t v = fresh(j);
         if (held) numbers[j - begin] = v;
         there += v != 0;
+        if (v == LAST_POSITION) ++last;
+        else if (v) atomicAdd(&bins[v >> 21], 1u);
     }
     there = __reduce_add_sync(~0u, there);
-    if (lane == 0) warp_sum[warp] = there;
+    last = __reduce_add_sync(~0u, last);
+    if (lane == 0) {
+        warp_sum[warp] = there;
+        if (last) atomicAdd(&bins[LAST_POSITION >> 21], last);
+    }
     __syncthreads();
     if (warp == 0) {
-        const uint32_t sum = __reduce_add_sync(~0u, warp_sum[lane]);
+        const uint32_t sum = __reduce_add_sync(~0u, lane < WARPS ? warp_sum[lane] : 0u);
         if (lane == 0) totals[0] = sum;
     }
     meet();
@@ -94,43 +104,49 @@ __global__ void __launch_bounds__(SELECT_THREADS) evict_select_kernel(const Evic
     uint32_t border = 0, wanted = 0;            // 0: everything that there is stays
     if (all > stay) {
         wanted = stay;
-        int shift = 32;
         for (int digit = 0; digit < 3; ++digit) {
-            const int bits = digit < 2 ? 11 : 10, size = 1 << bits;
-            const uint32_t high = shift == 32 ? 0u : ~0u << shift;          // the digits that are found
-            shift -= bits;
-            for (int k = threadIdx.x; k < size; k += SELECT_THREADS) bins[k] = 0;
-            __syncthreads();
-            for (long long j0 = w0; j0 < w1; j0 += 32) {
-                const long long j = j0 + lane;
-                const uint32_t v = j < w1 ? number(j) : 0;
-                const bool in = v != 0 && (v & high) == border;
-                // numbers of one digit come in crowds (the last positions, weights of zero): the lanes of the first one's digit count at once
-                const uint32_t d = v >> shift & (size - 1), some = __ballot_sync(~0u, in);
-                if (some) {
-                    const int first = __ffs(some) - 1;
-                    const uint32_t first_digit = __shfl_sync(~0u, d, first);            // (all lanes take part)
-                    const uint32_t same = __ballot_sync(~0u, in && d == first_digit);
-                    if (lane == first) atomicAdd(&bins[d], __popc(same));
-                    else if (in && !(same >> lane & 1)) atomicAdd(&bins[d], 1u);
-                }
+            const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, size = digit < 2 ? 2048 : 1024;
+            if (digit) {
+                const uint32_t high = ~0u << (digit == 1 ? 21 : 10);            // the digits that are found
+                for (int k = threadIdx.x; k < size; k += THREADS) bins[k] = 0;
+                __syncthreads();
+                if (border == (LAST_POSITION & high)) {         // (the last positions may be most of these)
+                    last = 0;
+                    for (int j = w0 + lane; j < w1; j += 32) {
+                        const uint32_t v = number(j);
+                        if (v == LAST_POSITION) ++last;
+                        else if ((v & high) == border) atomicAdd(&bins[v >> shift & (size - 1)], 1u);
+                    }
+                    last = __reduce_add_sync(~0u, last);
+                    if (lane == 0 && last) atomicAdd(&bins[size - 1], last);
+                } else
+#pragma unroll 4
+                    for (int j = w0 + lane; j < w1; j += 32) {
+                        const uint32_t v = number(j);
+                        if ((v & high) == border && v) atomicAdd(&bins[v >> shift & (size - 1)], 1u);
+                    }
+                meet();
             }
-            meet();
-            // thread k has two bins, counted from the top
-            const int top = size - 1 - 2 * (int)threadIdx.x;
-            uint32_t a = 0, b = 0;
-            if (top > 0)
-                for (int k = 0; k < CLUSTER; ++k) { const uint32_t* o = of_block(bins, k); a += o[top]; b += o[top - 1]; }
-            uint32_t run = a + b;
+            // thread k has `per` bins, counted from the top
+            const int per = size / THREADS > 0 ? size / THREADS : 1, top = size - 1 - per * (int)threadIdx.x;
+            uint32_t mine = 0, run;
+            if (top >= 0)
+                for (int b = 0; b < CLUSTER; ++b) { const uint32_t* o = of_block(bins, b); for (int k = 0; k < per; ++k) mine += o[top - k]; }
+            run = mine;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) { const uint32_t u = __shfl_up_sync(~0u, run, o); if (lane >= o) run += u; }
             if (lane == 31) warp_sum[warp] = run;
             __syncthreads();
-            uint32_t before = run - a - b;
-            const uint32_t mine = warp_sum[lane];
-            before += __reduce_add_sync(~0u, lane < warp ? mine : 0u);
-            if (before < wanted && wanted <= before + a) { found[0] = top; found[1] = wanted - before; }
-            else if (before + a < wanted && wanted <= before + a + b) { found[0] = top - 1; found[1] = wanted - before - a; }
+            const uint32_t in_front = lane < warp ? warp_sum[lane] : 0u;
+            uint32_t before = run - mine + __reduce_add_sync(~0u, in_front);
+            if (before < wanted && wanted <= before + mine) {           // one thread
+                for (int k = 0; k < per; ++k) {
+                    uint32_t count = 0;
+                    for (int b = 0; b < CLUSTER; ++b) count += of_block(bins, b)[top - k];
+                    if (wanted <= before + count) { found[0] = top - k; found[1] = wanted - before; break; }
+                    before += count;
+                }
+            }
             meet();             // (nobody clears its bins while they are read)
             border |= found[0] << shift;
             wanted = found[1];
@@ -139,7 +155,8 @@ __global__ void __launch_bounds__(SELECT_THREADS) evict_select_kernel(const Evic
 
     // ---- where they go: numbers above the border and the first ones equal to it, in the order of their positions
     uint32_t n_above = 0, n_equal = 0;
-    for (long long j = w0 + lane; j < w1; j += 32) {
+#pragma unroll 4
+    for (int j = w0 + lane; j < w1; j += 32) {
         const uint32_t v = number(j);
         n_above += v > border;
         n_equal += v == border && v != 0;
@@ -148,31 +165,33 @@ __global__ void __launch_bounds__(SELECT_THREADS) evict_select_kernel(const Evic
     n_equal = __reduce_add_sync(~0u, n_equal);
     if (lane == 0) { above[warp] = n_above; equal[warp] = n_equal; }
     __syncthreads();
-    uint32_t ahead_above = __reduce_add_sync(~0u, lane < warp ? above[lane] : 0u), ahead_equal = __reduce_add_sync(~0u, lane < warp ? equal[lane] : 0u);
+    const uint32_t above_in_front = lane < warp ? above[lane] : 0u, equal_in_front = lane < warp ? equal[lane] : 0u;
+    uint32_t ahead_above = __reduce_add_sync(~0u, above_in_front), ahead_equal = __reduce_add_sync(~0u, equal_in_front);
     if (CLUSTER > 1) {
-        if (warp == SELECT_WARPS - 1 && lane == 0) { totals[1] = ahead_above + n_above; totals[2] = ahead_equal + n_equal; }
+        if (warp == WARPS - 1 && lane == 0) { totals[1] = ahead_above + n_above; totals[2] = ahead_equal + n_equal; }
         meet();
         for (int b = 0; b < part; ++b) { ahead_above += of_block(totals, b)[1]; ahead_equal += of_block(totals, b)[2]; }
         meet();                 // (a block's shared memory is there until the last one has read it)
     }
     int32_t* kept = p.kept + (long long)list * p.keep;
     float* to = p.to_weights ? p.to_weights + s * p.o_seg + h * p.o_head : nullptr;
-    for (long long j0 = w0; j0 < w1; j0 += 32) {
-        const long long j = j0 + lane;
+#pragma unroll 2
+    for (int j0 = w0; j0 < w1; j0 += 32) {
+        const int j = j0 + lane;
         const uint32_t v = j < w1 ? number(j) : 0;
         const uint32_t over = __ballot_sync(~0u, v > border), same = __ballot_sync(~0u, v == border && v != 0), behind = (1u << lane) - 1;
         const uint32_t before_equal = ahead_equal + __popc(same & behind);
         const uint32_t at = ahead_above + __popc(over & behind) + min(before_equal, wanted);
         if (v > border || (v == border && v != 0 && before_equal < wanted)) {
-            kept[at] = (int32_t)j;
-            if (to && at < p.o_length) to[at] = j < p.w_length ? weights[j] : 0.f;
+            kept[at] = j;
+            if (to && at < p.o_length) to[at] = j < weighed ? weights[j] : 0.f;
         }
         ahead_above += __popc(over);
         ahead_equal += __popc(same);
     }
-    const long long thread = (long long)part * SELECT_THREADS + threadIdx.x;
-    for (long long k = stay + thread; k < p.keep; k += CLUSTER * SELECT_THREADS) kept[k] = -1;
-    if (to) for (long long k = stay + thread; k < p.o_length; k += CLUSTER * SELECT_THREADS) to[k] = 0.f;
+    const long long thread = (long long)part * THREADS + threadIdx.x;
+    for (long long k = stay + thread; k < p.keep; k += CLUSTER * THREADS) kept[k] = -1;
+    if (to) for (long long k = stay + thread; k < p.o_length; k += CLUSTER * THREADS) to[k] = 0.f;
     if (h == 0 && thread == 0) p.to_len[s] = (int32_t)stay;
 }
 
@@ -225,14 +244,17 @@ __global__ void __launch_bounds__(MOVE_THREADS) evict_move_kernel(const EvictPar
     }
 }
 
-template <int CLUSTER>
-static cudaError_t launch_select(const EvictParams& p, long long lists, cudaStream_t s) {
+template <int THREADS, int CLUSTER>
+static cudaError_t launch_select(EvictParams p, long long most, long long lists, cudaStream_t s) {
+    // a block's part of the longest list, as it is cut there
+    const long long share = (most + CLUSTER * THREADS - 1) / (CLUSTER * THREADS) * THREADS;
+    p.held = (int)(share < SELECT_HELD ? share : SELECT_HELD);
     const size_t smem = (size_t)p.held * 4;
-    cudaError_t e = cudaFuncSetAttribute(evict_select_kernel<CLUSTER>, cudaFuncAttributeMaxDynamicSharedMemorySize, SELECT_HELD * 4);
+    cudaError_t e = cudaFuncSetAttribute(evict_select_kernel<THREADS, CLUSTER>, cudaFuncAttributeMaxDynamicSharedMemorySize, SELECT_HELD * 4);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t c{};
     c.gridDim = dim3((unsigned)(lists * CLUSTER));
-    c.blockDim = dim3(SELECT_THREADS);
+    c.blockDim = dim3(THREADS);
     c.dynamicSmemBytes = smem;
     c.stream = s;
     cudaLaunchAttribute a{};
@@ -242,7 +264,7 @@ static cudaError_t launch_select(const EvictParams& p, long long lists, cudaStre
     c.attrs = &a;
     c.numAttrs = CLUSTER > 1;
     note_launch();
-    return cudaLaunchKernelEx(&c, evict_select_kernel<CLUSTER>, p);
+    return cudaLaunchKernelEx(&c, evict_select_kernel<THREADS, CLUSTER>, p);
 }
 
 }  // namespace tiga
@@ -282,11 +304,11 @@ extern "C" tiga_status tiga_paged_evict(const tiga_pages* from, const tiga_pages
     int dev = 0, sms = 0;
     TIGA_CUDA_TRY(cudaGetDevice(&dev));
     TIGA_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-    // a cluster for each list where the lists alone leave most SMs idle and are long enough to be worth the meetings
-    const bool clusters = lists * SELECT_CLUSTER <= 2 * sms && most > 8192;
-    const long long share = (most + (clusters ? SELECT_CLUSTER : 1) * 1024 - 1) / ((clusters ? SELECT_CLUSTER : 1) * 1024) * 1024;
-    p.held = (int)(share < SELECT_HELD ? share : SELECT_HELD);
-    TIGA_CUDA_TRY(clusters ? launch_select<SELECT_CLUSTER>(p, lists, s) : launch_select<1>(p, lists, s));
+    // A cluster for each list where the lists alone leave most SMs idle and are long enough to be worth the meetings; small blocks where there
+    // are several for each SM, whose shared memory holds their numbers.
+    if (lists * SELECT_CLUSTER <= 2 * sms && most > 8192) TIGA_CUDA_TRY((launch_select<SELECT_FEW, SELECT_CLUSTER>(p, most, lists, s)));
+    else if (lists <= sms || most > 12288) TIGA_CUDA_TRY((launch_select<SELECT_FEW, 1>(p, most, lists, s)));
+    else TIGA_CUDA_TRY((launch_select<SELECT_MANY, 1>(p, most, lists, s)));
     const long long tasks = lists * ((keep + 31) / 32);
     const long long grid = (tasks + MOVE_THREADS / 32 - 1) / (MOVE_THREADS / 32);
     if (grid > 0x7fffffffLL) return TIGA_ERR_UNSUPPORTED;
