@@ -733,7 +733,8 @@ static tiga_status launch_backward(AttnParams p, const BwdWork& w, cudaStream_t 
         TIGA_CUDA_TRY(launch_after(attention_prepare_kernel<T, DP / 8>, dim3((unsigned)grid), PREP_THREADS, 0, s, p, w, prep_q, prep_v));
     } else attention_prepare_kernel<T, DP / 8><<<counted((unsigned)grid), PREP_THREADS, 0, s>>>(p, w, prep_q, prep_v);
     TIGA_CUDA_TRY(launch_after(kernel, dim3(kv_blocks + q_blocks), BWD_THREADS, Bwd<DP>::SMEM, s, p, w, maps, kv_blocks));
-    TIGA_CUDA_TRY(launch_after(attention_sum_kernel<T, DP>, dim3(kv_blocks + q_blocks, SUM_Y), SUM_WARPS * 32, 0, s, p, w, kv_blocks));
+    // tiles of a single step are whole
+    if ((kv_blocks && (long long)p.n_q * p.group > BWD_STEP) || (q_blocks && p.n_kv > BWD_STEP)) TIGA_CUDA_TRY(launch_after(attention_sum_kernel<T, DP>, dim3(kv_blocks + q_blocks, SUM_Y), SUM_WARPS * 32, 0, s, p, w, kv_blocks));
     return launch_status();
 }
 

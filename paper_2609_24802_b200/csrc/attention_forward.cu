@@ -547,7 +547,8 @@ static tiga_status launch_forward(AttnParams p, const FwdWork& w, cudaStream_t s
     if (w.unit_start) forward_plan_kernel<<<counted(1), PLAN_THREADS, 0, s>>>(p, w.unit_start);
     if (w.unit_start) TIGA_CUDA_TRY(launch_after(attention_forward_kernel<T, DP, false>, dim3(sms), FWD_THREADS, Fwd<DP>::SMEM, s, p, w, maps));
     else attention_forward_kernel<T, DP, false><<<counted((unsigned)sms), FWD_THREADS, Fwd<DP>::SMEM, s>>>(p, w, maps);
-    TIGA_CUDA_TRY(launch_after(attention_join_kernel<T, DP>, dim3(sms, JOIN_Y), JOIN_WARPS * 32, 0, s, p, w));
+    // tiles of a single step are whole
+    if (p.table || p.n_kv > FWD_STEP) TIGA_CUDA_TRY(launch_after(attention_join_kernel<T, DP>, dim3(sms, JOIN_Y), JOIN_WARPS * 32, 0, s, p, w));
     return launch_status();
 }
 

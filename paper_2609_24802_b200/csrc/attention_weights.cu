@@ -427,7 +427,8 @@ static tiga_status launch_weights(AttnParams p, const WtSums& sums, const WtWork
         weights_plan_kernel<<<counted(1), PLAN_THREADS, 0, s>>>(p, w.unit_start);
         TIGA_CUDA_TRY(launch_after(attention_weights_kernel<T, DP>, dim3(sms), WT_THREADS, Wt<DP>::SMEM, s, p, sums, w, maps));
     } else attention_weights_kernel<T, DP><<<counted((unsigned)sms), WT_THREADS, Wt<DP>::SMEM, s>>>(p, sums, w, maps);
-    TIGA_CUDA_TRY(launch_after(weights_sum_kernel, dim3(sms), WT_TILE, 0, s, p, sums, w));
+    // no sequence has more than n_q rows: if those are few, no sum is in parts
+    if ((long long)p.n_q * p.group > WT_TILE) TIGA_CUDA_TRY(launch_after(weights_sum_kernel, dim3(sms), WT_TILE, 0, s, p, sums, w));
     return launch_status();
 }
 

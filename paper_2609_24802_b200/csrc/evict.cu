@@ -44,7 +44,52 @@ __device__ __forceinline__ uint32_t rank_of(float w) {
 }
 constexpr uint32_t LAST_POSITION = 0xffffffffu;
 
-template <int THREADS, int CLUSTER>
+// Keys and values of 32 places of a list, from `place` on, by a warp, 16 bytes a lane: a lane looks up where one of them comes from and goes to,
+// then the lanes of a row copy it together.  Bound by memory: what stays is read and written once.
+template <typename F>
+__device__ __forceinline__ void move_places(const EvictParams& p, const long long list, const long long first, F wait_for_kept) {
+    const int lane = threadIdx.x % 32, s = (int)quotient(list, p.kv_heads), h = (int)(list - (long long)s * p.kv_heads);
+    const long long place = first + lane;
+    long long to = -1, from = -1;
+    if (place < p.keep) {                   // (the target's page does not depend on what stays)
+        const long long page = quotient(place, p.to_page_size);
+        const int id = page < p.to_max_pages ? page_of(p.to_table, p.to_table_stride, s, page, p.to_pages) : -1;
+        if (id >= 0) to = id * p.to_page_stride + (place - page * p.to_page_size) * p.to_slot_stride + h * p.to_head_stride;
+    }
+    wait_for_kept();
+    if (to >= 0) {
+        const int j = p.kept[list * p.keep + place];
+        if (j >= 0) {
+            const long long page = quotient(j, p.page_size);
+            const int id = page_of(p.table, p.table_stride, s, page, p.n_pages);
+            if (id >= 0) from = id * p.page_stride + (j - page * p.page_size) * p.slot_stride + h * p.head_stride;
+        }
+    }
+    const int rows = 32 / p.pieces, row = lane / p.pieces, piece = lane - row * p.pieces;           // rows at once; the lanes behind them are idle
+    for (int r0 = 0; r0 < 32; r0 += 4 * rows) {
+        uint4 k[4], v[4];
+        long long a[4], b[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int r = r0 + u * rows + row;
+            a[u] = __shfl_sync(~0u, from, r & 31);
+            b[u] = __shfl_sync(~0u, to, r & 31);
+            if (r >= 32 || row >= rows) a[u] = -1;
+            if (a[u] >= 0) {
+                k[u] = __ldcs(reinterpret_cast<const uint4*>(p.key + a[u]) + piece);
+                v[u] = __ldcs(reinterpret_cast<const uint4*>(p.value + a[u]) + piece);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (a[u] >= 0) {
+                reinterpret_cast<uint4*>(p.to_key + b[u])[piece] = k[u];
+                reinterpret_cast<uint4*>(p.to_value + b[u])[piece] = v[u];
+            }
+    }
+}
+
+template <int THREADS, int CLUSTER, bool MOVE>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_select_kernel(const EvictParams p) {
     namespace cg = cooperative_groups;
     constexpr int WARPS = THREADS / 32;
@@ -193,65 +238,31 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_select_kernel(c
     for (long long k = stay + thread; k < p.keep; k += CLUSTER * THREADS) kept[k] = -1;
     if (to) for (long long k = stay + thread; k < p.o_length; k += CLUSTER * THREADS) to[k] = 0.f;
     if (h == 0 && thread == 0) p.to_len[s] = (int32_t)stay;
+    if (MOVE) {
+        __syncthreads();
+        for (long long place = 32 * warp; place < stay; place += THREADS) move_places(p, list, place, [] {});
+    }
 }
 
-// ---- Their keys and values, 16 bytes a thread.  A warp has 32 places of a list; a lane looks up where one of them comes from and goes to,
-// then the lanes of a row copy it together.  Bound by memory: what stays is read and written once.
+// ---- Few short lists are moved by the block that selects (a launch less: 5 us of the host), others by a kernel with a warp for 32 places.
 constexpr int MOVE_THREADS = 256;
 __global__ void __launch_bounds__(MOVE_THREADS) evict_move_kernel(const EvictParams p, const long long tasks) {
     const long long task = (long long)blockIdx.x * (MOVE_THREADS / 32) + threadIdx.x / 32;
     if (task >= tasks) return;
-    const int lane = threadIdx.x % 32;
-    const long long per_list = quotient(p.keep + 31, 32), list = quotient(task, per_list), place = (task - list * per_list) * 32 + lane;
-    const int s = (int)quotient(list, p.kv_heads), h = (int)(list - (long long)s * p.kv_heads);
-    // the target's page does not depend on the kernel in front
-    long long to = -1, from = -1;
-    if (place < p.keep) {
-        const long long page = quotient(place, p.to_page_size);
-        const int id = page < p.to_max_pages ? page_of(p.to_table, p.to_table_stride, s, page, p.to_pages) : -1;
-        if (id >= 0) to = id * p.to_page_stride + (place - page * p.to_page_size) * p.to_slot_stride + h * p.to_head_stride;
-    }
-    wait_for_previous_kernel();
-    if (to >= 0) {
-        const int j = p.kept[list * p.keep + place];
-        if (j >= 0) {
-            const long long page = quotient(j, p.page_size);
-            const int id = page_of(p.table, p.table_stride, s, page, p.n_pages);
-            if (id >= 0) from = id * p.page_stride + (j - page * p.page_size) * p.slot_stride + h * p.head_stride;
-        }
-    }
-    const int rows = 32 / p.pieces, row = lane / p.pieces, piece = lane - row * p.pieces;           // rows at once; the lanes behind them are idle
-    for (int r0 = 0; r0 < 32; r0 += 4 * rows) {
-        uint4 k[4], v[4];
-        long long a[4], b[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int r = r0 + u * rows + row;
-            a[u] = __shfl_sync(~0u, from, r & 31);
-            b[u] = __shfl_sync(~0u, to, r & 31);
-            if (r >= 32 || row >= rows) a[u] = -1;
-            if (a[u] >= 0) {
-                k[u] = __ldcs(reinterpret_cast<const uint4*>(p.key + a[u]) + piece);
-                v[u] = __ldcs(reinterpret_cast<const uint4*>(p.value + a[u]) + piece);
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-            if (a[u] >= 0) {
-                reinterpret_cast<uint4*>(p.to_key + b[u])[piece] = k[u];
-                reinterpret_cast<uint4*>(p.to_value + b[u])[piece] = v[u];
-            }
-    }
+    const long long per_list = quotient(p.keep + 31, 32), list = quotient(task, per_list);
+    move_places(p, list, (task - list * per_list) * 32, [] { wait_for_previous_kernel(); });
 }
 
-template <int THREADS, int CLUSTER>
+template <int THREADS, int CLUSTER, bool MOVE>
 static cudaError_t launch_select(EvictParams p, long long most, long long lists, cudaStream_t s) {
     // a block's part of the longest list, as it is cut there
     const long long share = (most + CLUSTER * THREADS - 1) / (CLUSTER * THREADS) * THREADS;
     p.held = (int)(share < SELECT_HELD ? share : SELECT_HELD);
     const size_t smem = (size_t)p.held * 4;
-    cudaError_t e = cudaFuncSetAttribute(evict_select_kernel<THREADS, CLUSTER>, cudaFuncAttributeMaxDynamicSharedMemorySize, SELECT_HELD * 4);
-    if (e != cudaSuccess) return e;
+    if (smem > 32 * 1024) {         // (beside the counts; more than any kernel may have unasked)
+        const cudaError_t e = cudaFuncSetAttribute(evict_select_kernel<THREADS, CLUSTER, MOVE>, cudaFuncAttributeMaxDynamicSharedMemorySize, SELECT_HELD * 4);
+        if (e != cudaSuccess) return e;
+    }
     cudaLaunchConfig_t c{};
     c.gridDim = dim3((unsigned)(lists * CLUSTER));
     c.blockDim = dim3(THREADS);
@@ -264,7 +275,7 @@ static cudaError_t launch_select(EvictParams p, long long most, long long lists,
     c.attrs = &a;
     c.numAttrs = CLUSTER > 1;
     note_launch();
-    return cudaLaunchKernelEx(&c, evict_select_kernel<THREADS, CLUSTER>, p);
+    return cudaLaunchKernelEx(&c, evict_select_kernel<THREADS, CLUSTER, MOVE>, p);
 }
 
 }  // namespace tiga
@@ -305,10 +316,15 @@ extern "C" tiga_status tiga_paged_evict(const tiga_pages* from, const tiga_pages
     TIGA_CUDA_TRY(cudaGetDevice(&dev));
     TIGA_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
     // A cluster for each list where the lists alone leave most SMs idle and are long enough to be worth the meetings; small blocks where there
-    // are several for each SM, whose shared memory holds their numbers.
-    if (lists * SELECT_CLUSTER <= 2 * sms && most > 8192) TIGA_CUDA_TRY((launch_select<SELECT_FEW, SELECT_CLUSTER>(p, most, lists, s)));
-    else if (lists <= sms || most > 12288) TIGA_CUDA_TRY((launch_select<SELECT_FEW, 1>(p, most, lists, s)));
-    else TIGA_CUDA_TRY((launch_select<SELECT_MANY, 1>(p, most, lists, s)));
+    // are several for each SM, whose shared memory holds their numbers.  Up to 512 places are moved by the block that selects them.
+    const bool few = lists <= sms;
+    if (few && most <= 8192 && keep <= 512) {
+        TIGA_CUDA_TRY((launch_select<SELECT_FEW, 1, true>(p, most, lists, s)));
+        return launch_status();
+    }
+    if (lists * SELECT_CLUSTER <= 2 * sms && most > 8192) TIGA_CUDA_TRY((launch_select<SELECT_FEW, SELECT_CLUSTER, false>(p, most, lists, s)));
+    else if (few || most > 12288) TIGA_CUDA_TRY((launch_select<SELECT_FEW, 1, false>(p, most, lists, s)));
+    else TIGA_CUDA_TRY((launch_select<SELECT_MANY, 1, false>(p, most, lists, s)));
     const long long tasks = lists * ((keep + 31) / 32);
     const long long grid = (tasks + MOVE_THREADS / 32 - 1) / (MOVE_THREADS / 32);
     if (grid > 0x7fffffffLL) return TIGA_ERR_UNSUPPORTED;
