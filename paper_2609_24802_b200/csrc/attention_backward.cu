@@ -19,10 +19,7 @@ namespace tiga {
 // the largest value cannot overflow, the smallest keep as many digits as there are.
 constexpr int BWD_WEIGHT_WARPS = 16, BWD_PRODUCER = BWD_WEIGHT_WARPS, BWD_MMA = BWD_PRODUCER + 4, BWD_WALKER = BWD_MMA + 1;
 constexpr int BWD_THREADS = 32 * (BWD_WALKER + 1), BWD_ROWS = 128, BWD_STEP = 128;
-typedef Cut<BWD_ROWS, BWD_STEP, true> KvCut;
-typedef Cut<BWD_ROWS, BWD_STEP, false> QCut;
-template <bool KV> struct CutOf { typedef QCut type; };
-template <> struct CutOf<true> { typedef KvCut type; };
+template <bool KV, bool CAUSAL> using BwdCut = Cut<BWD_ROWS, BWD_STEP, KV, CAUSAL ? CUT_COSTS : CUT_STEPS>;
 template <int DP> struct Bwd {
     static constexpr int TILE = 128 * DP * 2;
     static constexpr int SLOTS = DP == 128 ? 5 : 8;         // tiles of the ring, in the order Y1 Y2 Y1 Y2 ...
@@ -42,7 +39,7 @@ template <int AUX, typename C> struct BwdControl {
     alignas(16) float minus_lse[AUX][BWD_STEP], minus_delta[AUX][BWD_STEP];     // keys stationary: of the step's rows
     uint32_t mask[AUX][4];                                                      // queries stationary: the step's keys
 };
-static_assert(sizeof(BwdControl<2, KvCut>) <= 3 * 1024 && sizeof(BwdControl<8, KvCut>) <= 10 * 1024, "control block");
+static_assert(sizeof(BwdControl<2, BwdCut<true, true>>) <= 3 * 1024 && sizeof(BwdControl<8, BwdCut<true, true>>) <= 10 * 1024, "control block");
 
 struct BwdWork {
     long long *kv_start_unit, *q_start_unit;        // NULL: the blocks count for themselves
@@ -240,7 +237,7 @@ __global__ void __launch_bounds__(PREP_THREADS, PREP_BLOCKS) attention_prepare_k
 template <typename T, int DP, bool KV, bool CAUSAL>
 __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork& w, const TileMaps& maps, const int block, const int blocks) {
     typedef Bwd<DP> C;
-    typedef typename CutOf<KV>::type WorkCut;
+    typedef BwdCut<KV, CAUSAL> WorkCut;
     constexpr bool F16 = operand_type<T>() == 0;
     constexpr float BIAS = F16 ? 14.f : 0.f;
     extern __shared__ __align__(1024) unsigned char smem[];
@@ -268,7 +265,13 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
         ctl.abort_word = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == BWD_WALKER) walk_begin(&ctl.walk, p, KV ? w.kv_start_unit : w.q_start_unit, block, blocks);
+    Walker<WorkCut> walk;
+    const long long* unit_start = KV ? w.kv_start_unit : w.q_start_unit;
+    if (CAUSAL) { if (warp == BWD_WALKER) walk_begin(&ctl.walk, p, unit_start, block, blocks); }
+    else {
+        walk.here = false;
+        if (warp == BWD_WALKER) walk.here = walk.begin(p, unit_start, block, blocks);
+    }
     if (warp == BWD_MMA) tmem_alloc(smem_u32(&ctl.tmem), 512);
     tmem_fence_before();
     __syncthreads();
@@ -278,7 +281,7 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
 
     if (warp == BWD_WALKER) {
         if (lane == 0) {
-            Walker<WorkCut> walk = ctl.walk;
+            if (CAUSAL) walk = ctl.walk;
             (KV ? w.kv_joints : w.q_joints)[block] = joint_of(p, walk, walk.here, block);
             int of = -1;
             float factor = 1.f;
@@ -614,7 +617,7 @@ constexpr int SUM_WARPS = 8, SUM_Y = 16, SUM_FEW = 8;
 
 template <typename T, int DP, bool KV>
 __device__ __forceinline__ void sum_pass(const AttnParams& p, const BwdWork& w, const int block) {
-    typedef typename CutOf<KV>::type WorkCut;
+    typedef BwdCut<KV, false> WorkCut;             // (rows of a tile: the same for all)
     constexpr int SIDES = KV ? 2 : 1, E = DP / 32;
     constexpr bool F16 = operand_type<T>() == 0;
     const Joint& j = (KV ? w.kv_joints : w.q_joints)[block];
@@ -686,8 +689,11 @@ __global__ void __launch_bounds__(SUM_WARPS * 32) attention_sum_kernel(const Att
 static __global__ void __launch_bounds__(PLAN_THREADS) backward_plan_kernel(const AttnParams p, const BwdWork w, const bool norms) {
     let_next_kernel_start();
     if (norms) for (int i = blockIdx.x * PLAN_THREADS + threadIdx.x; i < 2 * p.n_seg; i += 2 * PLAN_THREADS) w.norms[i] = 0;
-    if (blockIdx.x == 0) { if (w.kv_start_unit) plan_units<KvCut>(p, w.kv_start_unit); }
-    else if (w.q_start_unit) plan_units<QCut>(p, w.q_start_unit);
+    long long* units = blockIdx.x == 0 ? w.kv_start_unit : w.q_start_unit;
+    if (!units) return;
+    if (p.causal) { if (blockIdx.x == 0) plan_units<BwdCut<true, true>>(p, units); else plan_units<BwdCut<false, true>>(p, units); }
+    else if (blockIdx.x == 0) plan_units<BwdCut<true, false>>(p, units);
+    else plan_units<BwdCut<false, false>>(p, units);
 }
 
 static size_t backward_carve(const AttnParams& p, void* ws, BwdWork* w) {
@@ -696,7 +702,7 @@ static size_t backward_carve(const AttnParams& p, void* ws, BwdWork* w) {
     w->kv_rows = p.n_kv < BWD_ROWS ? p.n_kv : BWD_ROWS;
     w->q_rows = (int)(packed < BWD_ROWS ? packed : BWD_ROWS);
     Carver cv(ws);
-    const bool counted_there = counts_itself(p);
+    const bool counted_there = counts_itself(p, BWD_ROWS, p.item_cost != 0);
     w->kv_start_unit = counted_there ? nullptr : cv.take<long long>((size_t)p.n_seg + 1);
     w->q_start_unit = counted_there ? nullptr : cv.take<long long>((size_t)p.n_seg + 1);
     w->kv_joints = cv.take<Joint>(MAX_SMS);

@@ -20,7 +20,8 @@ namespace tiga {
 // alone, 1.0 PFLOP/s; single tokens read their cache at 6.3 TB/s between the ends of items.
 constexpr int FWD_SOFTMAX_WARPS = 16, FWD_PRODUCER = FWD_SOFTMAX_WARPS, FWD_MMA = FWD_PRODUCER + 4, FWD_WALKER = FWD_MMA + 1;
 constexpr int FWD_THREADS = 32 * (FWD_WALKER + 1), FWD_ROWS = 256, FWD_STEP = 128;
-typedef Cut<FWD_ROWS, FWD_STEP, false> FwdCut;
+template <int MODE> using FwdCut = Cut<FWD_ROWS, FWD_STEP, false, MODE>;
+typedef FwdCut<CUT_LINE> SharedCut;
 constexpr int MASK_RING = 8;            // the producers are at most 6 steps ahead of the softmax (ring of at most 10 tiles)
 constexpr float RESCALE_AT = 8.f;
 
@@ -34,7 +35,7 @@ template <int DP> struct Fwd {
 struct FwdControl {
     unsigned long long full[10], empty[10], q_full, q_empty, s_full[2], p_full[2], o_full[2], mask_full[MASK_RING], drain;
     ItemRing items;
-    Walker<FwdCut> walk;
+    alignas(8) unsigned char walk[sizeof(Walker<FwdCut<CUT_LINE>>)];      // a Walker of the kernel's cut
     uint32_t tmem, abort_word, mask[MASK_RING][4];
     float share[2][2][128];             // what a row's threads tell each other
 };
@@ -59,11 +60,16 @@ struct FwdWork {
 // Whether a segment of the line has the only state of its rows.
 __device__ __forceinline__ bool only_state(const FwdWork& w, int s, int k0) { return s >= w.n_groups && k0 == 0; }
 
-static __global__ void __launch_bounds__(PLAN_THREADS) forward_plan_kernel(const AttnParams p, long long* unit_start) { plan_units<FwdCut>(p, unit_start); }
+static __global__ void __launch_bounds__(PLAN_THREADS) forward_plan_kernel(const AttnParams p, long long* unit_start) {
+    if (p.item_cost) plan_units<FwdCut<CUT_COSTS>>(p, unit_start);
+    else plan_units<FwdCut<CUT_STEPS>>(p, unit_start);
+}
 
-template <typename T, int DP, bool SHARED>
+template <typename T, int DP, int MODE>
 __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const __grid_constant__ AttnParams p, const FwdWork w, const __grid_constant__ TileMaps maps) {
     typedef Fwd<DP> C;
+    typedef Walker<FwdCut<MODE>> Walk;
+    constexpr bool SHARED = MODE == CUT_LINE;
     extern __shared__ __align__(1024) unsigned char smem[];
     FwdControl& ctl = *reinterpret_cast<FwdControl*>(smem + C::CONTROL);
     const uint32_t q_tile = smem_u32(smem), ring = q_tile + 2 * C::TILE;
@@ -84,7 +90,12 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
         ctl.abort_word = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == FWD_WALKER) walk_begin(&ctl.walk, p, w.unit_start, blockIdx.x, gridDim.x);
+    Walk walk;
+    if (MODE != CUT_STEPS) { if (warp == FWD_WALKER) walk_begin(reinterpret_cast<Walk*>(ctl.walk), p, w.unit_start, blockIdx.x, gridDim.x); }
+    else {
+        walk.here = false;
+        if (warp == FWD_WALKER) walk.here = walk.begin(p, w.unit_start, blockIdx.x, gridDim.x);
+    }
     if (warp == FWD_MMA) tmem_alloc(smem_u32(&ctl.tmem), 512);
     tmem_fence_before();
     __syncthreads();
@@ -94,7 +105,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
 
     if (warp == FWD_WALKER) {
         if (lane == 0) {
-            Walker<FwdCut> walk = ctl.walk;
+            if (MODE != CUT_STEPS) walk = *reinterpret_cast<Walk*>(ctl.walk);
             w.joints[blockIdx.x] = joint_of(p, walk, walk.here && (!SHARED || only_state(w, walk.s, walk.g.k0)), blockIdx.x);
             items_hand_out(ctl.items, p, walk, walk.here);
         }
@@ -116,7 +127,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
                 return j >= g.nk ? Place{-1, 0} : SHARED ? shared_place(p, g, row, j) : key_place(p, g, row, j);
             };
             Place at = place(i0);
-            for (int i = i0; i < i1 && ok; ++i, ++steps) {
+                        for (int i = i0; i < i1 && ok; ++i, ++steps) {
                 const Place here = at;
                 const uint32_t valid = __ballot_sync(~0u, here.at >= 0);
                 if (lane == 0) {
@@ -528,7 +539,7 @@ size_t attention_forward_carve(const AttnParams& p, void* ws, FwdWork* w) {
     w->rows = (int)(packed < FWD_ROWS ? packed : FWD_ROWS);
     Carver cv(ws);
     w->unit_start = cv.take<long long>((size_t)p.n_seg + 1);       // (room for it whether or not this call needs it)
-    if (counts_itself(p)) w->unit_start = nullptr;
+    if (counts_itself(p, FWD_ROWS, p.item_cost != 0)) w->unit_start = nullptr;
     w->joints = cv.take<Joint>(MAX_SMS);
     w->part_ml = cv.take<float2>(slots * w->rows);
     w->part_o = cv.take<float>(slots * w->rows * (p.D > 64 ? 128 : 64));
@@ -543,10 +554,11 @@ static tiga_status launch_forward(AttnParams p, const FwdWork& w, cudaStream_t s
     const int sms = attention_grid();
     if (sms <= 0) return TIGA_ERR_CUDA;
     // asked for on every call: the attribute belongs to the current device
-    TIGA_CUDA_TRY(cudaFuncSetAttribute(attention_forward_kernel<T, DP, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, Fwd<DP>::SMEM));
+    const auto kernel = p.item_cost ? attention_forward_kernel<T, DP, CUT_COSTS> : attention_forward_kernel<T, DP, CUT_STEPS>;
+    TIGA_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Fwd<DP>::SMEM));
     if (w.unit_start) forward_plan_kernel<<<counted(1), PLAN_THREADS, 0, s>>>(p, w.unit_start);
-    if (w.unit_start) TIGA_CUDA_TRY(launch_after(attention_forward_kernel<T, DP, false>, dim3(sms), FWD_THREADS, Fwd<DP>::SMEM, s, p, w, maps));
-    else attention_forward_kernel<T, DP, false><<<counted((unsigned)sms), FWD_THREADS, Fwd<DP>::SMEM, s>>>(p, w, maps);
+    if (w.unit_start) TIGA_CUDA_TRY(launch_after(kernel, dim3(sms), FWD_THREADS, Fwd<DP>::SMEM, s, p, w, maps));
+    else kernel<<<counted((unsigned)sms), FWD_THREADS, Fwd<DP>::SMEM, s>>>(p, w, maps);
     // tiles of a single step are whole
     if (p.table || p.n_kv > FWD_STEP) TIGA_CUDA_TRY(launch_after(attention_join_kernel<T, DP>, dim3(sms, JOIN_Y), JOIN_WARPS * 32, 0, s, p, w));
     return launch_status();
@@ -590,8 +602,10 @@ struct SharedPlan {
 // it fits: this kernel is a chain of latencies in front of everything else.
 constexpr int PLAN_HELD = 1024;
 static __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(AttnParams p, Prefixes x, const SharedPlan plan, const long long state_rows) {
-    __shared__ int32_t rows[PLAN_HELD], lengths[PLAN_HELD], members[PLAN_HELD];
-    __shared__ Segment held[PLAN_HELD];             // of the groups
+    __shared__ int32_t rows[PLAN_HELD], lengths[PLAN_HELD], members[PLAN_HELD], said[PLAN_HELD];
+    __shared__ Segment held[PLAN_HELD];             // of the groups, and what is added to their rows' numbers
+    __shared__ long long held_state[PLAN_HELD];
+    __shared__ long long totals[PLAN_THREADS / 32];
     wait_for_previous_kernel();
     let_next_kernel_start();
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, n_seq = p.n_seg;
@@ -601,11 +615,15 @@ static __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(AttnPa
         p.q_start = rows;
         p.kv_len = lengths;
     }
-    if (x.n_groups < PLAN_HELD) {
+    const bool few = x.n_groups < PLAN_HELD;
+    if (few) {
         if ((int)threadIdx.x <= x.n_groups) members[threadIdx.x] = x.group_start[threadIdx.x];
+        if ((int)threadIdx.x < x.n_groups) said[threadIdx.x] = x.shared[threadIdx.x];
         x.group_start = members;
+        x.shared = said;
     }
-    Segment* groups = x.n_groups < PLAN_HELD ? held : plan.line;
+    Segment* groups = few ? held : plan.line;
+    long long* states = few ? held_state : plan.line_state;
     __syncthreads();
     const long long most = min(min(p.max_pages * p.page_size, MOST_ROWS), 1LL << 30);
     for (int g = warp; g < x.n_groups; g += PLAN_THREADS / 32) {
@@ -632,9 +650,8 @@ static __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(AttnPa
             const long long n = g < x.n_groups ? groups[g].nq : 0, run = warp_running(n);
             if (g < x.n_groups) {
                 plan.state_start[g] = base + run - n;
-                plan.line_state[g] = base + run - n - groups[g].q0;
+                states[g] = base + run - n - groups[g].q0;
                 if (base + run > state_rows) groups[g] = {0, 0, 0, 0, 0};
-                plan.line[g] = groups[g];
                 plan.line_row[g] = plan.first_member[g] = clamp_to(x.group_start[g], n_seq);
             }
             base += __shfl_sync(~0u, run, 31);
@@ -642,33 +659,54 @@ static __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(AttnPa
         if (lane == 0) plan.state_start[x.n_groups] = min(base, state_rows);
     }
     __syncthreads();
-    for (int s = threadIdx.x; s < n_seq; s += PLAN_THREADS) {
-        int lo = 0, hi = x.n_groups;                // the last group that begins at or before it
-        while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            if (x.group_start[mid] <= s) lo = mid + 1; else hi = mid;
-        }
-        const int g = lo - 1;
-        Segment e = segment_of(p, s);
-        long long state = 0;
-        if (g >= 0 && s < clamp_to(x.group_start[g + 1], n_seq) && e.nq > 0) {
-            const Segment of = groups[g];
-            if (of.nk > 0 && e.q0 >= of.q0 && (long long)e.q0 + e.nq <= (long long)of.q0 + of.nq) {            // (bounds that do not ascend lead nowhere)
-                const int base = of.nk & ~31;
-                e.k0 = of.nk;
-                e.nk = max(e.nk - base, 0);
-                e.length -= base;
-                state = plan.line_state[g];
+    // the line, and its units
+    const int n_line = x.n_groups + n_seq;
+    long long before = 0;
+    for (int i0 = 0; i0 < n_line; i0 += PLAN_THREADS) {
+        const int i = i0 + (int)threadIdx.x, s = i - x.n_groups;
+        long long n = 0;
+        if (i < n_line) {
+            Segment e;
+            long long state = 0;
+            if (s < 0) {
+                e = groups[i];
+                state = states[i];
+            } else {
+                e = segment_of(p, s);
+                int lo = 0, hi = x.n_groups;                // the last group that begins at or before the sequence
+                while (lo < hi) {
+                    const int mid = (lo + hi) >> 1;
+                    if (x.group_start[mid] <= s) lo = mid + 1; else hi = mid;
+                }
+                const int g = lo - 1;
+                if (g >= 0 && s < clamp_to(x.group_start[g + 1], n_seq) && e.nq > 0) {
+                    const Segment of = groups[g];
+                    if (of.nk > 0 && e.q0 >= of.q0 && (long long)e.q0 + e.nq <= (long long)of.q0 + of.nq) {            // (bounds that do not ascend lead nowhere)
+                        const int base = of.nk & ~31;
+                        e.k0 = of.nk;
+                        e.nk = max(e.nk - base, 0);
+                        e.length -= base;
+                        state = states[g];
+                    }
+                }
+                plan.line_row[i] = s;
             }
+            plan.line[i] = e;
+            plan.line_state[i] = state;
+            n = SharedCut::units(p, e) * p.kv_heads;
         }
-        plan.line[x.n_groups + s] = e;
-        plan.line_row[x.n_groups + s] = s;
-        plan.line_state[x.n_groups + s] = state;
+        const long long run = warp_running(n);
+        if (lane == 31) totals[warp] = run;
+        __syncthreads();
+        long long sum = before + run;
+        for (int k = 0; k < PLAN_THREADS / 32; ++k) {
+            if (k < warp) sum += totals[k];
+            before += totals[k];
+        }
+        if (i < n_line) plan.unit_start[i + 1] = sum;
+        __syncthreads();
     }
-    __syncthreads();
-    p.line = plan.line;
-    p.n_seg = x.n_groups + n_seq;
-    plan_units<FwdCut>(p, plan.unit_start);
+    if (threadIdx.x == 0) plan.unit_start[0] = 0;
 }
 
 // Joins the two states of every row that has two (the first blocks): a warp has one head of a row.  A state lies among the states
@@ -682,7 +720,7 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32, SHARED_JOIN_BLOCKS) shared_jo
     if (behind >= 0) return join_block<T, DP>(p, w, behind / SHARED_JOIN_SLICES, behind % SHARED_JOIN_SLICES, SHARED_JOIN_SLICES);
     constexpr int E = DP / 32;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const long long units = w.unit_start[p.n_seg], blocks = Walker<FwdCut>::pieces(p, units, sms);
+    const long long units = w.unit_start[p.n_seg], blocks = Walker<SharedCut>::pieces(p, units, sms);
     auto block_of = [&](long long unit) { return (int)quotient((unit + 1) * blocks - 1, units); };
     const long long tasks = w.state_start[w.n_groups] * p.heads, stride = (long long)state_blocks * JOIN_WARPS;
     for (long long task = (long long)blockIdx.x * JOIN_WARPS + warp; task < tasks; task += stride) {
@@ -697,11 +735,11 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32, SHARED_JOIN_BLOCKS) shared_jo
         if (own.k0 == 0) continue;
         int first0, first1, parts0, parts1, r0, r1;
         auto find = [&](const Segment& seg, int line, int& first, int& parts, int& r) {
-            const int packed = (row - seg.q0) * p.group + head % p.group, t = packed / FWD_ROWS, cost = FwdCut::step_cost(p, seg);
-            const long long start = w.unit_start[line] + h * FwdCut::units(p, seg) + FwdCut::before(p, seg, t) + p.item_cost - 1;
+            const int packed = (row - seg.q0) * p.group + head % p.group, t = packed / FWD_ROWS, cost = SharedCut::step_cost(p, seg);
+            const long long start = w.unit_start[line] + h * SharedCut::units(p, seg) + SharedCut::before(p, seg, t) + p.item_cost - 1;
             r = packed % FWD_ROWS;
             first = block_of(start + cost);                 // the blocks that have the last unit of the tile's first and last step
-            parts = block_of(start + (long long)cost * FwdCut::steps(p, seg, t)) - first + 1;
+            parts = block_of(start + (long long)cost * SharedCut::steps(p, seg, t)) - first + 1;
         };
         find(shared, g, first0, parts0, r0);
         find(own, w.n_groups + s, first1, parts1, r1);
@@ -788,13 +826,13 @@ static tiga_status launch_shared(AttnParams p, const Prefixes& g, const FwdWork&
     make_tile_maps(&p, operand_type<T>() == 1, &maps);
     const int sms = attention_grid();
     if (sms <= 0) return TIGA_ERR_CUDA;
-    TIGA_CUDA_TRY(cudaFuncSetAttribute(attention_forward_kernel<T, DP, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Fwd<DP>::SMEM));
+    TIGA_CUDA_TRY(cudaFuncSetAttribute(attention_forward_kernel<T, DP, CUT_LINE>, cudaFuncAttributeMaxDynamicSharedMemorySize, Fwd<DP>::SMEM));
     p.item_cost = SHARED_ITEM_COST;
     p.uneven = 1;
     shared_plan_kernel<<<counted(1), PLAN_THREADS, 0, s>>>(p, g, plan, w.state_rows);
     p.line = plan.line;
     p.n_seg = w.n_groups + w.n_seq;
-    TIGA_CUDA_TRY(launch_after(attention_forward_kernel<T, DP, true>, dim3(sms), FWD_THREADS, Fwd<DP>::SMEM, s, p, w, maps));
+    TIGA_CUDA_TRY(launch_after(attention_forward_kernel<T, DP, CUT_LINE>, dim3(sms), FWD_THREADS, Fwd<DP>::SMEM, s, p, w, maps));
     const long long warps = w.state_rows * p.heads, blocks = (warps + JOIN_WARPS - 1) / JOIN_WARPS, most = 8LL * sms;
     TIGA_CUDA_TRY(launch_after(shared_join_kernel<T, DP>, dim3((unsigned)(sms * SHARED_JOIN_SLICES + (blocks < most ? blocks : most))), JOIN_WARPS * 32, 0, s, p, w, sms));
     return launch_status();

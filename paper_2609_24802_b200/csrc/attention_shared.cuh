@@ -35,7 +35,6 @@ __device__ __forceinline__ int clamp_to(int v, int hi) { return min(max(v, 0), h
 
 // (the bounds of rows and of dense keys: p.q_start and p.kv_start, or a copy of them)
 __device__ __forceinline__ Segment segment_of(const AttnParams& p, int s, const int32_t* q_start, const int32_t* kv_start) {
-    if (p.line) return p.line[s];
     Segment g;
     g.q0 = clamp_to(q_start[s], p.n_q);
     g.nq = max(clamp_to(q_start[s + 1], p.n_q) - g.q0, 0);
@@ -53,9 +52,7 @@ __device__ __forceinline__ Segment segment_of(const AttnParams& p, int s) { retu
 
 // keys that row t of the segment's nq rows reads: [0, this)
 __host__ __device__ __forceinline__ int keys_of_row(const AttnParams& p, const Segment& g, int t) {
-    if (!p.causal) return g.nk;
-    const int n = g.length - g.nq + t + 1;
-    return n < 0 ? 0 : n < g.nk ? n : g.nk;
+    return p.causal ? min(max(g.length - g.nq + t + 1, 0), g.nk) : g.nk;
 }
 
 // Where key j of segment s (0 <= j < g.nk) lies: paged, its page and slot; dense, its row and 0.  at < 0: it is masked, or has no page.
@@ -110,6 +107,15 @@ __device__ __forceinline__ Place shared_place(const AttnParams& p, const Segment
 template <typename V>
 __device__ __forceinline__ int last_place(const V* start, int n, V v) {
     int lo = 0, hi = n;
+    if (n <= 128) {             // few: all at once
+        int count = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int at = 32 * k + (int)(threadIdx.x % 32);
+            count += __popc(__ballot_sync(~0u, at < n && start[at] <= v));
+        }
+        return max(count - 1, 0);
+    }
     while (hi - lo > 1) {
         const int gap = (hi - lo + 31) / 32, at = lo + (int)(threadIdx.x % 32) * gap;
         const unsigned before = __ballot_sync(~0u, at < hi && start[at] <= v) | 1u;
@@ -183,11 +189,14 @@ __host__ __device__ __forceinline__ long long lattice_points(long long n, long l
 // times the work, so a tile counts item_cost units more, in front of its steps.  Under them nothing is done: a piece that ends there has
 // none of the tile, one that begins there has its first step.  Where full tiles stand beside tiles of a few rows, whose steps wait for memory
 // (2500 cycles against 3750), a step costs two or three units; it is done by the piece that has its last one.
-template <int TILE_, int STEP_, bool KEYS_>
+enum CutMode { CUT_STEPS, CUT_COSTS, CUT_LINE };          // units are steps; tiles and steps cost as p says; the same, and p.line has the segments
+template <int TILE_, int STEP_, bool KEYS_, int MODE = CUT_STEPS>
 struct Cut {
     static constexpr int TILE = TILE_, STEP = STEP_;      // stationary rows of a tile, rows of a step: powers of two
     static constexpr bool KEYS = KEYS_;                   // the keys are stationary
+    static constexpr bool PLAIN = MODE == CUT_STEPS;
 
+    static __device__ __forceinline__ Segment segment(const AttnParams& p, int s) { return MODE == CUT_LINE ? p.line[s] : segment_of(p, s); }
     static __host__ __device__ __forceinline__ int rows(const AttnParams& p, const Segment& g) { return KEYS ? g.nk : g.nq * p.group; }
     static __host__ __device__ __forceinline__ int tiles(const AttnParams& p, const Segment& g) {
         const int n = rows(p, g);
@@ -234,12 +243,21 @@ struct Cut {
         const long long k1 = lo < 0 ? 0 : lo < n ? lo : n, k2 = hi < k1 ? k1 : hi < n ? hi : n;
         return k1 + (k1 < k2 ? lattice_points(k2 - k1, TILE, TILE * k1 + b, m) : 0) + (n - k2) * most + (t > last ? steps(p, g, last) : 0);
     }
-    static __host__ __device__ __forceinline__ int step_cost(const AttnParams& p, const Segment& g) { return !p.uneven ? 1 : (long long)rows(p, g) <= 128 ? 2 : 3; }
+    static __host__ __device__ __forceinline__ int item_cost(const AttnParams& p) { return MODE == CUT_STEPS ? 0 : p.item_cost; }
+    static __host__ __device__ __forceinline__ bool uneven(const AttnParams& p) { return MODE != CUT_STEPS && p.uneven; }
+    static __host__ __device__ __forceinline__ int step_cost(const AttnParams& p, const Segment& g) { return !uneven(p) ? 1 : rows(p, g) <= 128 ? 2 : 3; }
     // units of the first t tiles, and of all tiles of a kv head
     static __host__ __device__ __forceinline__ long long before(const AttnParams& p, const Segment& g, int t) {
-        return steps_before(p, g, t) * step_cost(p, g) + (long long)t * p.item_cost;
+        return steps_before(p, g, t) * step_cost(p, g) + (long long)t * item_cost(p);
     }
-    static __host__ __device__ __forceinline__ long long units(const AttnParams& p, const Segment& g) { return before(p, g, tiles(p, g)); }
+    static __host__ __device__ __forceinline__ long long units(const AttnParams& p, const Segment& g) {
+        if (!PLAIN) return before(p, g, tiles(p, g));
+        const int n = tiles(p, g);
+        if (KEYS || !p.causal) return n ? (long long)n * steps(p, g, 0) : 0;
+        long long sum = 0;
+        for (int t = 0; t < n; ++t) sum += steps(p, g, t);
+        return sum;
+    }
 };
 
 __device__ __forceinline__ long long warp_total(long long v) {
@@ -269,17 +287,23 @@ struct Walker {
     // the tile's steps from its unit `off` on; false: the piece ends in front of the tile's first step
     __device__ __forceinline__ bool open(const AttnParams& p, long long off) {
         steps = C::steps(p, g, t);
+        if (C::PLAIN) {
+            i0 = (int)off;
+            i1 = (int)min((long long)steps, i0 + left);
+            left -= i1 - i0;
+            return true;
+        }
         const int cost = C::step_cost(p, g);
-        const long long end = min((long long)steps * cost + p.item_cost, off + left);
+        const long long end = min((long long)steps * cost + C::item_cost(p), off + left);
         left -= end - off;
         auto steps_of = [&](long long u) { return u <= 0 ? 0 : cost == 1 ? (int)u : (int)quotient(u, cost); };
-        i0 = steps_of(off - p.item_cost);
-        i1 = steps_of(end - p.item_cost);
+        i0 = steps_of(off - C::item_cost(p));
+        i1 = steps_of(end - C::item_cost(p));
         return i1 > i0;
     }
     // blocks that take part: every piece has a step's units, so that the blocks between a tile's first and last one all have steps of it
     static __device__ __forceinline__ long long pieces(const AttnParams& p, long long units, int grid) {
-        return min((long long)grid, max(p.uneven ? units / 3 : units, 1LL));
+        return min((long long)grid, max(C::uneven(p) ? units / 3 : units, 1LL));
     }
     __device__ __forceinline__ long long first_unit(long long block) const { return quotient(block * units, blocks); }
 
@@ -291,7 +315,7 @@ struct Walker {
         if (unit_start) units = unit_start[p.n_seg];
         else {
             units = 0;
-            for (int k = 0; k < p.n_seg; k += 32) units += k + lane < p.n_seg ? C::units(p, segment_of(p, k + lane)) * p.kv_heads : 0;
+            for (int k = 0; k < p.n_seg; k += 32) units += k + lane < p.n_seg ? C::units(p, C::segment(p, k + lane)) * p.kv_heads : 0;
             units = warp_total(units);
         }
         blocks = pieces(p, units, grid);
@@ -304,7 +328,7 @@ struct Walker {
             mine = unit_start[s + 1] - unit_start[s];
         } else {
             for (int k = 0;; k += 32) {
-                const long long n = k + lane < p.n_seg ? C::units(p, segment_of(p, k + lane)) * p.kv_heads : 0;
+                const long long n = k + lane < p.n_seg ? C::units(p, C::segment(p, k + lane)) * p.kv_heads : 0;
                 const long long run = warp_running(n);
                 const unsigned beyond = __ballot_sync(~0u, run > off);
                 if (beyond) {
@@ -317,7 +341,7 @@ struct Walker {
                 off -= __shfl_sync(~0u, run, 31);
             }
         }
-        g = segment_of(p, s);
+        g = C::segment(p, s);
         const long long per_head = quotient(mine, p.kv_heads);
         h = (int)quotient(off, per_head);
         off -= h * per_head;
@@ -325,6 +349,19 @@ struct Walker {
             const long long n = C::before(p, g, 1);
             t = (int)quotient(off, n);
             off -= t * n;
+        } else if (C::PLAIN) {
+            const int tiles = C::tiles(p, g);
+            for (t = 0;; t += 32) {
+                const long long run = warp_running(t + lane < tiles ? C::steps(p, g, t + lane) : 0);
+                const unsigned beyond = __ballot_sync(~0u, run > off);
+                if (beyond) {
+                    const int at = __ffs(beyond) - 1;
+                    if (at) off -= __shfl_sync(~0u, run, at - 1);
+                    t += at;
+                    break;
+                }
+                off -= __shfl_sync(~0u, run, 31);
+            }
         } else {            // the last tile that begins at or before this unit, 32 places a round
             int hi = C::tiles(p, g);
             t = 0;
@@ -345,19 +382,21 @@ struct Walker {
             t = 0;
             if (++h >= p.kv_heads) {
                 h = 0;
-                do { g = segment_of(p, ++s); } while (C::rows(p, g) == 0);
+                do { g = C::segment(p, ++s); } while (C::rows(p, g) == 0);
             }
         }
         return open(p, 0);
     }
     // after begin() inside of a tile's steps: the block that has its first step
     __device__ __forceinline__ int first_block(const AttnParams& p, int block) const {
-        return (int)quotient((first_unit(block) - start + p.item_cost + C::step_cost(p, g)) * blocks - 1, units);
+        if (C::PLAIN) return (int)quotient((first_unit(block) - i0 + 1) * blocks - 1, units);
+        return (int)quotient((first_unit(block) - start + C::item_cost(p) + C::step_cost(p, g)) * blocks - 1, units);
     }
 };
 
-// The beginning of a block's piece, out of line: the triangle's closed forms want many registers for a moment, which inlined were spilled from
-// the loops of the other warps (chunk of 2048 on 16384: 559 us instead of 510).
+// The beginning of a block's piece, out of line: the closed forms want many registers for a moment, which inlined were spilled from the loops
+// of the other warps (chunk of 2048 on 16384: 559 us instead of 510).  Plain cuts, whose chunks have few tiles, go through them and stay
+// inline, as even the call cost 2 %.
 template <typename C>
 static __device__ __noinline__ void walk_begin(Walker<C>* to, const AttnParams& p, const long long* unit_start, int block, int grid) {
     Walker<C> w{};
@@ -374,7 +413,7 @@ static __device__ void plan_units(const AttnParams& p, long long* unit_start) {
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     for (int s0 = 0; s0 < p.n_seg; s0 += PLAN_THREADS) {
         const int s = s0 + threadIdx.x;
-        const long long n = warp_running(s < p.n_seg ? C::units(p, segment_of(p, s)) * p.kv_heads : 0);
+        const long long n = warp_running(s < p.n_seg ? C::units(p, C::segment(p, s)) * p.kv_heads : 0);
         if (lane == 31) totals[warp] = n;
         __syncthreads();
         long long sum = before;
@@ -388,8 +427,10 @@ static __device__ void plan_units(const AttnParams& p, long long* unit_start) {
     if (threadIdx.x == 0) unit_start[0] = 0;
 }
 // Whether the blocks count the units themselves: a launch less, for a few hundred instructions in every warp.
-constexpr int COUNT_SEGMENTS = 256;
-static inline bool counts_itself(const AttnParams& p) { return p.n_seg <= COUNT_SEGMENTS; }
+constexpr int COUNT_SEGMENTS = 256, COUNT_TILES = 64;
+static inline bool counts_itself(const AttnParams& p, int tile, bool closed_form) {
+    return p.n_seg <= COUNT_SEGMENTS && (closed_form || !p.causal || (long long)p.n_q * p.group <= (long long)COUNT_TILES * tile);
+}
 
 // A kernel may start before the one in front of it in the stream has ended; it waits where it first reads what that one wrote.
 __device__ __forceinline__ void wait_for_previous_kernel() { asm volatile("griddepcontrol.wait;" ::: "memory"); }

@@ -33,6 +33,6 @@ extern "C" int run_cut(int keys, int causal, int group, int nq, int nk, int leng
     p.group = group;
     p.causal = causal;
     const tiga::Segment g{0, nq, 0, nk, length};
-    return keys ? differs<tiga::Cut<128, 128, true>>(p, g) : differs<tiga::Cut<256, 128, false>>(p, g) | differs<tiga::Cut<128, 128, false>>(p, g);
+    return keys ? differs<tiga::Cut<128, 128, true, tiga::CUT_COSTS>>(p, g) : differs<tiga::Cut<256, 128, false, tiga::CUT_COSTS>>(p, g) | differs<tiga::Cut<128, 128, false, tiga::CUT_COSTS>>(p, g);
 }
 extern "C" long long run_lattice(long long n, long long a, long long b, long long m) { return tiga::lattice_points(n, a, b, m); }
