@@ -40,6 +40,8 @@ static bool encode(CUtensorMap* m, bool bf16, const void* base, const long long 
 }
 
 void make_tile_maps(AttnParams* p, bool bf16, TileMaps* m) {
+    auto whole = [p](const void* out, int bit) { return p->D % 16 == 0 && (reinterpret_cast<uintptr_t>(out) & 31) == 0 ? bit : 0; };
+    p->whole_sectors = whole(p->out, WHOLE_OUT) | whole(p->gq, WHOLE_GQ) | whole(p->gk, WHOLE_GK) | whole(p->gv, WHOLE_GV);
     p->kv_box = p->q_box = 0;
     if (!encoder()) return;
     if (p->n_q > 0 && 32 % p->group == 0) {

@@ -589,10 +589,10 @@ __device__ __forceinline__ void backward_pass(const AttnParams& p, const BwdWork
                                 h[k] = zero && ok ? 0u : pack_half<T>(__uint_as_float(v[8 * c + 2 * k]) * finish, __uint_as_float(v[8 * c + 2 * k + 1]) * finish);
                             o[c] = make_uint4(h[0], h[1], h[2], h[3]);
                         }
-                        store_rows<2>(o, out + out_row * p.D + f, valid && out, (p.D - f) / 8);
+                        store_pieces(o, out + out_row * p.D + f, valid && out, (p.D - f) / 8, p.whole_sectors & (KV ? (side ? WHOLE_GV : WHOLE_GK) : WHOLE_GQ));
                     } else if (valid) {
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) reinterpret_cast<uint4*>(part + f)[k] = make_uint4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+                        store_sector(part + f, v);
+                        store_sector(part + f + 8, v + 8);
                     }
                 }
             tmem_fence_before();
@@ -746,7 +746,7 @@ static tiga_status launch_backward(AttnParams p, const BwdWork& w, cudaStream_t 
 
 tiga_status attention_backward(const AttnParams& p, bool bf16, void* ws, cudaStream_t s) {
     BwdWork w;
-    backward_carve(p, ws, &w);
+    backward_carve(p, on_sectors(ws), &w);
     if (bf16) return p.D > 64 ? launch_backward<__nv_bfloat16, 128>(p, w, s) : launch_backward<__nv_bfloat16, 64>(p, w, s);
     return p.D > 64 ? launch_backward<__half, 128>(p, w, s) : launch_backward<__half, 64>(p, w, s);
 }

@@ -146,10 +146,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
                         const int r = x * 128 + 32 * pw + lane;
                         if (x == 1 && rows <= 128) {
                             if (lane == 0) mbar_arrive(bar(ctl.q_full), 32);
-                        } else {
-                            // whatever a row of the queries holds stays in that row: boxes bring it where there is no such row, too
-                            fetch_packed<DP>(q_tile + x * C::TILE, 32 * pw, bar(ctl.q_full), p, g, maps, false, h, e.t * FWD_ROWS + r, p.q_box || r < rows, p.q);
-                        }
+                        } else fetch_packed<DP>(q_tile + x * C::TILE, 32 * pw, bar(ctl.q_full), p, g, maps, false, h, e.t * FWD_ROWS + r, r < rows, p.q);
                     }
                     ++items;
                 }
@@ -420,11 +417,10 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
                                 h[k] = finish == 0.f ? 0u : pack_half<T>(__uint_as_float(v[8 * c + 2 * k]) * finish, __uint_as_float(v[8 * c + 2 * k + 1]) * finish);
                             o[c] = make_uint4(h[0], h[1], h[2], h[3]);
                         }
-                        store_rows<2>(o, (T*)p.out + out_row * p.D + f, valid, (p.D - f) / 8);
+                        store_pieces(o, (T*)p.out + out_row * p.D + f, valid, (p.D - f) / 8, p.whole_sectors & WHOLE_OUT);
                     } else if (valid) {
-                        uint4* out = reinterpret_cast<uint4*>(put_aside + part * DP + f);
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) out[k] = make_uint4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+                        store_sector(put_aside + part * DP + f, v);
+                        store_sector(put_aside + part * DP + f + 8, v + 8);
                     }
                 }
             if (valid && y == 0 && (two || x == 0)) {
@@ -566,7 +562,7 @@ static tiga_status launch_forward(AttnParams p, const FwdWork& w, cudaStream_t s
 
 tiga_status attention_forward(const AttnParams& p, bool bf16, void* ws, cudaStream_t s) {
     FwdWork w;
-    attention_forward_carve(p, ws, &w);
+    attention_forward_carve(p, on_sectors(ws), &w);
     if (bf16) return p.D > 64 ? launch_forward<__nv_bfloat16, 128>(p, w, s) : launch_forward<__nv_bfloat16, 64>(p, w, s);
     return p.D > 64 ? launch_forward<__half, 128>(p, w, s) : launch_forward<__half, 64>(p, w, s);
 }
@@ -841,7 +837,7 @@ static tiga_status launch_shared(AttnParams p, const Prefixes& g, const FwdWork&
 tiga_status attention_shared(const AttnParams& p, const Prefixes& g, bool bf16, void* ws, cudaStream_t s) {
     FwdWork w;
     SharedPlan plan;
-    shared_carve(p, g.n_groups, ws, &w, &plan);
+    shared_carve(p, g.n_groups, on_sectors(ws), &w, &plan);
     if (bf16) return p.D > 64 ? launch_shared<__nv_bfloat16, 128>(p, g, w, plan, s) : launch_shared<__nv_bfloat16, 64>(p, g, w, plan, s);
     return p.D > 64 ? launch_shared<__half, 128>(p, g, w, plan, s) : launch_shared<__half, 64>(p, g, w, plan, s);
 }

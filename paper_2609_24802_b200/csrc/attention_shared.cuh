@@ -21,8 +21,11 @@ struct AttnParams {
     long long n_pages, page_size, table_stride, max_pages, page_stride, slot_stride;
     float scale;
     int item_cost, uneven;          // units that a tile costs beside its steps; whether steps cost several (see Cut)
+    int whole_sectors;              // of which outputs 16 features of a row are a whole sector (WHOLE_OUT, ...)
     int kv_box, q_box;              // rows that a box of the tensor maps brings (0: rows are copied one by one)
 };
+
+enum { WHOLE_OUT = 1, WHOLE_GQ = 2, WHOLE_GK = 4, WHOLE_GV = 8 };
 
 // A segment's rows [q0, q0 + nq) and its keys [k0, k0 + nk) (paged: k0 = 0), bounds clamped to the arrays.  length: its tokens, of which a
 // cache may hold fewer (the rows' positions count from its end, not from that of the table).
@@ -452,6 +455,8 @@ static inline cudaError_t launch_after(void (*kernel)(A...), dim3 grid, int thre
 }
 
 constexpr int MAX_SMS = 160;            // blocks that workspaces provide for
+// Workspaces come on a boundary of 16 bytes; states are put aside in sectors of 32.  (Their sizes have 256 bytes to spare.)
+static inline void* on_sectors(void* ws) { return reinterpret_cast<void*>(align_up(reinterpret_cast<uintptr_t>(ws), 256)); }
 
 // Sequences whose caches begin with the same pages: those of group g, [group_start[g], group_start[g + 1]), share positions [0, shared[g]).
 struct Prefixes { const int32_t *group_start, *shared; int n_groups; };

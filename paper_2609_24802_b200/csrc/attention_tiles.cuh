@@ -172,6 +172,19 @@ __device__ __forceinline__ void store_rows(uint4 (&v)[C], void* to, bool on, int
     }
 }
 
+// 32 bytes, on a boundary of 32, by one lane
+__device__ __forceinline__ void store_sector(void* to, const uint32_t* v) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(to), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+}
+// Two pieces of each lane's row: a store of 32 bytes where the rows' pieces lie on whole sectors, which needs no exchange.
+__device__ __forceinline__ void store_pieces(uint4 (&v)[2], void* to, bool on, int wanted, bool whole_sectors) {
+    if (whole_sectors) {
+        const uint32_t w[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
+        if (on && wanted > 0) store_sector(to, w);
+    } else store_rows<2>(v, to, on, wanted);
+}
+
 // host: the maps, and the boxes that they allow (attention.cu)
 void make_tile_maps(AttnParams* p, bool bf16, TileMaps* m);
 bool make_row_map(const AttnParams& p, bool bf16, int packed, CUtensorMap* m);

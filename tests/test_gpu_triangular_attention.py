@@ -247,3 +247,28 @@ def test_agrees_with_the_dense_relation_where_every_row_reads_all_keys(tiga):
     grads = tiga.tiga_apply_dense_attention_backward(g, c["q"], c["k"], c["v"], out, lse, c["go"], c["scale"])
     for name, x in zip(("out", "lse", "grad_q", "grad_key", "grad_value"), (out, lse, *grads[:3])):
         assert torch.equal(x, got[name]), name
+
+
+@pytest.mark.parametrize("D", [64, 72, 128])
+def test_outputs_and_workspaces_on_any_boundary_of_16_bytes(tiga, D):
+    """Results do not depend on whether rows begin on a sector."""
+    c = case([300, 40], [300, 70], 4, 2, D, BF16, seed=27)
+    want = run(tiga, c)
+    g = tiga.TriangularRelation(starts(c["q_len"]), starts(c["kv_len"]))
+
+    def shifted(shape, dtype):
+        n = 1
+        for s in shape:
+            n *= s
+        raw = torch.zeros(n + 64, dtype=dtype, device="cuda")
+        raw = raw[(-raw.data_ptr() % 32) // raw.element_size() + 16 // raw.element_size():]
+        assert raw.data_ptr() % 32 == 16
+        return raw[:n].view(shape)
+    out, lse = shifted(c["q"].shape, BF16), shifted(c["q"].shape[:2], torch.float32)
+    ws = shifted((tiga.tiga_triangular_attention_workspace_bytes(g, c["q"], c["k"], c["v"]),), torch.uint8)
+    tiga.tiga_apply_triangular_attention(g, c["q"], c["k"], c["v"], c["scale"], out=out, lse=lse, ws=ws)
+    grads = [shifted(x.shape, BF16) for x in (c["q"], c["k"], c["k"])]
+    ws = shifted((tiga.tiga_triangular_attention_workspace_bytes(g, c["q"], c["k"], c["v"], True),), torch.uint8)
+    tiga.tiga_apply_triangular_attention_backward(g, c["q"], c["k"], c["v"], out, lse, c["go"], c["scale"], *grads, ws=ws)
+    for name, x in zip(("out", "lse", "grad_q", "grad_key", "grad_value"), (out, lse, *grads)):
+        assert torch.equal(x, want[name]), name
