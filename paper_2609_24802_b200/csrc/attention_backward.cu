@@ -153,6 +153,7 @@ __global__ void __launch_bounds__(PREP_THREADS, PREP_BLOCKS) attention_prepare_k
             uint4 a = make_uint4(0, 0, 0, 0), b = a;
             float lse = 0.f;
             int few = 0;
+            bool later = false;
             if (r < q_to) {
                 if (in_width) {
                     a = *reinterpret_cast<const uint4*>((const T*)p.go + row * p.go_row + here.head * p.go_head + lane * 8);
@@ -165,8 +166,11 @@ __global__ void __launch_bounds__(PREP_THREADS, PREP_BLOCKS) attention_prepare_k
                     top = 0.f;
                     g = segment_of(p, at_seg.s, q_start, kv_start);
                 }
-                const int n = keys_of_row(p, g, (int)row - g.q0);
-                if (n <= FEW_KEYS && lse != -INFINITY) few = n;
+                if (p.causal) {
+                    const int n = keys_of_row(p, g, (int)row - g.q0);
+                    later = n > 0 && n <= FEW_KEYS;
+                }
+                else if (g.nk <= FEW_KEYS && lse != -INFINITY) few = g.nk;
             }
             float dot = fold(dot8<T>(a, b));
             const float norm = NORMS ? fold(dot8<T>(a, a)) : 0.f;
@@ -190,7 +194,7 @@ __global__ void __launch_bounds__(PREP_THREADS, PREP_BLOCKS) attention_prepare_k
             }
             if (r >= q_to) continue;
             const bool reads = lse != -INFINITY;
-            if (lane == 0) w.stats[at] = make_float2(reads ? lse * LOG2E_F : INFINITY, reads ? dot : 0.f);
+            if (lane == 0 && !later) w.stats[at] = make_float2(reads ? lse * LOG2E_F : INFINITY, reads ? dot : 0.f);
             if (NORMS && reads) top = norm == norm ? fmaxf(top, norm) : INFINITY;
         }
         if (NORMS) put_last_norms<LANES>(w.norms, at_seg.s, first_s, top);
@@ -230,6 +234,44 @@ __global__ void __launch_bounds__(PREP_THREADS, PREP_BLOCKS) attention_prepare_k
                 }
             }
             put_last_norms<LANES>(w.norms + 1, at_seg.s, first_s, top);
+        }
+    }
+    if (p.causal) {
+        // The rows of few keys are the first ones of every segment, one behind the other: dealt out to all warps of the grid, a row and some of its
+        // heads at a time (in the loop above their block was the last to end, by 30 us).
+        constexpr int HEADS = 32 / LANES;
+        const int pieces = (p.heads + HEADS - 1) / HEADS;
+        const long long tasks = (long long)p.n_seg * FEW_KEYS * pieces, stride = (long long)gridDim.x * (PREP_THREADS / 32);
+        for (long long task = (long long)blockIdx.x * (PREP_THREADS / 32) + threadIdx.x / 32; task < tasks; task += stride) {
+            const long long of_row = quotient(task, pieces);
+            const int s = (int)(of_row / FEW_KEYS), n = (int)(of_row % FEW_KEYS) + 1, head = (int)(task - of_row * pieces) * HEADS + (int)(threadIdx.x % 32) / LANES;
+            const Segment g = segment_of(p, s, q_start, kv_start);
+            const int t = n - 1 - (g.length - g.nq), row = g.q0 + t;            // the row that reads n keys
+            if (t < 0 || t >= g.nq || n > g.nk) continue;
+            const bool on = head < p.heads;
+            const int kv_head = on ? head / p.group : 0;
+            const long long at = (long long)row * p.heads + head;
+            const float lse = on ? p.lse_in[at] : -INFINITY;
+            uint4 q = make_uint4(0, 0, 0, 0), a = q;
+            if (on && in_width) {
+                q = *reinterpret_cast<const uint4*>((const T*)p.q + row * p.q_row + head * p.q_head + lane * 8);
+                a = *reinterpret_cast<const uint4*>((const T*)p.go + row * p.go_row + head * p.go_head + lane * 8);
+            }
+            float sum = 0.f;
+#pragma unroll 4
+            for (int j = 0; j < n; ++j) {               // (masked keys are loaded as well, so that no load waits for the mask)
+                uint4 k = make_uint4(0, 0, 0, 0), v = k;
+                const Place at_key = {g.k0 + j, 0};
+                const bool read = !p.mask || p.mask[at_key.at];
+                if (in_width) {
+                    k = *reinterpret_cast<const uint4*>((const T*)p.k + key_offset(p, at_key, kv_head) + lane * 8);
+                    v = *reinterpret_cast<const uint4*>((const T*)p.v + value_offset(p, at_key, kv_head) + lane * 8);
+                }
+                const float score = fold(dot8<T>(q, k)), dp = fold(dot8<T>(a, v));
+                if (read) sum += ex2((score * p.scale - lse) * LOG2E_F) * dp;
+            }
+            const bool reads = lse != -INFINITY;
+            if (on && lane == 0) w.stats[at] = make_float2(reads ? lse * LOG2E_F : INFINITY, reads ? sum : 0.f);
         }
     }
 }
