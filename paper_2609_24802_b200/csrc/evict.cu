@@ -292,6 +292,8 @@ extern "C" tiga_status tiga_paged_evict(const tiga_pages* from, const tiga_pages
     if (attention_bad_weights(weights) || (to_weights && attention_bad_weights(to_weights))) return TIGA_ERR_INVALID_ARG;
     if (keep > MOST_ROWS || from->n_seg * h->kv_heads > (1 << 24)) return TIGA_ERR_UNSUPPORTED;
     if (from->n_seg == 0) return TIGA_OK;
+    // slots or heads of a page that share storage would be written twice
+    if ((to->page_size > 1 && to->slot_stride == 0) || (h->kv_heads > 1 && to->head_stride == 0) || (to->n_pages > 1 && to->page_stride == 0)) return TIGA_ERR_INVALID_ARG;
     if (attention_bad_ints(from->kv_len) || attention_bad_ints(to_len) || attention_bad_ints(kept) || to_len == from->kv_len) return TIGA_ERR_INVALID_ARG;
     if (attention_bad_ints(to->table) || (from->max_pages > 0 && attention_bad_ints(from->table))) return TIGA_ERR_INVALID_ARG;
     auto bad = [](const void* a) { return !a || !aligned16(a); };
