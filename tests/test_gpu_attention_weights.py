@@ -214,3 +214,17 @@ def test_captured_and_replayed(tiga):
         graph.replay()
     torch.cuda.synchronize()
     assert torch.allclose(total, 3 * once, rtol=2.0 ** -22, atol=0)
+
+
+def test_pages_beyond_32_bits(tiga):
+    """Pages whose elements lie behind the 2^31st, brought in boxes and row by row."""
+    for page in (16, 7):
+        c = make([1, 40], [50, 60], 4, 2, 64, BF16, page, seed=15)
+        n = c["pages"].shape[0]
+        stride = (1 << 31) // (n - 2) // 8 * 8 + 8
+        pool = torch.as_strided(torch.empty((n - 1) * stride + 4096, dtype=BF16, device="cuda"), (n, page, 2, 64), (stride, 128, 64, 1))
+        pool.copy_(c["pages"])
+        c["pages"] = pool
+        check(tiga, c)
+        del c, pool
+        torch.cuda.empty_cache()

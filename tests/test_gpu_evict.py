@@ -183,3 +183,24 @@ def test_on_another_stream(tiga):
     kept, left = tiga.tiga_paged_evict(cache, to, c["weights"], 48, 8, stream=side)
     side.synchronize()
     assert torch.equal(kept, want[2]) and torch.equal(left, want[3]) and torch.equal(c["to_value"].view(torch.int16), want[1])
+
+
+@pytest.mark.parametrize("kind", ["spread", "ties", "near"])
+def test_many_lists(tiga, kind):
+    """More lists than the device has SMs: small blocks."""
+    check(tiga, make([1 + (i * 53) % 900 for i in range(90)], 2, 8, F16, 16, 16, 200, seed=15, kind=kind), 200, 30)
+
+
+def test_pages_beyond_32_bits(tiga):
+    """Pages whose elements lie behind the 2^31st."""
+    stride = (1 << 31) // 3 + 8 - ((1 << 31) // 3) % 8
+    raw = [torch.empty(4 * stride + 4096, dtype=BF16, device="cuda") for _ in range(2)]
+    pool = [torch.as_strided(t, (5, 16, 2, 64), (stride, 128, 64, 1)) for t in raw]
+    c = make([60], 2, 64, BF16, 16, 16, 20, seed=16)
+    for t, name in zip(pool, ("key", "value")):
+        t[1:].copy_(c[name][c["table"][0].long()].flip(0))
+    want = plain(c, 20, 5)
+    cache = tiga.PagedCache(*pool, torch.tensor([[4, 3, 2, 1]], dtype=torch.int32, device="cuda"), c["lens"])
+    to = tiga.PagedCache(c["to_key"], c["to_value"], c["to_table"], c["to_lens"])
+    kept, left = tiga.tiga_paged_evict(cache, to, c["weights"], 20, 5)
+    assert torch.equal(kept, want[2]) and torch.equal(c["to_key"].view(torch.int16), want[0]) and torch.equal(c["to_value"].view(torch.int16), want[1])

@@ -224,3 +224,34 @@ def test_on_another_stream_with_strided_queries(tiga):
     out, lse, _ = tiga.tiga_apply_shared_attention(cache, prefixes, wide[:, 1::2], start, c["scale"], stream=side)
     side.synchronize()
     assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
+def test_more_groups_and_sequences_than_the_plan_holds(tiga):
+    """Over a thousand groups of two, and a thousand sequences in one group."""
+    check(tiga, make([(128 + 16 * (i % 3), [(1, 1 + i % 5), (1, 2)]) for i in range(1100)], 8, 1, 32, F16, 16, seed=14))
+    check(tiga, make([(256, [(1, 1 + i % 7) for i in range(1100)])], 4, 2, 32, BF16, 16, seed=15))
+
+
+def test_lengths_beyond_the_table(tiga):
+    """Rows count their positions from the sequence's length, of which the table holds less."""
+    c = make([(512, [(1, 30), (2, 60), (1, 5), (1, 9)])], 4, 2, 64, F16, 16, seed=16)
+    c["table"] = c["table"][:, :33].contiguous()
+    c["lens"] = ints([600, 529, 700, 10 ** 9])
+    for name in ("key_pages", "value_pages"):           # (slots behind the sequences' tokens are NaN, and now some are read)
+        c[name] = torch.nan_to_num(c[name], nan=0.5)
+    out, lse = run(tiga, c)
+    cache = tiga.PagedCache(c["key_pages"], c["value_pages"], c["table"], c["lens"])
+    want, want_lse, _ = tiga.tiga_apply_paged_attention(cache, c["q"], starts(c["q_len"]), c["scale"])
+    # both are within 2 u + u^2 of sum |p v| (attention_reference.py); values here are below 6
+    assert float((out.double() - want.double()).abs().max()) <= 2 * 2.1 * 2.0 ** -11 * 6 and torch.allclose(lse, want_lse, rtol=0, atol=2e-5)
+
+
+def test_pages_beyond_32_bits(tiga):
+    c = make([(128, [(1, 30), (2, 17), (1, 5), (1, 9)])], 8, 2, 64, BF16, 16, seed=17)
+    n = c["key_pages"].shape[0]
+    stride = (1 << 31) // (n - 2) // 8 * 8 + 8
+    for name in ("key_pages", "value_pages"):
+        pool = torch.as_strided(torch.empty((n - 1) * stride + 4096, dtype=BF16, device="cuda"), (n, 16, 2, 64), (stride, 128, 64, 1))
+        pool.copy_(c[name])
+        c[name] = pool
+    check(tiga, c)

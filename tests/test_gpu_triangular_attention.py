@@ -272,3 +272,26 @@ def test_outputs_and_workspaces_on_any_boundary_of_16_bytes(tiga, D):
     tiga.tiga_apply_triangular_attention_backward(g, c["q"], c["k"], c["v"], out, lse, c["go"], c["scale"], *grads, ws=ws)
     for name, x in zip(("out", "lse", "grad_q", "grad_key", "grad_value"), (out, lse, *grads)):
         assert torch.equal(x, want[name]), name
+
+
+@pytest.mark.parametrize("lens", [[65], [300, 40]])
+def test_gradients_that_are_wanted(tiga, lens):
+    """Each gradient by itself is what it is beside the others."""
+    c = case(lens, lens, 4, 2, 64, F16, seed=28)
+    want = run(tiga, c)
+    g = tiga.TriangularRelation(starts(lens))
+    gq, none, no, _ = tiga.tiga_apply_triangular_attention_backward(g, c["q"], c["k"], c["v"], want["out"], want["lse"], c["go"], c["scale"], want_kv=False)
+    assert none is None and no is None and torch.equal(gq, want["grad_q"])
+    none, gk, gv, _ = tiga.tiga_apply_triangular_attention_backward(g, c["q"], c["k"], c["v"], want["out"], want["lse"], c["go"], c["scale"], want_q=False)
+    assert none is None and torch.equal(gk, want["grad_key"]) and torch.equal(gv, want["grad_value"])
+    only = torch.empty_like(c["k"])
+    tiga.tiga_apply_triangular_attention_backward(g, c["q"], c["k"], c["v"], want["out"], want["lse"], c["go"], c["scale"], grad_value=only, want_q=False, want_kv=False)
+    assert torch.equal(only, want["grad_value"])
+
+
+def test_mask_that_leaves_one_key_under_the_triangle(tiga):
+    c = case([20], [20], 2, 1, 64, BF16, seed=29)
+    c["mask"] = torch.zeros(20, dtype=torch.bool, device="cuda")
+    c["mask"][7] = True
+    got = check(tiga, c)
+    assert torch.all(got["out"][:7] == 0) and torch.all(got["grad_q"] == 0) and torch.all(got["grad_key"] == 0)
