@@ -1,6 +1,7 @@
 // Attention over dense and paged relations: what the kernels and the host share.
 #pragma once
 #include <cuda_bf16.h>
+#include <limits.h>
 #include <math.h>
 #include "common.cuh"
 
@@ -226,7 +227,7 @@ struct Cut {
     }
     // Steps of the first t tiles (t <= tiles()).  Under the triangle steps(k) is max(1, floor((x k + y) / z)), cut off at the segment's
     // keys or rows: a sum of floors in the middle.
-    static __host__ __device__ __forceinline__ long long steps_before(const AttnParams& p, const Segment& g, int t) {
+    static __host__ __device__ __noinline__ long long steps_before(const AttnParams& p, const Segment& g, int t) {
         if (t == 0) return 0;
         if (t == 1 || !p.causal) return (long long)t * steps(p, g, 0);
         const long long c = (long long)g.length - g.nq;
@@ -315,10 +316,15 @@ struct Walker {
     // false: nothing to do.
     __device__ __forceinline__ bool begin(const AttnParams& p, const long long* unit_start, int block, int grid) {
         const int lane = threadIdx.x % 32;
+        long long first = 0;            // of segment `lane`
         if (unit_start) units = unit_start[p.n_seg];
         else {
             units = 0;
-            for (int k = 0; k < p.n_seg; k += 32) units += k + lane < p.n_seg ? C::units(p, C::segment(p, k + lane)) * p.kv_heads : 0;
+            for (int k = 0; k < p.n_seg; k += 32) {
+                const long long n = k + lane < p.n_seg ? C::units(p, C::segment(p, k + lane)) * p.kv_heads : 0;
+                if (k == 0) first = n;
+                units += n;
+            }
             units = warp_total(units);
         }
         blocks = pieces(p, units, grid);
@@ -331,7 +337,7 @@ struct Walker {
             mine = unit_start[s + 1] - unit_start[s];
         } else {
             for (int k = 0;; k += 32) {
-                const long long n = k + lane < p.n_seg ? C::units(p, C::segment(p, k + lane)) * p.kv_heads : 0;
+                const long long n = k == 0 ? first : k + lane < p.n_seg ? C::units(p, C::segment(p, k + lane)) * p.kv_heads : 0;
                 const long long run = warp_running(n);
                 const unsigned beyond = __ballot_sync(~0u, run > off);
                 if (beyond) {
@@ -349,7 +355,7 @@ struct Walker {
         h = (int)quotient(off, per_head);
         off -= h * per_head;
         if (!p.causal) {
-            const long long n = C::before(p, g, 1);
+            const long long n = (long long)C::steps(p, g, 0) * C::step_cost(p, g) + C::item_cost(p);
             t = (int)quotient(off, n);
             off -= t * n;
         } else if (C::PLAIN) {
@@ -365,16 +371,26 @@ struct Walker {
                 }
                 off -= __shfl_sync(~0u, run, 31);
             }
-        } else {            // the last tile that begins at or before this unit, 32 places a round
-            int hi = C::tiles(p, g);
+        } else {            // the last tile that begins at or before this unit: 32 places a round, the last few tiles one by one
+            const int tiles = C::tiles(p, g);
+            int hi = tiles;
+            long long ahead = 0;            // units in front of tile t
             t = 0;
-            while (hi - t > 1) {
+            while (hi - t > 8) {
                 const int gap = (hi - t + 31) / 32, at = t + lane * gap;
-                const unsigned before = __ballot_sync(~0u, at < hi && C::before(p, g, at) <= off) | 1u;
-                t += (31 - __clz(before)) * gap;
+                const long long here = at < hi ? C::before(p, g, at) : LLONG_MAX;
+                const unsigned before = __ballot_sync(~0u, here <= off) | 1u;
+                const int last = 31 - __clz(before);
+                ahead = __shfl_sync(~0u, here, last);
+                t += last * gap;
                 hi = min(hi, t + gap);
             }
-            off -= C::before(p, g, t);
+            off -= ahead;
+            for (; t + 1 < hi; ++t) {
+                const long long n = (long long)C::steps(p, g, t) * C::step_cost(p, g) + C::item_cost(p);
+                if (off < n) break;
+                off -= n;
+            }
         }
         start = off;
         return open(p, off);
