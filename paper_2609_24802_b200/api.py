@@ -647,6 +647,11 @@ def _same(like, *arrays):
             raise ValueError("all arrays of a call must lie on one device")
 
 
+def _like(t):
+    """An array of the shape and type of t whose rows follow one another."""
+    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
+
+
 def _scratch(nbytes, like):
     return like.new_empty(nbytes if nbytes > 256 else 256, dtype=torch.uint8)
 
@@ -763,7 +768,7 @@ def _segments_forward(name, size, call, kind, g, q, key, value, scale, out, lse,
     with _on(q, stream):
         c, h = _dense_args(g, q, key, value, scale, None, kind)
         if out is None:
-            out = q.new_empty(q.shape)
+            out = _like(q)
         if want_lse and lse is None:
             lse = q.new_empty(q.shape[:2], dtype=torch.float32)
         _same(q, out, lse, ws)
@@ -778,11 +783,11 @@ def _segments_backward(name, size, call, kind, g, q, key, value, out, lse, grad_
     with _on(q, stream):
         c, h = _dense_args(g, q, key, value, scale, grad_out, kind)
         if want_q and grad_q is None:
-            grad_q = q.new_empty(q.shape)
+            grad_q = _like(q)
         if want_kv and grad_key is None:
-            grad_key = q.new_empty(key.shape)
+            grad_key = _like(key)
         if want_kv and grad_value is None:
-            grad_value = q.new_empty(key.shape)
+            grad_value = _like(key)
         _same(q, out, lse, grad_q, grad_key, grad_value, ws)
         if ws is None:
             ws = _scratch(size(ctypes.byref(c), ctypes.byref(h), 1), q)
@@ -839,20 +844,24 @@ class PagedCache(_Held):
     _held = ("key", "value", "table", "kv_len")
 
     def __init__(self, key, value, table, kv_len):
-        if key.dim() != 4 or key.shape != value.shape or key.dtype != value.dtype or key.dtype not in _HALF:
-            raise ValueError("key and value must be fp16 or bf16 arrays [n_pages, page_size, kv_heads, D] of one shape")
         shape, steps = key.shape, key.stride()
-        step = [s if n > 1 else 0 for s, n in zip(steps, shape)]                 # (the stride of a single entry means nothing)
-        if (steps != value.stride() and step != [s if n > 1 else 0 for s, n in zip(value.stride(), shape)]) or (step[3] != 1 and shape[3] > 1):
+        if len(shape) != 4 or shape != value.shape or key.dtype is not value.dtype or key.dtype not in _HALF:
+            raise ValueError("key and value must be fp16 or bf16 arrays [n_pages, page_size, kv_heads, D] of one shape")
+        n_pages, page_size, kv_heads, D = shape
+
+        def used(s):            # (the stride of a single entry means nothing)
+            return s[0] if n_pages > 1 else 0, s[1] if page_size > 1 else 0, s[2] if kv_heads > 1 else 0, s[3] if D > 1 else 1
+        step, of_value = used(steps), value.stride()
+        if (steps != of_value and step != used(of_value)) or step[3] != 1:
             raise ValueError("key and value must have the same strides and contiguous features")
         if table.dtype is not torch.int32 or table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
             raise ValueError("table must be an int32 array [n_seg, max_pages] with contiguous rows")
         n_seg, max_pages = table.shape
         _ints(kv_len, n_seg, "kv_len")
         _same(key, value, table, kv_len)
-        c = _PAGES_OF(_PAGES_BYTES.pack(key.data_ptr(), value.data_ptr(), table.data_ptr(), kv_len.data_ptr(), n_seg, shape[0], shape[1],
-                                        _step(table, 0), max_pages, step[0], step[1], step[2]))
-        self.__dict__.update(key=key, value=value, table=table, kv_len=kv_len, n_seg=n_seg, c=c, ref=ctypes.byref(c))
+        c = _PAGES_OF(_PAGES_BYTES.pack(key.data_ptr(), value.data_ptr(), table.data_ptr(), kv_len.data_ptr(), n_seg, n_pages, page_size,
+                                        table.stride(0) if n_seg > 1 else 0, max_pages, step[0], step[1], step[2]))
+        self.__dict__.update(key=key, value=value, table=table, kv_len=kv_len, n_seg=n_seg, kv_heads=kv_heads, c=c, ref=ctypes.byref(c))
 
 
 def _paged_heads(cache, q, scale):
@@ -874,7 +883,7 @@ def tiga_apply_paged_attention(cache: PagedCache, q, q_start, scale: float, caus
         _same(q, q_start, out, lse, ws)
         start = _ints(q_start, cache.n_seg + 1, "q_start")
         if out is None:
-            out = q.new_empty(q.shape)
+            out = _like(q)
         if want_lse and lse is None:
             lse = q.new_empty(q.shape[:2], dtype=torch.float32)
         if ws is None:
@@ -912,7 +921,7 @@ def tiga_apply_shared_attention(cache: PagedCache, prefixes: SharedPrefixes, q, 
         _same(q, q_start, prefixes.shared, out, lse, ws)
         start = _ints(q_start, cache.n_seg + 1, "q_start")
         if out is None:
-            out = q.new_empty(q.shape)
+            out = _like(q)
         if want_lse and lse is None:
             lse = q.new_empty(q.shape[:2], dtype=torch.float32)
         if ws is None:
@@ -925,10 +934,15 @@ def tiga_apply_shared_attention(cache: PagedCache, prefixes: SharedPrefixes, q, 
 
 
 def _weights_of(t, cache, name):
-    if t.dtype is not torch.float32 or t.dim() != 3 or t.shape[:2] != (cache.n_seg, cache.key.shape[2]) or (t.shape[2] > 1 and t.stride(2) != 1):
-        raise ValueError(f"{name} must be an fp32 array [n_seg, kv_heads, positions] whose positions are contiguous")
-    _same(t, cache.key)
-    return ctypes.byref(_WEIGHTS_OF(_WEIGHTS_BYTES.pack(t.data_ptr(), _step(t, 0), _step(t, 1), t.shape[2])))
+    shape = t.shape
+    if t.dtype is not torch.float32 or len(shape) != 3 or shape[0] != cache.n_seg or shape[1] != cache.kv_heads:
+        raise ValueError(f"{name} must be an fp32 array [n_seg, kv_heads, positions]")
+    seg, head, one = t.stride()
+    if one != 1 and shape[2] > 1:
+        raise ValueError(f"the positions of {name} must be contiguous")
+    if t.get_device() != cache.key.get_device():
+        raise ValueError("all arrays of a call must lie on one device")
+    return ctypes.byref(_WEIGHTS_OF(_WEIGHTS_BYTES.pack(t.data_ptr(), seg if shape[0] > 1 else 0, head if shape[1] > 1 else 0, shape[2])))
 
 
 def tiga_paged_weights_workspace_bytes(cache: PagedCache, q) -> int:
@@ -944,7 +958,7 @@ def tiga_paged_attention_weights(cache: PagedCache, q, q_start, lse, scale: floa
         h = _paged_heads(cache, q, scale)
         start = _ints(q_start, cache.n_seg + 1, "q_start")
         if weights is None:
-            like = (cache.n_seg, cache.key.shape[2], cache.table.shape[1] * cache.key.shape[1] if before is None else before.shape[2])
+            like = (cache.n_seg, cache.kv_heads, cache.table.shape[1] * cache.key.shape[1] if before is None else before.shape[2])
             weights = q.new_zeros(like, dtype=torch.float32)
         b, o = None if before is None else _weights_of(before, cache, "before"), _weights_of(weights, cache, "weights")
         _same(q, q_start, lse, ws)
@@ -962,7 +976,7 @@ def tiga_paged_evict(cache: PagedCache, to: PagedCache, weights, keep: int, rece
     `to`]: their weights, zeros behind them, or None)."""
     with _on(cache.key, stream):
         _, _, kv_heads, D = cache.key.shape
-        if to.key.dtype is not cache.key.dtype or to.key.shape[2:] != cache.key.shape[2:] or to.n_seg != cache.n_seg:
+        if to.key.dtype is not cache.key.dtype or to.kv_heads != kv_heads or to.key.shape[3] != D or to.n_seg != cache.n_seg:
             raise ValueError("both caches must have one storage type, number of sequences and heads, and width")
         _same(cache.key, to.key, kept)
         if kept is None:
