@@ -35,7 +35,7 @@ template <int DP> struct Fwd {
 struct FwdControl {
     unsigned long long full[10], empty[10], q_full, q_empty, s_full[2], p_full[2], o_full[2], mask_full[MASK_RING], drain;
     ItemRing items;
-    alignas(8) unsigned char walk[sizeof(Walker<FwdCut<CUT_LINE>>)];      // a Walker of the kernel's cut
+    alignas(8) unsigned char walk[sizeof(Walker<FwdCut<CUT_COSTS>>)];      // a Walker of the kernel's cut
     uint32_t tmem, abort_word, mask[MASK_RING][4];
     float share[2][2][128];             // what a row's threads tell each other
 };
@@ -53,6 +53,7 @@ struct FwdWork {
     const int32_t* line_row;        // [n_groups + n_seq]: the row of the page table that a segment of the line reads
     const long long* line_state;    // [n_groups + n_seq]: what is added to a row's number for its place among the states
     const int32_t* first_member;    // [n_groups]
+    const Walker<SharedCut>* walks; // [grid]: where the blocks' pieces of the line begin
     const long long* state_start;   // [n_groups + 1]: rows of the groups in front that share
     float2* state_ml;               // [2][state_rows][heads]: as part_ml, of the shared and of the own keys
     float* state_o;                 // [2][state_rows][heads][DP]
@@ -91,8 +92,8 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     Walk walk;
-    if (MODE != CUT_STEPS) { if (warp == FWD_WALKER) walk_begin(reinterpret_cast<Walk*>(ctl.walk), p, w.unit_start, blockIdx.x, gridDim.x); }
-    else {
+    if (MODE == CUT_COSTS) { if (warp == FWD_WALKER) walk_begin(reinterpret_cast<Walk*>(ctl.walk), p, w.unit_start, blockIdx.x, gridDim.x); }
+    else if (MODE == CUT_STEPS) {
         walk.here = false;
         if (warp == FWD_WALKER) walk.here = walk.begin(p, w.unit_start, blockIdx.x, gridDim.x);
     }
@@ -105,7 +106,8 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
 
     if (warp == FWD_WALKER) {
         if (lane == 0) {
-            if (MODE != CUT_STEPS) walk = *reinterpret_cast<Walk*>(ctl.walk);
+            if (MODE == CUT_COSTS) walk = *reinterpret_cast<Walk*>(ctl.walk);
+            if constexpr (SHARED) walk = w.walks[blockIdx.x];
             w.joints[blockIdx.x] = joint_of(p, walk, walk.here && (!SHARED || only_state(w, walk.s, walk.g.k0)), blockIdx.x);
             items_hand_out(ctl.items, p, walk, walk.here);
         }
@@ -592,15 +594,16 @@ struct SharedPlan {
     Segment* line;
     int32_t *line_row, *first_member;
     long long *line_state, *state_start, *unit_start;
+    Walker<SharedCut>* walks;
 };
 
 // One block: a warp for each group, a thread for each sequence, then the units.  What is looked up again and again lies in shared memory where
 // it fits: this kernel is a chain of latencies in front of everything else.
-constexpr int PLAN_HELD = 1024;
-static __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(AttnParams p, Prefixes x, const SharedPlan plan, const long long state_rows) {
+constexpr int PLAN_HELD = 768;
+static __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(AttnParams p, Prefixes x, const SharedPlan plan, const long long state_rows, const int sms) {
     __shared__ int32_t rows[PLAN_HELD], lengths[PLAN_HELD], members[PLAN_HELD], said[PLAN_HELD];
     __shared__ Segment held[PLAN_HELD];             // of the groups, and what is added to their rows' numbers
-    __shared__ long long held_state[PLAN_HELD];
+    __shared__ long long held_state[PLAN_HELD], held_units[PLAN_HELD];
     __shared__ long long totals[PLAN_THREADS / 32];
     wait_for_previous_kernel();
     let_next_kernel_start();
@@ -657,6 +660,7 @@ static __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(AttnPa
     __syncthreads();
     // the line, and its units
     const int n_line = x.n_groups + n_seq;
+    long long* units = n_line < PLAN_HELD ? held_units : plan.unit_start;
     long long before = 0;
     for (int i0 = 0; i0 < n_line; i0 += PLAN_THREADS) {
         const int i = i0 + (int)threadIdx.x, s = i - x.n_groups;
@@ -699,10 +703,15 @@ static __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(AttnPa
             if (k < warp) sum += totals[k];
             before += totals[k];
         }
-        if (i < n_line) plan.unit_start[i + 1] = sum;
+        if (i < n_line) plan.unit_start[i + 1] = units[i + 1] = sum;
         __syncthreads();
     }
-    if (threadIdx.x == 0) plan.unit_start[0] = 0;
+    if (threadIdx.x == 0) plan.unit_start[0] = units[0] = 0;
+    __syncthreads();
+    // where the blocks begin: each for itself would look at all of this again, one latency after the other (7 us at the start of the main kernel)
+    p.line = plan.line;
+    p.n_seg = n_line;
+    if ((int)threadIdx.x < sms) plan.walks[threadIdx.x].begin_alone(p, units, threadIdx.x, sms);
 }
 
 // Joins the two states of every row that has two (the first blocks): a warp has one head of a row.  A state lies among the states
@@ -803,6 +812,7 @@ static size_t shared_carve(const AttnParams& p, int n_groups, void* ws, FwdWork*
     plan->line_state = cv.take<long long>(line);
     plan->first_member = cv.take<int32_t>(n_groups);
     plan->state_start = cv.take<long long>((size_t)n_groups + 1);
+    w->walks = plan->walks = cv.take<Walker<SharedCut>>(MAX_SMS);
     w->line_row = plan->line_row;
     w->line_state = plan->line_state;
     w->first_member = plan->first_member;
@@ -825,7 +835,7 @@ static tiga_status launch_shared(AttnParams p, const Prefixes& g, const FwdWork&
     TIGA_CUDA_TRY(cudaFuncSetAttribute(attention_forward_kernel<T, DP, CUT_LINE>, cudaFuncAttributeMaxDynamicSharedMemorySize, Fwd<DP>::SMEM));
     p.item_cost = SHARED_ITEM_COST;
     p.uneven = 1;
-    shared_plan_kernel<<<counted(1), PLAN_THREADS, 0, s>>>(p, g, plan, w.state_rows);
+    shared_plan_kernel<<<counted(1), PLAN_THREADS, 0, s>>>(p, g, plan, w.state_rows, sms);
     p.line = plan.line;
     p.n_seg = w.n_groups + w.n_seq;
     TIGA_CUDA_TRY(launch_after(attention_forward_kernel<T, DP, CUT_LINE>, dim3(sms), FWD_THREADS, Fwd<DP>::SMEM, s, p, w, maps));

@@ -395,6 +395,30 @@ struct Walker {
         start = off;
         return open(p, off);
     }
+    // The same by a thread alone, for a plan that does it for all blocks.
+    __device__ __forceinline__ void begin_alone(const AttnParams& p, const long long* unit_start, int block, int grid) {
+        auto last = [](int n, auto at_most) {               // the last of n places that is not beyond; place 0 is not
+            int lo = 0, hi = n;
+            while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (at_most(mid)) lo = mid; else hi = mid; }
+            return lo;
+        };
+        units = unit_start[p.n_seg];
+        blocks = pieces(p, units, grid);
+        here = false;
+        if (block >= blocks || units == 0) return;
+        long long off = first_unit(block);
+        left = first_unit(block + 1) - off;
+        s = last(p.n_seg, [&](int k) { return unit_start[k] <= off; });
+        off -= unit_start[s];
+        g = C::segment(p, s);
+        const long long per_head = quotient(unit_start[s + 1] - unit_start[s], p.kv_heads);
+        h = (int)quotient(off, per_head);
+        off -= h * per_head;
+        t = last(C::tiles(p, g), [&](int k) { return C::before(p, g, k) <= off; });
+        off -= C::before(p, g, t);
+        start = off;
+        here = open(p, off);
+    }
     __device__ __forceinline__ bool next(const AttnParams& p) {
         if (left <= 0) return false;
         if (++t >= C::tiles(p, g)) {
