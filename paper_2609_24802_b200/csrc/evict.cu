@@ -11,8 +11,9 @@ namespace tiga {
 // far, added up from the top.  Then every warp, whose positions follow one another, knows from the warps in front how many it puts where.
 // A list has one block, or a cluster of SELECT_CLUSTER that share its positions and read one another's counts.  What bounds it: many lists, the
 // instructions of five passes over numbers in shared memory; few lists, the steps one after the other.  So many lists have small blocks, of which
-// an SM holds several (512 lists of up to 8192: 62 us with 1024 threads each and the same passes, here 27).
+// an SM holds several (512 lists of up to 8192: 46 us with 1024 threads each, 34 with 256).
 constexpr int SELECT_MANY = 256, SELECT_FEW = 1024, SELECT_BINS = 2048, SELECT_CLUSTER = 8;            // threads
+constexpr int SELECT_AT_ONCE = 8;               // positions that a lane loads together
 constexpr int SELECT_HELD = 40960;              // numbers that a block's shared memory holds
 
 struct EvictParams {
@@ -108,12 +109,11 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_select_kernel(c
     const bool held = end - begin <= p.held;
     const float* weights = p.weights + s * p.w_seg + h * p.w_head;
     const uint32_t page_size = (uint32_t)p.page_size;
-    auto fresh = [&](int j) -> uint32_t {
-        const float w = j < weighed ? weights[j] : 0.f;
-        const int page = page_of(p.table, p.table_stride, s, (uint32_t)j / page_size, p.n_pages);
-        return page < 0 ? 0 : j >= recent ? LAST_POSITION : rank_of(w);
-    };
-    auto number = [&](int j) { return held ? numbers[j - begin] : fresh(j); };
+    const int32_t* table = p.table + s * p.table_stride;
+    auto weight_of = [&](int j) { return j < min(weighed, w1) ? __ldg(weights + j) : 0.f; };
+    auto id_of = [&](int j, uint32_t page) { return j < w1 ? __ldg(table + page) : -1; };
+    auto number_of = [&](int j, float w, int id) -> uint32_t { return id < 0 || id >= p.n_pages ? 0 : j >= recent ? LAST_POSITION : rank_of(w); };
+    auto number = [&](int j) { return held ? numbers[j - begin] : number_of(j, weight_of(j), id_of(j, (uint32_t)j / page_size)); };
     auto meet = [&]() { if (CLUSTER > 1) cg::this_cluster().sync(); else __syncthreads(); };
     auto of_block = [&](uint32_t* a, int b) { return CLUSTER > 1 ? cg::this_cluster().map_shared_rank(a, b) : a; };
 
@@ -121,13 +121,31 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_select_kernel(c
     for (int k = threadIdx.x; k < SELECT_BINS; k += THREADS) bins[k] = 0;
     __syncthreads();
     uint32_t there = 0, last = 0;
-#pragma unroll 4
-    for (int j = w0 + lane; j < w1; j += 32) {
-        const uint32_t v = fresh(j);
-        if (held) numbers[j - begin] = v;
-        there += v != 0;
-        if (v == LAST_POSITION) ++last;
-        else if (v) atomicAdd(&bins[v >> 21], 1u);
+    // (a lane's loads stand in front of its stores, for which they would wait: these lists 44 us instead of 36, the pass at the end included)
+    const uint32_t pages_on = 32 / page_size, slots_on = 32 % page_size;            // 32 positions on (with a division for each 2 us more)
+    uint32_t page = (uint32_t)(w0 + lane) / page_size, slot = (uint32_t)(w0 + lane) % page_size;
+    for (int j0 = w0; j0 < w1; j0 += 32 * SELECT_AT_ONCE) {
+        float w[SELECT_AT_ONCE];
+        int id[SELECT_AT_ONCE];
+#pragma unroll
+        for (int u = 0; u < SELECT_AT_ONCE; ++u) {
+            const int j = j0 + 32 * u + lane;
+            w[u] = weight_of(j);
+            id[u] = id_of(j, page);
+            page += pages_on;
+            slot += slots_on;
+            if (slot >= page_size) { slot -= page_size; ++page; }
+        }
+#pragma unroll
+        for (int u = 0; u < SELECT_AT_ONCE; ++u) {
+            const int j = j0 + 32 * u + lane;
+            if (j >= w1) break;
+            const uint32_t v = number_of(j, w[u], id[u]);
+            if (held) numbers[j - begin] = v;
+            there += v != 0;
+            if (v == LAST_POSITION) ++last;
+            else if (v) atomicAdd(&bins[v >> 21], 1u);
+        }
     }
     there = __reduce_add_sync(~0u, there);
     last = __reduce_add_sync(~0u, last);
@@ -220,19 +238,25 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_select_kernel(c
     }
     int32_t* kept = p.kept + (long long)list * p.keep;
     float* to = p.to_weights ? p.to_weights + s * p.o_seg + h * p.o_head : nullptr;
-#pragma unroll 2
-    for (int j0 = w0; j0 < w1; j0 += 32) {
-        const int j = j0 + lane;
-        const uint32_t v = j < w1 ? number(j) : 0;
-        const uint32_t over = __ballot_sync(~0u, v > border), same = __ballot_sync(~0u, v == border && v != 0), behind = (1u << lane) - 1;
-        const uint32_t before_equal = ahead_equal + __popc(same & behind);
-        const uint32_t at = ahead_above + __popc(over & behind) + min(before_equal, wanted);
-        if (v > border || (v == border && v != 0 && before_equal < wanted)) {
-            kept[at] = j;
-            if (to && at < p.o_length) to[at] = j < weighed ? weights[j] : 0.f;
+    for (int j0 = w0; j0 < w1; j0 += 32 * SELECT_AT_ONCE) {
+        float w[SELECT_AT_ONCE];
+        if (to)
+#pragma unroll
+            for (int u = 0; u < SELECT_AT_ONCE; ++u) w[u] = weight_of(j0 + 32 * u + lane);
+#pragma unroll
+        for (int u = 0; u < SELECT_AT_ONCE; ++u) {
+            const int j = j0 + 32 * u + lane;
+            const uint32_t v = j < w1 ? number(j) : 0;
+            const uint32_t over = __ballot_sync(~0u, v > border), same = __ballot_sync(~0u, v == border && v != 0), behind = (1u << lane) - 1;
+            const uint32_t before_equal = ahead_equal + __popc(same & behind);
+            const uint32_t at = ahead_above + __popc(over & behind) + min(before_equal, wanted);
+            if (v > border || (v == border && v != 0 && before_equal < wanted)) {
+                kept[at] = j;
+                if (to && at < p.o_length) to[at] = w[u];
+            }
+            ahead_above += __popc(over);
+            ahead_equal += __popc(same);
         }
-        ahead_above += __popc(over);
-        ahead_equal += __popc(same);
     }
     const long long thread = (long long)part * THREADS + threadIdx.x;
     for (long long k = stay + thread; k < p.keep; k += CLUSTER * THREADS) kept[k] = -1;
