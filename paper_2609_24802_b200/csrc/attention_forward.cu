@@ -715,9 +715,12 @@ static __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(AttnPa
 }
 
 // Joins the two states of every row that has two (the first blocks): a warp has one head of a row.  A state lies among the states
-// where one block had its tile, else in as many parts; the parts of both are looked up at once.  The last blocks join the tiles of rows with one state that several blocks shared, as above.
-// (With 16 slices of each of these, which mostly have nothing to do, the kernel took 25 us whatever the size: eight rounds of blocks.)
-constexpr int SHARED_JOIN_SLICES = 4, SHARED_JOIN_BLOCKS = 3;           // ... and blocks of an SM
+// where one block had its tile, else in as many parts; the parts of both are looked up at once.  Whose tile it is and which blocks had it takes
+// a few dozen divisions: a block has up to SHARED_JOIN_TASKS heads of rows one behind the other, for each of whose states a thread finds out
+// (when each warp did for its own, 6 groups of 8 samples of 5 tokens, 32 heads, took 20 us instead of 14).  The last blocks join the tiles of
+// rows with one state that several blocks shared, as above.  (With 16 slices of each of these, which mostly have nothing to do, the kernel took
+// 25 us whatever the size: eight rounds of blocks.)
+constexpr int SHARED_JOIN_SLICES = 4, SHARED_JOIN_BLOCKS = 3, SHARED_JOIN_TASKS = 32;           // ... and blocks of an SM
 template <typename T, int DP>
 __global__ void __launch_bounds__(JOIN_WARPS * 32, SHARED_JOIN_BLOCKS) shared_join_kernel(const AttnParams p, const FwdWork w, const int sms) {
     wait_for_previous_kernel();
@@ -727,74 +730,96 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32, SHARED_JOIN_BLOCKS) shared_jo
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const long long units = w.unit_start[p.n_seg], blocks = Walker<SharedCut>::pieces(p, units, sms);
     auto block_of = [&](long long unit) { return (int)quotient((unit + 1) * blocks - 1, units); };
-    const long long tasks = w.state_start[w.n_groups] * p.heads, stride = (long long)state_blocks * JOIN_WARPS;
-    for (long long task = (long long)blockIdx.x * JOIN_WARPS + warp; task < tasks; task += stride) {
-        const long long at = quotient(task, p.heads);
-        const int head = (int)(task - at * p.heads), h = head / p.group, g = last_place(w.state_start, w.n_groups, at);
-        const Segment shared = p.line[g];
-        const long long row_ll = at - w.line_state[g];
-        if (shared.nq == 0 || row_ll < shared.q0 || row_ll >= (long long)shared.q0 + shared.nq) continue;
-        const int row = (int)row_ll;
-        const int a = w.first_member[g], s = a + last_place(p.q_start + a, w.n_seq - a, row);
-        const Segment own = p.line[w.n_groups + s];
-        if (own.k0 == 0) continue;
-        int first0, first1, parts0, parts1, r0, r1;
-        auto find = [&](const Segment& seg, int line, int& first, int& parts, int& r) {
-            const int packed = (row - seg.q0) * p.group + head % p.group, t = packed / FWD_ROWS, cost = SharedCut::step_cost(p, seg);
-            const long long start = w.unit_start[line] + h * SharedCut::units(p, seg) + SharedCut::before(p, seg, t) + p.item_cost - 1;
-            r = packed % FWD_ROWS;
-            first = block_of(start + cost);                 // the blocks that have the last unit of the tile's first and last step
-            parts = block_of(start + (long long)cost * SharedCut::steps(p, seg, t)) - first + 1;
-        };
-        find(shared, g, first0, parts0, r0);
-        find(own, w.n_groups + s, first1, parts1, r1);
-        // part k of both: where its maximum and mass lie, and (times DP) its accumulator
-        auto place = [&](int k, const float2*& ml, const float*& o) -> long long {
-            const bool kind = k >= parts0, whole = (kind ? parts1 : parts0) == 1;
-            const int of = kind ? k - parts0 : k;
-            ml = whole ? w.state_ml : w.part_ml;
-            o = whole ? w.state_o : w.part_o;
-            return whole ? ((kind ? w.state_rows : 0) + at) * p.heads + head : (2LL * ((kind ? first1 : first0) + of) + (of == 0)) * w.rows + (kind ? r1 : r0);
-        };
-        const int n = parts0 + parts1;
-        float top = -INFINITY, mass = 0.f, o[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = 0.f;
-        for (int k0 = 0; k0 < n; k0 += 32) {
-            const int here = min(32, n - k0);
-            const float2* from_ml;
-            const float* from_o;
-            float2 ml = make_float2(-INFINITY, 0.f);
-            if (k0 + lane < n) {
-                const long long i = place(k0 + lane, from_ml, from_o);
-                ml = from_ml[i];
+    struct TwoStates { int row, g, s; };                    // a row, its group (-1: it has no two states) and sequence
+    struct Parts { int first, parts, r; };                  // where a state lies
+    __shared__ TwoStates rows[SHARED_JOIN_TASKS];
+    __shared__ Parts found[SHARED_JOIN_TASKS][2];
+    const long long tasks = w.state_start[w.n_groups] * p.heads, round = (long long)SHARED_JOIN_BLOCKS * sms * JOIN_WARPS;
+    const int each = JOIN_WARPS * (int)min(quotient(tasks + round - 1, round), (long long)(SHARED_JOIN_TASKS / JOIN_WARPS));        // few: a block for every eight
+    for (long long base = (long long)blockIdx.x * each; base < tasks; base += (long long)state_blocks * each) {
+        const int n_tasks = (int)min((long long)each, tasks - base);
+        const long long at0 = quotient(base, p.heads);
+        const int head0 = (int)(base - at0 * p.heads);
+        __syncthreads();
+        for (int k = warp; k <= (head0 + n_tasks - 1) / p.heads; k += JOIN_WARPS) {
+            const int g = last_place(w.state_start, w.n_groups, at0 + k);
+            const Segment shared = p.line[g];
+            const long long row = at0 + k - w.line_state[g];
+            TwoStates two = {0, -1, 0};
+            if (shared.nq != 0 && row >= shared.q0 && row < (long long)shared.q0 + shared.nq) {
+                const int a = w.first_member[g], s = a + last_place(p.q_start + a, w.n_seq - a, (int)row);
+                if (p.line[w.n_groups + s].k0 != 0) two = {(int)row, g, s};
             }
-            float most = ml.x != ml.x ? INFINITY : ml.x;
-#pragma unroll
-            for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(~0u, most, d));
-            most = fmaxf(most, top);
-            const float fade = top == -INFINITY ? 0.f : ex2(top - most), f = ml.x == -INFINITY ? 0.f : ex2(ml.x - most);
-            float sum = f * ml.y;
-#pragma unroll
-            for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
-            mass = mass * fade + sum;
-#pragma unroll
-            for (int e = 0; e < E; ++e) o[e] *= fade;
-            top = most;
-#pragma unroll 4
-            for (int k = 0; k < here; ++k) {
-                const float fk = __shfl_sync(~0u, f, k);
-                const long long i = place(k0 + k, from_ml, from_o);
-#pragma unroll
-                for (int e = 0; e < E; ++e) o[e] += fk * from_o[i * DP + lane + 32 * e];
+            if (lane == 0) rows[k] = two;
+        }
+        __syncthreads();
+        if ((int)threadIdx.x < 2 * n_tasks) {
+            const int k = threadIdx.x / 2, kind = threadIdx.x % 2, head = (head0 + k) % p.heads;
+            const TwoStates two = rows[(head0 + k) / p.heads];
+            if (two.g >= 0) {
+                const int line = kind ? w.n_groups + two.s : two.g;
+                const Segment seg = p.line[line];
+                const int packed = (two.row - seg.q0) * p.group + head % p.group, t = packed / FWD_ROWS, cost = SharedCut::step_cost(p, seg);
+                const long long start = w.unit_start[line] + head / p.group * SharedCut::units(p, seg) + SharedCut::before(p, seg, t) + p.item_cost - 1;
+                const int first = block_of(start + cost);               // the blocks that have the last unit of the tile's first and last step
+                found[k][kind] = {first, block_of(start + (long long)cost * SharedCut::steps(p, seg, t)) - first + 1, packed % FWD_ROWS};
             }
         }
-        const long long out_row = (long long)row * p.heads + head;
-        const float finish = mass > 0.f || mass != mass ? 1.f / mass : 0.f;
+        __syncthreads();
+        for (int task = warp; task < n_tasks; task += JOIN_WARPS) {
+            const int head = (head0 + task) % p.heads, ahead = (head0 + task) / p.heads, row = rows[ahead].row;
+            if (rows[ahead].g < 0) continue;
+            const long long at = at0 + ahead;
+            const int first0 = found[task][0].first, parts0 = found[task][0].parts, r0 = found[task][0].r;
+            const int first1 = found[task][1].first, parts1 = found[task][1].parts, r1 = found[task][1].r;
+            // part k of both: where its maximum and mass lie, and (times DP) its accumulator
+            auto place = [&](int k, const float2*& ml, const float*& o) -> long long {
+                const bool kind = k >= parts0, whole = (kind ? parts1 : parts0) == 1;
+                const int of = kind ? k - parts0 : k;
+                ml = whole ? w.state_ml : w.part_ml;
+                o = whole ? w.state_o : w.part_o;
+                return whole ? ((kind ? w.state_rows : 0) + at) * p.heads + head : (2LL * ((kind ? first1 : first0) + of) + (of == 0)) * w.rows + (kind ? r1 : r0);
+            };
+            const int n = parts0 + parts1;
+            float top = -INFINITY, mass = 0.f, o[E];
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (lane + 32 * e < p.D) ((T*)p.out)[out_row * p.D + lane + 32 * e] = Half<T>::from(finish == 0.f ? 0.f : o[e] * finish);
-        if (lane == 0 && p.lse) p.lse[out_row] = mass == 0.f ? -INFINITY : (top + log2f(mass)) * LN2_F;
+            for (int e = 0; e < E; ++e) o[e] = 0.f;
+            for (int k0 = 0; k0 < n; k0 += 32) {
+                const int here = min(32, n - k0);
+                const float2* from_ml;
+                const float* from_o;
+                float2 ml = make_float2(-INFINITY, 0.f);
+                if (k0 + lane < n) {
+                    const long long i = place(k0 + lane, from_ml, from_o);
+                    ml = from_ml[i];
+                }
+                float most = ml.x != ml.x ? INFINITY : ml.x;
+#pragma unroll
+                for (int d = 16; d; d >>= 1) most = fmaxf(most, __shfl_xor_sync(~0u, most, d));
+                most = fmaxf(most, top);
+                const float fade = top == -INFINITY ? 0.f : ex2(top - most), f = ml.x == -INFINITY ? 0.f : ex2(ml.x - most);
+                float sum = f * ml.y;
+#pragma unroll
+                for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
+                mass = mass * fade + sum;
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[e] *= fade;
+                top = most;
+#pragma unroll 4
+                for (int k = 0; k < here; ++k) {
+                    const float fk = __shfl_sync(~0u, f, k);
+                    const long long i = place(k0 + k, from_ml, from_o);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) o[e] += fk * from_o[i * DP + lane + 32 * e];
+                }
+            }
+            const long long out_row = (long long)row * p.heads + head;
+            const float finish = mass > 0.f || mass != mass ? 1.f / mass : 0.f;
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (lane + 32 * e < p.D) ((T*)p.out)[out_row * p.D + lane + 32 * e] = Half<T>::from(finish == 0.f ? 0.f : o[e] * finish);
+            if (lane == 0 && p.lse) p.lse[out_row] = mass == 0.f ? -INFINITY : (top + log2f(mass)) * LN2_F;
+        }
     }
 }
 
@@ -839,7 +864,7 @@ static tiga_status launch_shared(AttnParams p, const Prefixes& g, const FwdWork&
     p.line = plan.line;
     p.n_seg = w.n_groups + w.n_seq;
     TIGA_CUDA_TRY(launch_after(attention_forward_kernel<T, DP, CUT_LINE>, dim3(sms), FWD_THREADS, Fwd<DP>::SMEM, s, p, w, maps));
-    const long long warps = w.state_rows * p.heads, blocks = (warps + JOIN_WARPS - 1) / JOIN_WARPS, most = 8LL * sms;
+    const long long warps = w.state_rows * p.heads, blocks = (warps + JOIN_WARPS - 1) / JOIN_WARPS, most = (long long)SHARED_JOIN_BLOCKS * sms;
     TIGA_CUDA_TRY(launch_after(shared_join_kernel<T, DP>, dim3((unsigned)(sms * SHARED_JOIN_SLICES + (blocks < most ? blocks : most))), JOIN_WARPS * 32, 0, s, p, w, sms));
     return launch_status();
 }
