@@ -497,7 +497,7 @@ tiga_status tiga_paged_attention_weights(const tiga_pages* c, const tiga_heads* 
  *     to->key, to->value   the kept rows (places of which the table of `to` names no page are not written)
  *     to_len[s]            how many they are (device, int32 [n_seg]; may be to->kv_len, which is not read; not from->kv_len)
  *     kept                 device, int32 [n_seg, kv_heads, keep]: their positions, -1 behind them
- *     to_weights           their weights, zeros behind them (a new token's count begins there); NULL: not wanted
+ *     to_weights           their weights, zeros behind them (a new token's count begins there), apart from weights; NULL: not wanted
  * Keys keep the rotation of their positions: the next token is rotated by its own position (tiga_apply_rotary) and appended without
  * one.  Pages that are written must be apart from those that sequences of `from` name, and belong to one sequence alone; both caches
  * may lie in the same arrays.

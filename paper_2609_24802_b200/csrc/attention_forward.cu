@@ -129,7 +129,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_forward_kernel(const
                 return j >= g.nk ? Place{-1, 0} : SHARED ? shared_place(p, g, row, j) : key_place(p, g, row, j);
             };
             Place at = place(i0);
-                        for (int i = i0; i < i1 && ok; ++i, ++steps) {
+            for (int i = i0; i < i1 && ok; ++i, ++steps) {
                 const Place here = at;
                 const uint32_t valid = __ballot_sync(~0u, here.at >= 0);
                 if (lane == 0) {
@@ -748,7 +748,8 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32, SHARED_JOIN_BLOCKS) shared_jo
             TwoStates two = {0, -1, 0};
             if (shared.nq != 0 && row >= shared.q0 && row < (long long)shared.q0 + shared.nq) {
                 const int a = w.first_member[g], s = a + last_place(p.q_start + a, w.n_seq - a, (int)row);
-                if (p.line[w.n_groups + s].k0 != 0) two = {(int)row, g, s};
+                const Segment own = p.line[w.n_groups + s];
+                if (own.k0 != 0 && row >= own.q0 && row < (long long)own.q0 + own.nq) two = {(int)row, g, s};
             }
             if (lane == 0) rows[k] = two;
         }

@@ -191,6 +191,16 @@ def test_many_lists(tiga, kind):
     check(tiga, make([1 + (i * 53) % 900 for i in range(90)], 2, 8, F16, 16, 16, 200, seed=15, kind=kind), 200, 30)
 
 
+@pytest.mark.parametrize("page", [1, 3, 5, 24, 31, 33, 63, 65, 100])
+def test_page_sizes(tiga, page):
+    """Pages of odd sizes, some of them missing: every position is looked up in its own page, whatever the sizes of the steps along a list."""
+    for seed, lens in ((17, [1200, 40, 0, 333]), (18, [9000])):             # a block a list, a cluster
+        c = make(lens, 2, 8, F16, page, 16, 250, seed=seed)
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        c["table"][torch.rand(c["table"].shape, generator=g, device="cuda") < 0.3] = -1
+        check(tiga, c, 250, 40)
+
+
 def test_pages_beyond_32_bits(tiga):
     """Pages whose elements lie behind the 2^31st."""
     stride = (1 << 31) // 3 + 8 - ((1 << 31) // 3) % 8
