@@ -457,7 +457,8 @@ tiga_status tiga_apply_paged_attention(const tiga_pages* c, const tiga_heads* h,
                                        int causal, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
 
 /* Sequences whose caches begin alike: the sequences [group_start[g], group_start[g+1]) of group g find their positions [0, shared[g]) in
- * the same pages (those that the table names for the group's first sequence are read).  Sequences in no group share nothing. */
+ * the same pages (those that the table names for the group's first sequence with new tokens are read; of sequences without any neither
+ * the length nor the row of the table matters).  Sequences in no group share nothing. */
 typedef struct {
     const int32_t* group_start; /* device, int32 [n_groups + 1], ascending numbers of sequences */
     const int32_t* shared;      /* device, int32 [n_groups] */

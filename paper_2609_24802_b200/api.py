@@ -896,8 +896,8 @@ def tiga_apply_paged_attention(cache: PagedCache, q, q_start, scale: float, caus
 
 
 class SharedPrefixes(_Held):
-    """Sequences whose caches begin with the same pages: those of group g, [group_start[g], group_start[g+1]), share their positions
-    [0, shared[g]); group_start int32 [n_groups + 1], shared int32 [n_groups], both on the device."""
+    """Sequences whose caches begin with the same pages: those of group g, [group_start[g], group_start[g+1]), that have new tokens share
+    their positions [0, shared[g]); group_start int32 [n_groups + 1], shared int32 [n_groups], both on the device."""
     _held = ("group_start", "shared")
 
     def __init__(self, group_start, shared):

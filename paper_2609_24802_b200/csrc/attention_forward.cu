@@ -627,19 +627,24 @@ static __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(AttnPa
     const long long most = min(min(p.max_pages * p.page_size, MOST_ROWS), 1LL << 30);
     for (int g = warp; g < x.n_groups; g += PLAN_THREADS / 32) {
         const int a = clamp_to(x.group_start[g], n_seq), b = max(clamp_to(x.group_start[g + 1], n_seq), a);
-        int shared = (int)min((long long)max(x.shared[g], 0), most), halves = 0;
+        int shared = (int)min((long long)max(x.shared[g], 0), most), halves = 0, reader = n_seq;
         for (int s = a + lane; s < b; s += 32) {
             const Segment e = segment_of(p, s);
-            if (e.nq == 0) continue;
+            if (e.nq == 0) continue;            // (reads nothing: its length and its pages may be another's by now)
+            reader = min(reader, s);
             shared = min(shared, p.causal ? max(e.length - e.nq + 1, 0) : e.length);
             halves += tile_halves(e.nq * p.group);
         }
         shared = __reduce_min_sync(~0u, shared);
         halves = __reduce_add_sync(~0u, halves);
+        reader = __reduce_min_sync(~0u, reader);
         const int q0 = clamp_to(p.q_start[a], p.n_q), nq = max(clamp_to(p.q_start[b], p.n_q) - q0, 0);
         const long long steps = quotient(shared + FWD_STEP - 1, FWD_STEP), tiles = quotient((long long)nq * p.group + FWD_ROWS - 1, FWD_ROWS);
         const bool pays = (long long)nq * p.group <= (long long)(b - a) * FWD_ROWS && (halves - tile_halves(nq * p.group)) * steps > 8 * tiles && nq < 1 << 30;
-        if (lane == 0) groups[g] = {q0, pays ? nq : 0, 0, pays ? shared : 0, pays ? shared + nq : 0};
+        if (lane == 0) {
+            groups[g] = {q0, pays ? nq : 0, 0, pays ? shared : 0, pays ? shared + nq : 0};
+            plan.line_row[g] = reader;          // (n_seq: the group has no rows, and nothing is looked up)
+        }
     }
     __syncthreads();
     if (warp == 0) {            // places of the groups' states; a group for which there is no room (bounds that overlap) shares nothing
@@ -651,7 +656,7 @@ static __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(AttnPa
                 plan.state_start[g] = base + run - n;
                 states[g] = base + run - n - groups[g].q0;
                 if (base + run > state_rows) groups[g] = {0, 0, 0, 0, 0};
-                plan.line_row[g] = plan.first_member[g] = clamp_to(x.group_start[g], n_seq);
+                plan.first_member[g] = clamp_to(x.group_start[g], n_seq);
             }
             base += __shfl_sync(~0u, run, 31);
         }
