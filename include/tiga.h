@@ -481,10 +481,11 @@ typedef struct { float* data; int64_t seg, head, length; } tiga_weights;
 /* How much attention the cached positions have received: with lse of tiga_apply_paged_attention for the same chunk,
  *     weights[s, h', j] = before[s, h', j] + sum over the chunk's rows i of s that read position j, and the heads h of group h', of
  *                         exp(scale <q[i,h,:], key[j,h',:]> - lse[i,h]),          for j < kv_len[s].
- * Entries behind a sequence's end are left as they were; positions from weights->length on are not counted, positions without a page
- * receive nothing, and neither do rows whose lse is -inf give anything.  before == NULL: zeros; it may be the same array (with equal strides)
- * as weights, and is otherwise apart from it; before->length >= weights->length.  Values are not read (c->value may be NULL).  Sums are
- * fp32, in one order.
+ * Entries behind a sequence's end are left as they were; positions from weights->length on are not counted, positions without a page (also
+ * those that the sequence's row of the table does not reach) receive nothing, so that their entries are before, and rows whose lse is -inf
+ * give nothing.  before == NULL: zeros (and with a table without entries, max_pages 0, nothing is written); it may be the same array (with
+ * equal strides) as weights, and is otherwise apart from it; before->length >= weights->length.  Values are not read (c->value may be NULL).
+ * Sums are fp32, in one order.
  * ws: tiga_paged_weights_workspace_bytes(c, h, n_q) bytes. */
 size_t tiga_paged_weights_workspace_bytes(const tiga_pages* c, const tiga_heads* h, int64_t n_q);
 tiga_status tiga_paged_attention_weights(const tiga_pages* c, const tiga_heads* h, const void* q, const int32_t* q_start, int64_t n_q,

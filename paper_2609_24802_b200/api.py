@@ -952,8 +952,8 @@ def tiga_paged_weights_workspace_bytes(cache: PagedCache, q) -> int:
 def tiga_paged_attention_weights(cache: PagedCache, q, q_start, lse, scale: float, causal=True, before=None, weights=None, ws=None, stream=None):
     """weights[s,h',j] = before[s,h',j] + the softmax weights that position j of sequence s receives from the chunk's rows and the heads of
     group h'; q, q_start, scale, causal and lse as in, and from, tiga_apply_paged_attention.  weights and before fp32 [n_seg, kv_heads,
-    positions]; weights may be before (the sums are kept in place).  Entries behind a sequence's end are left alone (zeros where weights is
-    allocated here).  Returns (weights, ws)."""
+    positions]; weights may be before (the sums are kept in place).  Positions without a page receive nothing.  Entries behind a sequence's
+    end are left alone (zeros where weights is allocated here).  Returns (weights, ws)."""
     with _on(q, stream):
         h = _paged_heads(cache, q, scale)
         start = _ints(q_start, cache.n_seg + 1, "q_start")

@@ -412,6 +412,19 @@ static __global__ void __launch_bounds__(WT_TILE) weights_sum_kernel(const AttnP
     put_weight(sums, j.item.s, j.item.h, key, weight_before(sums, j.item.s, j.item.h, key) + sum);
 }
 
+// A sequence may be longer than its row of the table: entries of the positions from `room` on, which receive nothing, are what was before.  By
+// pieces of a list.
+constexpr int REST_THREADS = 256, REST_PIECE = 16 * REST_THREADS;
+static __global__ void __launch_bounds__(REST_THREADS) weights_rest_kernel(const AttnParams p, const WtSums sums, const long long room, const long long pieces) {
+    const long long tasks = (long long)p.n_seg * p.kv_heads * pieces;
+    for (long long task = blockIdx.x; task < tasks; task += gridDim.x) {
+        const long long list = quotient(task, pieces), first = room + (task - list * pieces) * REST_PIECE;
+        const int s = (int)quotient(list, p.kv_heads), h = (int)(list - (long long)s * p.kv_heads);
+        const long long end = min(min((long long)p.kv_len[s], sums.length), first + REST_PIECE);
+        for (long long j = first + threadIdx.x; j < end; j += REST_THREADS) put_weight(sums, s, h, (int)j, weight_before(sums, s, h, (int)j));
+    }
+}
+
 static size_t weights_carve(const AttnParams& p, void* ws, WtWork* w) {
     Carver cv(ws);
     w->unit_start = cv.take<long long>((size_t)p.n_seg + 1);
@@ -464,12 +477,18 @@ extern "C" tiga_status tiga_paged_attention_weights(const tiga_pages* c, const t
     if (n_q > 0 && (!q || !aligned16(q) || !lse || !aligned16(lse))) return TIGA_ERR_INVALID_ARG;
     if ((c->max_pages > 0 && attention_bad_ints(c->table)) || (c->n_pages > 0 && (!c->key || !aligned16(c->key)))) return TIGA_ERR_INVALID_ARG;
     if (!ws || !aligned16(ws) || ws_bytes < tiga_paged_weights_workspace_bytes(c, h, n_q)) return TIGA_ERR_WORKSPACE;
-    if (c->max_pages == 0) return TIGA_OK;          // no position
+    if (c->max_pages == 0 && !before) return TIGA_OK;           // neither positions nor what they had before
+    const WtSums sums = {before ? before->data : nullptr, weights->data, before ? before->seg : 0, before ? before->head : 0, weights->seg, weights->head, weights->length};
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const long long room = c->max_pages * c->page_size;
+    if (room < sums.length && sums.before != sums.out) {
+        const long long pieces = (sums.length - room + REST_PIECE - 1) / REST_PIECE, tasks = c->n_seg * h->kv_heads * pieces;
+        weights_rest_kernel<<<counted((unsigned)(tasks < 4096 ? tasks : 4096)), REST_THREADS, 0, s>>>(p, sums, room, pieces);
+    }
+    if (c->max_pages == 0) return launch_status();
     WtWork w;
     weights_carve(p, ws, &w);
     p.q = q; p.v = p.k; p.q_start = q_start; p.causal = causal != 0; p.lse_in = lse;
-    const WtSums sums = {before ? before->data : nullptr, weights->data, before ? before->seg : 0, before ? before->head : 0, weights->seg, weights->head, weights->length};
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (h->dtype == TIGA_BF16) return p.D > 64 ? launch_weights<__nv_bfloat16, 128>(p, sums, w, s) : launch_weights<__nv_bfloat16, 64>(p, sums, w, s);
     return p.D > 64 ? launch_weights<__half, 128>(p, sums, w, s) : launch_weights<__half, 64>(p, sums, w, s);
 }
