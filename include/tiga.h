@@ -502,7 +502,8 @@ tiga_status tiga_paged_attention_weights(const tiga_pages* c, const tiga_heads* 
  *     to_weights           their weights, zeros behind them (a new token's count begins there), apart from weights; NULL: not wanted
  * Keys keep the rotation of their positions: the next token is rotated by its own position (tiga_apply_rotary) and appended without
  * one.  Pages that are written must be apart from those that sequences of `from` name, and belong to one sequence alone; both caches
- * may lie in the same arrays.
+ * may lie in the same arrays.  Rows of `to` lie apart: of the strides of its pages, slots and heads each is at least as long as what the
+ * shorter ones span (TIGA_ERR_INVALID_ARG).
  *   h : dtype, kv_heads, D;  1 <= keep <= to->max_pages * to->page_size;  0 <= recent <= keep. */
 tiga_status tiga_paged_evict(const tiga_pages* from, const tiga_pages* to, const tiga_heads* h, const tiga_weights* weights,
                              int64_t keep, int64_t recent, const tiga_weights* to_weights, int32_t* to_len, int32_t* kept, void* stream);

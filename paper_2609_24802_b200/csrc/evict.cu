@@ -1,4 +1,5 @@
 // A paged cache is cut to a budget: every kv head of a sequence keeps its last positions and those that carry the most weight.
+#include <algorithm>
 #include <cooperative_groups.h>
 #include "attention_shared.cuh"
 
@@ -302,6 +303,20 @@ static cudaError_t launch_select(EvictParams p, long long most, long long lists,
     return cudaLaunchKernelEx(&c, evict_select_kernel<THREADS, CLUSTER, MOVE>, p);
 }
 
+// Whether rows (of a page, slot and head) lie in one another, so that two warps would write the same place: of the three strides each has to
+// be as long as what the shorter ones span.
+static bool rows_share_storage(const tiga_pages* c, int kv_heads, int D) {
+    struct Axis { long long stride, n; } axes[3] = {{c->page_stride, c->n_pages}, {c->slot_stride, c->page_size}, {c->head_stride, kv_heads}};
+    std::sort(axes, axes + 3, [](const Axis& a, const Axis& b) { return a.stride < b.stride; });
+    __int128 span = D;
+    for (const Axis& a : axes) {
+        if (a.n < 2) continue;
+        if (a.stride < span) return true;
+        span += (__int128)a.stride * (a.n - 1);
+    }
+    return false;
+}
+
 }  // namespace tiga
 
 using namespace tiga;
@@ -316,8 +331,7 @@ extern "C" tiga_status tiga_paged_evict(const tiga_pages* from, const tiga_pages
     if (attention_bad_weights(weights) || (to_weights && attention_bad_weights(to_weights))) return TIGA_ERR_INVALID_ARG;
     if (keep > MOST_ROWS || from->n_seg * h->kv_heads > (1 << 24)) return TIGA_ERR_UNSUPPORTED;
     if (from->n_seg == 0) return TIGA_OK;
-    // slots or heads of a page that share storage would be written twice
-    if ((to->page_size > 1 && to->slot_stride == 0) || (h->kv_heads > 1 && to->head_stride == 0) || (to->n_pages > 1 && to->page_stride == 0)) return TIGA_ERR_INVALID_ARG;
+    if (rows_share_storage(to, h->kv_heads, h->D)) return TIGA_ERR_INVALID_ARG;
     if (attention_bad_ints(from->kv_len) || attention_bad_ints(to_len) || attention_bad_ints(kept) || to_len == from->kv_len) return TIGA_ERR_INVALID_ARG;
     if (attention_bad_ints(to->table) || (from->max_pages > 0 && attention_bad_ints(from->table))) return TIGA_ERR_INVALID_ARG;
     auto bad = [](const void* a) { return !a || !aligned16(a); };
