@@ -62,7 +62,6 @@ __device__ __forceinline__ float gradient_factor(const uint32_t* norms, int s) {
 // are read once (fp16: value too).  A block has rows that follow one another, so that it passes through their segments in order.  Of few
 // keys delta is summed as sum p dP: out is then as large as the values, and its rounding would show in dP - delta (over n keys it is
 // smaller by the root of n).
-constexpr int FEW_KEYS = 16;
 template <typename T>
 __device__ __forceinline__ float dot8(const uint4& a, const uint4& b) {
     const T* x = reinterpret_cast<const T*>(&a);
@@ -72,8 +71,6 @@ __device__ __forceinline__ float dot8(const uint4& a, const uint4& b) {
     for (int e = 0; e < 8; ++e) d += Half<T>::to(x[e]) * Half<T>::to(y[e]);
     return d;
 }
-constexpr int PREP_THREADS = 256, PREP_BLOCKS = 4;      // of an SM
-constexpr int PREP_ALONE = 16;                          // blocks of work that one block does alone
 // The largest norm of a segment, as far as this thread's rows go, to memory: a maximum does not depend on the order.
 __device__ __forceinline__ void put_norm(uint32_t* norm, float top) {
     const uint32_t bits = __float_as_uint(top);
@@ -241,7 +238,7 @@ __global__ void __launch_bounds__(PREP_THREADS, PREP_BLOCKS) attention_prepare_k
         // heads at a time (in the loop above their block was the last to end, by 30 us).
         constexpr int HEADS = 32 / LANES;
         const int pieces = (p.heads + HEADS - 1) / HEADS;
-        const long long tasks = (long long)p.n_seg * FEW_KEYS * pieces, stride = (long long)gridDim.x * (PREP_THREADS / 32);
+        const long long tasks = looks_for_few_keys(p, LANES), stride = (long long)gridDim.x * (PREP_THREADS / 32);
         for (long long task = (long long)blockIdx.x * (PREP_THREADS / 32) + threadIdx.x / 32; task < tasks; task += stride) {
             const long long of_row = quotient(task, pieces);
             const int s = (int)(of_row / FEW_KEYS), n = (int)(of_row % FEW_KEYS) + 1, head = (int)(task - of_row * pieces) * HEADS + (int)(threadIdx.x % 32) / LANES;
@@ -767,12 +764,9 @@ static tiga_status launch_backward(AttnParams p, const BwdWork& w, cudaStream_t 
     if (kv_blocks + q_blocks == 0) return TIGA_OK;
     const auto kernel = p.causal ? attention_backward_kernel<T, DP, true> : attention_backward_kernel<T, DP, false>;
     TIGA_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Bwd<DP>::SMEM));
-    // blocks by the work there may be: a row of values costs about half of one of queries
+    // a row of values costs about half of one of queries
     const long long q_work = (long long)p.n_q * p.heads, v_work = operand_type<T>() == 0 ? ((long long)p.n_kv * p.kv_heads + 1) / 2 : 0;
-    long long grid = ((q_work + v_work) * (DP / 8) + PREP_THREADS - 1) / PREP_THREADS;
-    // Little work is prepared by one block, which clears the words for its maxima itself: a launch less (about 5 us of the
-    // host's time against 1 us for each 256 rows of 64 features).
-    grid = grid <= PREP_ALONE ? 1 : grid < PREP_BLOCKS * sms ? grid : PREP_BLOCKS * sms;
+    const long long grid = prepare_blocks(p, q_work + v_work, DP / 8, sms);
     const int prep_v = !v_work ? 0 : grid == 1 ? 1 : (int)min(max(grid * v_work / (q_work + v_work), 1LL), grid - 1);
     const int prep_q = grid == 1 ? 1 : (int)grid - prep_v;
     const bool plan = w.kv_start_unit || (operand_type<T>() == 0 && grid > 1);

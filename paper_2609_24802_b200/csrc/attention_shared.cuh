@@ -494,6 +494,24 @@ static inline cudaError_t launch_after(void (*kernel)(A...), dim3 grid, int thre
     return cudaLaunchKernelEx(&c, kernel, args...);
 }
 
+// ---- The preparation of the backward pass: blocks by the work there may be, `rows` rows of `lanes` threads.
+constexpr int FEW_KEYS = 16;                            // up to so many keys a row's delta is summed over them
+constexpr int PREP_THREADS = 256, PREP_BLOCKS = 4;      // of an SM
+// Little work is done by one block, which clears the words for its maxima itself: a launch less (about 5 us of the host's time against
+// 1 us for each 256 rows of 64 features).
+constexpr int PREP_ALONE = 16;                          // blocks of work
+// Under the triangle: looks for rows of few keys, one for each such row that a segment may have and as many of its heads as a warp takes at a
+// time.  They are work of their own, as segments may be empty (125 rows in 10000 segments, 2 heads of 64: 5150 us of one block's, now 72; 4 or 64
+// looks to a block 72 too, but 16 segments of 20 rows 43 and 42 instead of 41).
+constexpr int LOOKS_OF_A_BLOCK = 16;
+static __host__ __device__ __forceinline__ long long looks_for_few_keys(const AttnParams& p, int lanes) {
+    return p.causal ? (long long)p.n_seg * FEW_KEYS * ((p.heads * lanes + 31) / 32) : 0;
+}
+static inline long long prepare_blocks(const AttnParams& p, long long rows, int lanes, int sms) {
+    const long long n = (rows * lanes + PREP_THREADS - 1) / PREP_THREADS + looks_for_few_keys(p, lanes) / LOOKS_OF_A_BLOCK;
+    return n <= PREP_ALONE ? 1 : n < PREP_BLOCKS * sms ? n : PREP_BLOCKS * sms;
+}
+
 constexpr int MAX_SMS = 160;            // blocks that workspaces provide for
 // Workspaces come on a boundary of 16 bytes; states are put aside in sectors of 32.  (Their sizes have 256 bytes to spare.)
 static inline void* on_sectors(void* ws) { return reinterpret_cast<void*>(align_up(reinterpret_cast<uintptr_t>(ws), 256)); }
