@@ -410,7 +410,9 @@ tiga_status tiga_apply_dense_attention(const tiga_dense* g, const tiga_heads* h,
  * key and value gradients summed over the heads of their group.  p is recomputed from lse; nothing of size rows x keys is
  * stored.  out and lse are the forward's outputs for these inputs.  Gradients have the storage type and are dense,
  * [n_q, heads, D] and [n_kv, kv_heads, D]; any of them may be NULL (skipped).  Masked keys have zero gradients, and so have
- * the scores of rows that read a single key.  Of up to 16 keys delta is summed as sum_j p_ij dP_ij.
+ * the scores of rows that read a single key, if their segment has at most 32 (of a longer one whose mask leaves a single key they have what
+ * rounding leaves of dP - delta, two sums of D products: D 2^-22 of sum_d |grad_out value|).  Of up to 16 keys delta is summed as
+ * sum_j p_ij dP_ij.
  * TIGA_F16: p and dS are scaled by powers of two before they are rounded (dS by one of each segment, from the largest norms
  * of its rows of grad_out and value), so that small weights and small gradients keep their digits.
  * ws: tiga_dense_attention_workspace_bytes(g, h, 1) bytes. */
@@ -422,7 +424,8 @@ tiga_status tiga_apply_dense_attention_backward(const tiga_dense* g, const tiga_
 /* The same reducer over a triangular relation (causal attention): row t of the n rows of segment s reads, of its m keys, those up to
  * m - n + t (the rows are the segment's last ones: with as many keys as rows each reads up to its own place), of which kv_mask leaves
  * out more.  Rows in front of the first key (n > m) read nothing.  Packed sequences of different lengths are segments.  Arguments,
- * outputs, gradients and workspace as above; scores of rows that read a single key have no gradient in grad_q. */
+ * outputs, gradients and workspace as above; scores of rows that read a single key have no gradient in grad_q, if the row reaches at most
+ * 32 keys without the mask (and what rounding leaves of dP - delta if it reaches more). */
 size_t tiga_triangular_attention_workspace_bytes(const tiga_dense* g, const tiga_heads* h, int backward);
 tiga_status tiga_apply_triangular_attention(const tiga_dense* g, const tiga_heads* h, const void* q, const void* key, const void* value,
                                             void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
