@@ -734,7 +734,6 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32, SHARED_JOIN_BLOCKS) shared_jo
     constexpr int E = DP / 32;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const long long units = w.unit_start[p.n_seg], blocks = Walker<SharedCut>::pieces(p, units, sms);
-    auto block_of = [&](long long unit) { return (int)quotient((unit + 1) * blocks - 1, units); };
     struct TwoStates { int row, g, s; };                    // a row, its group (-1: it has no two states) and sequence
     struct Parts { int first, parts, r; };                  // where a state lies
     __shared__ TwoStates rows[SHARED_JOIN_TASKS];
@@ -765,10 +764,9 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32, SHARED_JOIN_BLOCKS) shared_jo
             if (two.g >= 0) {
                 const int line = kind ? w.n_groups + two.s : two.g;
                 const Segment seg = p.line[line];
-                const int packed = (two.row - seg.q0) * p.group + head % p.group, t = packed / FWD_ROWS, cost = SharedCut::step_cost(p, seg);
-                const long long start = w.unit_start[line] + head / p.group * SharedCut::units(p, seg) + SharedCut::before(p, seg, t) + p.item_cost - 1;
-                const int first = block_of(start + cost);               // the blocks that have the last unit of the tile's first and last step
-                found[k][kind] = {first, block_of(start + (long long)cost * SharedCut::steps(p, seg, t)) - first + 1, packed % FWD_ROWS};
+                const int packed = (two.row - seg.q0) * p.group + head % p.group;
+                const auto had = Walker<SharedCut>::blocks_of_tile(p, seg, w.unit_start[line], head / p.group, packed / FWD_ROWS, units, blocks);
+                found[k][kind] = {had.first, had.parts, packed % FWD_ROWS};
             }
         }
         __syncthreads();

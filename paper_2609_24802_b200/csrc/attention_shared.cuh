@@ -35,10 +35,10 @@ struct Segment { int q0, nq, k0, nk, length; };
 // Rows and positions end here, so that a tile's last row number fits 32 bits.
 constexpr long long MOST_ROWS = 0x7fff0000LL;
 
-__device__ __forceinline__ int clamp_to(int v, int hi) { return min(max(v, 0), hi); }
+__host__ __device__ __forceinline__ int clamp_to(int v, int hi) { return min(max(v, 0), hi); }
 
 // (the bounds of rows and of dense keys: p.q_start and p.kv_start, or a copy of them)
-__device__ __forceinline__ Segment segment_of(const AttnParams& p, int s, const int32_t* q_start, const int32_t* kv_start) {
+__host__ __device__ __forceinline__ Segment segment_of(const AttnParams& p, int s, const int32_t* q_start, const int32_t* kv_start) {
     Segment g;
     g.q0 = clamp_to(q_start[s], p.n_q);
     g.nq = max(clamp_to(q_start[s + 1], p.n_q) - g.q0, 0);
@@ -52,7 +52,7 @@ __device__ __forceinline__ Segment segment_of(const AttnParams& p, int s, const 
     }
     return g;
 }
-__device__ __forceinline__ Segment segment_of(const AttnParams& p, int s) { return segment_of(p, s, p.q_start, p.kv_start); }
+__host__ __device__ __forceinline__ Segment segment_of(const AttnParams& p, int s) { return segment_of(p, s, p.q_start, p.kv_start); }
 
 // keys that row t of the segment's nq rows reads: [0, this)
 __host__ __device__ __forceinline__ int keys_of_row(const AttnParams& p, const Segment& g, int t) {
@@ -200,7 +200,7 @@ struct Cut {
     static constexpr bool KEYS = KEYS_;                   // the keys are stationary
     static constexpr bool PLAIN = MODE == CUT_STEPS;
 
-    static __device__ __forceinline__ Segment segment(const AttnParams& p, int s) { return MODE == CUT_LINE ? p.line[s] : segment_of(p, s); }
+    static __host__ __device__ __forceinline__ Segment segment(const AttnParams& p, int s) { return MODE == CUT_LINE ? p.line[s] : segment_of(p, s); }
     static __host__ __device__ __forceinline__ int rows(const AttnParams& p, const Segment& g) { return KEYS ? g.nk : g.nq * p.group; }
     static __host__ __device__ __forceinline__ int tiles(const AttnParams& p, const Segment& g) {
         const int n = rows(p, g);
@@ -264,6 +264,27 @@ struct Cut {
     }
 };
 
+// The cut of accumulated weights: of a segment with few packed rows the rows stay, in one tile, and steps are tiles of keys; of more the keys
+// stay.
+constexpr int WT_TILE = 128;
+struct WtCut {
+    static constexpr bool PLAIN = false;
+    typedef Cut<WT_TILE, WT_TILE, true, CUT_COSTS> Wide;        // (tiles cost nothing)
+    static __host__ __device__ __forceinline__ bool narrow(const AttnParams& p, const Segment& g) { return (long long)g.nq * p.group <= WT_TILE; }
+    static __host__ __device__ __forceinline__ int rows(const AttnParams&, const Segment& g) { return g.nk; }
+    static __host__ __device__ __forceinline__ int tiles(const AttnParams& p, const Segment& g) { return narrow(p, g) ? g.nk > 0 : Wide::tiles(p, g); }
+    static __host__ __device__ __forceinline__ int skipped(const AttnParams& p, const Segment& g, int t) { return narrow(p, g) ? 0 : Wide::skipped(p, g, t); }
+    static __host__ __device__ __forceinline__ int steps(const AttnParams& p, const Segment& g, int t) { return narrow(p, g) ? Wide::tiles(p, g) : Wide::steps(p, g, t); }
+    static __host__ __device__ __forceinline__ Segment segment(const AttnParams& p, int s) { return segment_of(p, s); }
+    static __host__ __device__ __forceinline__ int item_cost(const AttnParams&) { return 0; }
+    static __host__ __device__ __forceinline__ bool uneven(const AttnParams&) { return false; }
+    static __host__ __device__ __forceinline__ int step_cost(const AttnParams&, const Segment&) { return 1; }
+    static __host__ __device__ __forceinline__ long long before(const AttnParams& p, const Segment& g, int t) {
+        return narrow(p, g) ? (long long)t * Wide::tiles(p, g) : Wide::before(p, g, t);
+    }
+    static __host__ __device__ __forceinline__ long long units(const AttnParams& p, const Segment& g) { return before(p, g, tiles(p, g)); }
+};
+
 __device__ __forceinline__ long long warp_total(long long v) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
@@ -289,7 +310,7 @@ struct Walker {
     bool here;                  // this block has any
 
     // the tile's steps from its unit `off` on; false: the piece ends in front of the tile's first step
-    __device__ __forceinline__ bool open(const AttnParams& p, long long off) {
+    __host__ __device__ __forceinline__ bool open(const AttnParams& p, long long off) {
         steps = C::steps(p, g, t);
         if (C::PLAIN) {
             i0 = (int)off;
@@ -306,10 +327,10 @@ struct Walker {
         return i1 > i0;
     }
     // blocks that take part: every piece has a step's units, so that the blocks between a tile's first and last one all have steps of it
-    static __device__ __forceinline__ long long pieces(const AttnParams& p, long long units, int grid) {
+    static __host__ __device__ __forceinline__ long long pieces(const AttnParams& p, long long units, int grid) {
         return min((long long)grid, max(C::uneven(p) ? units / 3 : units, 1LL));
     }
-    __device__ __forceinline__ long long first_unit(long long block) const { return quotient(block * units, blocks); }
+    __host__ __device__ __forceinline__ long long first_unit(long long block) const { return quotient(block * units, blocks); }
 
     // The piece of block `block` of `grid`, by a warp with all its lanes; of few units every one has a block of its own (two units a block:
     // a single token on 777 keys 14.2 us on the device instead of 11.0).  unit_start: units in front of every segment; NULL (few segments, few tiles): they are counted here.
@@ -396,7 +417,7 @@ struct Walker {
         return open(p, off);
     }
     // The same by a thread alone, for a plan that does it for all blocks.
-    __device__ __forceinline__ void begin_alone(const AttnParams& p, const long long* unit_start, int block, int grid) {
+    __host__ __device__ __forceinline__ void begin_alone(const AttnParams& p, const long long* unit_start, int block, int grid) {
         auto last = [](int n, auto at_most) {               // the last of n places that is not beyond; place 0 is not
             int lo = 0, hi = n;
             while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (at_most(mid)) lo = mid; else hi = mid; }
@@ -419,7 +440,7 @@ struct Walker {
         start = off;
         here = open(p, off);
     }
-    __device__ __forceinline__ bool next(const AttnParams& p) {
+    __host__ __device__ __forceinline__ bool next(const AttnParams& p) {
         if (left <= 0) return false;
         if (++t >= C::tiles(p, g)) {
             t = 0;
@@ -431,9 +452,19 @@ struct Walker {
         return open(p, 0);
     }
     // after begin() inside of a tile's steps: the block that has its first step
-    __device__ __forceinline__ int first_block(const AttnParams& p, int block) const {
+    __host__ __device__ __forceinline__ int first_block(const AttnParams& p, int block) const {
         if (C::PLAIN) return (int)quotient((first_unit(block) - i0 + 1) * blocks - 1, units);
         return (int)quotient((first_unit(block) - start + C::item_cost(p) + C::step_cost(p, g)) * blocks - 1, units);
+    }
+    // The same of any tile, and how many blocks have steps of it: those with the last unit of its first and of its last step.  begin: the units in
+    // front of the segment.
+    struct Blocks { int first, parts; };
+    static __host__ __device__ __forceinline__ Blocks blocks_of_tile(const AttnParams& p, const Segment& g, long long begin, int h, int t, long long units, long long blocks) {
+        const long long start = begin + h * C::units(p, g) + C::before(p, g, t) + C::item_cost(p) - 1;
+        const int cost = C::step_cost(p, g);
+        auto block_of = [&](long long unit) { return (int)quotient((unit + 1) * blocks - 1, units); };
+        const int first = block_of(start + cost);
+        return {first, block_of(start + (long long)cost * C::steps(p, g, t)) - first + 1};
     }
 };
 

@@ -17,25 +17,7 @@ namespace tiga {
 // exponentials; a quarter of them by polynomials on the other pipes 360 to 423 (the warps are in order, and wait for their longer chains).
 // 64 single tokens on up to 8192: 122 us, 5.7 TB/s.
 constexpr int WT_WARPS = 16, WT_PRODUCER = WT_WARPS, WT_MMA = WT_PRODUCER + 4, WT_WALKER = WT_MMA + 1;
-constexpr int WT_THREADS = 32 * (WT_WALKER + 1), WT_TILE = 128, WT_BUFFERS = 4, WT_AUX = 8;
-
-struct WtCut {
-    static constexpr bool PLAIN = false;
-    typedef Cut<WT_TILE, WT_TILE, true, CUT_COSTS> Wide;        // (tiles cost nothing)
-    static __host__ __device__ __forceinline__ bool narrow(const AttnParams& p, const Segment& g) { return (long long)g.nq * p.group <= WT_TILE; }
-    static __host__ __device__ __forceinline__ int rows(const AttnParams&, const Segment& g) { return g.nk; }
-    static __host__ __device__ __forceinline__ int tiles(const AttnParams& p, const Segment& g) { return narrow(p, g) ? g.nk > 0 : Wide::tiles(p, g); }
-    static __host__ __device__ __forceinline__ int skipped(const AttnParams& p, const Segment& g, int t) { return narrow(p, g) ? 0 : Wide::skipped(p, g, t); }
-    static __host__ __device__ __forceinline__ int steps(const AttnParams& p, const Segment& g, int t) { return narrow(p, g) ? Wide::tiles(p, g) : Wide::steps(p, g, t); }
-    static __device__ __forceinline__ Segment segment(const AttnParams& p, int s) { return segment_of(p, s); }
-    static __host__ __device__ __forceinline__ int item_cost(const AttnParams&) { return 0; }
-    static __host__ __device__ __forceinline__ bool uneven(const AttnParams&) { return false; }
-    static __host__ __device__ __forceinline__ int step_cost(const AttnParams&, const Segment&) { return 1; }
-    static __host__ __device__ __forceinline__ long long before(const AttnParams& p, const Segment& g, int t) {
-        return narrow(p, g) ? (long long)t * Wide::tiles(p, g) : Wide::before(p, g, t);
-    }
-    static __host__ __device__ __forceinline__ long long units(const AttnParams& p, const Segment& g) { return before(p, g, tiles(p, g)); }
-};
+constexpr int WT_THREADS = 32 * (WT_WALKER + 1), WT_BUFFERS = 4, WT_AUX = 8;
 
 template <int DP> struct Wt {
     static constexpr int TILE = 128 * DP * 2;
