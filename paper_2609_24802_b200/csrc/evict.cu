@@ -355,14 +355,18 @@ extern "C" tiga_status tiga_paged_evict(const tiga_pages* from, const tiga_pages
     int dev = 0, sms = 0;
     TIGA_CUDA_TRY(cudaGetDevice(&dev));
     TIGA_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-    // A cluster for each list where the lists alone leave most SMs idle and are long enough to be worth the meetings; small blocks where there
-    // are several for each SM, whose shared memory holds their numbers.  Up to 512 places are moved by the block that selects them.
+    // Up to 512 places of few short lists are moved by the block that selects them: 2 to 4 us more on the device for 5 us of the host's launch (2 lists
+    // of 8192, 512 kept: 22.7 against 18.6; 1024 kept: 27.6 against 18.6; behind longer lists the launch does not show).
+    // A cluster for each list where one block's shared memory does not hold it and the lists alone leave most SMs idle: a list's meetings cost 15 us, and
+    // no more than about 16 clusters find room at once (16 lists of 40960: 59 us, a block each 40; of 45056: 60 and 99; 64 lists of 57344: 145 and 121).
+    // Small blocks where there are several for each SM, whose shared memory holds their numbers (2048 lists of 8192: 97 us, with 1024 threads 154; 512 of
+    // 16384: 63 and 68; 152 of 12288, 2048 kept: 87 and 78); of few lists the large ones (16 of 8192: 18.6 us, 24.8; of 1024: 16.5, 14.5).
     const bool few = lists <= sms;
     if (few && most <= 8192 && keep <= 512) {
         TIGA_CUDA_TRY((launch_select<SELECT_FEW, 1, true>(p, most, lists, s)));
         return launch_status();
     }
-    if (lists * SELECT_CLUSTER <= 2 * sms && most > 8192) TIGA_CUDA_TRY((launch_select<SELECT_FEW, SELECT_CLUSTER, false>(p, most, lists, s)));
+    if (lists * SELECT_CLUSTER <= 2 * sms && most > SELECT_HELD) TIGA_CUDA_TRY((launch_select<SELECT_FEW, SELECT_CLUSTER, false>(p, most, lists, s)));
     else if (few || most > 12288) TIGA_CUDA_TRY((launch_select<SELECT_FEW, 1, false>(p, most, lists, s)));
     else TIGA_CUDA_TRY((launch_select<SELECT_MANY, 1, false>(p, most, lists, s)));
     const long long tasks = lists * ((keep + 31) / 32);
