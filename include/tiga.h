@@ -471,7 +471,8 @@ typedef struct {
 /* tiga_apply_paged_attention for a batch whose sequences share prefixes: a group's rows meet the shared positions together, once, and
  * each sequence's rows the positions behind them; the two states of a row are joined as partial states are.  The result is that of
  * tiga_apply_paged_attention (in another order of the sums), whatever shared says: positions that some row of the group does not read
- * are not taken as shared, and a group shares nothing where that saves no work.
+ * are not taken as shared, and a group shares nothing where that saves no work.  (The call has one kernel more than that one, and what there is to
+ * share is found on the device: a few users of a short prompt, or users who share nothing, are served sooner by that one.)
  *   ws: tiga_shared_attention_workspace_bytes(c, h, g, n_q) bytes. */
 size_t tiga_shared_attention_workspace_bytes(const tiga_pages* c, const tiga_heads* h, const tiga_prefixes* g, int64_t n_q);
 tiga_status tiga_apply_shared_attention(const tiga_pages* c, const tiga_heads* h, const tiga_prefixes* g, const void* q, const int32_t* q_start,

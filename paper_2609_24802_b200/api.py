@@ -914,8 +914,8 @@ def tiga_shared_attention_workspace_bytes(cache: PagedCache, prefixes: SharedPre
 
 def tiga_apply_shared_attention(cache: PagedCache, prefixes: SharedPrefixes, q, q_start, scale: float, causal=True, out=None, lse=None, want_lse=True,
                                 ws=None, stream=None):
-    """tiga_apply_paged_attention for sequences that share prefixes: what a group shares is read once for all of its rows.  Returns
-    (out, lse, ws)."""
+    """tiga_apply_paged_attention for sequences that share prefixes: what a group shares is read once for all of its rows (a few users of
+    a short prompt are served sooner by that call).  Returns (out, lse, ws)."""
     with _on(q, stream):
         h = _paged_heads(cache, q, scale)
         _same(q, q_start, prefixes.shared, out, lse, ws)

@@ -14,8 +14,8 @@ namespace tiga {
 // of the halves take the even and the odd steps with a state each, joined at the end, so a single token keeps both busy too.
 // The accumulator is rescaled only when a row's maximum grew by more than 2^8 since the last time: weights up to 2^8 do no harm,
 // and the mass carries the same factor.
-// What bounds it: the chain S -> maximum -> P -> O of a half, 4050 cycles a step of 128 keys at a width of 128 where its products take
-// 1024 and its 16384 exponentials another 1024.  Two threads a row halve what one would take (a warp alone on its scheduler needs
+// What bounds it: the chain S -> maximum -> P -> O of a half, 3700 cycles a step of 128 keys at a width of 128 (3550 at 64; what twice the keys
+// take more) where its products take 1024 and its 16384 exponentials another 1024.  Two threads a row halve what one would take (a warp alone on its scheduler needs
 // about 13 cycles a column); the exchange of their maxima costs 100.  4 segments of 4096 rows and keys, 16/4 heads of 128, bf16: 543 us
 // alone, 1.0 PFLOP/s; single tokens read their cache at 6.3 TB/s between the ends of items.
 constexpr int FWD_SOFTMAX_WARPS = 16, FWD_PRODUCER = FWD_SOFTMAX_WARPS, FWD_MMA = FWD_PRODUCER + 4, FWD_WALKER = FWD_MMA + 1;
@@ -583,7 +583,15 @@ __device__ __forceinline__ int tile_halves(int packed) {            // of a segm
     const int rest = packed % FWD_ROWS;
     return 2 * (packed / FWD_ROWS) + (rest == 0 ? 0 : rest <= 128 ? 1 : 2);
 }
-constexpr int SHARED_ITEM_COST = 5;         // of a tile, in units of which a step has two or three (attention_shared.cuh)
+// Whether a group shares: halves of a step that it saves, more than 8 for each of its tiles (one new token each, 32/8 heads of 128, on the device,
+// shared and alone: 8 users of 4096 positions 33 and 43 us, 16 groups of 8 of 256 positions 72 and 78, 4 users of 128 positions 26.6 and
+// 22.7.  It is off where states outweigh steps, 64 users of 128 positions 51 and 43, and where steps are many but users two, 32 pairs of 1024
+// positions 74 and 83.)
+constexpr int SHARED_PAYS = 8;
+// What a tile costs beside its steps, of which each is two or three units (attention_shared.cuh).  64 users of 8192 positions and 48 samples of 16384
+// (32/8 heads; width 128, then 64): 84 and 118, 75 and 105 us; with a cost of 1 89 and 187, 76 and 147; of 10 99 and 124, 87 and 113; with
+// equal steps 101 and 132, 88 and 110.
+constexpr int SHARED_ITEM_COST = 5;
 // Rows of a group that shares: up to a full tile for each member on average (longer chunks fill their tiles alone).
 __host__ __device__ __forceinline__ long long most_state_rows(long long n_seq, long long n_q, int group) {
     const long long n = (n_seq * FWD_ROWS + group - 1) / group;
@@ -640,7 +648,7 @@ static __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(AttnPa
         reader = __reduce_min_sync(~0u, reader);
         const int q0 = clamp_to(p.q_start[a], p.n_q), nq = max(clamp_to(p.q_start[b], p.n_q) - q0, 0);
         const long long steps = quotient(shared + FWD_STEP - 1, FWD_STEP), tiles = quotient((long long)nq * p.group + FWD_ROWS - 1, FWD_ROWS);
-        const bool pays = (long long)nq * p.group <= (long long)(b - a) * FWD_ROWS && (halves - tile_halves(nq * p.group)) * steps > 8 * tiles && nq < 1 << 30;
+        const bool pays = (long long)nq * p.group <= (long long)(b - a) * FWD_ROWS && (halves - tile_halves(nq * p.group)) * steps > SHARED_PAYS * tiles && nq < 1 << 30;
         if (lane == 0) {
             groups[g] = {q0, pays ? nq : 0, 0, pays ? shared : 0, pays ? shared + nq : 0};
             plan.line_row[g] = reader;          // (n_seq: the group has no rows, and nothing is looked up)
